@@ -7,15 +7,12 @@ from dataclasses import dataclass
 
 import numpy as np
 
+from . import clear
+from .clear import SheError
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 
 GATES = {"NAND": 0, "AND": 1, "OR": 2, "XOR": 3, "XNOR": 4, "NOR": 5, "ANDNY": 6, "ANDYN": 7, "ORNY": 8, "ORYN": 9}
-
-
-class SheError(RuntimeError):
-    def __init__(self, code: int, text: str):
-        super().__init__(f"she error {code}: {text}")
-        self.code = code
 
 
 class _CParams(C.Structure):
@@ -120,6 +117,7 @@ def load_library() -> C.CDLL:
         "she_last_level_sizes": (C.c_int, [ctx, C.POINTER(C.c_uint64), C.POINTER(C.c_uint64), C.c_size_t,
                                             C.POINTER(C.c_size_t)]),
         "she_last_error": (C.c_char_p, [ctx]),
+        **clear.SIGNATURES,
     }
     for name, (res, args) in sigs.items():
         fn = getattr(L, name)
@@ -245,7 +243,7 @@ def plan_circuit(capacity: int, types, in0, in1, in2, fold: bool = False, native
     return _plan(rc, g, lv) + (rot.value,)
 
 
-class Context:
+class Context(clear.Calls):
     """Owns one she_ctx.  Method names mirror the C calls (she_ prefix dropped)."""
 
     def __init__(self, params: Params, seed: int, pool_capacity: int, use_torch_pool: bool = True):
@@ -260,6 +258,7 @@ class Context:
             raise SheError(rc, (self._L.she_last_error(None) or b"").decode())
         self._h = h
         self._pool_tensor = None
+        self._stream = 0
         if use_torch_pool:
             import torch
             nbytes = self._L.she_pool_bytes(self._h)
@@ -309,6 +308,7 @@ class Context:
 
     def set_stream(self, hip_stream: int):
         self._check(self._L.she_set_stream(self._h, C.c_void_p(hip_stream)))
+        self._stream = hip_stream
 
     # ---- the paper's problem statement
     def encrypt_bits(self, bits, enc_seed: int, dst_ids):

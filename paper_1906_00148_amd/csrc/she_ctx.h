@@ -29,6 +29,12 @@ struct LeveledPools {         // leveled mode: TRGSW selectors (spectral form) a
     size_t ids_cap = 0;
     hipEvent_t around[2] = {nullptr, nullptr};   // recorded around a level's kernel
 };
+struct ClearWork {            // the clear side's scratch (she_clear.h); freed with the context
+    void *scratch = nullptr;
+    size_t bytes = 0;
+    uint32_t *d_bad = nullptr;      // ids out of range that its kernels have met
+    ~ClearWork() { hipFree(scratch); hipFree(d_bad); }
+};
 // Layer operators recorded between she_defer_begin and she_defer_run: one netlist for all of them, so that the
 // scheduler can overlap the tail of one operator with the head of the next.
 struct Deferred {
@@ -71,6 +77,7 @@ struct she_ctx {
     std::vector<uint64_t> level_gates, level_muxes;   // schedule of the last circuit (she_last_level_sizes)
     double last_ms[4] = {0, 0, 0, 0};
     she::LeveledPools lev;
+    she::ClearWork clear;
     std::unique_ptr<she::Deferred> deferred;   // non-null between she_defer_begin and she_defer_run
     void *na_scratch = nullptr;          // this device's copy of the static scratch buffer (never freed)
     size_t na_bytes = 0;
