@@ -9,6 +9,8 @@ from __future__ import annotations
 
 import ctypes as C
 
+import torch
+
 EINVAL = -1
 
 
@@ -65,7 +67,6 @@ def _refuse(text):
 
 
 def _half(t, name):
-    import torch
     if t.dtype is torch.bfloat16:
         return 0
     if t.dtype is torch.float16:
@@ -74,17 +75,20 @@ def _half(t, name):
 
 
 def _see(t, name, dtype, shape):
-    """Refuses a tensor of another type, shape (None: any size) or place, or without a contiguous last axis."""
+    """A tensor's address; refuses one of another type, shape or place, or without a contiguous last axis."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or (t.stride(-1) != 1 and shape[-1] > 1):
+        _refuse_tensor(t, name, dtype, shape)
+    return t.data_ptr()
+
+
+def _refuse_tensor(t, name, dtype, shape):
     if t.dtype is not dtype:
         _refuse(f"{name} must be {dtype}, not {t.dtype}")
-    got = t.shape
-    if len(got) != len(shape) or any(w is not None and w != g for g, w in zip(got, shape)):
-        _refuse(f"{name} must have the shape {tuple('any' if w is None else w for w in shape)}, not {tuple(got)}")
+    if t.shape != shape:
+        _refuse(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
     if not t.is_cuda:
         _refuse(f"{name} must be on the GPU")
-    if got[-1] > 1 and t.stride(-1) != 1:
-        _refuse(f"{name} must be contiguous along its last axis")
-    return t.data_ptr()
+    _refuse(f"{name} must be contiguous along its last axis")
 
 
 def _line(t, name, dtype, size):
@@ -92,33 +96,25 @@ def _line(t, name, dtype, size):
     return None if t is None else _see(t, name, dtype, (size,))
 
 
-class _Ordered:
-    """Orders torch's current stream and the context's around a call, where they differ."""
-
-    def __init__(self, ctx):
-        import torch
-        self.current = torch.cuda.current_stream()
-        self.mine = None
-        if self.current.cuda_stream != ctx._stream:
-            if not ctx._stream and torch.cuda.is_current_stream_capturing():
-                _refuse("the default stream cannot be captured: give the context the capturing stream first (set_stream)")
-            self.mine = torch.cuda.ExternalStream(ctx._stream) if ctx._stream else torch.cuda.default_stream()
-
-    def __enter__(self):
-        if self.mine is not None:
-            self.mine.wait_stream(self.current)
-
-    def __exit__(self, *exc):
-        if self.mine is not None:
-            self.current.wait_stream(self.mine)
-
-
 class Calls:
     """Mixed into Context."""
 
     def _call(self, fn, args):
-        with _Ordered(self):
+        """Runs a call on the context's stream, ordered with torch's current stream where that is another one."""
+        if torch._C._cuda_getCurrentRawStream(self._device) == self._stream:
+            rc = fn(self._h, C.byref(args))
+            if rc:
+                self._check(rc)
+            return
+        if not self._stream and torch.cuda.is_current_stream_capturing():
+            _refuse("the default stream cannot be captured: give the context the capturing stream first (set_stream)")
+        current = torch.cuda.current_stream(self._device)
+        mine = torch.cuda.ExternalStream(self._stream, self._device) if self._stream else torch.cuda.default_stream(self._device)
+        mine.wait_stream(current)
+        try:
             self._check(fn(self._h, C.byref(args)))
+        finally:
+            current.wait_stream(mine)
 
     def adapters(self, x, down, up, starts, which, scale, ranks=None, base=None, step=None, out=None):
         """base + scale[a] * up[a]^T (down[a] x) for the tokens of every segment, a = which[segment] (-1: none).
@@ -126,7 +122,6 @@ class Calls:
         x [tokens, inputs]; down [adapters, rank, inputs], up [adapters, rank, outputs]; starts [segments + 1], which [segments],
         ranks [adapters] or None: int32; scale [adapters] float32; base [tokens, outputs] of x's type, float32, or int32 sums times
         step [outputs] float32, or None.  Returns out [tokens, outputs]; base itself may be given for it."""
-        import torch
         ty, dtype = _half(x, "x"), x.dtype
         (T, K), (A, r, N) = x.shape, up.shape
         S = which.shape[0]
@@ -145,7 +140,6 @@ class Calls:
 
     @staticmethod
     def _base(base, dtype, ty, shape):
-        import torch
         if base is None:
             return _NO_BASE, None, 0
         kind = {dtype: ty, torch.float32: _F32, torch.int32: _I32}.get(base.dtype)
@@ -156,7 +150,6 @@ class Calls:
     def adapters_grad(self, dy, x, down, up, starts, which, scale, ranks=None, base=None):
         """Gradients of `adapters` for dy [tokens, outputs]: (dx, ddown, dup), dx with `base` (the gradient that reaches x through the
         projection itself, of x's type or float32) added to it."""
-        import torch
         ty, dtype = _half(x, "x"), x.dtype
         (T, K), (A, r, N) = x.shape, up.shape
         S = which.shape[0]
@@ -176,7 +169,6 @@ class Calls:
     @staticmethod
     def _rotation(q, k, wq, wk, cos, sin, positions):
         """What the three calls on queries and keys have in common, checked: the first fields of their structs, and pointers."""
-        import torch
         ty, dtype = _half(q, "q"), q.dtype
         (T, Hq, D), Hkv = q.shape, k.shape[1]
         P, half = cos.shape
@@ -191,7 +183,6 @@ class Calls:
         """Norm of every head of q [tokens, q_heads, head] and k [tokens, kv_heads, head] with the weights wq, wk [head] float32 (or
         None), and the rotation by cos, sin [places, rot / 2] float32 at positions [tokens] int32.  Returns (q', k'); out: a pair
         for them, which may be (q, k)."""
-        import torch
         ty, dtype, (T, Hq, Hkv, D, rot, P), tables = self._rotation(q, k, wq, wk, cos, sin, positions)
         if out is None:
             out = torch.empty(T, Hq, D, dtype=dtype, device=q.device), torch.empty(T, Hkv, D, dtype=dtype, device=q.device)
@@ -205,7 +196,6 @@ class Calls:
     def qk_rotate_append(self, q, k, v, wq, wk, cos, sin, positions, k_pages, v_pages, slots, eps=1e-6, interleaved=False, out=None):
         """qk_rotate whose keys, with the values v [tokens, kv_heads, head], go to the places slots [tokens] int64 (-1: nowhere) of
         k_pages, v_pages [pages, page_size, kv_heads, head].  Returns q'."""
-        import torch
         ty, dtype, (T, Hq, Hkv, D, rot, P), tables = self._rotation(q, k, wq, wk, cos, sin, positions)
         pages, size = k_pages.shape[:2]
         v_at, pages_at = _see(v, "v", dtype, (T, Hkv, D)), self._pages(k_pages, v_pages, dtype, Hkv, D)
@@ -226,7 +216,6 @@ class Calls:
 
     def qk_rotate_grad(self, dq_out, dk_out, q, k, wq, wk, cos, sin, positions, eps=1e-6, interleaved=False):
         """Gradients of qk_rotate: (dq, dk, dwq, dwk), the weights' in float32."""
-        import torch
         ty, dtype, (T, Hq, Hkv, D, rot, P), tables = self._rotation(q, k, wq, wk, cos, sin, positions)
         dq, dk = (torch.empty(T, h, D, dtype=dtype, device=q.device) for h in (Hq, Hkv))
         dw = torch.empty(2, D, dtype=torch.float32, device=q.device)
@@ -242,7 +231,6 @@ class Calls:
         """Attention of the new tokens q [tokens, q_heads, head] of every request, starts [requests + 1] int32, over its lengths
         [requests] int32 places in k_pages, v_pages [pages, page_size, kv_heads, head], found through table [requests, width] int32;
         causal, and over the last `window` places alone if that is not 0.  scale: head ** -0.5 if None.  Returns out like q."""
-        import torch
         ty, dtype = _half(q, "q"), q.dtype
         T, Hq, D = q.shape
         pages, size, Hkv = k_pages.shape[:3]
