@@ -11,8 +11,9 @@
 // type for the second product (their sum is not): an error of the size of the result's own rounding.
 //
 // Masks: a place that no row of the tile attends to is not read at all.  A place that some rows attend to and others do not has weight
-// 0 for the others, which a matrix instruction multiplies with the value all the same; so where values of such places are
-// infinite or NaN, the step is done row by row with the hidden places' values taken out.
+// 0 for the others, which a matrix instruction multiplies with the value all the same.  So where a step's places are not attended to
+// by all rows and some of their values are infinite or NaN, those values are taken out, and products of the weights with ones in
+// their places say which rows they reach.
 #include <algorithm>
 #include <type_traits>
 
@@ -23,13 +24,24 @@ namespace she { namespace clear {
 namespace {
 
 constexpr int FEW_ROWS = 16, FEW_WAVES = 4, MOST_CHUNK = 2048;
+constexpr int TILE_WAVES = 4, TILE_ROWS = 32 * TILE_WAVES, STEP = 64;   // rows of a workgroup, places of a step
 constexpr float LOG2E = 1.4426950408889634f;
 
 struct Work {                            // of the pieces of a cut row, [tokens * q_heads][splits]
     float *o;                            // [..][head]
     float2 *ml;
-    uint32_t chunk, splits;
+    uint32_t few_chunk, tile_chunk, splits;
+    uint32_t few_most;                   // rows that a request has at most to be k_attend_few's
+    uint32_t few_each;                   // slots of every request there; 0: they are found by find_piece
 };
+__device__ inline Piece few_piece(const she_attend_pages_args &a, uint32_t group, const Work &w)
+{
+    if (!w.few_each) return find_piece(a.starts, a.requests, a.tokens, group, FEW_ROWS, blockIdx.x);
+    const int r = blockIdx.x / w.few_each;
+    const int64_t b = bounded_start(a.starts, r, a.tokens) * group, e = bounded_start(a.starts, r + 1, a.tokens) * group;
+    const int index = blockIdx.x % w.few_each;
+    return Piece{b + (int64_t)index * FEW_ROWS < e ? r : -1, index, b, e};
+}
 
 // A tile of rows and the places that any of them attends to.
 struct Span {
@@ -84,6 +96,29 @@ template <class T> __device__ inline bool has_special(u32x4 v)
     return any;
 }
 
+// Of eight values: the finite ones, zeros in the places of the others; and ones in the places of those of a kind, zeros elsewhere.
+enum { UP_INF, DOWN_INF, NOT_A_NUMBER, KINDS };
+template <class T> __device__ inline u32x4 finite_part(u32x4 v)
+{
+    constexpr uint32_t E = std::is_same<T, __bf16>::value ? 0x7F80u : 0x7C00u;
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+        v[i] &= ((v[i] & E) == E ? 0u : 0xFFFFu) | ((v[i] & E << 16) == E << 16 ? 0u : 0xFFFF0000u);
+    return v;
+}
+template <class T> __device__ inline u32x4 ones_at(u32x4 v, int kind)
+{
+    constexpr uint32_t E = std::is_same<T, __bf16>::value ? 0x7F80u : 0x7C00u, ONE = std::is_same<T, __bf16>::value ? 0x3F80u : 0x3C00u;
+    auto is = [&](uint32_t x) { return kind == NOT_A_NUMBER ? (x & 0x7FFFu) > E : x == (kind == UP_INF ? E : E | 0x8000u); };
+#pragma unroll
+    for (int i = 0; i < 4; i++) v[i] = (is(v[i] & 0xFFFFu) ? ONE : 0u) | (is(v[i] >> 16) ? ONE << 16 : 0u);
+    return v;
+}
+__device__ inline float value_of(int kind)
+{
+    return kind == UP_INF ? __builtin_inff() : kind == DOWN_INF ? -__builtin_inff() : __builtin_nanf("");
+}
+
 // Few rows: every wavefront walks places of its own, 32 a step, four steps of the workgroup side by side, straight from memory.  Lane
 // l reads d = 32 s + 8 (l/16) .. of the key of place l%16 for the scores, and EL elements from EL (l%16) on of the values of the
 // eight places that its scores belong to, whole rows over 16 lanes; the eight rows are transposed in registers.
@@ -97,10 +132,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void k_attend_few(she_attend_pag
     __shared__ int any_bad;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, quarter = lane >> 4;
     const int kv_head = blockIdx.y, D = (int)a.head;
-    const Piece piece = find_piece(a.starts, a.requests, a.tokens, group, FEW_ROWS, blockIdx.x);
-    const Span sp = span_of<FEW_ROWS>(a, group, piece, piece.index * FEW_ROWS, w.chunk);
-    if (sp.request < 0 || (int)blockIdx.z >= max(sp.parts, 1)) return;
-    const int from = sp.from + (int)blockIdx.z * (int)w.chunk, count = sp.parts ? min((int)w.chunk, sp.to - from) : 0;
+    const Piece piece = few_piece(a, group, w);
+    if (piece.segment < 0 || piece.last - piece.first > w.few_most) return;
+    const Span sp = span_of<FEW_ROWS>(a, group, piece, piece.index * FEW_ROWS, w.few_chunk);
+    if ((int)blockIdx.z >= max(sp.parts, 1)) return;
+    const int from = sp.from + (int)blockIdx.z * (int)w.few_chunk, count = sp.parts ? min((int)w.few_chunk, sp.to - from) : 0;
     if (tid == 0) any_bad = 0;
     __syncthreads();
     look_up(a, sp.request, kv_head, from, count, rows, &any_bad, d_bad);
@@ -161,17 +197,13 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void k_attend_few(she_attend_pag
 
         const bool masked = unsafe || k0 + 32 > count || from + k0 + 31 > high_min || from + k0 < low_max;
         float s[8], top = m;
-        uint32_t hidden = 0;                                      // which of the lane's eight places its row does not attend to
 #pragma unroll
         for (int e = 0; e < 8; e++) s[e] = st[e / 4][e % 4] * scale;
         if (masked) {
 #pragma unroll
             for (int e = 0; e < 8; e++) {
                 const int place = from + k0 + (e < 4 ? 0 : 16) + quarter * 4 + (e & 3);
-                if (!(there >> e & 1) || place > high || place < low) {
-                    s[e] = -__builtin_inff();
-                    hidden |= 1u << e;
-                }
+                if (!(there >> e & 1) || place > high || place < low) s[e] = -__builtin_inff();
             }
         }
 #pragma unroll
@@ -213,21 +245,25 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void k_attend_few(she_attend_pag
                 for (int e = 0; e < EL; e++) acc[b][e] = mfma16(v[e], p, acc[b][e]);
             }
         } else {
-            for (int c = 0; c < FEW_ROWS; c++) {
-                // the places that row c does not attend to: a quarter's eight are known to the quarter's lane of column c
-                const uint32_t out = __shfl(hidden, quarter * 16 + c);
 #pragma unroll
-                for (int b = 0; b < NB; b++) {
-                    u32x4 kept[8];
+            for (int b = 0; b < NB; b++) {
+                u32x4 some[8];
+                x8<T> v[EL];
 #pragma unroll
-                    for (int e = 0; e < 8; e++) kept[e] = out >> e & 1 ? u32x4{0, 0, 0, 0} : vraw[b][e];
-                    x8<T> v[EL];
-                    transpose8<T, EL>(kept, v);
+                for (int e = 0; e < 8; e++) some[e] = finite_part<T>(vraw[b][e]);
+                transpose8<T, EL>(some, v);
+#pragma unroll
+                for (int e = 0; e < EL; e++) acc[b][e] = mfma16(v[e], p, acc[b][e]);
+#pragma unroll 1
+                for (int kind = 0; kind < KINDS; kind++) {
+#pragma unroll
+                    for (int e = 0; e < 8; e++) some[e] = ones_at<T>(vraw[b][e], kind);
+                    transpose8<T, EL>(some, v);
 #pragma unroll
                     for (int e = 0; e < EL; e++) {
                         const f32x4 o = mfma16(v[e], p, f32x4{0, 0, 0, 0});
 #pragma unroll
-                        for (int i = 0; i < 4; i++) acc[b][e][i] += col == c ? o[i] : 0.0f;
+                        for (int i = 0; i < 4; i++) acc[b][e][i] += o[i] > 0 ? value_of(kind) : 0.0f;
                     }
                 }
             }
@@ -280,23 +316,242 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void k_attend_few(she_attend_pag
     }
 }
 
+// Many rows: a workgroup has TILE_ROWS of them, 32 a wavefront, and steps through the places STEP at a time with both tiles of the step
+// in LDS, twice over, so that the next step's are on their way while this one's are used.  The matrix instructions are 32 x 32 x 16:
+// lane l has row l%32 of the tile, and of every 32 places the scores of 8 (i/4) + 4 (l/32) + i%4.  The second product's operand is
+// V transposed, which LDS reads hand over four places at a time.
+//
+// LDS: a place's row of DP elements, its 16-byte units exchanged by place so that neighbouring lanes, which read the same unit of
+// neighbouring places (keys) or four places of one pair of units (values), reach all banks.
+template <int DP> __device__ inline int key_unit(int place, int unit)
+{
+    return unit ^ (DP == 64 ? (place >> 1) & 7 : place & 15);
+}
+template <int DP> __device__ inline int value_unit(int place, int unit)
+{
+    return unit ^ (DP == 64 ? ((place >> 1) & 3) << 1 : (place & 7) << 1);
+}
+
+template <class T, int DP>
+__global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_tile(she_attend_pages_args a, uint32_t group, Work w, const void *zeros, uint32_t *d_bad)
+{
+    constexpr int UNITS = DP / 8, KS = DP / 16, DB = DP / 32, BLOCK = 4 * STEP;      // places that are looked up together
+    constexpr int EACH = STEP * UNITS / (64 * TILE_WAVES);                           // units of either tile that a thread brings
+    __shared__ __align__(16) T even_keys[STEP * DP], even_values[STEP * DP], odd_keys[STEP * DP], odd_values[STEP * DP];
+    __shared__ int64_t rows[2][BLOCK];
+    __shared__ uint64_t missing[2][BLOCK / 64];                                      // places that their page id keeps out
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
+    const int kv_head = blockIdx.x, D = (int)a.head;
+    // late tokens have most to attend to: they come first
+    const Piece piece = find_piece(a.starts, a.requests, a.tokens, group, TILE_ROWS, gridDim.y - 1 - blockIdx.y);
+    if (piece.segment < 0 || piece.last - piece.first <= w.few_most) return;
+    const Span sp = span_of<TILE_ROWS>(a, group, piece, piece.index * TILE_ROWS, w.tile_chunk);
+    if ((int)blockIdx.z >= max(sp.parts, 1)) return;
+    const int from = sp.from + (int)(blockIdx.z * w.tile_chunk), count = sp.parts ? min((int)w.tile_chunk, sp.to - from) : 0;
+    const int steps = (count + STEP - 1) / STEP;
+
+    // this lane's row, and what the wavefront's rows attend to
+    const int last_row = sp.row + sp.rows - 1, first_here = sp.row + wave * 32, last_here = min(first_here + 31, last_row);
+    const int my_row = min(first_here + col, last_row), my_token = my_row / (int)group, my_head = kv_head * (int)group + my_row % (int)group;
+    const int64_t reach = a.window ? (int64_t)a.window - 1 : (int64_t)1 << 40;
+    const int high = sp.first + my_token, low = (int)max(high - reach, (int64_t)0);
+    const int high_min = sp.first + min(first_here, last_row) / (int)group, high_max = sp.first + last_here / (int)group;
+    const int low_min = (int)max(high_min - reach, (int64_t)0), low_max = (int)max(high_max - reach, (int64_t)0);
+
+    // the rows of a block of places: thread tid has place BLOCK * b + tid, a wavefront a step
+    auto page_of = [&](int b) {
+        const int i = b * BLOCK + tid;
+        if (i >= count) return -1;
+        const int32_t page = a.table[sp.request * a.table_stride + (uint32_t)(from + i) / a.page_size];
+        if (page >= 0 && (uint32_t)page < a.pages) return (int)page;
+        if ((uint32_t)(from + i) % a.page_size == 0 || i == 0) count_bad(d_bad);
+        return -1;
+    };
+    auto keep_rows = [&](int b, int page) {
+        const int i = b * BLOCK + tid;
+        rows[b & 1][tid] = page < 0 ? -1 : page * a.page_stride + (int64_t)((uint32_t)(from + i) % a.page_size) * a.slot_stride + kv_head * a.page_head;
+        const uint64_t out = __ballot(page < 0 && i < count);
+        if (lane == 0) missing[b & 1][wave] = out;
+    };
+    // a step's tiles on their way into LDS: a wavefront's 64 units lie side by side there, so each lane picks the one that belongs in
+    // its place; what is not there comes from a unit of zeros
+    auto request = [&](int step, T *keys, T *values) {
+#pragma unroll
+        for (int e = 0; e < EACH; e++) {
+            const int first = (e * TILE_WAVES + wave) * 64, place = tid / UNITS + e * (64 * TILE_WAVES / UNITS), unit = tid % UNITS;
+            const int64_t row = rows[step / 4 & 1][step % 4 * STEP + place];
+            const int key = key_unit<DP>(place, unit) * 8, value = value_unit<DP>(place, unit) * 8;
+            to_lds(row >= 0 && key < D ? (const T *)a.k_pages + row + key : (const T *)zeros, keys + first * 8);
+            to_lds(row >= 0 && value < D ? (const T *)a.v_pages + row + value : (const T *)zeros, values + first * 8);
+        }
+    };
+
+    x8<T> q[KS];
+    {
+        const T *p = (const T *)a.q + (sp.token0 + my_token) * a.q_token + my_head * a.q_head + half * 8;
+#pragma unroll
+        for (int s = 0; s < KS; s++) {
+            u32x4 v = load8<T, true>(p + s * 16, D - (s * 16 + half * 8));
+            if (a.scale < 0) v ^= 0x80008000u;                    // so that the largest score is the largest product
+            q[s] = as_x8<T>(v);
+        }
+    }
+    const float scale = fmaxf(fabsf(a.scale) * LOG2E, 1e-37f);    // not 0: hidden places are -inf before it
+    float m = -__builtin_inff(), l = 0;
+    f32x16 acc[DB];
+#pragma unroll
+    for (int b = 0; b < DB; b++) acc[b] = f32x16{};
+
+    if (steps) {
+        keep_rows(0, page_of(0));
+        __syncthreads();
+        request(0, even_keys, even_values);
+    }
+    // Bytes from a tile's start: of the key of place `col`, its unit `half`; and of the value of place half * 4 + (lane & 15) / 4, from
+    // element (lane & 16) + (lane & 3) * 4 on.  Later units are exchanged alike, so that theirs follow by exclusive or, and the
+    // same unit of 8, 16 or 32 places later follows by adding.
+    const int key_at = col * DP * 2 + key_unit<DP>(col, half) * 16;
+    const int value_place = half * 4 + (lane & 15) / 4, value_d = (lane & 16) + (lane & 3) * 4;
+    const int value_at = value_place * DP * 2 + value_unit<DP>(value_place, value_d / 8) * 16 + value_d % 8 * 2;
+    int page = -1;
+    auto do_step = [&](int step, const T *key_tile, const T *value_tile, T *next_keys, T *next_values) {
+        wait_for_lds_loads();
+        __syncthreads();                                          // this step's tiles are there, the others are free
+        if (step % 4 == 0) page = page_of(step / 4 + 1);
+        if (step % 4 == 1) keep_rows(step / 4 + 1, page);
+        if (step + 1 < steps) request(step + 1, next_keys, next_values);
+        const char *keys = reinterpret_cast<const char *>(key_tile), *values = reinterpret_cast<const char *>(value_tile);
+        const int p0 = from + step * STEP;
+        const uint64_t gone = missing[step / 4 & 1][step % 4];
+        if (first_here <= last_row && p0 <= high_max && p0 + STEP > low_min) {
+            f32x16 s[2];
+#pragma unroll
+            for (int t = 0; t < 2; t++) {
+                s[t] = f32x16{};
+#pragma unroll
+                for (int k = 0; k < KS; k++) s[t] = mfma32(*reinterpret_cast<const x8<T> *>(keys + t * 32 * DP * 2 + (key_at ^ k * 32)), q[k], s[t]);
+            }
+                const bool masked = gone || p0 + STEP - 1 > high_min || p0 < low_max || step * STEP + STEP > count;
+            bool special = false;
+            if (masked) {
+                const int from_here = p0 + 4 * half, most = high - from_here, least = low - from_here;
+                const uint64_t out = gone >> 4 * half;
+#pragma unroll
+                for (int t = 0; t < 2; t++)
+#pragma unroll
+                    for (int i = 0; i < 16; i++) {
+                        const int n = t * 32 + 8 * (i / 4) + i % 4;
+                        if (n > most || n < least || (out >> n & 1)) s[t][i] = -__builtin_inff();
+                    }
+                for (int i = lane; i < STEP * UNITS; i += 64) special |= has_special<T>(*reinterpret_cast<const u32x4 *>(values + i * 16));
+            }
+            float top = s[0][0];
+#pragma unroll
+            for (int t = 0; t < 2; t++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) top = fmaxf(top, s[t][i]);
+            top = fmaxf(top, __shfl_xor(top, 32)) * scale;
+            // the reference need not be the top itself: it is raised where a weight would exceed 2^8
+            if (__ballot(top > m + 8.0f)) {
+                const float to = fmaxf(m, top), ref = to == -__builtin_inff() ? 0.0f : to, alpha = __builtin_amdgcn_exp2f(m - ref);
+                m = to;
+                l *= alpha;
+#pragma unroll
+                for (int b = 0; b < DB; b++)
+#pragma unroll
+                    for (int i = 0; i < 16; i++) acc[b][i] *= alpha;
+            }
+            const float ref = m == -__builtin_inff() ? 0.0f : m;
+            x8<T> p[4];
+#pragma unroll
+            for (int t = 0; t < 2; t++)
+#pragma unroll
+                for (int i = 0; i < 16; i++) {
+                    const float v = __builtin_amdgcn_exp2f(fmaf(s[t][i], scale, -ref));
+                    l += v;
+                    p[t * 2 + i / 8][i % 8] = (T)v;
+                }
+                // V^T of the 32 elements from 32 b on and the sixteen places from 16 k on, in the scores' order
+            auto columns = [&](int b, int k) {
+                u32x4 v;
+#pragma unroll
+                for (int e = 0; e < 2; e++) {
+                    const u32x2 c = lds_columns(values + (k * 16 + e * 8) * DP * 2 + (value_at ^ b * 64));
+                    v[e * 2] = c[0];
+                    v[e * 2 + 1] = c[1];
+                }
+                return v;
+            };
+            if (!__ballot(special)) {
+#pragma unroll
+                for (int k = 0; k < 4; k++)
+#pragma unroll
+                    for (int b = 0; b < DB; b++) acc[b] = mfma32(as_x8<T>(columns(b, k)), p[k], acc[b]);
+            } else {
+#pragma unroll
+                for (int b = 0; b < DB; b++) {
+#pragma unroll
+                    for (int k = 0; k < 4; k++) acc[b] = mfma32(as_x8<T>(finite_part<T>(columns(b, k))), p[k], acc[b]);
+#pragma unroll 1
+                    for (int kind = 0; kind < KINDS; kind++) {
+                        f32x16 o{};
+#pragma unroll
+                        for (int k = 0; k < 4; k++) o = mfma32(as_x8<T>(ones_at<T>(columns(b, k), kind)), p[k], o);
+#pragma unroll
+                        for (int i = 0; i < 16; i++) acc[b][i] += o[i] > 0 ? value_of(kind) : 0.0f;
+                    }
+                }
+            }
+        }
+    };
+    for (int step = 0; step < steps; step += 2) {
+        do_step(step, even_keys, even_values, odd_keys, odd_values);
+        if (step + 1 < steps) do_step(step + 1, odd_keys, odd_values, even_keys, even_values);
+    }
+
+    l += __shfl_xor(l, 32);
+    if (first_here + col > last_row) return;
+    const int64_t token = sp.token0 + my_token;
+    const size_t at = (size_t)(token * a.q_heads + my_head) * w.splits + blockIdx.z;
+    const float inv = sp.parts > 1 ? 1.0f : l == 0 ? 0.0f : 1.0f / l;
+    if (sp.parts > 1 && half == 0) w.ml[at] = float2{m, l};
+#pragma unroll
+    for (int b = 0; b < DB; b++)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const int d = b * 32 + 2 * i + 4 * half;
+            if (d >= D) continue;
+            if (sp.parts > 1) {
+                *reinterpret_cast<f32x4 *>(w.o + at * D + d) = f32x4{acc[b][i], acc[b][i + 1], acc[b][i + 2], acc[b][i + 3]};
+            } else {
+                T *to = (T *)a.out + token * a.out_token + my_head * a.out_head + d;
+                T v[4];
+#pragma unroll
+                for (int e = 0; e < 4; e++) v[e] = (T)(acc[b][i + e] * inv);
+                *reinterpret_cast<uint2 *>(to) = *reinterpret_cast<const uint2 *>(v);
+            }
+        }
+}
+
 // The rows that were cut: a wavefront a row.
 template <class T>
 __global__ __launch_bounds__(256) void k_attend_join(she_attend_pages_args a, uint32_t group, Work w)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = (int)a.head;
     const Piece piece = find_piece(a.starts, a.requests, a.tokens, group, FEW_ROWS, blockIdx.x);
-    const Span sp = span_of<FEW_ROWS>(a, group, piece, piece.index * FEW_ROWS, w.chunk);
-    if (sp.request < 0 || sp.parts <= 1) return;
-    for (int r = wave; r < sp.rows; r += 4) {
-        const int row = sp.row + r;
-        const int64_t token = sp.token0 + row / (int)group;
-        const int head = blockIdx.y * (int)group + row % (int)group;
+    if (piece.segment < 0) return;
+    const int first = piece.index * FEW_ROWS, rows = (int)min((int64_t)FEW_ROWS, piece.last - piece.first - first);
+    const int parts = piece.last - piece.first <= w.few_most ? span_of<FEW_ROWS>(a, group, piece, first, w.few_chunk).parts
+                                                             : span_of<TILE_ROWS>(a, group, piece, first / TILE_ROWS * TILE_ROWS, w.tile_chunk).parts;
+    if (parts <= 1) return;
+    for (int r = wave; r < rows; r += 4) {
+        const int64_t row = piece.first + first + r, token = row / group;
+        const int head = blockIdx.y * (int)group + (int)(row % group);
         const size_t at = (size_t)(token * a.q_heads + head) * w.splits;
         float top = -__builtin_inff(), sum = 0;
-        for (int k = 0; k < sp.parts; k++) top = fmaxf(top, w.ml[at + k].x);
+        for (int k = 0; k < parts; k++) top = fmaxf(top, w.ml[at + k].x);
         float o[4] = {0, 0, 0, 0};
-        for (int k = 0; k < sp.parts; k++) {
+        for (int k = 0; k < parts; k++) {
             const float2 ml = w.ml[at + k];
             const float f = ml.x == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(ml.x - top);
             sum = fmaf(ml.y, f, sum);
@@ -312,16 +567,28 @@ __global__ __launch_bounds__(256) void k_attend_join(she_attend_pages_args a, ui
     }
 }
 
-template <class T> hipError_t attend(const she_attend_pages_args &a, const AttendShape &s, const Work &w, uint32_t *d_bad, hipStream_t st)
+template <class T, int DP> hipError_t attend_rows(const she_attend_pages_args &a, const AttendShape &s, const Work &w, uint32_t *d_bad, hipStream_t st)
 {
     const uint32_t group = a.q_heads / a.kv_heads;
-    const dim3 grid((uint32_t)s.few_slots, a.kv_heads, s.splits);
-    if (a.head <= 64) k_attend_few<T, 64><<<grid, 64 * FEW_WAVES, 0, st>>>(a, group, w, d_bad);
-    else if (a.head <= 128) k_attend_few<T, 128><<<grid, 64 * FEW_WAVES, 0, st>>>(a, group, w, d_bad);
-    else k_attend_few<T, 256><<<grid, 64 * FEW_WAVES, 0, st>>>(a, group, w, d_bad);
-    hipError_t rc = hipGetLastError();
-    if (rc != hipSuccess || s.splits <= 1) return rc;
-    k_attend_join<T><<<dim3((uint32_t)s.few_slots, a.kv_heads), 256, 0, st>>>(a, group, w);
+    hipError_t rc = hipSuccess;
+    if (s.few_slots) {
+        k_attend_few<T, DP><<<dim3((uint32_t)s.few_slots, a.kv_heads, s.few_splits), 64 * FEW_WAVES, 0, st>>>(a, group, w, d_bad);
+        rc = hipGetLastError();
+    }
+    if (rc == hipSuccess && s.tile_slots) {
+        k_attend_tile<T, DP><<<dim3(a.kv_heads, (uint32_t)s.tile_slots, s.tile_splits), 64 * TILE_WAVES, 0, st>>>(a, group, w, zeros_of(d_bad), d_bad);
+        rc = hipGetLastError();
+    }
+    return rc;
+}
+
+template <class T> hipError_t attend(const she_attend_pages_args &a, const AttendShape &s, const Work &w, uint32_t *d_bad, hipStream_t st)
+{
+    hipError_t rc = a.head <= 64 ? attend_rows<T, 64>(a, s, w, d_bad, st) : a.head <= 128 ? attend_rows<T, 128>(a, s, w, d_bad, st)
+                                                                                          : attend_rows<T, 256>(a, s, w, d_bad, st);
+    if (rc != hipSuccess || w.splits <= 1) return rc;
+    const uint32_t group = a.q_heads / a.kv_heads;
+    k_attend_join<T><<<dim3((uint32_t)(a.tokens * (uint64_t)group / FEW_ROWS + a.requests), a.kv_heads), 256, 0, st>>>(a, group, w);
     return hipGetLastError();
 }
 
@@ -331,25 +598,35 @@ AttendShape attend_shape(const she_attend_pages_args &a, uint32_t cus)
 {
     AttendShape s{};
     const uint64_t group = a.q_heads / a.kv_heads, longest = std::min<uint64_t>((uint64_t)a.table_width * a.page_size, 0x7FFFFFFF);
-    s.few_slots = a.tokens * group / FEW_ROWS + a.requests;
-    s.tile_slots = 0;
+    const uint64_t rows = a.tokens * group;
+    if (!cus) cus = 1;
+    // Requests of few rows go to k_attend_few and the others to k_attend_tile.  The lengths are on the device; the host knows that
+    // there is one request, or that they have a token each on average, and leaves the other kernel out.
+    s.few_most = a.requests == 1 ? (rows <= 64 ? 0x7FFFFFFF : 0) : a.tokens <= a.requests ? 0x7FFFFFFF : 2 * FEW_ROWS;
+    s.few_each = s.few_most == 0x7FFFFFFF ? 0 : s.few_most / FEW_ROWS;
+    s.few_slots = s.few_most == 0x7FFFFFFF ? rows / FEW_ROWS + a.requests : (uint64_t)a.requests * s.few_each;
+    s.tile_slots = s.few_most == 0x7FFFFFFF ? 0 : rows / TILE_ROWS + a.requests;
     // pieces short enough for eight workgroups per compute unit, long enough that joining them costs little
-    const uint64_t places = s.few_slots * a.kv_heads * longest;
-    s.chunk = (uint32_t)std::min<uint64_t>(MOST_CHUNK, std::max<uint64_t>(256, ceil_div(places / (8 * (cus ? cus : 1)), 128) * 128));
-    // a span starts at a multiple of 32 below its first place
-    s.splits = (uint32_t)std::max<uint64_t>(1, ceil_div(longest, s.chunk));
+    s.few_chunk = (uint32_t)std::min<uint64_t>(MOST_CHUNK, std::max<uint64_t>(256, ceil_div(s.few_slots * a.kv_heads * longest / (8 * cus), 128) * 128));
+    s.few_splits = s.few_slots ? (uint32_t)std::max<uint64_t>(1, ceil_div(longest, s.few_chunk)) : 1;
+    // and for two of k_attend_tile's
+    s.tile_chunk = (uint32_t)std::max<uint64_t>(512, ceil_div(s.tile_slots * a.kv_heads * longest / (2 * cus), STEP) * STEP);
+    s.tile_splits = s.tile_slots ? (uint32_t)std::max<uint64_t>(1, ceil_div(longest, s.tile_chunk)) : 1;
     return s;
 }
 
 size_t attend_scratch(const she_attend_pages_args &a, const AttendShape &s)
 {
-    return s.splits <= 1 ? 0 : (size_t)a.tokens * a.q_heads * s.splits * (a.head * sizeof(float) + sizeof(float2));
+    const uint32_t splits = std::max(s.few_splits, s.tile_splits);
+    return splits <= 1 ? 0 : (size_t)a.tokens * a.q_heads * splits * (a.head * sizeof(float) + sizeof(float2));
 }
 
 hipError_t launch_attend_pages(const she_attend_pages_args &a, const AttendShape &s, void *scratch, uint32_t *d_bad, hipStream_t st)
 {
-    const size_t rows = (size_t)a.tokens * a.q_heads * s.splits;
-    const Work w{static_cast<float *>(scratch), reinterpret_cast<float2 *>(static_cast<float *>(scratch) + rows * a.head), s.chunk, s.splits};
+    const uint32_t splits = std::max(s.few_splits, s.tile_splits);
+    const size_t rows = (size_t)a.tokens * a.q_heads * splits;
+    const Work w{static_cast<float *>(scratch), reinterpret_cast<float2 *>(static_cast<float *>(scratch) + rows * a.head),
+                 s.few_chunk, s.tile_chunk, splits, s.few_most, s.few_each};
     return a.type == SHE_BF16 ? attend<__bf16>(a, s, w, d_bad, st) : attend<_Float16>(a, s, w, d_bad, st);
 }
 

@@ -75,6 +75,21 @@ template <class T, int COLS> __device__ inline void transpose8(const u32x4 rows[
     }
 }
 
+// Of the 4 x 16 elements that sixteen neighbouring lanes point at, four neighbours each and four lanes a row, lane c gets column c.
+using u32x2 = uint32_t __attribute__((ext_vector_type(2)));
+using s16x4 = short __attribute__((ext_vector_type(4)));
+__device__ inline u32x2 lds_columns(const void *p)
+{
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p));
+}
+
+// A wavefront's 64 units of 16 bytes, each from its lane's address, to LDS from `to` on; they are there after wait_for_lds_loads.
+__device__ inline void to_lds(const void *from, void *to)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
+__device__ inline void wait_for_lds_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }      // vmcnt(0)
+
 // LDS that one wavefront alone uses: its operations run in order, and this keeps the compiler from moving them.
 __device__ inline void wave_lds_fence()
 {

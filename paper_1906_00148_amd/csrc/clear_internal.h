@@ -7,6 +7,10 @@
 
 namespace she { namespace clear {
 
+// Beside the count of bad ids the context keeps a unit of zeros, for kernels that bring tiles with holes.
+constexpr uint32_t COUNTERS = 8, ZEROS_AT = 4;   // words of that memory, and where the unit starts
+inline const void *zeros_of(const uint32_t *d_bad) { return d_bad + ZEROS_AT; }
+
 inline uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
 // ---- queries and keys
@@ -33,9 +37,10 @@ hipError_t launch_adapters_grad(const she_adapters_grad_args &a, void *scratch, 
 
 // ---- attention
 struct AttendShape {
-    uint32_t chunk;          // places of the cache that a workgroup walks
-    uint32_t splits;         // workgroups that share a row's places at most
-    uint64_t few_slots, tile_slots;
+    uint64_t few_slots, tile_slots;      // tiles of rows, at most, of either kernel; 0: it is not launched
+    uint32_t few_chunk, tile_chunk;      // places of the cache that a workgroup walks
+    uint32_t few_splits, tile_splits;    // workgroups that share a row's places at most
+    uint32_t few_most, few_each;         // rows of a request that the first kernel takes, slots that it has for each
 };
 AttendShape attend_shape(const she_attend_pages_args &a, uint32_t cus);
 size_t attend_scratch(const she_attend_pages_args &a, const AttendShape &s);

@@ -11,8 +11,8 @@ constexpr uint64_t MOST_TOKENS = 1u << 24, MOST_WIDTH = 1u << 24, MOST_PLACES = 
 int ready(she_ctx *c)
 {
     if (c->clear.d_bad) return SHE_OK;
-    HIP_TRY(c, hipMalloc((void **)&c->clear.d_bad, sizeof(uint32_t)));
-    hipError_t rc = hipMemset(c->clear.d_bad, 0, sizeof(uint32_t));
+    HIP_TRY(c, hipMalloc((void **)&c->clear.d_bad, clear::COUNTERS * sizeof(uint32_t)));
+    hipError_t rc = hipMemset(c->clear.d_bad, 0, clear::COUNTERS * sizeof(uint32_t));
     if (rc == hipSuccess) rc = hipStreamSynchronize(nullptr);
     if (rc != hipSuccess) {
         hipFree(c->clear.d_bad);

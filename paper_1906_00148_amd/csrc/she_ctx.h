@@ -32,7 +32,7 @@ struct LeveledPools {         // leveled mode: TRGSW selectors (spectral form) a
 struct ClearWork {            // the clear side's scratch (she_clear.h); freed with the context
     void *scratch = nullptr;
     size_t bytes = 0;
-    uint32_t *d_bad = nullptr;      // ids out of range that its kernels have met
+    uint32_t *d_bad = nullptr;      // ids out of range that its kernels have met, and a unit of zeros (clear::COUNTERS words)
     ~ClearWork() { hipFree(scratch); hipFree(d_bad); }
 };
 // Layer operators recorded between she_defer_begin and she_defer_run: one netlist for all of them, so that the
