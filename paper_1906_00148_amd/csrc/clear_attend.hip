@@ -11,9 +11,8 @@
 // type for the second product (their sum is not): an error of the size of the result's own rounding.
 //
 // Masks: a place that no row of the tile attends to is not read at all.  A place that some rows attend to and others do not has weight
-// 0 for the others, which a matrix instruction multiplies with the value all the same.  So where a step's places are not attended to
-// by all rows and some of their values are infinite or NaN, those values are taken out, and products of the weights with ones in
-// their places say which rows they reach.
+// 0 for the others, which a matrix instruction multiplies with the value all the same.  So where some of such places' values are
+// infinite or NaN, the tile's rows are done again, one by one and over the places that they attend to alone.
 #include <algorithm>
 #include <type_traits>
 
@@ -96,27 +95,56 @@ template <class T> __device__ inline bool has_special(u32x4 v)
     return any;
 }
 
-// Of eight values: the finite ones, zeros in the places of the others; and ones in the places of those of a kind, zeros elsewhere.
-enum { UP_INF, DOWN_INF, NOT_A_NUMBER, KINDS };
-template <class T> __device__ inline u32x4 finite_part(u32x4 v)
+// One row over those of the places [from, to) that it attends to, by one wavefront: scores with a place a lane, sums with elements on
+// the lanes.  Writes the row's result, or its piece's.
+template <class T>
+__device__ void attend_row(const she_attend_pages_args &a, uint32_t group, const Work &w, const Span &sp, int kv_head, int row, int from, int to)
 {
-    constexpr uint32_t E = std::is_same<T, __bf16>::value ? 0x7F80u : 0x7C00u;
-#pragma unroll
-    for (int i = 0; i < 4; i++)
-        v[i] &= ((v[i] & E) == E ? 0u : 0xFFFFu) | ((v[i] & E << 16) == E << 16 ? 0u : 0xFFFF0000u);
-    return v;
-}
-template <class T> __device__ inline u32x4 ones_at(u32x4 v, int kind)
-{
-    constexpr uint32_t E = std::is_same<T, __bf16>::value ? 0x7F80u : 0x7C00u, ONE = std::is_same<T, __bf16>::value ? 0x3F80u : 0x3C00u;
-    auto is = [&](uint32_t x) { return kind == NOT_A_NUMBER ? (x & 0x7FFFu) > E : x == (kind == UP_INF ? E : E | 0x8000u); };
-#pragma unroll
-    for (int i = 0; i < 4; i++) v[i] = (is(v[i] & 0xFFFFu) ? ONE : 0u) | (is(v[i] >> 16) ? ONE << 16 : 0u);
-    return v;
-}
-__device__ inline float value_of(int kind)
-{
-    return kind == UP_INF ? __builtin_inff() : kind == DOWN_INF ? -__builtin_inff() : __builtin_nanf("");
+    const int lane = threadIdx.x & 63, D = (int)a.head;
+    const int64_t token = sp.token0 + row / (int)group;
+    const int head = kv_head * (int)group + row % (int)group, high = sp.first + row / (int)group;
+    const int low = a.window ? (int)max((int64_t)high - (int64_t)a.window + 1, (int64_t)0) : 0;
+    const T *q = (const T *)a.q + token * a.q_token + head * a.q_head;
+    float top = -__builtin_inff(), sum = 0, o[4] = {0, 0, 0, 0};
+    to = min(to, high + 1);
+    for (int first = max(from, low); first < to; first += 64) {
+        const int place = first + lane;
+        const int32_t page = place < to ? a.table[sp.request * a.table_stride + (uint32_t)place / a.page_size] : -1;
+        const bool there = page >= 0 && (uint32_t)page < a.pages;
+        const int64_t at = there ? page * a.page_stride + (int64_t)((uint32_t)place % a.page_size) * a.slot_stride + kv_head * a.page_head : 0;
+        float s = 0;
+        if (there)
+            for (int d = 0; d < D; d += 8) {
+                float x[8], y[8];
+                unpack<T>(load8<T, true>(q + d, 8), x);
+                unpack<T>(load8<T, true>((const T *)a.k_pages + at + d, 8), y);
+                for (int i = 0; i < 8; i++) s = fmaf(x[i], y[i], s);
+            }
+        s = there ? s * a.scale * LOG2E : -__builtin_inff();
+        float next = fmaxf(top, s);
+        for (int m = 1; m < 64; m *= 2) next = fmaxf(next, __shfl_xor(next, m));
+        const float ref = next == -__builtin_inff() ? 0.0f : next, alpha = __builtin_amdgcn_exp2f(top - ref), p = __builtin_amdgcn_exp2f(s - ref);
+        top = next;
+        sum *= alpha;
+        for (int i = 0; i < 4; i++) o[i] *= alpha;
+        for (uint64_t left = __ballot(there); left; left &= left - 1) {
+            const int from_lane = __builtin_ctzll(left);
+            const float weight = __shfl(p, from_lane);
+            const T *v = (const T *)a.v_pages + __shfl(at, from_lane);
+            sum += weight;
+            for (int i = 0; i < 4; i++)
+                if (lane + 64 * i < D) o[i] = fmaf(weight, (float)v[lane + 64 * i], o[i]);
+        }
+    }
+    const size_t part = (size_t)(token * a.q_heads + head) * w.splits + blockIdx.z;
+    const float inv = sp.parts > 1 ? 1.0f : sum == 0 ? 0.0f : 1.0f / sum;
+    if (sp.parts > 1 && lane == 0) w.ml[part] = float2{top, sum};
+    for (int i = 0; i < 4; i++) {
+        const int d = lane + 64 * i;
+        if (d >= D) continue;
+        if (sp.parts > 1) w.o[part * D + d] = o[i];
+        else ((T *)a.out)[token * a.out_token + head * a.out_head + d] = (T)(o[i] * inv);
+    }
 }
 
 // Few rows: every wavefront walks places of its own, 32 a step, four steps of the workgroup side by side, straight from memory.  Lane
@@ -129,7 +157,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void k_attend_few(she_attend_pag
     __shared__ int64_t rows[MOST_CHUNK];
     __shared__ float joined[FEW_WAVES][FEW_ROWS][DP];
     __shared__ float tops[FEW_WAVES][FEW_ROWS], sums[FEW_WAVES][FEW_ROWS];
-    __shared__ int any_bad;
+    __shared__ int any_bad, any_special;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, quarter = lane >> 4;
     const int kv_head = blockIdx.y, D = (int)a.head;
     const Piece piece = few_piece(a, group, w);
@@ -137,7 +165,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void k_attend_few(she_attend_pag
     const Span sp = span_of<FEW_ROWS>(a, group, piece, piece.index * FEW_ROWS, w.few_chunk);
     if ((int)blockIdx.z >= max(sp.parts, 1)) return;
     const int from = sp.from + (int)blockIdx.z * (int)w.few_chunk, count = sp.parts ? min((int)w.few_chunk, sp.to - from) : 0;
-    if (tid == 0) any_bad = 0;
+    if (tid == 0) any_bad = any_special = 0;
     __syncthreads();
     look_up(a, sp.request, kv_head, from, count, rows, &any_bad, d_bad);
 
@@ -160,6 +188,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void k_attend_few(she_attend_pag
         for (int e = 0; e < EL; e++) acc[b][e] = f32x4{0, 0, 0, 0};
     __syncthreads();
     const bool unsafe = any_bad != 0;
+    bool special = false;                                         // infinite or NaN values where not all rows attend
 
     for (int k0 = wave * 32; k0 < count; k0 += FEW_WAVES * 32) {
         u32x4 kraw[2][KS];
@@ -229,46 +258,21 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void k_attend_few(she_attend_pag
 #pragma unroll
                     for (int i = 0; i < 4; i++) acc[b][e][i] *= alpha;
         }
-        bool special = false;
         if (masked) {
 #pragma unroll
             for (int b = 0; b < NB; b++)
 #pragma unroll
                 for (int e = 0; e < 8; e++) special |= has_special<T>(vraw[b][e]);
         }
-        if (!__ballot(special)) {
 #pragma unroll
-            for (int b = 0; b < NB; b++) {
-                x8<T> v[EL];
-                transpose8<T, EL>(vraw[b], v);
+        for (int b = 0; b < NB; b++) {
+            x8<T> v[EL];
+            transpose8<T, EL>(vraw[b], v);
 #pragma unroll
-                for (int e = 0; e < EL; e++) acc[b][e] = mfma16(v[e], p, acc[b][e]);
-            }
-        } else {
-#pragma unroll
-            for (int b = 0; b < NB; b++) {
-                u32x4 some[8];
-                x8<T> v[EL];
-#pragma unroll
-                for (int e = 0; e < 8; e++) some[e] = finite_part<T>(vraw[b][e]);
-                transpose8<T, EL>(some, v);
-#pragma unroll
-                for (int e = 0; e < EL; e++) acc[b][e] = mfma16(v[e], p, acc[b][e]);
-#pragma unroll 1
-                for (int kind = 0; kind < KINDS; kind++) {
-#pragma unroll
-                    for (int e = 0; e < 8; e++) some[e] = ones_at<T>(vraw[b][e], kind);
-                    transpose8<T, EL>(some, v);
-#pragma unroll
-                    for (int e = 0; e < EL; e++) {
-                        const f32x4 o = mfma16(v[e], p, f32x4{0, 0, 0, 0});
-#pragma unroll
-                        for (int i = 0; i < 4; i++) acc[b][e][i] += o[i] > 0 ? value_of(kind) : 0.0f;
-                    }
-                }
-            }
+            for (int e = 0; e < EL; e++) acc[b][e] = mfma16(v[e], p, acc[b][e]);
         }
     }
+    if (special) any_special = 1;
 
     // the wavefronts' results, and the piece's
     l += __shfl_xor(l, 16);
@@ -283,6 +287,10 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void k_attend_few(she_attend_pag
                 *reinterpret_cast<f32x4 *>(&joined[wave][col][b * 128 + (quarter * 4 + i) * EL + e]) =
                     f32x4{acc[b][e][i], acc[b][e + 1][i], acc[b][e + 2][i], acc[b][e + 3][i]};
     __syncthreads();
+    if (any_special) {
+        for (int r = wave; r < sp.rows; r += FEW_WAVES) attend_row<T>(a, group, w, sp, kv_head, sp.row + r, from, from + count);
+        return;
+    }
     constexpr int EACH = DP / 16;                                 // elements of a row that a thread joins
     const int r = tid / 16, d0 = tid % 16 * EACH;
     if (r >= sp.rows) return;
@@ -414,6 +422,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
     const int value_place = half * 4 + (lane & 15) / 4, value_d = (lane & 16) + (lane & 3) * 4;
     const int value_at = value_place * DP * 2 + value_unit<DP>(value_place, value_d / 8) * 16 + value_d % 8 * 2;
     int page = -1;
+    bool special = false;                                         // infinite or NaN values where not all rows attend
     auto do_step = [&](int step, const T *key_tile, const T *value_tile, T *next_keys, T *next_values) {
         wait_for_lds_loads();
         __syncthreads();                                          // this step's tiles are there, the others are free
@@ -432,8 +441,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
                 for (int k = 0; k < KS; k++) s[t] = mfma32(*reinterpret_cast<const x8<T> *>(keys + t * 32 * DP * 2 + (key_at ^ k * 32)), q[k], s[t]);
             }
                 const bool masked = gone || p0 + STEP - 1 > high_min || p0 < low_max || step * STEP + STEP > count;
-            bool special = false;
-            if (masked) {
+            if (__builtin_expect(masked, 0)) {
                 const int from_here = p0 + 4 * half, most = high - from_here, least = low - from_here;
                 const uint64_t out = gone >> 4 * half;
 #pragma unroll
@@ -452,7 +460,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
                 for (int i = 0; i < 16; i++) top = fmaxf(top, s[t][i]);
             top = fmaxf(top, __shfl_xor(top, 32)) * scale;
             // the reference need not be the top itself: it is raised where a weight would exceed 2^8
-            if (__ballot(top > m + 8.0f)) {
+            if (__builtin_expect(__ballot(top > m + 8.0f) != 0, 0)) {
                 const float to = fmaxf(m, top), ref = to == -__builtin_inff() ? 0.0f : to, alpha = __builtin_amdgcn_exp2f(m - ref);
                 m = to;
                 l *= alpha;
@@ -482,26 +490,10 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
                 }
                 return v;
             };
-            if (!__ballot(special)) {
 #pragma unroll
-                for (int k = 0; k < 4; k++)
+            for (int k = 0; k < 4; k++)
 #pragma unroll
-                    for (int b = 0; b < DB; b++) acc[b] = mfma32(as_x8<T>(columns(b, k)), p[k], acc[b]);
-            } else {
-#pragma unroll
-                for (int b = 0; b < DB; b++) {
-#pragma unroll
-                    for (int k = 0; k < 4; k++) acc[b] = mfma32(as_x8<T>(finite_part<T>(columns(b, k))), p[k], acc[b]);
-#pragma unroll 1
-                    for (int kind = 0; kind < KINDS; kind++) {
-                        f32x16 o{};
-#pragma unroll
-                        for (int k = 0; k < 4; k++) o = mfma32(as_x8<T>(ones_at<T>(columns(b, k), kind)), p[k], o);
-#pragma unroll
-                        for (int i = 0; i < 16; i++) acc[b][i] += o[i] > 0 ? value_of(kind) : 0.0f;
-                    }
-                }
-            }
+                for (int b = 0; b < DB; b++) acc[b] = mfma32(as_x8<T>(columns(b, k)), p[k], acc[b]);
         }
     };
     for (int step = 0; step < steps; step += 2) {
@@ -509,6 +501,10 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
         if (step + 1 < steps) do_step(step + 1, odd_keys, odd_values, even_keys, even_values);
     }
 
+    if (__ballot(special)) {
+        for (int row = first_here; row <= last_here; row++) attend_row<T>(a, group, w, sp, kv_head, row, from, from + count);
+        return;
+    }
     l += __shfl_xor(l, 32);
     if (first_here + col > last_row) return;
     const int64_t token = sp.token0 + my_token;
