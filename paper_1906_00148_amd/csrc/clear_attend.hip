@@ -384,13 +384,24 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
     // a step's tiles on their way into LDS: a wavefront's 64 units lie side by side there, so each lane picks the one that belongs in
     // its place; what is not there comes from a unit of zeros
     auto request = [&](int step, T *keys, T *values) {
+        const int64_t *row = &rows[step / 4 & 1][step % 4 * STEP + tid / UNITS];
+        constexpr int PLACES = 64 * TILE_WAVES / UNITS;
+        const int unit = tid % UNITS;
+        if (D == DP && (step + 1) * STEP <= count && !missing[step / 4 & 1][step % 4]) {
 #pragma unroll
-        for (int e = 0; e < EACH; e++) {
-            const int first = (e * TILE_WAVES + wave) * 64, place = tid / UNITS + e * (64 * TILE_WAVES / UNITS), unit = tid % UNITS;
-            const int64_t row = rows[step / 4 & 1][step % 4 * STEP + place];
-            const int key = key_unit<DP>(place, unit) * 8, value = value_unit<DP>(place, unit) * 8;
-            to_lds(row >= 0 && key < D ? (const T *)a.k_pages + row + key : (const T *)zeros, keys + first * 8);
-            to_lds(row >= 0 && value < D ? (const T *)a.v_pages + row + value : (const T *)zeros, values + first * 8);
+            for (int e = 0; e < EACH; e++) {
+                const int place = tid / UNITS + e * PLACES;
+                to_lds((const T *)a.k_pages + row[e * PLACES] + key_unit<DP>(place, unit) * 8, keys + (e * TILE_WAVES + wave) * 64 * 8);
+                to_lds((const T *)a.v_pages + row[e * PLACES] + value_unit<DP>(place, unit) * 8, values + (e * TILE_WAVES + wave) * 64 * 8);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < EACH; e++) {
+                const int place = tid / UNITS + e * PLACES, key = key_unit<DP>(place, unit) * 8, value = value_unit<DP>(place, unit) * 8;
+                const bool there = row[e * PLACES] >= 0;
+                to_lds(there && key < D ? (const T *)a.k_pages + row[e * PLACES] + key : (const T *)zeros, keys + (e * TILE_WAVES + wave) * 64 * 8);
+                to_lds(there && value < D ? (const T *)a.v_pages + row[e * PLACES] + value : (const T *)zeros, values + (e * TILE_WAVES + wave) * 64 * 8);
+            }
         }
     };
 
@@ -458,7 +469,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
             for (int t = 0; t < 2; t++)
 #pragma unroll
                 for (int i = 0; i < 16; i++) top = fmaxf(top, s[t][i]);
-            top = fmaxf(top, __shfl_xor(top, 32)) * scale;
+            top = other_half_max(top) * scale;
             // the reference need not be the top itself: it is raised where a weight would exceed 2^8
             if (__builtin_expect(__ballot(top > m + 8.0f) != 0, 0)) {
                 const float to = fmaxf(m, top), ref = to == -__builtin_inff() ? 0.0f : to, alpha = __builtin_amdgcn_exp2f(m - ref);
@@ -602,12 +613,15 @@ AttendShape attend_shape(const she_attend_pages_args &a, uint32_t cus)
     s.few_each = s.few_most == 0x7FFFFFFF ? 0 : s.few_most / FEW_ROWS;
     s.few_slots = s.few_most == 0x7FFFFFFF ? rows / FEW_ROWS + a.requests : (uint64_t)a.requests * s.few_each;
     s.tile_slots = s.few_most == 0x7FFFFFFF ? 0 : rows / TILE_ROWS + a.requests;
+    // places of a span at most: a window's, those that the tile's later tokens see further, and those before it down to a multiple of 32
+    const auto span = [&](uint64_t tile) { return a.window ? std::min<uint64_t>(longest, (uint64_t)a.window + tile + 31) : longest; };
+    const uint64_t few_span = span(FEW_ROWS), tile_span = span(TILE_ROWS);
     // pieces short enough for eight workgroups per compute unit, long enough that joining them costs little
-    s.few_chunk = (uint32_t)std::min<uint64_t>(MOST_CHUNK, std::max<uint64_t>(256, ceil_div(s.few_slots * a.kv_heads * longest / (8 * cus), 128) * 128));
-    s.few_splits = s.few_slots ? (uint32_t)std::max<uint64_t>(1, ceil_div(longest, s.few_chunk)) : 1;
+    s.few_chunk = (uint32_t)std::min<uint64_t>(MOST_CHUNK, std::max<uint64_t>(256, ceil_div(s.few_slots * a.kv_heads * few_span / (8 * cus), 128) * 128));
+    s.few_splits = s.few_slots ? (uint32_t)std::max<uint64_t>(1, ceil_div(few_span, s.few_chunk)) : 1;
     // and for two of k_attend_tile's
-    s.tile_chunk = (uint32_t)std::max<uint64_t>(512, ceil_div(s.tile_slots * a.kv_heads * longest / (2 * cus), STEP) * STEP);
-    s.tile_splits = s.tile_slots ? (uint32_t)std::max<uint64_t>(1, ceil_div(longest, s.tile_chunk)) : 1;
+    s.tile_chunk = (uint32_t)std::max<uint64_t>(512, ceil_div(s.tile_slots * a.kv_heads * tile_span / (2 * cus), STEP) * STEP);
+    s.tile_splits = s.tile_slots ? (uint32_t)std::max<uint64_t>(1, ceil_div(tile_span, s.tile_chunk)) : 1;
     return s;
 }
 

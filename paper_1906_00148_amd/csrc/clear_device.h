@@ -90,6 +90,13 @@ __device__ inline void to_lds(const void *from, void *to)
 }
 __device__ inline void wait_for_lds_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }      // vmcnt(0)
 
+// The larger of a lane's number and that of the lane 32 away.
+__device__ inline float other_half_max(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
 // LDS that one wavefront alone uses: its operations run in order, and this keeps the compiler from moving them.
 __device__ inline void wave_lds_fence()
 {
