@@ -22,6 +22,7 @@ struct QkShape {
     uint32_t chunks;         // wavefronts' shares of a token
     uint32_t blocks;
     bool wide;               // every row starts on 16 bytes and has whole vectors
+    bool aligned;            // and so do a lane's cosines and sines
 };
 QkShape qk_shape(const she_qk_rotate_args &a, uint32_t cus);
 QkShape qk_grad_shape(const she_qk_rotate_grad_args &a, uint32_t cus);

@@ -17,6 +17,7 @@ namespace she { namespace clear {
 namespace {
 
 constexpr int WAVES = 4;                       // wavefronts of a workgroup
+constexpr uint32_t GRAD_RESIDENT = 3;           // of the backward kernel's workgroups on a compute unit
 constexpr int BATCH = 4;                       // steps whose loads are requested before the first is used
 
 // Sum over the LANES lanes of a head.
@@ -32,11 +33,32 @@ template <int LANES> __device__ inline float head_sum(float v)
 struct Turn {
     float c[8], s[8];
 };
-__device__ inline Turn load_turn(const float *cosines, const float *sines, uint32_t rot, bool interleaved, uint32_t place, int d0, float sign)
+__device__ inline Turn load_turn(const float *cosines, const float *sines, uint32_t rot, bool interleaved, bool aligned, uint32_t place, int d0, float sign)
 {
     Turn t;
     const uint32_t half = rot / 2;
     const float *c = cosines + (size_t)place * half, *s = sines + (size_t)place * half;
+    if (aligned) {                             // a lane's pairs are eight, or four, neighbours on 16 bytes
+        const bool turns = (uint32_t)d0 < rot;
+        const uint32_t pair = !turns ? 0 : interleaved ? d0 / 2 : (uint32_t)d0 < half ? d0 : d0 - half;
+        f32x4 cv[2] = {f32x4{1, 1, 1, 1}, f32x4{1, 1, 1, 1}}, sv[2] = {f32x4{0, 0, 0, 0}, f32x4{0, 0, 0, 0}};
+        if (turns) {
+            cv[0] = *reinterpret_cast<const f32x4 *>(c + pair);
+            sv[0] = *reinterpret_cast<const f32x4 *>(s + pair);
+            if (!interleaved) {
+                cv[1] = *reinterpret_cast<const f32x4 *>(c + pair + 4);
+                sv[1] = *reinterpret_cast<const f32x4 *>(s + pair + 4);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const int k = interleaved ? i / 2 : i;
+            const bool first = interleaved ? !(i & 1) : (uint32_t)d0 < half;
+            t.c[i] = cv[k / 4][k % 4];
+            t.s[i] = first ? -sign * sv[k / 4][k % 4] : sign * sv[k / 4][k % 4];
+        }
+        return t;
+    }
 #pragma unroll
     for (int i = 0; i < 8; i++) {
         const uint32_t d = d0 + i;
@@ -81,7 +103,7 @@ __device__ inline void turn(const Turn &t, const float v[8], const float other[8
 }
 
 template <class T, bool WIDE, bool INTERLEAVED, int LANES>
-__global__ __launch_bounds__(64 * WAVES) void k_qk_rotate(she_qk_rotate_args a, uint32_t steps, uint32_t per_wave, uint32_t chunks,
+__global__ __launch_bounds__(64 * WAVES) void k_qk_rotate(she_qk_rotate_args a, uint32_t steps, uint32_t per_wave, uint32_t chunks, bool aligned,
                                                           uint32_t *d_bad)
 {
     constexpr int ROWS = 64 / LANES;
@@ -102,7 +124,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_qk_rotate(she_qk_rotate_args a, 
     const int64_t at = slot >= 0 ? page * a.page_stride + (slot - (int64_t)page * a.page_size) * a.slot_stride : 0;
     const int here = D - d0 < 0 ? 0 : D - d0 > 8 ? 8 : D - d0;     // of the lane's eight elements
 
-    const Turn tr = load_turn(a.cosines, a.sines, placed ? a.rot : 0, INTERLEAVED, placed ? (uint32_t)position : 0, d0, 1.0f);
+    const Turn tr = load_turn(a.cosines, a.sines, placed ? a.rot : 0, INTERLEAVED, aligned, placed ? (uint32_t)position : 0, d0, 1.0f);
     float wq[8], wk[8];
 #pragma unroll
     for (int i = 0; i < 8; i++) {
@@ -155,7 +177,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_qk_rotate(she_qk_rotate_args a, 
 
 // Wavefronts walk the shares of all tokens and keep their sums of both weights' gradients; partial [blocks][2][D].
 template <class T, bool WIDE, bool INTERLEAVED, int LANES>
-__global__ __launch_bounds__(64 * WAVES) void k_qk_rotate_grad(she_qk_rotate_grad_args a, uint32_t steps, uint32_t per_wave, uint32_t chunks,
+__global__ __launch_bounds__(64 * WAVES) void k_qk_rotate_grad(she_qk_rotate_grad_args a, uint32_t steps, uint32_t per_wave, uint32_t chunks, bool aligned,
                                                                float *partial, uint32_t *d_bad)
 {
     constexpr int ROWS = 64 / LANES, PAIR = 2;
@@ -178,7 +200,7 @@ __global__ __launch_bounds__(64 * WAVES) void k_qk_rotate_grad(she_qk_rotate_gra
         const int32_t position = a.positions[t];
         const bool placed = position >= 0 && (uint32_t)position < a.places;
         if (lane == 0 && chunk == 0 && !placed) count_bad(d_bad);
-        const Turn tr = load_turn(a.cosines, a.sines, placed ? a.rot : 0, INTERLEAVED, placed ? (uint32_t)position : 0, d0, -1.0f);
+        const Turn tr = load_turn(a.cosines, a.sines, placed ? a.rot : 0, INTERLEAVED, aligned, placed ? (uint32_t)position : 0, d0, -1.0f);
         const uint32_t end = min((chunk + 1) * per_wave, steps);
         for (uint32_t step = chunk * per_wave; step < end; step += PAIR) {
             u32x4 raw_x[PAIR], raw_y[PAIR];
@@ -238,24 +260,41 @@ __global__ __launch_bounds__(64 * WAVES) void k_qk_rotate_grad(she_qk_rotate_gra
     }
 }
 
-// dwq, dwk = sums of the workgroups' partial sums: sixteen columns a workgroup, sixteen threads a column.
-__global__ __launch_bounds__(256) void k_qk_weight_sums(const float *partial, uint32_t rows, uint32_t D, float *dwq, float *dwk)
+// dwq, dwk = sums of the workgroups' partial sums: SUM_COLS columns a workgroup, SUM_PARTS threads a column, whose loads are
+// requested eight at a time.
+constexpr int SUM_COLS = 8, SUM_PARTS = 128;
+__global__ __launch_bounds__(SUM_COLS * SUM_PARTS) void k_qk_weight_sums(const float *partial, uint32_t rows, uint32_t D, float *dwq, float *dwk)
 {
-    __shared__ float sums[16][17];
-    const uint32_t col = blockIdx.x * 16 + threadIdx.x % 16, part = threadIdx.x / 16;
+    __shared__ float sums[SUM_PARTS][SUM_COLS + 1];
+    const uint32_t col = blockIdx.x * SUM_COLS + threadIdx.x % SUM_COLS, part = threadIdx.x / SUM_COLS;
     float v = 0;
     if (col < 2 * D)
-        for (uint32_t r = part; r < rows; r += 16) v += partial[(size_t)r * 2 * D + col];
-    sums[part][threadIdx.x % 16] = v;
+        for (uint32_t r0 = part; r0 < rows; r0 += 8 * SUM_PARTS) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) x[i] = r0 + i * SUM_PARTS < rows ? partial[(size_t)(r0 + i * SUM_PARTS) * 2 * D + col] : 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; i++) v += x[i];
+        }
+    sums[part][threadIdx.x % SUM_COLS] = v;
     __syncthreads();
-    if (part || col >= 2 * D) return;
+    if (part >= 8) return;                                        // eight threads a column, then one
     v = 0;
-    for (int p = 0; p < 16; p++) v += sums[p][threadIdx.x];
+    for (int p = part; p < SUM_PARTS; p += 8) v += sums[p][threadIdx.x % SUM_COLS];
+#pragma unroll
+    for (int m = SUM_COLS; m < 64; m *= 2) v += __shfl_xor(v, m);
+    if (part || col >= 2 * D) return;
     float *to = col < D ? dwq : dwk;
     if (to) to[col < D ? col : col - D] = v;
 }
 
 bool on16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+// whether a lane's cosines and sines are neighbours on 16 bytes
+bool turn_aligned(const float *cosines, const float *sines, uint32_t rot, bool interleaved)
+{
+    return on16(cosines) && on16(sines) && rot % (interleaved ? 8 : 16) == 0;
+}
 
 uint32_t lanes_of(uint32_t head) { return head <= 64 ? 8 : head <= 128 ? 16 : head <= 256 ? 32 : 64; }
 
@@ -284,14 +323,14 @@ template <template <class, bool, bool, int> class Launch, class... A> hipError_t
 template <class T, bool W, bool I, int L> struct Rotate {
     static hipError_t go(const she_qk_rotate_args &a, const QkShape &s, uint32_t *d_bad, hipStream_t st)
     {
-        k_qk_rotate<T, W, I, L><<<s.blocks, 64 * WAVES, 0, st>>>(a, s.steps, s.per_wave, s.chunks, d_bad);
+        k_qk_rotate<T, W, I, L><<<s.blocks, 64 * WAVES, 0, st>>>(a, s.steps, s.per_wave, s.chunks, s.aligned, d_bad);
         return hipGetLastError();
     }
 };
 template <class T, bool W, bool I, int L> struct RotateGrad {
     static hipError_t go(const she_qk_rotate_grad_args &a, const QkShape &s, float *partial, uint32_t *d_bad, hipStream_t st)
     {
-        k_qk_rotate_grad<T, W, I, L><<<s.blocks, 64 * WAVES, 0, st>>>(a, s.steps, s.per_wave, s.chunks, partial, d_bad);
+        k_qk_rotate_grad<T, W, I, L><<<s.blocks, 64 * WAVES, 0, st>>>(a, s.steps, s.per_wave, s.chunks, s.aligned, partial, d_bad);
         return hipGetLastError();
     }
 };
@@ -314,6 +353,7 @@ QkShape qk_shape(const she_qk_rotate_args &a, uint32_t cus)
         s.wide = s.wide && on16(a.k_out);
     }
     s.wide = s.wide && strides % 8 == 0;
+    s.aligned = turn_aligned(a.cosines, a.sines, a.rot, a.interleaved != 0);
     share_out(s, a.tokens, cus);
     return s;
 }
@@ -326,8 +366,11 @@ QkShape qk_grad_shape(const she_qk_rotate_grad_args &a, uint32_t cus)
     const int64_t strides = a.q_token | a.q_head | a.k_token | a.k_head | a.dq_out_token | a.dq_out_head | a.dk_out_token | a.dk_out_head |
                             a.dq_token | a.dq_head | a.dk_token | a.dk_head | a.head;
     s.wide = strides % 8 == 0 && on16(a.q) && on16(a.k) && on16(a.dq_out) && on16(a.dk_out) && on16(a.dq) && on16(a.dk);
+    s.aligned = turn_aligned(a.cosines, a.sines, a.rot, a.interleaved != 0);
     share_out(s, a.tokens, cus);
-    s.blocks = std::max(1u, std::min(s.blocks, 4 * cus));        // each leaves a row of partial sums
+    // Each leaves a row of partial sums: no more than are resident together, and all with as many shares, so that they end together.
+    const uint32_t resident = GRAD_RESIDENT * (cus ? cus : 1), rounds = std::max(1u, (uint32_t)ceil_div(s.blocks, resident));
+    s.blocks = std::max(1u, (uint32_t)ceil_div(s.blocks, rounds));
     return s;
 }
 
@@ -343,7 +386,7 @@ hipError_t launch_qk_rotate_grad(const she_qk_rotate_grad_args &a, const QkShape
     float *partial = static_cast<float *>(scratch);
     hipError_t rc = choose<RotateGrad>(a.type, s.wide, a.interleaved != 0, s.lanes, a, s, partial, d_bad, st);
     if (rc != hipSuccess || (!a.dwq && !a.dwk)) return rc;
-    k_qk_weight_sums<<<(uint32_t)ceil_div(2 * a.head, 16), 256, 0, st>>>(partial, s.blocks, a.head, a.dwq, a.dwk);
+    k_qk_weight_sums<<<(uint32_t)ceil_div(2 * a.head, SUM_COLS), SUM_COLS * SUM_PARTS, 0, st>>>(partial, s.blocks, a.head, a.dwq, a.dwk);
     return hipGetLastError();
 }
 
