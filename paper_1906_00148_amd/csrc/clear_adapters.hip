@@ -28,12 +28,21 @@ constexpr int CHUNK = 64;                // ranks that a workgroup of k_adapter_
 constexpr int UP_WAVES = 4, SPAN = 128;  // wavefronts of k_adapter_up, outputs of one
 constexpr int OUTER_WAVES = 8;
 
-// The hidden values of all tiles.  rows: r rounded up to 16.
+// The hidden values of all tiles, value and rest, in the order of the operands that they become, so that a wavefront reads 16 bytes
+// a lane side by side.  rows: r rounded up to 16.  Null: not wanted.
 struct Hidden {
-    uint16_t *by_token[2];               // [slots][TILE][rows], value and rest; null: not wanted
-    uint16_t *by_rank[2];                // [slots][rows][TILE]
+    uint16_t *by_token[2];               // [slots][TILE / 16][rows / 8][16 tokens][8 ranks]
+    uint16_t *by_rank[2];                // [slots][rows / 16][TILE / 8][16 ranks][8 tokens]
     float *unscale;                      // [slots][chunks]: f16, what a tile's values are to be multiplied by
 };
+__device__ inline size_t by_token_at(size_t slot, int t, int j, uint32_t rows)
+{
+    return slot * TILE * rows + ((t >> 4) * (rows / 8) + (j >> 3)) * 128 + (t & 15) * 8 + (j & 7);
+}
+__device__ inline size_t by_rank_at(size_t slot, int j, int t, uint32_t rows)
+{
+    return slot * TILE * rows + ((j >> 4) * (TILE / 8) + (t >> 3)) * 128 + (j & 15) * 8 + (t & 7);
+}
 struct Segments {
     const int32_t *starts, *which, *ranks;
     const float *scale;
@@ -73,64 +82,70 @@ template <class T> __device__ inline void split(float v, uint16_t &value, uint16
     rest = __builtin_bit_cast(uint16_t, (T)(fabsf(left) < __builtin_inff() ? left : 0.0f));
 }
 
-struct Down {
-    Rows x;
-    Matrix w;
-    Hidden h;
+struct Tile {                            // the tokens [first, first + live) of a segment whose adapter is `adapter` (-1: none)
+    int adapter, live;
+    int64_t first;
+    uint32_t rank;
 };
+__device__ inline Tile tile_of(const Segments &s, const Piece &p, uint32_t *d_bad)
+{
+    Tile t;
+    t.adapter = adapter_of(s, p.segment, d_bad);
+    t.first = p.first + (int64_t)p.index * TILE;
+    t.live = (int)min((int64_t)TILE, p.last - t.first);
+    t.rank = t.adapter < 0 ? 0 : rank_of(s, t.adapter);
+    return t;
+}
 
-// One tile, up to CHUNK ranks (RT tiles of 16) of it: the wavefronts share the width out, 32 columns a step.
-template <class T, bool WIDE, int RT, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void k_adapter_down(Down job0, Down job1, Segments s, uint32_t *d_bad)
+// One tile, up to CHUNK ranks (RT tiles of 16) of it from r0 on: the wavefronts share the width out and are
+// summed in LDS.  keep(j, t, value, rest) gets every number; returns what they are to be multiplied by.
+template <class T, bool WIDE, int RT, int WAVES, class Keep>
+__device__ inline float hidden_values(const Rows &rows, const Matrix &matrix, const Segments &s, const Tile &tile, uint32_t r0, Keep keep)
 {
     __shared__ float part[WAVES][RT * 16][TILE];
     __shared__ float tops[WAVES];
-    const Down &job = blockIdx.z ? job1 : job0;
-    const uint32_t slot = blockIdx.x, r0 = blockIdx.y * CHUNK;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, quarter = lane >> 4;
-    const Piece piece = find_piece(s.starts, s.segments, s.tokens, 1, TILE, slot);
-    if (piece.segment < 0) return;
-    const int a = adapter_of(s, piece.segment, tid == 0 && blockIdx.y == 0 && blockIdx.z == 0 && piece.index == 0 ? d_bad : nullptr);
-    if (a < 0) return;
-    const uint32_t rank = rank_of(s, a), K = job.w.width;
-    const int64_t t0 = piece.first + (int64_t)piece.index * TILE;
-    const int live = (int)min((int64_t)TILE, piece.last - t0);
-
+    const uint32_t K = matrix.width;
     const T *x[2], *w[RT];
     bool has_x[2], has_w[RT];
 #pragma unroll
     for (int c = 0; c < 2; c++) {
-        has_x[c] = c * 16 + col < live;
-        x[c] = (const T *)job.x.p + (t0 + (has_x[c] ? c * 16 + col : 0)) * job.x.stride + quarter * 8;
+        has_x[c] = c * 16 + operand_row() < tile.live;
+        x[c] = (const T *)rows.p + (tile.first + (has_x[c] ? c * 16 + operand_row() : 0)) * rows.stride + operand_unit() * 8;
     }
 #pragma unroll
     for (int r = 0; r < RT; r++) {
-        const uint32_t j = r0 + r * 16 + col;
-        has_w[r] = j < rank;
-        w[r] = (const T *)job.w.p + a * job.w.adapter + (has_w[r] ? j : 0) * job.w.row + quarter * 8;
+        const uint32_t j = r0 + r * 16 + operand_row();
+        has_w[r] = j < tile.rank;
+        w[r] = (const T *)matrix.p + tile.adapter * matrix.adapter + (has_w[r] ? j : 0) * matrix.row + operand_unit() * 8;
     }
     f32x4 acc[RT][2];
 #pragma unroll
     for (int r = 0; r < RT; r++) acc[r][0] = acc[r][1] = f32x4{0, 0, 0, 0};
     constexpr int AHEAD = !WIDE ? 1 : RT == 4 ? 2 : 4;     // steps whose loads are requested together
     for (uint32_t k0 = wave * 32; k0 < K; k0 += AHEAD * WAVES * 32) {
-        x8<T> xv[AHEAD][2], wv[AHEAD][RT];
+        u32x4 xv[AHEAD][2], wv[AHEAD][RT];
 #pragma unroll
         for (int e = 0; e < AHEAD; e++) {
             const uint32_t k = k0 + e * WAVES * 32;
-            const int count = (int)K - (int)(k + quarter * 8);
+            const int count = min(8, (int)K - (int)(k + operand_unit() * 8));
 #pragma unroll
-            for (int c = 0; c < 2; c++) xv[e][c] = as_x8<T>(load8<T, WIDE>(x[c] + k, has_x[c] ? min(count, 8) : 0));
+            for (int c = 0; c < 2; c++) xv[e][c] = load8<T, WIDE>(x[c] + k, has_x[c] ? count : 0);
 #pragma unroll
-            for (int r = 0; r < RT; r++) wv[e][r] = as_x8<T>(load8<T, WIDE>(w[r] + k, has_w[r] ? min(count, 8) : 0));
+            for (int r = 0; r < RT; r++) wv[e][r] = load8<T, WIDE>(w[r] + k, has_w[r] ? count : 0);
         }
 #pragma unroll
-        for (int e = 0; e < AHEAD; e++)
+        for (int e = 0; e < AHEAD; e++) {
+            x8<T> xo[2];
+#pragma unroll
+            for (int c = 0; c < 2; c++) xo[c] = as_x8<T>(to_operand(xv[e][c]));
 #pragma unroll
             for (int r = 0; r < RT; r++) {
-                acc[r][0] = mfma16(wv[e][r], xv[e][0], acc[r][0]);
-                if (live > 16) acc[r][1] = mfma16(wv[e][r], xv[e][1], acc[r][1]);
+                const x8<T> wo = as_x8<T>(to_operand(wv[e][r]));
+                acc[r][0] = mfma16(wo, xo[0], acc[r][0]);
+                if (tile.live > 16) acc[r][1] = mfma16(wo, xo[1], acc[r][1]);
             }
+        }
     }
 #pragma unroll
     for (int r = 0; r < RT; r++)
@@ -141,8 +156,8 @@ __global__ __launch_bounds__(64 * WAVES) void k_adapter_down(Down job0, Down job
     __syncthreads();
 
     constexpr int VALUES = RT * 16 * TILE, EACH = (VALUES + 64 * WAVES - 1) / (64 * WAVES);
-    const float scale = s.scale[a];
-    float v[EACH], top = 0;
+    const float scale = s.scale[tile.adapter];
+    float v[EACH], top = 0, by = 1, unscale = 1;
 #pragma unroll
     for (int e = 0; e < EACH; e++) {
         const int n = e * 64 * WAVES + tid;
@@ -152,10 +167,9 @@ __global__ __launch_bounds__(64 * WAVES) void k_adapter_down(Down job0, Down job
 #pragma unroll
         for (int k = 0; k < WAVES; k++) v[e] += p[k * VALUES];
         // what no token or rank stands behind is zero, not what an infinity makes of zeros
-        v[e] = n % TILE < live && r0 + n / TILE < rank ? v[e] * scale : 0.0f;
+        v[e] = n % TILE < tile.live && r0 + n / TILE < tile.rank ? v[e] * scale : 0.0f;
         if (fabsf(v[e]) < __builtin_inff()) top = fmaxf(top, fabsf(v[e]));
     }
-    float by = 1;
     if constexpr (std::is_same<T, _Float16>::value) {
 #pragma unroll
         for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
@@ -166,25 +180,47 @@ __global__ __launch_bounds__(64 * WAVES) void k_adapter_down(Down job0, Down job
         for (int k = 0; k < WAVES; k++) top = fmaxf(top, tops[k]);
         const int e = top > 0 ? min(max(ilogbf(top), -100), 120) : 0;          // the largest becomes 2^13 .. 2^14
         by = ldexpf(1.0f, 13 - e);
-        if (tid == 0) job.h.unscale[(size_t)slot * s.chunks + blockIdx.y] = ldexpf(1.0f, e - 13);
+        unscale = ldexpf(1.0f, e - 13);
     }
 #pragma unroll
     for (int e = 0; e < EACH; e++) {
-        const int n = e * 64 * WAVES + tid, j = r0 + n / TILE, t = n % TILE;
+        const int n = e * 64 * WAVES + tid, j = r0 + n / TILE;
         if (n >= VALUES || (uint32_t)j >= s.rows) continue;
         uint16_t value, rest;
         split<T>(v[e] * by, value, rest);
+        keep(j, n % TILE, value, rest);
+    }
+    return unscale;
+}
+
+struct Down {
+    Rows x;
+    Matrix w;
+    Hidden h;
+};
+
+template <class T, bool WIDE, int RT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void k_adapter_down(Down job0, Down job1, Segments s, uint32_t *d_bad)
+{
+    const Down &job = blockIdx.z ? job1 : job0;
+    const uint32_t slot = blockIdx.x, r0 = blockIdx.y * CHUNK;
+    const Piece piece = find_piece(s.starts, s.segments, s.tokens, 1, TILE, slot);
+    if (piece.segment < 0) return;
+    const Tile tile = tile_of(s, piece, threadIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && piece.index == 0 ? d_bad : nullptr);
+    if (tile.adapter < 0) return;
+    const float unscale = hidden_values<T, WIDE, RT, WAVES>(job.x, job.w, s, tile, r0, [&](int j, int t, uint16_t value, uint16_t rest) {
         if (job.h.by_token[0]) {
-            const size_t at = ((size_t)slot * TILE + t) * s.rows + j;
+            const size_t at = by_token_at(slot, t, j, s.rows);
             job.h.by_token[0][at] = value;
             job.h.by_token[1][at] = rest;
         }
         if (job.h.by_rank[0]) {
-            const size_t at = ((size_t)slot * s.rows + j) * TILE + t;
+            const size_t at = by_rank_at(slot, j, t, s.rows);
             job.h.by_rank[0][at] = value;
             job.h.by_rank[1][at] = rest;
         }
-    }
+    });
+    if (threadIdx.x == 0 && std::is_same<T, _Float16>::value) job.h.unscale[(size_t)slot * s.chunks + blockIdx.y] = unscale;
 }
 
 struct Up {
@@ -198,111 +234,196 @@ struct Up {
     int64_t out_stride;
 };
 
-// Eight elements of the base as numbers of 32 bits.
-template <class T, bool WIDE> __device__ inline void load_base(const Up &u, int64_t t, uint32_t n, int count, float out[8])
+// A wavefront's SPAN outputs from n_first on: lane l has four from n_first + 4 (l % 16) on and four from 64 later on, of the tokens
+// 4 (l / 16) + i, i < 4, of sixteen, so that sixteen lanes read and write whole lines of a row, of 16-bit elements and of 32-bit ones.
+__device__ inline uint32_t lane_output(uint32_t n_first) { return n_first + (threadIdx.x & 15) * 4; }
+__device__ inline int lane_token(int i) { return (threadIdx.x >> 4 & 3) * 4 + i; }
+
+// The operands of 32 ranks from j0 on: for each of the lane's eight outputs its numbers of ranks j0 + 8 (lane / 16) .. + 7.
+template <class T, bool WIDE> __device__ inline void load_columns(const Matrix &w, int adapter, uint32_t rank, uint32_t j0, uint32_t n_first, x8<T> cols[8])
 {
-    if (u.base_type == SHE_NO_BASE) {
+    const uint32_t j = j0 + (threadIdx.x >> 4 & 3) * 8, n = lane_output(n_first);
+    const int count = (int)w.width - (int)n;
+    u32x4 raw[8];
 #pragma unroll
-        for (int i = 0; i < 8; i++) out[i] = 0;
-    } else if (u.base_type == SHE_F32 || u.base_type == SHE_I32) {
+    for (int i = 0; i < 8; i++) {
+        const bool there = j + i < rank;
+        raw[i] = load_quads<T, WIDE>((const T *)w.p + (int64_t)adapter * w.adapter + (int64_t)(there ? j + i : 0) * w.row + n, there ? count : 0, there ? count - 64 : 0);
+    }
+    transpose8<T, 8>(raw, cols);
+}
+
+// Eight elements of the base: their words, and the numbers that these stand for.
+struct BaseWords {
+    u32x4 v[2];
+};
+template <class T, bool WIDE> __device__ inline BaseWords load_base(const Up &u, int64_t t, uint32_t n, int count)
+{
+    BaseWords b{{u32x4{0, 0, 0, 0}, u32x4{0, 0, 0, 0}}};
+    if (u.base_type == SHE_F32 || u.base_type == SHE_I32) {
         const uint32_t *p = (const uint32_t *)u.base + t * u.base_stride + n;
-        u32x4 v[2] = {u32x4{0, 0, 0, 0}, u32x4{0, 0, 0, 0}};
         if constexpr (WIDE) {
-            if (count > 0) { v[0] = *reinterpret_cast<const u32x4 *>(p); v[1] = *reinterpret_cast<const u32x4 *>(p + 4); }
+            if (count > 0) b.v[0] = *reinterpret_cast<const u32x4 *>(p);
+            if (count > 64) b.v[1] = *reinterpret_cast<const u32x4 *>(p + 64);
         } else {
             for (int i = 0; i < 8; i++)
-                if (i < count) v[i / 4][i % 4] = p[i];
+                if (i / 4 * 64 + i % 4 < count) b.v[i / 4][i % 4] = p[i / 4 * 64 + i % 4];
         }
+    } else if (u.base_type != SHE_NO_BASE) {
+        b.v[0] = load_quads<T, WIDE>((const T *)u.base + t * u.base_stride + n, count, count - 64);
+    }
+    return b;
+}
+template <class T> __device__ inline void base_numbers(const Up &u, const BaseWords &b, const float step[8], float out[8])
+{
+    if (u.base_type == SHE_F32 || u.base_type == SHE_I32) {
         const bool sums = u.base_type == SHE_I32;
 #pragma unroll
-        for (int i = 0; i < 8; i++)
-            out[i] = !sums ? __uint_as_float(v[i / 4][i % 4])
-                           : (float)(int32_t)v[i / 4][i % 4] * (u.step && i < count ? u.step[n + i] : 1.0f);
+        for (int i = 0; i < 8; i++) {
+            const uint32_t w = b.v[i / 4][i % 4];
+            out[i] = sums ? (float)(int32_t)w * step[i] : __uint_as_float(w);
+        }
     } else {
-        unpack<T>(load8<T, WIDE>((const T *)u.base + t * u.base_stride + n, count), out);
+        unpack<T>(b.v[0], out);                  // zeros without a base
     }
 }
 
-// A wavefront: SPAN outputs of one tile.  Lane l reads the eight outputs of block (l%4)*4 + (l%16)/4, so that after the matrix
-// instructions the four lanes that share a token hold four neighbouring blocks and write 64 bytes side by side.
-// MANY: several chunks of ranks whose tiles' powers of two differ, summed apart.
-template <class T, bool WIDE, bool MANY>
-__global__ __launch_bounds__(64 * UP_WAVES) void k_adapter_up(Up u, Segments s)
+// Sixteen tokens from `first` on, `live` of them: their bases; and acc[m] added to the lane's output m, and written.
+template <class T, bool WIDE> __device__ inline void load_bases(const Up &u, int64_t first, int live, uint32_t n_first, BaseWords base[4])
 {
-    const uint32_t slot = blockIdx.x, N = u.w.width;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quarter = lane >> 4;
-    const uint32_t n_first = (blockIdx.y * UP_WAVES + wave) * SPAN;
-    if (n_first >= N) return;
+    const uint32_t n = lane_output(n_first);
+    const int count = (int)u.w.width - (int)n;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        const bool there = lane_token(i) < live && count > 0;
+        base[i] = load_base<T, WIDE>(u, first + (there ? lane_token(i) : 0), there ? n : 0, there ? count : 0);
+    }
+}
+template <class T, bool WIDE> __device__ inline void write_outputs(const Up &u, int64_t first, int live, uint32_t n_first, const BaseWords base[4], const f32x4 acc[8])
+{
+    const uint32_t n = lane_output(n_first);
+    const int count = (int)u.w.width - (int)n;
+    if (count <= 0) return;
+    float step[8];
+#pragma unroll
+    for (int m = 0; m < 8; m++) step[m] = u.step && m / 4 * 64 + m % 4 < count ? u.step[n + m / 4 * 64 + m % 4] : 1.0f;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        if (lane_token(i) >= live) break;
+        float v[8];
+        base_numbers<T>(u, base[i], step, v);
+#pragma unroll
+        for (int m = 0; m < 8; m++) v[m] += acc[m][i];
+        store_quads<T, WIDE>((T *)u.out + (first + lane_token(i)) * u.out_stride + n, pack<T>(v), count, count - 64);
+    }
+}
+
+// A wavefront: SPAN outputs of one tile, 32 ranks a step.  CHUNKS: several chunks of ranks whose tiles' powers of two (f16) differ,
+// summed apart.
+template <class T, bool WIDE, bool CHUNKS>
+__global__ __launch_bounds__(64 * UP_WAVES, WIDE && !CHUNKS ? 3 : 1) void k_adapter_up(Up u, Segments s)
+{
+    const int wave = threadIdx.x >> 6, col = threadIdx.x & 15, quarter = threadIdx.x >> 4 & 3;
+    const uint32_t slot = blockIdx.x, n_first = (blockIdx.y * UP_WAVES + wave) * SPAN;
+    if (n_first >= u.w.width) return;
     const Piece piece = find_piece(s.starts, s.segments, s.tokens, 1, TILE, slot);
     if (piece.segment < 0) return;
-    const int a = adapter_of(s, piece.segment, nullptr);
-    const int64_t t0 = piece.first + (int64_t)piece.index * TILE;
-    const int live = (int)min((int64_t)TILE, piece.last - t0);
-    const uint32_t rank = a < 0 ? 0 : rank_of(s, a);
-    const uint32_t n_lane = n_first + ((col & 3) * 4 + (col >> 2)) * 8;
-    const int w_count = min(8, (int)N - (int)n_lane);
-
-    constexpr bool SCALED = std::is_same<T, _Float16>::value;
-    f32x4 total[MANY ? 8 : 1][2], acc[8][2];
+    const Tile tile = tile_of(s, piece, nullptr);
+    f32x4 acc[2][8], total[CHUNKS ? 2 : 1][8];
 #pragma unroll
-    for (int m = 0; m < 8; m++) {
-        acc[m][0] = acc[m][1] = f32x4{0, 0, 0, 0};
-        if constexpr (MANY) total[m][0] = total[m][1] = f32x4{0, 0, 0, 0};
+    for (int c = 0; c < 2; c++) {
+#pragma unroll
+        for (int m = 0; m < 8; m++) {
+            acc[c][m] = f32x4{0, 0, 0, 0};
+            if constexpr (CHUNKS) total[c][m] = acc[c][m];
+        }
     }
-    for (uint32_t r0 = 0; r0 < rank; r0 += CHUNK) {
-        for (uint32_t j0 = r0; j0 < min(rank, r0 + CHUNK); j0 += 32) {
-            const uint32_t j = j0 + quarter * 8;
-            u32x4 raw[8];
+    for (uint32_t j0 = 0; j0 < tile.rank; j0 += 32) {
+        x8<T> cols[8], h[2][2];
+        const uint32_t j = j0 + quarter * 8;
 #pragma unroll
-            for (int i = 0; i < 8; i++)
-                raw[i] = load8<T, WIDE>((const T *)u.w.p + (int64_t)a * u.w.adapter + (int64_t)min(j + i, rank - 1) * u.w.row + n_lane,
-                                        j + i < rank ? w_count : 0);
-            x8<T> h[2][2], cols[8];
+        for (int c = 0; c < 2; c++)
 #pragma unroll
-            for (int c = 0; c < 2; c++)
+            for (int p = 0; p < 2; p++)
+                h[c][p] = as_x8<T>(j < s.rows ? *reinterpret_cast<const u32x4 *>(u.h.by_token[p] + by_token_at(slot, c * 16 + col, j, s.rows))
+                                              : u32x4{0, 0, 0, 0});
+        load_columns<T, WIDE>(u.w, tile.adapter, tile.rank, j0, n_first, cols);
 #pragma unroll
-                for (int p = 0; p < 2; p++)
-                    h[c][p] = as_x8<T>(j < s.rows ? *reinterpret_cast<const u32x4 *>(u.h.by_token[p] + ((size_t)slot * TILE + c * 16 + col) * s.rows + j)
-                                                  : u32x4{0, 0, 0, 0});
-            transpose8<T, 8>(raw, cols);
+        for (int m = 0; m < 8; m++)
+#pragma unroll
+            for (int c = 0; c < 2; c++) {
+                acc[c][m] = mfma16(h[c][0], cols[m], acc[c][m]);
+                acc[c][m] = mfma16(h[c][1], cols[m], acc[c][m]);
+            }
+        if constexpr (CHUNKS) {
+            const float unscale = u.h.unscale[(size_t)slot * s.chunks + j0 / CHUNK];
 #pragma unroll
             for (int m = 0; m < 8; m++)
 #pragma unroll
                 for (int c = 0; c < 2; c++) {
-                    acc[m][c] = mfma16(cols[m], h[c][0], acc[m][c]);
-                    acc[m][c] = mfma16(cols[m], h[c][1], acc[m][c]);
+                    total[c][m] += acc[c][m] * unscale;
+                    acc[c][m] = f32x4{0, 0, 0, 0};
                 }
         }
-        if constexpr (SCALED) {
-            const float unscale = u.h.unscale[(size_t)slot * s.chunks + r0 / CHUNK];
-#pragma unroll
-            for (int m = 0; m < 8; m++)
-#pragma unroll
-                for (int c = 0; c < 2; c++)
-#pragma unroll
-                    for (int i = 0; i < 4; i++) {
-                        if constexpr (MANY) {
-                            total[m][c][i] = fmaf(acc[m][c][i], unscale, total[m][c][i]);
-                            acc[m][c][i] = 0;
-                        } else acc[m][c][i] *= unscale;
-                    }
-        }
     }
+    BaseWords base[2][4];
+#pragma unroll
+    for (int c = 0; c < 2; c++) load_bases<T, WIDE>(u, tile.first + c * 16, tile.live - c * 16, n_first, base[c]);
+    const float unscale = std::is_same<T, _Float16>::value && !CHUNKS && tile.rank ? u.h.unscale[(size_t)slot * s.chunks] : 1.0f;
 #pragma unroll
     for (int c = 0; c < 2; c++) {
-        if (c * 16 + col >= live) continue;
-        const int64_t t = t0 + c * 16 + col;
+        if constexpr (std::is_same<T, _Float16>::value && !CHUNKS) {
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const uint32_t n = n_first + (i * 4 + quarter) * 8;
-            const int count = min(8, (int)N - (int)n);
-            if (count <= 0) continue;
-            float v[8];
-            load_base<T, WIDE>(u, t, n, count, v);
-#pragma unroll
-            for (int m = 0; m < 8; m++) v[m] += MANY ? total[MANY ? m : 0][c][i] : acc[m][c][i];
-            store8<T, WIDE>((T *)u.out + t * u.out_stride + n, pack<T>(v), count);
+            for (int m = 0; m < 8; m++) acc[c][m] *= unscale;
         }
+        write_outputs<T, WIDE>(u, tile.first + c * 16, tile.live - c * 16, n_first, base[c], CHUNKS ? total[CHUNKS ? c : 0] : acc[c]);
+    }
+}
+
+// Few tiles: a workgroup of sixteen wavefronts makes a tile's hidden values in LDS and takes SPAN outputs a wavefront of them, in one
+// launch and without a word of scratch.  Tiles of more outputs than that have several workgroups, each with all of the values.
+constexpr int STEP_WAVES = 16;
+template <class T, bool WIDE, int RT>
+__global__ __launch_bounds__(64 * STEP_WAVES) void k_adapter_step(Rows x, Matrix w_down, Up u, Segments s, uint32_t *d_bad)
+{
+    __shared__ __align__(16) uint16_t h[2][TILE][RT * 16];
+    const int wave = threadIdx.x >> 6, col = threadIdx.x & 15, quarter = threadIdx.x >> 4 & 3;
+    const Piece piece = find_piece(s.starts, s.segments, s.tokens, 1, TILE, blockIdx.x);
+    if (piece.segment < 0) return;
+    const Tile tile = tile_of(s, piece, threadIdx.x == 0 && blockIdx.y == 0 && piece.index == 0 ? d_bad : nullptr);
+    const uint32_t n_first = (blockIdx.y * STEP_WAVES + wave) * SPAN;
+    float unscale = 1;
+    if (tile.adapter >= 0) {
+        unscale = hidden_values<T, WIDE, RT, STEP_WAVES>(x, w_down, s, tile, 0, [&](int j, int t, uint16_t value, uint16_t rest) {
+            h[0][t][j] = value;
+            h[1][t][j] = rest;
+        });
+        __syncthreads();
+    }
+    if (n_first >= u.w.width) return;
+    x8<T> cols[8];
+    const bool some = tile.adapter >= 0 && tile.rank;
+    if (some) load_columns<T, WIDE>(u.w, tile.adapter, tile.rank, 0, n_first, cols);
+#pragma unroll 1
+    for (int c = 0; c < 2 && c * 16 < tile.live; c++) {
+        BaseWords base[4];
+        load_bases<T, WIDE>(u, tile.first + c * 16, tile.live - c * 16, n_first, base);
+        f32x4 acc[8];
+#pragma unroll
+        for (int m = 0; m < 8; m++) acc[m] = f32x4{0, 0, 0, 0};
+        if (some) {
+            x8<T> hv[2];
+#pragma unroll
+            for (int p = 0; p < 2; p++)
+                hv[p] = as_x8<T>(quarter * 8 < RT * 16 ? *reinterpret_cast<const u32x4 *>(&h[p][c * 16 + col][quarter * 8]) : u32x4{0, 0, 0, 0});
+#pragma unroll
+            for (int m = 0; m < 8; m++) {
+                acc[m] = mfma16(hv[0], cols[m], acc[m]);
+                acc[m] = mfma16(hv[1], cols[m], acc[m]);
+                if constexpr (std::is_same<T, _Float16>::value) acc[m] *= unscale;
+            }
+        }
+        write_outputs<T, WIDE>(u, tile.first + c * 16, tile.live - c * 16, n_first, base, acc);
     }
 }
 
@@ -388,7 +509,7 @@ __global__ __launch_bounds__(64 * OUTER_WAVES) void k_adapter_outer(Outer job0, 
 #pragma unroll
                     for (int p = 0; p < 2; p++) {
                         const uint32_t j = r0 + r * 16 + col;
-                        h[r][p] = as_x8<T>(j < s.rows ? *reinterpret_cast<const u32x4 *>(job.h.by_rank[p] + (slot * s.rows + j) * TILE + quarter * 8)
+                        h[r][p] = as_x8<T>(j < s.rows ? *reinterpret_cast<const u32x4 *>(job.h.by_rank[p] + by_rank_at(slot, j, quarter * 8, s.rows))
                                                       : u32x4{0, 0, 0, 0});
                     }
                 transpose8<T, 8>(raw, cols);
@@ -508,8 +629,9 @@ template <class T, bool WIDE> hipError_t down(const Down &d0, const Down &d1, in
 }
 template <class T, bool WIDE> hipError_t up(const Up &u, const Segments &s, hipStream_t st)
 {
+    constexpr bool F16 = std::is_same<T, _Float16>::value;
     const dim3 grid(slots_of(s.tokens, s.segments), (uint32_t)ceil_div(u.w.width, SPAN * UP_WAVES));
-    if (std::is_same<T, _Float16>::value && s.chunks > 1) k_adapter_up<T, WIDE, std::is_same<T, _Float16>::value><<<grid, 64 * UP_WAVES, 0, st>>>(u, s);
+    if (F16 && s.chunks > 1) k_adapter_up<T, WIDE, F16><<<grid, 64 * UP_WAVES, 0, st>>>(u, s);
     else k_adapter_up<T, WIDE, false><<<grid, 64 * UP_WAVES, 0, st>>>(u, s);
     return hipGetLastError();
 }
@@ -548,7 +670,7 @@ GradRoom lay_out(Room &room, const she_adapters_grad_args &a)
     return r;
 }
 
-template <class T> hipError_t forward(const she_adapters_args &a, void *scratch, uint32_t *d_bad, hipStream_t st)
+template <class T> hipError_t forward(const she_adapters_args &a, void *scratch, uint32_t *d_bad, uint32_t cus, hipStream_t st)
 {
     const Segments s = segments_of(a);
     Room room{static_cast<char *>(scratch)};
@@ -557,13 +679,18 @@ template <class T> hipError_t forward(const she_adapters_args &a, void *scratch,
     const Up u{{a.up, a.up_adapter, a.up_rank, a.outputs}, h, a.base, a.base_stride, a.step, a.base_type, a.out, a.out_stride};
     const bool wide_down = on16(a.x) && on16(a.down) && (a.x_stride | a.down_adapter | a.down_rank | a.inputs) % 8 == 0;
     const bool wide_up = on16(a.up) && on16(a.base) && on16(a.out) && (a.up_adapter | a.up_rank | a.base_stride | a.out_stride | a.outputs) % 8 == 0;
-    hipError_t rc = hipSuccess;
-    if (s.rank && s.adapters) rc = wide_down ? down<T, true>(d, d, 1, s, d_bad, st) : down<T, false>(d, d, 1, s, d_bad, st);
+    const dim3 grid(slots_of(a.tokens, a.segments), (uint32_t)ceil_div(a.outputs, SPAN * STEP_WAVES));
+    if (wide_down && wide_up && s.rank <= 32 && (uint64_t)grid.x * grid.y <= cus) {
+        if (s.rank <= 16) k_adapter_step<T, true, 1><<<grid, 64 * STEP_WAVES, 0, st>>>(d.x, d.w, u, s, d_bad);
+        else k_adapter_step<T, true, 2><<<grid, 64 * STEP_WAVES, 0, st>>>(d.x, d.w, u, s, d_bad);
+        return hipGetLastError();
+    }
+    hipError_t rc = wide_down ? down<T, true>(d, d, 1, s, d_bad, st) : down<T, false>(d, d, 1, s, d_bad, st);
     if (rc == hipSuccess) rc = wide_up ? up<T, true>(u, s, st) : up<T, false>(u, s, st);
     return rc;
 }
 
-template <class T> hipError_t backward(const she_adapters_grad_args &a, void *scratch, uint32_t *d_bad, hipStream_t st)
+template <class T> hipError_t backward(const she_adapters_grad_args &a, void *scratch, uint32_t *d_bad, uint32_t cus, hipStream_t st)
 {
     const Segments s = segments_of(a);
     Room room{static_cast<char *>(scratch)};
@@ -600,13 +727,13 @@ size_t adapters_grad_scratch(const she_adapters_grad_args &a)
     lay_out(room, a);
     return room.used;
 }
-hipError_t launch_adapters(const she_adapters_args &a, void *scratch, uint32_t *d_bad, hipStream_t st)
+hipError_t launch_adapters(const she_adapters_args &a, void *scratch, uint32_t *d_bad, uint32_t cus, hipStream_t st)
 {
-    return a.type == SHE_BF16 ? forward<__bf16>(a, scratch, d_bad, st) : forward<_Float16>(a, scratch, d_bad, st);
+    return a.type == SHE_BF16 ? forward<__bf16>(a, scratch, d_bad, cus, st) : forward<_Float16>(a, scratch, d_bad, cus, st);
 }
-hipError_t launch_adapters_grad(const she_adapters_grad_args &a, void *scratch, uint32_t *d_bad, hipStream_t st)
+hipError_t launch_adapters_grad(const she_adapters_grad_args &a, void *scratch, uint32_t *d_bad, uint32_t cus, hipStream_t st)
 {
-    return a.type == SHE_BF16 ? backward<__bf16>(a, scratch, d_bad, st) : backward<_Float16>(a, scratch, d_bad, st);
+    return a.type == SHE_BF16 ? backward<__bf16>(a, scratch, d_bad, cus, st) : backward<_Float16>(a, scratch, d_bad, cus, st);
 }
 
 }}  // namespace she::clear

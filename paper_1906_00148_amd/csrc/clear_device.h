@@ -48,6 +48,35 @@ template <class T, bool WIDE> __device__ inline void store8(T *p, u32x4 words, i
             if (i < count) p[i] = v[i];
     }
 }
+// Four elements from p on and four from p + 64 on, of which the first `count` of the first and `more` of the others exist.  WIDE: all or
+// none of either four, p on 8 bytes.
+template <class T, bool WIDE> __device__ inline u32x4 load_quads(const T *p, int count, int more)
+{
+    if constexpr (WIDE) {
+        const uint2 a = count > 0 ? *reinterpret_cast<const uint2 *>(p) : uint2{0, 0}, b = more > 0 ? *reinterpret_cast<const uint2 *>(p + 64) : uint2{0, 0};
+        return u32x4{a.x, a.y, b.x, b.y};
+    } else {
+        x8<T> v;
+        for (int i = 0; i < 4; i++) {
+            v[i] = i < count ? p[i] : (T)0.0f;
+            v[4 + i] = i < more ? p[64 + i] : (T)0.0f;
+        }
+        return as_words<T>(v);
+    }
+}
+template <class T, bool WIDE> __device__ inline void store_quads(T *p, u32x4 words, int count, int more)
+{
+    if constexpr (WIDE) {
+        if (count > 0) *reinterpret_cast<uint2 *>(p) = uint2{words[0], words[1]};
+        if (more > 0) *reinterpret_cast<uint2 *>(p + 64) = uint2{words[2], words[3]};
+    } else {
+        const x8<T> v = as_x8<T>(words);
+        for (int i = 0; i < 4; i++) {
+            if (i < count) p[i] = v[i];
+            if (i < more) p[64 + i] = v[4 + i];
+        }
+    }
+}
 template <class T> __device__ inline void unpack(u32x4 words, float out[8])
 {
     const x8<T> v = as_x8<T>(words);
@@ -60,6 +89,19 @@ template <class T> __device__ inline u32x4 pack(const float in[8])
 #pragma unroll
     for (int i = 0; i < 8; i++) v[i] = (T)in[i];
     return as_words<T>(v);
+}
+
+// The operand of a matrix instruction of sixteen rows of 32 neighbours, loaded as memory has it: lane l the unit l % 4 of row l / 4, which
+// keeps the requests of neighbouring lanes in one line.  Lane l gets unit l / 16 of row l % 16.  (Loaded the operand's way round, every
+// lane's 16 bytes are a line of their own, and a compute unit takes in 16 bytes a cycle.)
+__device__ inline int operand_row() { return threadIdx.x >> 2 & 15; }
+__device__ inline int operand_unit() { return threadIdx.x & 3; }
+__device__ inline u32x4 to_operand(u32x4 v)
+{
+    const int from = ((threadIdx.x & 15) * 4 + (threadIdx.x >> 4 & 3)) * 4;
+#pragma unroll
+    for (int i = 0; i < 4; i++) v[i] = (uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)v[i]);
+    return v;
 }
 
 // Eight rows of COLS neighbours -> for each of these columns, its elements of the eight rows.

@@ -33,8 +33,8 @@ hipError_t launch_qk_rotate_grad(const she_qk_rotate_grad_args &a, const QkShape
 // ---- adapters
 size_t adapters_scratch(const she_adapters_args &a);
 size_t adapters_grad_scratch(const she_adapters_grad_args &a);
-hipError_t launch_adapters(const she_adapters_args &a, void *scratch, uint32_t *d_bad, hipStream_t st);
-hipError_t launch_adapters_grad(const she_adapters_grad_args &a, void *scratch, uint32_t *d_bad, hipStream_t st);
+hipError_t launch_adapters(const she_adapters_args &a, void *scratch, uint32_t *d_bad, uint32_t cus, hipStream_t st);
+hipError_t launch_adapters_grad(const she_adapters_grad_args &a, void *scratch, uint32_t *d_bad, uint32_t cus, hipStream_t st);
 
 // ---- attention
 struct AttendShape {

@@ -81,7 +81,7 @@ try {
     if (!a.tokens || !a.segments) return SHE_OK;
     if (!a.out) return fail(c, SHE_EINVAL, "she_adapters: null argument");
     if ((rc = ready(c)) || (rc = ensure_scratch(c, clear::adapters_scratch(a)))) return rc;
-    HIP_TRY(c, clear::launch_adapters(a, c->clear.scratch, c->clear.d_bad, c->stream));
+    HIP_TRY(c, clear::launch_adapters(a, c->clear.scratch, c->clear.d_bad, c->dk.cus, c->stream));
     return SHE_OK;
 } SHE_NOTHROW(c)
 
@@ -95,7 +95,7 @@ try {
     if (a.base_type == SHE_I32) return fail(c, SHE_EINVAL, "she_adapters_grad: base_type must be SHE_NO_BASE, the type or SHE_F32");
     if (!a.ddown || !a.dup || (a.tokens && (!a.dy || !a.dx))) return fail(c, SHE_EINVAL, "she_adapters_grad: null argument");
     if ((rc = ready(c)) || (rc = ensure_scratch(c, clear::adapters_grad_scratch(a)))) return rc;
-    HIP_TRY(c, clear::launch_adapters_grad(a, c->clear.scratch, c->clear.d_bad, c->stream));
+    HIP_TRY(c, clear::launch_adapters_grad(a, c->clear.scratch, c->clear.d_bad, c->dk.cus, c->stream));
     return SHE_OK;
 } SHE_NOTHROW(c)
 
