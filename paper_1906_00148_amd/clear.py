@@ -8,6 +8,7 @@ torch's current stream is another one, that work waits for it and it waits for t
 from __future__ import annotations
 
 import ctypes as C
+import struct
 
 import torch
 
@@ -20,44 +21,48 @@ class SheError(RuntimeError):
         self.code = code
 
 
-_i32, _u32, _i64, _f32, _p = C.c_int32, C.c_uint32, C.c_int64, C.c_float, C.c_void_p
+class _Layout:
+    """A struct of include/she_clear.h, packed into bytes of the native layout (a fifth of the time that a ctypes structure takes)."""
+
+    def __init__(self, name, fields):
+        """`fields`: a struct format character and the names that have it, in the header's order."""
+        self.name, self.fields = name, [(n, ty) for ty, names in fields for n in names.split()]
+        packer = struct.Struct("@" + "".join(ty for _, ty in self.fields))
+        self.pack, self.size = packer.pack, packer.size
+
+    def offsets(self):
+        at = {}
+        for k, (name, ty) in enumerate(self.fields):
+            before = "@" + "".join(t for _, t in self.fields[:k])
+            at[name] = struct.calcsize(before + ty) - struct.calcsize(ty)
+        return at
 
 
-def _struct(name, fields):
-    """A C struct of include/she_clear.h: `fields` is lines of a ctypes type and the names that have it, in the header's order."""
-    return type(name, (C.Structure,), {"_fields_": [(n, ty) for ty, names in fields for n in names.split()]})
+_ADAPTERS = _Layout("she_adapters_args", [
+    ("i", "type base_type"), ("I", "tokens inputs outputs adapters rank segments"), ("P", "x"), ("q", "x_stride"), ("P", "down"),
+    ("q", "down_adapter down_rank"), ("P", "up"), ("q", "up_adapter up_rank"), ("P", "starts which ranks scale base"),
+    ("q", "base_stride"), ("P", "step out"), ("q", "out_stride")])
+_ADAPTERS_GRAD = _Layout("she_adapters_grad_args", [
+    ("i", "type base_type"), ("I", "tokens inputs outputs adapters rank segments"), ("P", "dy"), ("q", "dy_stride"), ("P", "x"),
+    ("q", "x_stride"), ("P", "down"), ("q", "down_adapter down_rank"), ("P", "up"), ("q", "up_adapter up_rank"),
+    ("P", "starts which ranks scale base"), ("q", "base_stride"), ("P", "dx"), ("q", "dx_stride"), ("P", "ddown dup")])
+_QK_ROTATE = _Layout("she_qk_rotate_args", [
+    ("i", "type interleaved"), ("I", "tokens q_heads kv_heads head rot places"), ("f", "eps"), ("P", "q k v"),
+    ("q", "q_token q_head k_token k_head v_token v_head"), ("P", "wq wk cosines sines positions q_out k_out"),
+    ("q", "q_out_token q_out_head k_out_token k_out_head"), ("P", "k_pages v_pages"), ("q", "page_stride slot_stride page_head"),
+    ("I", "pages page_size"), ("P", "slots")])
+_QK_ROTATE_GRAD = _Layout("she_qk_rotate_grad_args", [
+    ("i", "type interleaved"), ("I", "tokens q_heads kv_heads head rot places"), ("f", "eps"), ("P", "dq_out dk_out"),
+    ("q", "dq_out_token dq_out_head dk_out_token dk_out_head"), ("P", "q k"), ("q", "q_token q_head k_token k_head"),
+    ("P", "wq wk cosines sines positions dq dk"), ("q", "dq_token dq_head dk_token dk_head"), ("P", "dwq dwk")])
+_ATTEND_PAGES = _Layout("she_attend_pages_args", [
+    ("i", "type"), ("I", "tokens requests q_heads kv_heads head window"), ("f", "scale"), ("P", "q"), ("q", "q_token q_head"),
+    ("P", "k_pages v_pages"), ("q", "page_stride slot_stride page_head"), ("I", "pages page_size"), ("P", "table"),
+    ("q", "table_stride"), ("I", "table_width"), ("P", "starts lengths out"), ("q", "out_token out_head")])
+LAYOUTS = [_ADAPTERS, _ADAPTERS_GRAD, _QK_ROTATE, _QK_ROTATE_GRAD, _ATTEND_PAGES]
 
-
-_Adapters = _struct("she_adapters_args", [
-    (_i32, "type base_type"), (_u32, "tokens inputs outputs adapters rank segments"), (_p, "x"), (_i64, "x_stride"), (_p, "down"),
-    (_i64, "down_adapter down_rank"), (_p, "up"), (_i64, "up_adapter up_rank"), (_p, "starts which ranks scale base"),
-    (_i64, "base_stride"), (_p, "step out"), (_i64, "out_stride")])
-_AdaptersGrad = _struct("she_adapters_grad_args", [
-    (_i32, "type base_type"), (_u32, "tokens inputs outputs adapters rank segments"), (_p, "dy"), (_i64, "dy_stride"), (_p, "x"),
-    (_i64, "x_stride"), (_p, "down"), (_i64, "down_adapter down_rank"), (_p, "up"), (_i64, "up_adapter up_rank"),
-    (_p, "starts which ranks scale base"), (_i64, "base_stride"), (_p, "dx"), (_i64, "dx_stride"), (_p, "ddown dup")])
-_QkRotate = _struct("she_qk_rotate_args", [
-    (_i32, "type interleaved"), (_u32, "tokens q_heads kv_heads head rot places"), (_f32, "eps"), (_p, "q k v"),
-    (_i64, "q_token q_head k_token k_head v_token v_head"), (_p, "wq wk cosines sines positions q_out k_out"),
-    (_i64, "q_out_token q_out_head k_out_token k_out_head"), (_p, "k_pages v_pages"), (_i64, "page_stride slot_stride page_head"),
-    (_u32, "pages page_size"), (_p, "slots")])
-_QkRotateGrad = _struct("she_qk_rotate_grad_args", [
-    (_i32, "type interleaved"), (_u32, "tokens q_heads kv_heads head rot places"), (_f32, "eps"), (_p, "dq_out dk_out"),
-    (_i64, "dq_out_token dq_out_head dk_out_token dk_out_head"), (_p, "q k"), (_i64, "q_token q_head k_token k_head"),
-    (_p, "wq wk cosines sines positions dq dk"), (_i64, "dq_token dq_head dk_token dk_head"), (_p, "dwq dwk")])
-_AttendPages = _struct("she_attend_pages_args", [
-    (_i32, "type"), (_u32, "tokens requests q_heads kv_heads head window"), (_f32, "scale"), (_p, "q"), (_i64, "q_token q_head"),
-    (_p, "k_pages v_pages"), (_i64, "page_stride slot_stride page_head"), (_u32, "pages page_size"), (_p, "table"),
-    (_i64, "table_stride"), (_u32, "table_width"), (_p, "starts lengths out"), (_i64, "out_token out_head")])
-
-SIGNATURES = {
-    "she_adapters": (C.c_int, [_p, C.POINTER(_Adapters)]),
-    "she_adapters_grad": (C.c_int, [_p, C.POINTER(_AdaptersGrad)]),
-    "she_qk_rotate": (C.c_int, [_p, C.POINTER(_QkRotate)]),
-    "she_qk_rotate_grad": (C.c_int, [_p, C.POINTER(_QkRotateGrad)]),
-    "she_attend_pages": (C.c_int, [_p, C.POINTER(_AttendPages)]),
-    "she_clear_bad_ids": (C.c_int, [_p, C.POINTER(C.c_uint64), C.c_int]),
-}
+SIGNATURES = {**{layout.name[:-len("_args")]: (C.c_int, [C.c_void_p, C.c_char_p]) for layout in LAYOUTS},
+              "she_clear_bad_ids": (C.c_int, [C.c_void_p, C.POINTER(C.c_uint64), C.c_int])}
 
 _NO_BASE, _F32, _I32 = -1, 2, 3
 
@@ -75,10 +80,11 @@ def _half(t, name):
 
 
 def _see(t, name, dtype, shape):
-    """A tensor's address; refuses one of another type, shape or place, or without a contiguous last axis."""
-    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or (t.stride(-1) != 1 and shape[-1] > 1):
+    """A tensor's address and strides; refuses one of another type, shape or place, or without a contiguous last axis."""
+    strides = t.stride()
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or (strides[-1] != 1 and shape[-1] > 1):
         _refuse_tensor(t, name, dtype, shape)
-    return t.data_ptr()
+    return t.data_ptr(), strides
 
 
 def _refuse_tensor(t, name, dtype, shape):
@@ -88,12 +94,16 @@ def _refuse_tensor(t, name, dtype, shape):
         _refuse(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
     if not t.is_cuda:
         _refuse(f"{name} must be on the GPU")
-    _refuse(f"{name} must be contiguous along its last axis")
+    _refuse(f"{name} must be contiguous{' along its last axis' if len(shape) > 1 else ''}")
 
 
 def _line(t, name, dtype, size):
-    """A vector that a kernel reads densely; None: a null pointer."""
-    return None if t is None else _see(t, name, dtype, (size,))
+    """The address of a vector that a kernel reads densely; None: a null pointer."""
+    if t is None:
+        return 0
+    if t.dtype is not dtype or t.shape != (size,) or not t.is_cuda or not t.is_contiguous():
+        _refuse_tensor(t, name, dtype, (size,))
+    return t.data_ptr()
 
 
 class Calls:
@@ -102,7 +112,7 @@ class Calls:
     def _call(self, fn, args):
         """Runs a call on the context's stream, ordered with torch's current stream where that is another one."""
         if torch._C._cuda_getCurrentRawStream(self._device) == self._stream:
-            rc = fn(self._h, C.byref(args))
+            rc = fn(self._h, args)
             if rc:
                 self._check(rc)
             return
@@ -112,7 +122,7 @@ class Calls:
         mine = torch.cuda.ExternalStream(self._stream, self._device) if self._stream else torch.cuda.default_stream(self._device)
         mine.wait_stream(current)
         try:
-            self._check(fn(self._h, C.byref(args)))
+            self._check(fn(self._h, args))
         finally:
             current.wait_stream(mine)
 
@@ -125,27 +135,32 @@ class Calls:
         ty, dtype = _half(x, "x"), x.dtype
         (T, K), (A, r, N) = x.shape, up.shape
         S = which.shape[0]
-        pointers = (_see(x, "x", dtype, (T, K)), _see(down, "down", dtype, (A, r, K)), _see(up, "up", dtype, (A, r, N)),
-                    _see(starts, "starts", torch.int32, (S + 1,)), _see(which, "which", torch.int32, (S,)))
+        x_at, xs = _see(x, "x", dtype, (T, K))
+        down_at, ds = _see(down, "down", dtype, (A, r, K))
+        up_at, us = _see(up, "up", dtype, (A, r, N))
         kind, base_at, base_stride = self._base(base, dtype, ty, (T, N))
         if step is not None and kind != _I32:
             _refuse("step belongs to int32 sums")
         if out is None:
             out = torch.empty(T, N, dtype=dtype, device=x.device)
-        self._call(self._L.she_adapters, _Adapters(
-            ty, kind, T, K, N, A, r, S, pointers[0], x.stride(0), pointers[1], down.stride(0), down.stride(1), pointers[2], up.stride(0),
-            up.stride(1), pointers[3], pointers[4], _line(ranks, "ranks", torch.int32, A), _line(scale, "scale", torch.float32, A),
-            base_at, base_stride, _line(step, "step", torch.float32, N), _see(out, "out", dtype, (T, N)), out.stride(0)))
+            out_at, out_stride = out.data_ptr(), N
+        else:
+            out_at, (out_stride, _) = _see(out, "out", dtype, (T, N))
+        self._call(self._L.she_adapters, _ADAPTERS.pack(
+            ty, kind, T, K, N, A, r, S, x_at, xs[0], down_at, ds[0], ds[1], up_at, us[0], us[1], _line(starts, "starts", torch.int32, S + 1),
+            _line(which, "which", torch.int32, S), _line(ranks, "ranks", torch.int32, A), _line(scale, "scale", torch.float32, A),
+            base_at, base_stride, _line(step, "step", torch.float32, N), out_at, out_stride))
         return out
 
     @staticmethod
     def _base(base, dtype, ty, shape):
         if base is None:
-            return _NO_BASE, None, 0
+            return _NO_BASE, 0, 0
         kind = {dtype: ty, torch.float32: _F32, torch.int32: _I32}.get(base.dtype)
         if kind is None:
             _refuse(f"base must be {dtype}, float32 or int32, not {base.dtype}")
-        return kind, _see(base, "base", base.dtype, shape), base.stride(0)
+        at, strides = _see(base, "base", base.dtype, shape)
+        return kind, at, strides[0]
 
     def adapters_grad(self, dy, x, down, up, starts, which, scale, ranks=None, base=None):
         """Gradients of `adapters` for dy [tokens, outputs]: (dx, ddown, dup), dx with `base` (the gradient that reaches x through the
@@ -153,78 +168,81 @@ class Calls:
         ty, dtype = _half(x, "x"), x.dtype
         (T, K), (A, r, N) = x.shape, up.shape
         S = which.shape[0]
-        pointers = (_see(dy, "dy", dtype, (T, N)), _see(x, "x", dtype, (T, K)), _see(down, "down", dtype, (A, r, K)),
-                    _see(up, "up", dtype, (A, r, N)), _see(starts, "starts", torch.int32, (S + 1,)),
-                    _see(which, "which", torch.int32, (S,)))
+        dy_at, dys = _see(dy, "dy", dtype, (T, N))
+        x_at, xs = _see(x, "x", dtype, (T, K))
+        down_at, ds = _see(down, "down", dtype, (A, r, K))
+        up_at, us = _see(up, "up", dtype, (A, r, N))
         kind, base_at, base_stride = self._base(base, dtype, ty, (T, K))
-        dx = torch.empty(T, K, dtype=dtype, device=x.device)
-        ddown = torch.empty(A, r, K, dtype=dtype, device=x.device)
-        dup = torch.empty(A, r, N, dtype=dtype, device=x.device)
-        self._call(self._L.she_adapters_grad, _AdaptersGrad(
-            ty, kind, T, K, N, A, r, S, pointers[0], dy.stride(0), pointers[1], x.stride(0), pointers[2], down.stride(0), down.stride(1),
-            pointers[3], up.stride(0), up.stride(1), pointers[4], pointers[5], _line(ranks, "ranks", torch.int32, A),
-            _line(scale, "scale", torch.float32, A), base_at, base_stride, dx.data_ptr(), dx.stride(0), ddown.data_ptr(), dup.data_ptr()))
+        dx, ddown, dup = (torch.empty(shape, dtype=dtype, device=x.device) for shape in ((T, K), (A, r, K), (A, r, N)))
+        self._call(self._L.she_adapters_grad, _ADAPTERS_GRAD.pack(
+            ty, kind, T, K, N, A, r, S, dy_at, dys[0], x_at, xs[0], down_at, ds[0], ds[1], up_at, us[0], us[1],
+            _line(starts, "starts", torch.int32, S + 1), _line(which, "which", torch.int32, S), _line(ranks, "ranks", torch.int32, A),
+            _line(scale, "scale", torch.float32, A), base_at, base_stride, dx.data_ptr(), K, ddown.data_ptr(), dup.data_ptr()))
         return dx, ddown, dup
 
     @staticmethod
     def _rotation(q, k, wq, wk, cos, sin, positions):
-        """What the three calls on queries and keys have in common, checked: the first fields of their structs, and pointers."""
+        """What the three calls on queries and keys have in common, checked: type, sizes, addresses and strides."""
         ty, dtype = _half(q, "q"), q.dtype
         (T, Hq, D), Hkv = q.shape, k.shape[1]
         P, half = cos.shape
-        _see(q, "q", dtype, (T, Hq, D)), _see(k, "k", dtype, (T, Hkv, D))
-        tables = (_line(wq, "wq", torch.float32, D), _line(wk, "wk", torch.float32, D), _see(cos, "cos", torch.float32, (P, half)),
-                  _see(sin, "sin", torch.float32, (P, half)), _see(positions, "positions", torch.int32, (T,)))
+        q_at, qs = _see(q, "q", dtype, (T, Hq, D))
+        k_at, ks = _see(k, "k", dtype, (T, Hkv, D))
+        tables = (_line(wq, "wq", torch.float32, D), _line(wk, "wk", torch.float32, D), _see(cos, "cos", torch.float32, (P, half))[0],
+                  _see(sin, "sin", torch.float32, (P, half))[0], _line(positions, "positions", torch.int32, T))
         if not (cos.is_contiguous() and sin.is_contiguous()):
             _refuse("cos and sin must be contiguous")
-        return ty, dtype, (T, Hq, Hkv, D, 2 * half, P), tables
+        return ty, dtype, (T, Hq, Hkv, D, 2 * half, P), (q_at, k_at), (qs[0], qs[1], ks[0], ks[1]), tables
 
     def qk_rotate(self, q, k, wq, wk, cos, sin, positions, eps=1e-6, interleaved=False, out=None):
         """Norm of every head of q [tokens, q_heads, head] and k [tokens, kv_heads, head] with the weights wq, wk [head] float32 (or
         None), and the rotation by cos, sin [places, rot / 2] float32 at positions [tokens] int32.  Returns (q', k'); out: a pair
         for them, which may be (q, k)."""
-        ty, dtype, (T, Hq, Hkv, D, rot, P), tables = self._rotation(q, k, wq, wk, cos, sin, positions)
+        ty, dtype, (T, Hq, Hkv, D, rot, P), at, strides, tables = self._rotation(q, k, wq, wk, cos, sin, positions)
         if out is None:
             out = torch.empty(T, Hq, D, dtype=dtype, device=q.device), torch.empty(T, Hkv, D, dtype=dtype, device=q.device)
-        qo, ko = out
-        self._call(self._L.she_qk_rotate, _QkRotate(
-            ty, bool(interleaved), T, Hq, Hkv, D, rot, P, eps, q.data_ptr(), k.data_ptr(), None, q.stride(0), q.stride(1), k.stride(0),
-            k.stride(1), 0, 0, *tables, _see(qo, "out", dtype, (T, Hq, D)), _see(ko, "out", dtype, (T, Hkv, D)), qo.stride(0),
-            qo.stride(1), ko.stride(0), ko.stride(1)))
-        return qo, ko
+        q_out, qs = _see(out[0], "out", dtype, (T, Hq, D))
+        k_out, ks = _see(out[1], "out", dtype, (T, Hkv, D))
+        self._call(self._L.she_qk_rotate, _QK_ROTATE.pack(
+            ty, bool(interleaved), T, Hq, Hkv, D, rot, P, eps, *at, 0, *strides, 0, 0, *tables, q_out, k_out, qs[0], qs[1], ks[0], ks[1],
+            0, 0, 0, 0, 0, 0, 0, 0))
+        return out[0], out[1]
 
     def qk_rotate_append(self, q, k, v, wq, wk, cos, sin, positions, k_pages, v_pages, slots, eps=1e-6, interleaved=False, out=None):
         """qk_rotate whose keys, with the values v [tokens, kv_heads, head], go to the places slots [tokens] int64 (-1: nowhere) of
         k_pages, v_pages [pages, page_size, kv_heads, head].  Returns q'."""
-        ty, dtype, (T, Hq, Hkv, D, rot, P), tables = self._rotation(q, k, wq, wk, cos, sin, positions)
-        pages, size = k_pages.shape[:2]
-        v_at, pages_at = _see(v, "v", dtype, (T, Hkv, D)), self._pages(k_pages, v_pages, dtype, Hkv, D)
-        qo = torch.empty(T, Hq, D, dtype=dtype, device=q.device) if out is None else out
-        self._call(self._L.she_qk_rotate, _QkRotate(
-            ty, bool(interleaved), T, Hq, Hkv, D, rot, P, eps, q.data_ptr(), k.data_ptr(), v_at, q.stride(0), q.stride(1), k.stride(0),
-            k.stride(1), v.stride(0), v.stride(1), *tables, _see(qo, "out", dtype, (T, Hq, D)), None, qo.stride(0), qo.stride(1), 0, 0,
-            *pages_at, pages, size, _see(slots, "slots", torch.int64, (T,))))
-        return qo
+        ty, dtype, (T, Hq, Hkv, D, rot, P), at, strides, tables = self._rotation(q, k, wq, wk, cos, sin, positions)
+        v_at, vs = _see(v, "v", dtype, (T, Hkv, D))
+        pages_at, pages, size = self._pages(k_pages, v_pages, dtype, Hkv, D)
+        if out is None:
+            out = torch.empty(T, Hq, D, dtype=dtype, device=q.device)
+        q_out, qs = _see(out, "out", dtype, (T, Hq, D))
+        self._call(self._L.she_qk_rotate, _QK_ROTATE.pack(
+            ty, bool(interleaved), T, Hq, Hkv, D, rot, P, eps, *at, v_at, *strides, vs[0], vs[1], *tables, q_out, 0, qs[0], qs[1], 0, 0,
+            *pages_at, pages, size, _line(slots, "slots", torch.int64, T)))
+        return out
 
     @staticmethod
     def _pages(k_pages, v_pages, dtype, Hkv, D):
-        shape = (*k_pages.shape[:2], Hkv, D)
-        at = _see(k_pages, "k_pages", dtype, shape), _see(v_pages, "v_pages", dtype, shape)
-        if k_pages.stride() != v_pages.stride():
+        """(addresses and strides, pages, page size)"""
+        pages, size = k_pages.shape[:2]
+        k_at, strides = _see(k_pages, "k_pages", dtype, (pages, size, Hkv, D))
+        v_at, other = _see(v_pages, "v_pages", dtype, (pages, size, Hkv, D))
+        if strides != other:
             _refuse("k_pages and v_pages must have the same strides")
-        return *at, *k_pages.stride()[:3]
+        return (k_at, v_at, strides[0], strides[1], strides[2]), pages, size
 
     def qk_rotate_grad(self, dq_out, dk_out, q, k, wq, wk, cos, sin, positions, eps=1e-6, interleaved=False):
         """Gradients of qk_rotate: (dq, dk, dwq, dwk), the weights' in float32."""
-        ty, dtype, (T, Hq, Hkv, D, rot, P), tables = self._rotation(q, k, wq, wk, cos, sin, positions)
+        ty, dtype, (T, Hq, Hkv, D, rot, P), at, strides, tables = self._rotation(q, k, wq, wk, cos, sin, positions)
+        dq_at, dqs = _see(dq_out, "dq_out", dtype, (T, Hq, D))
+        dk_at, dks = _see(dk_out, "dk_out", dtype, (T, Hkv, D))
         dq, dk = (torch.empty(T, h, D, dtype=dtype, device=q.device) for h in (Hq, Hkv))
         dw = torch.empty(2, D, dtype=torch.float32, device=q.device)
-        at = dw.data_ptr()
-        self._call(self._L.she_qk_rotate_grad, _QkRotateGrad(
-            ty, bool(interleaved), T, Hq, Hkv, D, rot, P, eps, _see(dq_out, "dq_out", dtype, (T, Hq, D)),
-            _see(dk_out, "dk_out", dtype, (T, Hkv, D)), dq_out.stride(0), dq_out.stride(1), dk_out.stride(0), dk_out.stride(1),
-            q.data_ptr(), k.data_ptr(), q.stride(0), q.stride(1), k.stride(0), k.stride(1), *tables, dq.data_ptr(), dk.data_ptr(),
-            dq.stride(0), dq.stride(1), dk.stride(0), dk.stride(1), at, at + 4 * D))
+        dw_at = dw.data_ptr()
+        self._call(self._L.she_qk_rotate_grad, _QK_ROTATE_GRAD.pack(
+            ty, bool(interleaved), T, Hq, Hkv, D, rot, P, eps, dq_at, dk_at, dqs[0], dqs[1], dks[0], dks[1], *at, *strides, *tables,
+            dq.data_ptr(), dk.data_ptr(), Hq * D, D, Hkv * D, D, dw_at, dw_at + 4 * D))
         return dq, dk, dw[0], dw[1]
 
     def attend_pages(self, q, k_pages, v_pages, table, starts, lengths, scale=None, window=0, out=None):
@@ -233,17 +251,21 @@ class Calls:
         causal, and over the last `window` places alone if that is not 0.  scale: head ** -0.5 if None.  Returns out like q."""
         ty, dtype = _half(q, "q"), q.dtype
         T, Hq, D = q.shape
-        pages, size, Hkv = k_pages.shape[:3]
+        Hkv = k_pages.shape[2]
         R, width = table.shape
-        q_at, pages_at = _see(q, "q", dtype, (T, Hq, D)), self._pages(k_pages, v_pages, dtype, Hkv, D)
+        q_at, qs = _see(q, "q", dtype, (T, Hq, D))
+        pages_at, pages, size = self._pages(k_pages, v_pages, dtype, Hkv, D)
+        table_at, ts = _see(table, "table", torch.int32, (R, width))
         if not 0 <= window < 1 << 32:
             _refuse("window must be a number of places")
         if out is None:
             out = torch.empty(T, Hq, D, dtype=dtype, device=q.device)
-        self._call(self._L.she_attend_pages, _AttendPages(
-            ty, T, R, Hq, Hkv, D, window, D ** -0.5 if scale is None else scale, q_at, q.stride(0), q.stride(1), *pages_at, pages, size,
-            _see(table, "table", torch.int32, (R, width)), table.stride(0), width, _see(starts, "starts", torch.int32, (R + 1,)),
-            _see(lengths, "lengths", torch.int32, (R,)), _see(out, "out", dtype, (T, Hq, D)), out.stride(0), out.stride(1)))
+            out_at, out_token, out_head = out.data_ptr(), Hq * D, D
+        else:
+            out_at, (out_token, out_head, _) = _see(out, "out", dtype, (T, Hq, D))
+        self._call(self._L.she_attend_pages, _ATTEND_PAGES.pack(
+            ty, T, R, Hq, Hkv, D, window, D ** -0.5 if scale is None else scale, q_at, qs[0], qs[1], *pages_at, pages, size, table_at, ts[0],
+            width, _line(starts, "starts", torch.int32, R + 1), _line(lengths, "lengths", torch.int32, R), out_at, out_token, out_head))
         return out
 
     def clear_bad_ids(self, reset: bool = True) -> int:

@@ -606,14 +606,14 @@ Hidden take_hidden(Room &room, uint32_t slots, uint32_t rows, uint32_t chunks, b
     h.unscale = room.take<float>((size_t)slots * chunks);
     return h;
 }
-// Backward, a workgroup sums four tiles a wavefront and more where an adapter would else be shared by more than 16.
+// Backward, a workgroup sums eight tiles a wavefront (four: 80 us of gradients over 8192 tokens and not 74), and more where an adapter would else be shared by more than 16.
 template <class Args> Segments segments_of(const Args &a)
 {
     Segments s{a.starts, a.which, a.ranks, a.scale, a.tokens, a.segments, a.adapters, a.rank};
     s.rows = (uint32_t)ceil_div(a.rank, 16) * 16;
     s.chunks = (uint32_t)ceil_div(a.rank, CHUNK);
     const uint32_t tiles = slots_of(a.tokens, a.segments);
-    s.share = std::max<uint32_t>(4 * OUTER_WAVES, (uint32_t)ceil_div(tiles, 16));
+    s.share = std::max<uint32_t>(8 * OUTER_WAVES, (uint32_t)ceil_div(tiles, 16));
     s.most = (uint32_t)std::max<uint64_t>(1, ceil_div(tiles, s.share));
     s.places = s.most > 1 ? tiles / s.share + a.adapters : 0;
     return s;
