@@ -540,37 +540,75 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
         }
 }
 
-// The rows that were cut: a wavefront a row.
+// Rows that were cut, `each` of a tile a workgroup: four, or one where there may be many pieces.  Up to JOIN_AHEAD pieces are a
+// wavefront's work; more are shared out among all four, a row after the other.  Pieces are requested JOIN_AHEAD at a time.  A token
+// over 32768 places, 4 rows of 64 pieces at 8 key heads, takes 32 us so, 43 with four rows a workgroup and 78 with a row a wavefront.
+constexpr int JOIN_AHEAD = 4;
 template <class T>
-__global__ __launch_bounds__(256) void k_attend_join(she_attend_pages_args a, uint32_t group, Work w)
+__device__ inline void join_row(const she_attend_pages_args &a, const Work &w, size_t at, int parts, int from, int by, float &sum, float o[4])
 {
+    const int lane = threadIdx.x & 63, D = (int)a.head;
+    float top = -__builtin_inff();
+    for (int k = lane; k < parts; k += 64) top = fmaxf(top, w.ml[at + k].x);
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
+    sum = 0;
+#pragma unroll
+    for (int i = 0; i < 4; i++) o[i] = 0;
+    for (int k0 = from; k0 < parts; k0 += by * JOIN_AHEAD) {
+        float2 ml[JOIN_AHEAD];
+        float v[JOIN_AHEAD][4];
+#pragma unroll
+        for (int e = 0; e < JOIN_AHEAD; e++) {
+            const int k = k0 + by * e;
+            ml[e] = k < parts ? w.ml[at + k] : float2{-__builtin_inff(), 0};
+#pragma unroll
+            for (int i = 0; i < 4; i++) v[e][i] = k < parts && lane + 64 * i < D ? w.o[(at + k) * D + lane + 64 * i] : 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < JOIN_AHEAD; e++) {
+            const float f = ml[e].x == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(ml[e].x - top);
+            sum = fmaf(ml[e].y, f, sum);
+#pragma unroll
+            for (int i = 0; i < 4; i++) o[i] = fmaf(v[e][i], f, o[i]);
+        }
+    }
+}
+template <class T, bool TILES>
+__global__ __launch_bounds__(256) void k_attend_join(she_attend_pages_args a, uint32_t group, Work w, int each)
+{
+    constexpr int ROWS = TILES ? TILE_ROWS : FEW_ROWS;
+    __shared__ float sums[4], joined[4][256];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = (int)a.head;
-    const Piece piece = find_piece(a.starts, a.requests, a.tokens, group, FEW_ROWS, blockIdx.x);
-    if (piece.segment < 0) return;
-    const int first = piece.index * FEW_ROWS, rows = (int)min((int64_t)FEW_ROWS, piece.last - piece.first - first);
-    const int parts = piece.last - piece.first <= w.few_most ? span_of<FEW_ROWS>(a, group, piece, first, w.few_chunk).parts
-                                                             : span_of<TILE_ROWS>(a, group, piece, first / TILE_ROWS * TILE_ROWS, w.tile_chunk).parts;
+    const Piece piece = TILES ? find_piece(a.starts, a.requests, a.tokens, group, TILE_ROWS, blockIdx.x) : few_piece(a, group, w);
+    if (piece.segment < 0 || (piece.last - piece.first > w.few_most) != TILES) return;
+    const int64_t first = piece.first + (int64_t)piece.index * ROWS + blockIdx.z * each;
+    if (first >= piece.last) return;
+    const int parts = span_of<ROWS>(a, group, piece, piece.index * ROWS, TILES ? w.tile_chunk : w.few_chunk).parts;
     if (parts <= 1) return;
-    for (int r = wave; r < rows; r += 4) {
-        const int64_t row = piece.first + first + r, token = row / group;
+    const int rows = (int)min((int64_t)each, piece.last - first);
+    for (int r = parts <= JOIN_AHEAD ? wave : 0; r < rows; r += parts <= JOIN_AHEAD ? 4 : 1) {
+        const int64_t row = first + r, token = row / group;
         const int head = blockIdx.y * (int)group + (int)(row % group);
         const size_t at = (size_t)(token * a.q_heads + head) * w.splits;
-        float top = -__builtin_inff(), sum = 0;
-        for (int k = 0; k < parts; k++) top = fmaxf(top, w.ml[at + k].x);
-        float o[4] = {0, 0, 0, 0};
-        for (int k = 0; k < parts; k++) {
-            const float2 ml = w.ml[at + k];
-            const float f = ml.x == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(ml.x - top);
-            sum = fmaf(ml.y, f, sum);
+        T *to = (T *)a.out + token * a.out_token + head * a.out_head;
+        float sum, o[4];
+        if (parts <= JOIN_AHEAD) {
+            join_row<T>(a, w, at, parts, 0, 1, sum, o);
 #pragma unroll
             for (int i = 0; i < 4; i++)
-                if (lane + 64 * i < D) o[i] = fmaf(w.o[(at + k) * D + lane + 64 * i], f, o[i]);
+                if (lane + 64 * i < D) to[lane + 64 * i] = (T)(o[i] * (sum == 0 ? 0.0f : 1.0f / sum));
+            continue;
         }
-        const float inv = sum == 0 ? 0.0f : 1.0f / sum;
-        T *to = (T *)a.out + token * a.out_token + head * a.out_head;
+        join_row<T>(a, w, at, parts, wave, 4, sum, o);
+        if (r) __syncthreads();
+        if (lane == 0) sums[wave] = sum;
 #pragma unroll
-        for (int i = 0; i < 4; i++)
-            if (lane + 64 * i < D) to[lane + 64 * i] = (T)(o[i] * inv);
+        for (int i = 0; i < 4; i++) joined[wave][lane + 64 * i] = o[i];
+        __syncthreads();
+        const int d = threadIdx.x;
+        sum = sums[0] + sums[1] + sums[2] + sums[3];
+        if (d < D) to[d] = (T)((joined[0][d] + joined[1][d] + joined[2][d] + joined[3][d]) * (sum == 0 ? 0.0f : 1.0f / sum));
     }
 }
 
@@ -593,10 +631,17 @@ template <class T> hipError_t attend(const she_attend_pages_args &a, const Atten
 {
     hipError_t rc = a.head <= 64 ? attend_rows<T, 64>(a, s, w, d_bad, st) : a.head <= 128 ? attend_rows<T, 128>(a, s, w, d_bad, st)
                                                                                           : attend_rows<T, 256>(a, s, w, d_bad, st);
-    if (rc != hipSuccess || w.splits <= 1) return rc;
     const uint32_t group = a.q_heads / a.kv_heads;
-    k_attend_join<T><<<dim3((uint32_t)(a.tokens * (uint64_t)group / FEW_ROWS + a.requests), a.kv_heads), 256, 0, st>>>(a, group, w);
-    return hipGetLastError();
+    if (rc == hipSuccess && s.few_slots && s.few_splits > 1) {
+        const int each = s.few_splits > 4 * JOIN_AHEAD ? 1 : 4;
+        k_attend_join<T, false><<<dim3((uint32_t)s.few_slots, a.kv_heads, FEW_ROWS / each), 256, 0, st>>>(a, group, w, each);
+        rc = hipGetLastError();
+    }
+    if (rc == hipSuccess && s.tile_slots && s.tile_splits > 1) {
+        k_attend_join<T, true><<<dim3((uint32_t)s.tile_slots, a.kv_heads, TILE_ROWS / 4), 256, 0, st>>>(a, group, w, 4);
+        rc = hipGetLastError();
+    }
+    return rc;
 }
 
 }  // namespace
@@ -616,10 +661,10 @@ AttendShape attend_shape(const she_attend_pages_args &a, uint32_t cus)
     // places of a span at most: a window's, those that the tile's later tokens see further, and those before it down to a multiple of 32
     const auto span = [&](uint64_t tile) { return a.window ? std::min<uint64_t>(longest, (uint64_t)a.window + tile + 31) : longest; };
     const uint64_t few_span = span(FEW_ROWS), tile_span = span(TILE_ROWS);
-    // pieces short enough for eight workgroups per compute unit, long enough that joining them costs little
-    s.few_chunk = (uint32_t)std::min<uint64_t>(MOST_CHUNK, std::max<uint64_t>(256, ceil_div(s.few_slots * a.kv_heads * few_span / (8 * cus), 128) * 128));
+    // Pieces for two workgroups per compute unit: shorter ones (for eight) cost more to join than they gain, 128 us and not 78 for a
+    // token over 32768 places, 84 and 76 for the mixed step.
+    s.few_chunk = (uint32_t)std::min<uint64_t>(MOST_CHUNK, std::max<uint64_t>(256, ceil_div(s.few_slots * a.kv_heads * few_span / (2 * cus), 128) * 128));
     s.few_splits = s.few_slots ? (uint32_t)std::max<uint64_t>(1, ceil_div(few_span, s.few_chunk)) : 1;
-    // and for two of k_attend_tile's
     s.tile_chunk = (uint32_t)std::max<uint64_t>(512, ceil_div(s.tile_slots * a.kv_heads * tile_span / (2 * cus), STEP) * STEP);
     s.tile_splits = s.tile_slots ? (uint32_t)std::max<uint64_t>(1, ceil_div(tile_span, s.tile_chunk)) : 1;
     return s;
