@@ -265,6 +265,9 @@ template <class T, bool WIDE> __device__ inline BaseWords load_base(const Up &u,
         if constexpr (WIDE) {
             if (count > 0) b.v[0] = *reinterpret_cast<const u32x4 *>(p);
             if (count > 64) b.v[1] = *reinterpret_cast<const u32x4 *>(p + 64);
+        } else if (count >= 68) {
+            __builtin_memcpy(&b.v[0], p, 16);
+            __builtin_memcpy(&b.v[1], p + 64, 16);
         } else {
             for (int i = 0; i < 8; i++)
                 if (i / 4 * 64 + i % 4 < count) b.v[i / 4][i % 4] = p[i / 4 * 64 + i % 4];
@@ -288,7 +291,7 @@ template <class T> __device__ inline void base_numbers(const Up &u, const BaseWo
     }
 }
 
-// Sixteen tokens from `first` on, `live` of them: their bases; and acc[m] added to the lane's output m, and written.
+// Sixteen tokens from `first` on, `live` of them: their bases; and `by` times acc[m] added to the lane's output m, and written.
 template <class T, bool WIDE> __device__ inline void load_bases(const Up &u, int64_t first, int live, uint32_t n_first, BaseWords base[4])
 {
     const uint32_t n = lane_output(n_first);
@@ -299,7 +302,7 @@ template <class T, bool WIDE> __device__ inline void load_bases(const Up &u, int
         base[i] = load_base<T, WIDE>(u, first + (there ? lane_token(i) : 0), there ? n : 0, there ? count : 0);
     }
 }
-template <class T, bool WIDE> __device__ inline void write_outputs(const Up &u, int64_t first, int live, uint32_t n_first, const BaseWords base[4], const f32x4 acc[8])
+template <class T, bool WIDE> __device__ inline void write_outputs(const Up &u, int64_t first, int live, uint32_t n_first, const BaseWords base[4], const f32x4 acc[8], float by)
 {
     const uint32_t n = lane_output(n_first);
     const int count = (int)u.w.width - (int)n;
@@ -313,7 +316,7 @@ template <class T, bool WIDE> __device__ inline void write_outputs(const Up &u, 
         float v[8];
         base_numbers<T>(u, base[i], step, v);
 #pragma unroll
-        for (int m = 0; m < 8; m++) v[m] += acc[m][i];
+        for (int m = 0; m < 8; m++) v[m] = fmaf(acc[m][i], by, v[m]);
         store_quads<T, WIDE>((T *)u.out + (first + lane_token(i)) * u.out_stride + n, pack<T>(v), count, count - 64);
     }
 }
@@ -372,11 +375,7 @@ __global__ __launch_bounds__(64 * UP_WAVES, WIDE && !CHUNKS ? 3 : 1) void k_adap
     const float unscale = std::is_same<T, _Float16>::value && !CHUNKS && tile.rank ? u.h.unscale[(size_t)slot * s.chunks] : 1.0f;
 #pragma unroll
     for (int c = 0; c < 2; c++) {
-        if constexpr (std::is_same<T, _Float16>::value && !CHUNKS) {
-#pragma unroll
-            for (int m = 0; m < 8; m++) acc[c][m] *= unscale;
-        }
-        write_outputs<T, WIDE>(u, tile.first + c * 16, tile.live - c * 16, n_first, base[c], CHUNKS ? total[CHUNKS ? c : 0] : acc[c]);
+        write_outputs<T, WIDE>(u, tile.first + c * 16, tile.live - c * 16, n_first, base[c], CHUNKS ? total[CHUNKS ? c : 0] : acc[c], unscale);
     }
 }
 
@@ -420,10 +419,9 @@ __global__ __launch_bounds__(64 * STEP_WAVES) void k_adapter_step(Rows x, Matrix
             for (int m = 0; m < 8; m++) {
                 acc[m] = mfma16(hv[0], cols[m], acc[m]);
                 acc[m] = mfma16(hv[1], cols[m], acc[m]);
-                if constexpr (std::is_same<T, _Float16>::value) acc[m] *= unscale;
             }
         }
-        write_outputs<T, WIDE>(u, tile.first + c * 16, tile.live - c * 16, n_first, base, acc);
+        write_outputs<T, WIDE>(u, tile.first + c * 16, tile.live - c * 16, n_first, base, acc, std::is_same<T, _Float16>::value ? unscale : 1.0f);
     }
 }
 

@@ -28,11 +28,17 @@ template <class T> __device__ inline x8<T> as_x8(u32x4 v) { return __builtin_bit
 template <class T> __device__ inline u32x4 as_words(x8<T> v) { return __builtin_bit_cast(u32x4, v); }
 
 // Eight elements from p on, of which the first `count` exist; the others are zeros.  WIDE: count is 8 or at most 0, p on 16 bytes.
+// Otherwise p is on its element's two bytes, where the device loads and stores as much at once, if with more requests for it.
 template <class T, bool WIDE> __device__ inline u32x4 load8(const T *p, int count)
 {
     if constexpr (WIDE) {
         return count > 0 ? *reinterpret_cast<const u32x4 *>(p) : u32x4{0, 0, 0, 0};
     } else {
+        if (count >= 8) {
+            u32x4 w;
+            __builtin_memcpy(&w, p, 16);
+            return w;
+        }
         x8<T> v;
         for (int i = 0; i < 8; i++) v[i] = i < count ? p[i] : (T)0.0f;
         return as_words<T>(v);
@@ -42,6 +48,8 @@ template <class T, bool WIDE> __device__ inline void store8(T *p, u32x4 words, i
 {
     if constexpr (WIDE) {
         if (count > 0) *reinterpret_cast<u32x4 *>(p) = words;
+    } else if (count >= 8) {
+        __builtin_memcpy(p, &words, 16);
     } else {
         const x8<T> v = as_x8<T>(words);
         for (int i = 0; i < 8; i++)
@@ -56,6 +64,12 @@ template <class T, bool WIDE> __device__ inline u32x4 load_quads(const T *p, int
         const uint2 a = count > 0 ? *reinterpret_cast<const uint2 *>(p) : uint2{0, 0}, b = more > 0 ? *reinterpret_cast<const uint2 *>(p + 64) : uint2{0, 0};
         return u32x4{a.x, a.y, b.x, b.y};
     } else {
+        if (count >= 4 && more >= 4) {
+            uint2 a, b;
+            __builtin_memcpy(&a, p, 8);
+            __builtin_memcpy(&b, p + 64, 8);
+            return u32x4{a.x, a.y, b.x, b.y};
+        }
         x8<T> v;
         for (int i = 0; i < 4; i++) {
             v[i] = i < count ? p[i] : (T)0.0f;
@@ -69,6 +83,10 @@ template <class T, bool WIDE> __device__ inline void store_quads(T *p, u32x4 wor
     if constexpr (WIDE) {
         if (count > 0) *reinterpret_cast<uint2 *>(p) = uint2{words[0], words[1]};
         if (more > 0) *reinterpret_cast<uint2 *>(p + 64) = uint2{words[2], words[3]};
+    } else if (count >= 4 && more >= 4) {
+        const uint2 a{words[0], words[1]}, b{words[2], words[3]};
+        __builtin_memcpy(p, &a, 8);
+        __builtin_memcpy(p + 64, &b, 8);
     } else {
         const x8<T> v = as_x8<T>(words);
         for (int i = 0; i < 4; i++) {
