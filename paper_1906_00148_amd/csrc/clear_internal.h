@@ -25,10 +25,15 @@ struct QkShape {
     bool aligned;            // and so do a lane's cosines and sines
 };
 QkShape qk_shape(const she_qk_rotate_args &a, uint32_t cus);
-QkShape qk_grad_shape(const she_qk_rotate_grad_args &a, uint32_t cus);
-size_t qk_grad_scratch(const QkShape &s, uint32_t head);
+struct QkGradShape {
+    uint32_t lanes;
+    bool wide, aligned;
+    QkShape q, k;            // their heads, steps, shares and workgroups
+};
+QkGradShape qk_grad_shape(const she_qk_rotate_grad_args &a, uint32_t cus);
+size_t qk_grad_scratch(const QkGradShape &s, uint32_t head);
 hipError_t launch_qk_rotate(const she_qk_rotate_args &a, const QkShape &s, uint32_t *d_bad, hipStream_t st);
-hipError_t launch_qk_rotate_grad(const she_qk_rotate_grad_args &a, const QkShape &s, void *scratch, uint32_t *d_bad, hipStream_t st);
+hipError_t launch_qk_rotate_grad(const she_qk_rotate_grad_args &a, const QkGradShape &s, void *scratch, uint32_t *d_bad, hipStream_t st);
 
 // ---- adapters
 size_t adapters_scratch(const she_adapters_args &a);

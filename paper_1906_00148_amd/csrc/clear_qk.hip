@@ -17,7 +17,7 @@ namespace she { namespace clear {
 namespace {
 
 constexpr int WAVES = 4;                       // wavefronts of a workgroup
-constexpr uint32_t GRAD_RESIDENT = 3;           // of the backward kernel's workgroups on a compute unit
+constexpr uint32_t GRAD_RESIDENT = 4;           // of the backward kernel's workgroups on a compute unit
 constexpr int BATCH = 4;                       // steps whose loads are requested before the first is used
 
 // Sum over the LANES lanes of a head.
@@ -175,51 +175,64 @@ __global__ __launch_bounds__(64 * WAVES) void k_qk_rotate(she_qk_rotate_args a, 
     }
 }
 
-// Wavefronts walk the shares of all tokens and keep their sums of both weights' gradients; partial [blocks][2][D].
+// What the backward pass does with the queries, or with the keys.
+struct GradSide {
+    const void *x, *dy;
+    int64_t x_token, x_head, dy_token, dy_head, dx_token, dx_head;
+    const float *w;
+    void *dx;
+    uint32_t heads, steps, per_wave, chunks;   // as in QkShape
+};
+struct GradTurn {
+    const float *cosines, *sines;
+    const int32_t *positions;
+    uint32_t tokens, head, rot, places;
+    float eps;
+    bool aligned;
+};
+
+// The first q_blocks workgroups have the queries, the others the keys, so that a lane keeps one weight and its sums.  Wavefronts walk
+// the shares of all tokens; partial [blocks][D].
 template <class T, bool WIDE, bool INTERLEAVED, int LANES>
-__global__ __launch_bounds__(64 * WAVES) void k_qk_rotate_grad(she_qk_rotate_grad_args a, uint32_t steps, uint32_t per_wave, uint32_t chunks, bool aligned,
-                                                               float *partial, uint32_t *d_bad)
+__global__ __launch_bounds__(64 * WAVES, GRAD_RESIDENT) void k_qk_rotate_grad(GradSide q, GradSide k, GradTurn a, uint32_t q_blocks, float *partial, uint32_t *d_bad)
 {
     constexpr int ROWS = 64 / LANES, PAIR = 2;
     __shared__ float rows[WAVES][64 * 8];
-    __shared__ float sums[WAVES][2][LANES * 8];
+    __shared__ float sums[WAVES][LANES * 8];
+    const bool is_q = blockIdx.x < q_blocks;
+    const GradSide &side = is_q ? q : k;
+    const uint32_t block = is_q ? blockIdx.x : blockIdx.x - q_blocks, blocks = is_q ? q_blocks : gridDim.x - q_blocks;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int c = lane % LANES, row = lane / LANES, d0 = 8 * c, D = (int)a.head;
     const int here = D - d0 < 0 ? 0 : D - d0 > 8 ? 8 : D - d0;
-    const uint32_t heads = a.q_heads + a.kv_heads;
-    float wq[8], wk[8], dwq[8], dwk[8];
+    float w[8], dw[8];
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-        wq[i] = a.wq ? (i < here ? a.wq[d0 + i] : 0.0f) : 1.0f;
-        wk[i] = a.wk ? (i < here ? a.wk[d0 + i] : 0.0f) : 1.0f;
-        dwq[i] = dwk[i] = 0;
+        w[i] = side.w ? (i < here ? side.w[d0 + i] : 0.0f) : 1.0f;
+        dw[i] = 0;
     }
-    const uint64_t units = (uint64_t)a.tokens * chunks;
-    for (uint64_t unit = (uint64_t)blockIdx.x * WAVES + wave; unit < units; unit += (uint64_t)gridDim.x * WAVES) {
-        const uint32_t t = (uint32_t)(unit / chunks), chunk = (uint32_t)(unit % chunks);
+    const uint64_t units = (uint64_t)a.tokens * side.chunks;
+    for (uint64_t unit = (uint64_t)block * WAVES + wave; unit < units; unit += (uint64_t)blocks * WAVES) {
+        const uint32_t t = (uint32_t)(unit / side.chunks), chunk = (uint32_t)(unit % side.chunks);
         const int32_t position = a.positions[t];
         const bool placed = position >= 0 && (uint32_t)position < a.places;
-        if (lane == 0 && chunk == 0 && !placed) count_bad(d_bad);
-        const Turn tr = load_turn(a.cosines, a.sines, placed ? a.rot : 0, INTERLEAVED, aligned, placed ? (uint32_t)position : 0, d0, -1.0f);
-        const uint32_t end = min((chunk + 1) * per_wave, steps);
-        for (uint32_t step = chunk * per_wave; step < end; step += PAIR) {
+        if (lane == 0 && chunk == 0 && is_q && !placed) count_bad(d_bad);
+        const Turn tr = load_turn(a.cosines, a.sines, placed ? a.rot : 0, INTERLEAVED, a.aligned, placed ? (uint32_t)position : 0, d0, -1.0f);
+        const uint32_t end = min((chunk + 1) * side.per_wave, side.steps);
+        for (uint32_t step = chunk * side.per_wave; step < end; step += PAIR) {
             u32x4 raw_x[PAIR], raw_y[PAIR];
 #pragma unroll
             for (int b = 0; b < PAIR; b++) {
                 const uint32_t h = (step + b) * ROWS + row;
                 raw_x[b] = raw_y[b] = u32x4{0, 0, 0, 0};
-                if (step + b >= end || h >= heads) continue;
-                const bool is_q = h < a.q_heads;
-                const int64_t hk = (int64_t)h - a.q_heads;
-                raw_x[b] = load8<T, WIDE>((is_q ? (const T *)a.q + t * a.q_token + h * a.q_head : (const T *)a.k + t * a.k_token + hk * a.k_head) + d0, here);
-                raw_y[b] = load8<T, WIDE>((is_q ? (const T *)a.dq_out + t * a.dq_out_token + h * a.dq_out_head
-                                                : (const T *)a.dk_out + t * a.dk_out_token + hk * a.dk_out_head) + d0, here);
+                if (step + b >= end || h >= side.heads) continue;
+                raw_x[b] = load8<T, WIDE>((const T *)side.x + t * side.x_token + h * side.x_head + d0, here);
+                raw_y[b] = load8<T, WIDE>((const T *)side.dy + t * side.dy_token + h * side.dy_head + d0, here);
             }
 #pragma unroll
             for (int b = 0; b < PAIR; b++) {
                 if (step + b >= end) break;
                 const uint32_t h = (step + b) * ROWS + row;
-                const bool is_q = h < a.q_heads;
                 float x[8], dy[8], other[8], g[8], sum = 0, dot = 0;
                 unpack<T>(raw_x[b], x);
                 unpack<T>(raw_y[b], dy);
@@ -231,48 +244,47 @@ __global__ __launch_bounds__(64 * WAVES) void k_qk_rotate_grad(she_qk_rotate_gra
 #pragma unroll
                 for (int i = 0; i < 8; i++) {
                     x[i] *= r;
-                    const float gu = placed && h < heads ? g[i] * x[i] : 0.0f, w = is_q ? wq[i] : wk[i];
-                    if (is_q) dwq[i] += gu; else dwk[i] += gu;
-                    g[i] *= w;
-                    dot = fmaf(w, gu, dot);
+                    const float gu = placed && h < side.heads ? g[i] * x[i] : 0.0f;
+                    dw[i] += gu;
+                    g[i] *= w[i];
+                    dot = fmaf(w[i], gu, dot);
                 }
                 dot = head_sum<LANES>(dot) / D;
-                if (h >= heads) continue;
+                if (h >= side.heads) continue;
 #pragma unroll
                 for (int i = 0; i < 8; i++) g[i] = placed ? r * (g[i] - x[i] * dot) : 0.0f;
-                const int64_t hk = (int64_t)h - a.q_heads;
-                T *to = is_q ? (T *)a.dq + t * a.dq_token + h * a.dq_head : (T *)a.dk + t * a.dk_token + hk * a.dk_head;
-                store8<T, WIDE>(to + d0, pack<T>(g), here);
+                store8<T, WIDE>((T *)side.dx + t * side.dx_token + h * side.dx_head + d0, pack<T>(g), here);
             }
         }
     }
 #pragma unroll
     for (int i = 0; i < 8; i++) {
 #pragma unroll
-        for (int m = LANES; m < 64; m *= 2) { dwq[i] += __shfl_xor(dwq[i], m); dwk[i] += __shfl_xor(dwk[i], m); }
-        if (row == 0) { sums[wave][0][d0 + i] = dwq[i]; sums[wave][1][d0 + i] = dwk[i]; }
+        for (int m = LANES; m < 64; m *= 2) dw[i] += __shfl_xor(dw[i], m);
+        if (row == 0) sums[wave][d0 + i] = dw[i];
     }
     __syncthreads();
-    for (int d = threadIdx.x; d < 2 * D; d += 64 * WAVES) {
+    for (int d = threadIdx.x; d < D; d += 64 * WAVES) {
         float v = 0;
-        for (int w = 0; w < WAVES; w++) v += sums[w][d / D][d % D];
-        partial[(size_t)blockIdx.x * 2 * D + d] = v;
+        for (int k = 0; k < WAVES; k++) v += sums[k][d];
+        partial[(size_t)blockIdx.x * D + d] = v;
     }
 }
 
 // dwq, dwk = sums of the workgroups' partial sums: SUM_COLS columns a workgroup, SUM_PARTS threads a column, whose loads are
 // requested eight at a time.
 constexpr int SUM_COLS = 8, SUM_PARTS = 128;
-__global__ __launch_bounds__(SUM_COLS * SUM_PARTS) void k_qk_weight_sums(const float *partial, uint32_t rows, uint32_t D, float *dwq, float *dwk)
+__global__ __launch_bounds__(SUM_COLS * SUM_PARTS) void k_qk_weight_sums(const float *partial, uint32_t q_blocks, uint32_t blocks, uint32_t D, float *dwq, float *dwk)
 {
     __shared__ float sums[SUM_PARTS][SUM_COLS + 1];
     const uint32_t col = blockIdx.x * SUM_COLS + threadIdx.x % SUM_COLS, part = threadIdx.x / SUM_COLS;
+    const uint32_t first = blockIdx.y ? q_blocks : 0, rows = blockIdx.y ? blocks : q_blocks;
     float v = 0;
-    if (col < 2 * D)
-        for (uint32_t r0 = part; r0 < rows; r0 += 8 * SUM_PARTS) {
+    if (col < D)
+        for (uint32_t r0 = first + part; r0 < rows; r0 += 8 * SUM_PARTS) {
             float x[8];
 #pragma unroll
-            for (int i = 0; i < 8; i++) x[i] = r0 + i * SUM_PARTS < rows ? partial[(size_t)(r0 + i * SUM_PARTS) * 2 * D + col] : 0.0f;
+            for (int i = 0; i < 8; i++) x[i] = r0 + i * SUM_PARTS < rows ? partial[(size_t)(r0 + i * SUM_PARTS) * D + col] : 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; i++) v += x[i];
         }
@@ -283,9 +295,8 @@ __global__ __launch_bounds__(SUM_COLS * SUM_PARTS) void k_qk_weight_sums(const f
     for (int p = part; p < SUM_PARTS; p += 8) v += sums[p][threadIdx.x % SUM_COLS];
 #pragma unroll
     for (int m = SUM_COLS; m < 64; m *= 2) v += __shfl_xor(v, m);
-    if (part || col >= 2 * D) return;
-    float *to = col < D ? dwq : dwk;
-    if (to) to[col < D ? col : col - D] = v;
+    float *to = blockIdx.y ? dwk : dwq;
+    if (to && !part && col < D) to[col] = v;
 }
 
 bool on16(const void *p) { return ((uintptr_t)p & 15) == 0; }
@@ -328,9 +339,9 @@ template <class T, bool W, bool I, int L> struct Rotate {
     }
 };
 template <class T, bool W, bool I, int L> struct RotateGrad {
-    static hipError_t go(const she_qk_rotate_grad_args &a, const QkShape &s, float *partial, uint32_t *d_bad, hipStream_t st)
+    static hipError_t go(const GradSide &q, const GradSide &k, const GradTurn &a, const QkGradShape &s, float *partial, uint32_t *d_bad, hipStream_t st)
     {
-        k_qk_rotate_grad<T, W, I, L><<<s.blocks, 64 * WAVES, 0, st>>>(a, s.steps, s.per_wave, s.chunks, s.aligned, partial, d_bad);
+        k_qk_rotate_grad<T, W, I, L><<<s.q.blocks + s.k.blocks, 64 * WAVES, 0, st>>>(q, k, a, s.q.blocks, partial, d_bad);
         return hipGetLastError();
     }
 };
@@ -358,35 +369,46 @@ QkShape qk_shape(const she_qk_rotate_args &a, uint32_t cus)
     return s;
 }
 
-QkShape qk_grad_shape(const she_qk_rotate_grad_args &a, uint32_t cus)
+QkGradShape qk_grad_shape(const she_qk_rotate_grad_args &a, uint32_t cus)
 {
-    QkShape s{};
+    QkGradShape s{};
     s.lanes = lanes_of(a.head);
-    s.heads = a.q_heads + a.kv_heads;
     const int64_t strides = a.q_token | a.q_head | a.k_token | a.k_head | a.dq_out_token | a.dq_out_head | a.dk_out_token | a.dk_out_head |
                             a.dq_token | a.dq_head | a.dk_token | a.dk_head | a.head;
     s.wide = strides % 8 == 0 && on16(a.q) && on16(a.k) && on16(a.dq_out) && on16(a.dk_out) && on16(a.dq) && on16(a.dk);
     s.aligned = turn_aligned(a.cosines, a.sines, a.rot, a.interleaved != 0);
-    share_out(s, a.tokens, cus);
-    // Each leaves a row of partial sums: no more than are resident together, and all with as many shares, so that they end together.
-    const uint32_t resident = GRAD_RESIDENT * (cus ? cus : 1), rounds = std::max(1u, (uint32_t)ceil_div(s.blocks, resident));
-    s.blocks = std::max(1u, (uint32_t)ceil_div(s.blocks, rounds));
+    // Each workgroup leaves a row of partial sums: no more than are resident together, the queries' and the keys' in proportion to
+    // their heads, and all of a side with as many shares, so that they end together.
+    const uint32_t resident = GRAD_RESIDENT * (cus ? cus : 1);
+    const auto side = [&](QkShape &q, uint32_t heads) {
+        q.lanes = s.lanes;
+        q.heads = heads;
+        share_out(q, a.tokens, cus);
+        const uint32_t part = std::max(1u, (uint32_t)((uint64_t)resident * heads / (a.q_heads + a.kv_heads)));
+        const uint32_t rounds = std::max(1u, (uint32_t)ceil_div(q.blocks, part));
+        q.blocks = std::max(1u, (uint32_t)ceil_div(q.blocks, rounds));
+    };
+    side(s.q, a.q_heads);
+    side(s.k, a.kv_heads);
     return s;
 }
 
-size_t qk_grad_scratch(const QkShape &s, uint32_t head) { return (size_t)s.blocks * 2 * head * sizeof(float); }
+size_t qk_grad_scratch(const QkGradShape &s, uint32_t head) { return (size_t)(s.q.blocks + s.k.blocks) * head * sizeof(float); }
 
 hipError_t launch_qk_rotate(const she_qk_rotate_args &a, const QkShape &s, uint32_t *d_bad, hipStream_t st)
 {
     return choose<Rotate>(a.type, s.wide, a.interleaved != 0, s.lanes, a, s, d_bad, st);
 }
 
-hipError_t launch_qk_rotate_grad(const she_qk_rotate_grad_args &a, const QkShape &s, void *scratch, uint32_t *d_bad, hipStream_t st)
+hipError_t launch_qk_rotate_grad(const she_qk_rotate_grad_args &a, const QkGradShape &s, void *scratch, uint32_t *d_bad, hipStream_t st)
 {
     float *partial = static_cast<float *>(scratch);
-    hipError_t rc = choose<RotateGrad>(a.type, s.wide, a.interleaved != 0, s.lanes, a, s, partial, d_bad, st);
+    const GradSide q{a.q, a.dq_out, a.q_token, a.q_head, a.dq_out_token, a.dq_out_head, a.dq_token, a.dq_head, a.wq, a.dq, s.q.heads, s.q.steps, s.q.per_wave, s.q.chunks};
+    const GradSide k{a.k, a.dk_out, a.k_token, a.k_head, a.dk_out_token, a.dk_out_head, a.dk_token, a.dk_head, a.wk, a.dk, s.k.heads, s.k.steps, s.k.per_wave, s.k.chunks};
+    const GradTurn t{a.cosines, a.sines, a.positions, a.tokens, a.head, a.rot, a.places, a.eps, s.aligned};
+    hipError_t rc = choose<RotateGrad>(a.type, s.wide, a.interleaved != 0, s.lanes, q, k, t, s, partial, d_bad, st);
     if (rc != hipSuccess || (!a.dwq && !a.dwk)) return rc;
-    k_qk_weight_sums<<<(uint32_t)ceil_div(2 * a.head, SUM_COLS), SUM_COLS * SUM_PARTS, 0, st>>>(partial, s.blocks, a.head, a.dwq, a.dwk);
+    k_qk_weight_sums<<<dim3((uint32_t)ceil_div(a.head, SUM_COLS), 2), SUM_COLS * SUM_PARTS, 0, st>>>(partial, s.q.blocks, s.q.blocks + s.k.blocks, a.head, a.dwq, a.dwk);
     return hipGetLastError();
 }
 

@@ -128,7 +128,7 @@ try {
     if (a.tokens && (!a.dq_out || !a.dk_out || !a.q || !a.k || !a.dq || !a.dk || !a.positions || (a.rot && a.places && (!a.cosines || !a.sines))))
         return fail(c, SHE_EINVAL, at + "null argument");
     if ((rc = ready(c))) return rc;
-    const clear::QkShape s = clear::qk_grad_shape(a, c->dk.cus);
+    const clear::QkGradShape s = clear::qk_grad_shape(a, c->dk.cus);
     if ((rc = ensure_scratch(c, clear::qk_grad_scratch(s, a.head)))) return rc;
     HIP_TRY(c, clear::launch_qk_rotate_grad(a, s, c->clear.scratch, c->clear.d_bad, c->stream));
     return SHE_OK;

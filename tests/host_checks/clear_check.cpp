@@ -12,14 +12,14 @@ static size_t wanted = 0;                                                    // 
 static hipError_t launched() { launches++; return fake::step(); }
 namespace she { namespace clear {
 QkShape qk_shape(const she_qk_rotate_args &, uint32_t) { return {}; }
-QkShape qk_grad_shape(const she_qk_rotate_grad_args &, uint32_t) { return {}; }
-size_t qk_grad_scratch(const QkShape &, uint32_t) { return wanted; }
+QkGradShape qk_grad_shape(const she_qk_rotate_grad_args &, uint32_t) { return {}; }
+size_t qk_grad_scratch(const QkGradShape &, uint32_t) { return wanted; }
 size_t adapters_scratch(const she_adapters_args &) { return wanted; }
 size_t adapters_grad_scratch(const she_adapters_grad_args &) { return wanted; }
 AttendShape attend_shape(const she_attend_pages_args &, uint32_t) { return {}; }
 size_t attend_scratch(const she_attend_pages_args &, const AttendShape &) { return wanted; }
 hipError_t launch_qk_rotate(const she_qk_rotate_args &, const QkShape &, uint32_t *, hipStream_t) { return launched(); }
-hipError_t launch_qk_rotate_grad(const she_qk_rotate_grad_args &, const QkShape &, void *, uint32_t *, hipStream_t) { return launched(); }
+hipError_t launch_qk_rotate_grad(const she_qk_rotate_grad_args &, const QkGradShape &, void *, uint32_t *, hipStream_t) { return launched(); }
 hipError_t launch_adapters(const she_adapters_args &, void *, uint32_t *, uint32_t, hipStream_t) { return launched(); }
 hipError_t launch_adapters_grad(const she_adapters_grad_args &, void *, uint32_t *, uint32_t, hipStream_t) { return launched(); }
 hipError_t launch_attend_pages(const she_attend_pages_args &, const AttendShape &, void *, uint32_t *, hipStream_t) { return launched(); }
