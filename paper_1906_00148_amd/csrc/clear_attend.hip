@@ -26,10 +26,19 @@ constexpr int FEW_ROWS = 16, FEW_WAVES = 4, MOST_CHUNK = 2048;
 constexpr int TILE_WAVES = 4, TILE_ROWS = 32 * TILE_WAVES, STEP = 64;   // rows of a workgroup, places of a step
 constexpr float LOG2E = 1.4426950408889634f;
 
-struct Work {                            // of the pieces of a cut row, [tokens * q_heads][splits]
+// What is left behind of the pieces of cut rows, by tile: [slots][rows of a tile][kv_heads][splits].
+struct Pieces {
     float *o;                            // [..][head]
     float2 *ml;
-    uint32_t few_chunk, tile_chunk, splits;
+    uint32_t splits;
+};
+__device__ inline size_t pieces_at(const Pieces &p, uint32_t kv_heads, size_t slot, int tile_rows, int row, int kv_head)
+{
+    return ((slot * tile_rows + row) * kv_heads + kv_head) * p.splits;
+}
+struct Work {
+    Pieces few, tile;
+    uint32_t few_chunk, tile_chunk;
     uint32_t few_most;                   // rows that a request has at most to be k_attend_few's
     uint32_t few_each;                   // slots of every request there; 0: they are found by find_piece
 };
@@ -95,10 +104,10 @@ template <class T> __device__ inline bool has_special(u32x4 v)
     return any;
 }
 
-// One row over those of the places [from, to) that it attends to, by one wavefront: scores with a place a lane, sums with elements on
+// One row over those of the places [from, to) that it attends to, its piece `part`, by one wavefront: scores with a place a lane, sums with elements on
 // the lanes.  Writes the row's result, or its piece's.
 template <class T>
-__device__ void attend_row(const she_attend_pages_args &a, uint32_t group, const Work &w, const Span &sp, int kv_head, int row, int from, int to)
+__device__ void attend_row(const she_attend_pages_args &a, uint32_t group, const Pieces &pieces, size_t part, const Span &sp, int kv_head, int row, int from, int to)
 {
     const int lane = threadIdx.x & 63, D = (int)a.head;
     const int64_t token = sp.token0 + row / (int)group;
@@ -136,13 +145,12 @@ __device__ void attend_row(const she_attend_pages_args &a, uint32_t group, const
                 if (lane + 64 * i < D) o[i] = fmaf(weight, (float)v[lane + 64 * i], o[i]);
         }
     }
-    const size_t part = (size_t)(token * a.q_heads + head) * w.splits + blockIdx.z;
     const float inv = sp.parts > 1 ? 1.0f : sum == 0 ? 0.0f : 1.0f / sum;
-    if (sp.parts > 1 && lane == 0) w.ml[part] = float2{top, sum};
+    if (sp.parts > 1 && lane == 0) pieces.ml[part] = float2{top, sum};
     for (int i = 0; i < 4; i++) {
         const int d = lane + 64 * i;
         if (d >= D) continue;
-        if (sp.parts > 1) w.o[part * D + d] = o[i];
+        if (sp.parts > 1) pieces.o[part * D + d] = o[i];
         else ((T *)a.out)[token * a.out_token + head * a.out_head + d] = (T)(o[i] * inv);
     }
 }
@@ -151,7 +159,7 @@ __device__ void attend_row(const she_attend_pages_args &a, uint32_t group, const
 // l reads d = 32 s + 8 (l/16) .. of the key of place l%16 for the scores, and EL elements from EL (l%16) on of the values of the
 // eight places that its scores belong to, whole rows over 16 lanes; the eight rows are transposed in registers.
 template <class T, int DP>
-__global__ __launch_bounds__(64 * FEW_WAVES, 2) void k_attend_few(she_attend_pages_args a, uint32_t group, Work w, uint32_t *d_bad)
+__global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_few(she_attend_pages_args a, uint32_t group, Work w, uint32_t *d_bad)
 {
     constexpr int EL = DP == 64 ? 4 : 8, NB = DP == 256 ? 2 : 1, KS = DP / 32;
     __shared__ int64_t rows[MOST_CHUNK];
@@ -288,7 +296,8 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void k_attend_few(she_attend_pag
                     f32x4{acc[b][e][i], acc[b][e + 1][i], acc[b][e + 2][i], acc[b][e + 3][i]};
     __syncthreads();
     if (any_special) {
-        for (int r = wave; r < sp.rows; r += FEW_WAVES) attend_row<T>(a, group, w, sp, kv_head, sp.row + r, from, from + count);
+        for (int r = wave; r < sp.rows; r += FEW_WAVES)
+            attend_row<T>(a, group, w.few, pieces_at(w.few, a.kv_heads, blockIdx.x, FEW_ROWS, r, kv_head) + blockIdx.z, sp, kv_head, sp.row + r, from, from + count);
         return;
     }
     constexpr int EACH = DP / 16;                                 // elements of a row that a thread joins
@@ -316,11 +325,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES, 2) void k_attend_few(she_attend_pag
         for (int i = 0; i < EACH; i++)
             if (d0 + i < D) to[i] = (T)(o[i] * inv);
     } else {
-        const size_t at = (size_t)(token * a.q_heads + head) * w.splits + blockIdx.z;
-        if (d0 == 0) w.ml[at] = float2{top, sum};
+        const size_t at = pieces_at(w.few, a.kv_heads, blockIdx.x, FEW_ROWS, r, kv_head) + blockIdx.z;
+        if (d0 == 0) w.few.ml[at] = float2{top, sum};
 #pragma unroll
         for (int i = 0; i < EACH; i++)
-            if (d0 + i < D) w.o[at * D + d0 + i] = o[i];
+            if (d0 + i < D) w.few.o[at * D + d0 + i] = o[i];
     }
 }
 
@@ -349,9 +358,11 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
     __shared__ int64_t rows[2][BLOCK];
     __shared__ uint64_t missing[2][BLOCK / 64];                                      // places that their page id keeps out
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
-    const int kv_head = blockIdx.x, D = (int)a.head;
-    // late tokens have most to attend to: they come first
-    const Piece piece = find_piece(a.starts, a.requests, a.tokens, group, TILE_ROWS, gridDim.y - 1 - blockIdx.y);
+    // A key head's tiles are one XCD's where there are eight of them: neighbouring workgroups have different heads.  Late tokens have
+    // most to attend to: they come first.
+    const int kv_head = blockIdx.x % a.kv_heads, D = (int)a.head;
+    const uint32_t slot = gridDim.x / a.kv_heads - 1 - blockIdx.x / a.kv_heads;
+    const Piece piece = find_piece(a.starts, a.requests, a.tokens, group, TILE_ROWS, slot);
     if (piece.segment < 0 || piece.last - piece.first <= w.few_most) return;
     const Span sp = span_of<TILE_ROWS>(a, group, piece, piece.index * TILE_ROWS, w.tile_chunk);
     if ((int)blockIdx.z >= max(sp.parts, 1)) return;
@@ -513,15 +524,16 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
     }
 
     if (__ballot(special)) {
-        for (int row = first_here; row <= last_here; row++) attend_row<T>(a, group, w, sp, kv_head, row, from, from + count);
+        for (int row = first_here; row <= last_here; row++)
+            attend_row<T>(a, group, w.tile, pieces_at(w.tile, a.kv_heads, slot, TILE_ROWS, row - sp.row, kv_head) + blockIdx.z, sp, kv_head, row, from, from + count);
         return;
     }
     l += __shfl_xor(l, 32);
     if (first_here + col > last_row) return;
     const int64_t token = sp.token0 + my_token;
-    const size_t at = (size_t)(token * a.q_heads + my_head) * w.splits + blockIdx.z;
+    const size_t at = pieces_at(w.tile, a.kv_heads, slot, TILE_ROWS, my_row - sp.row, kv_head) + blockIdx.z;
     const float inv = sp.parts > 1 ? 1.0f : l == 0 ? 0.0f : 1.0f / l;
-    if (sp.parts > 1 && half == 0) w.ml[at] = float2{m, l};
+    if (sp.parts > 1 && half == 0) w.tile.ml[at] = float2{m, l};
 #pragma unroll
     for (int b = 0; b < DB; b++)
 #pragma unroll
@@ -529,7 +541,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
             const int d = b * 32 + 2 * i + 4 * half;
             if (d >= D) continue;
             if (sp.parts > 1) {
-                *reinterpret_cast<f32x4 *>(w.o + at * D + d) = f32x4{acc[b][i], acc[b][i + 1], acc[b][i + 2], acc[b][i + 3]};
+                *reinterpret_cast<f32x4 *>(w.tile.o + at * D + d) = f32x4{acc[b][i], acc[b][i + 1], acc[b][i + 2], acc[b][i + 3]};
             } else {
                 T *to = (T *)a.out + token * a.out_token + my_head * a.out_head + d;
                 T v[4];
@@ -545,7 +557,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
 // over 32768 places, 4 rows of 64 pieces at 8 key heads, takes 32 us so, 43 with four rows a workgroup and 78 with a row a wavefront.
 constexpr int JOIN_AHEAD = 4;
 template <class T>
-__device__ inline void join_row(const she_attend_pages_args &a, const Work &w, size_t at, int parts, int from, int by, float &sum, float o[4])
+__device__ inline void join_row(const she_attend_pages_args &a, const Pieces &w, size_t at, int parts, int from, int by, float &sum, float o[4])
 {
     const int lane = threadIdx.x & 63, D = (int)a.head;
     float top = -__builtin_inff();
@@ -586,21 +598,22 @@ __global__ __launch_bounds__(256) void k_attend_join(she_attend_pages_args a, ui
     if (first >= piece.last) return;
     const int parts = span_of<ROWS>(a, group, piece, piece.index * ROWS, TILES ? w.tile_chunk : w.few_chunk).parts;
     if (parts <= 1) return;
+    const Pieces &pieces = TILES ? w.tile : w.few;
     const int rows = (int)min((int64_t)each, piece.last - first);
     for (int r = parts <= JOIN_AHEAD ? wave : 0; r < rows; r += parts <= JOIN_AHEAD ? 4 : 1) {
         const int64_t row = first + r, token = row / group;
         const int head = blockIdx.y * (int)group + (int)(row % group);
-        const size_t at = (size_t)(token * a.q_heads + head) * w.splits;
+        const size_t at = pieces_at(pieces, a.kv_heads, blockIdx.x, ROWS, blockIdx.z * each + r, blockIdx.y);
         T *to = (T *)a.out + token * a.out_token + head * a.out_head;
         float sum, o[4];
         if (parts <= JOIN_AHEAD) {
-            join_row<T>(a, w, at, parts, 0, 1, sum, o);
+            join_row<T>(a, pieces, at, parts, 0, 1, sum, o);
 #pragma unroll
             for (int i = 0; i < 4; i++)
                 if (lane + 64 * i < D) to[lane + 64 * i] = (T)(o[i] * (sum == 0 ? 0.0f : 1.0f / sum));
             continue;
         }
-        join_row<T>(a, w, at, parts, wave, 4, sum, o);
+        join_row<T>(a, pieces, at, parts, wave, 4, sum, o);
         if (r) __syncthreads();
         if (lane == 0) sums[wave] = sum;
 #pragma unroll
@@ -621,7 +634,7 @@ template <class T, int DP> hipError_t attend_rows(const she_attend_pages_args &a
         rc = hipGetLastError();
     }
     if (rc == hipSuccess && s.tile_slots) {
-        k_attend_tile<T, DP><<<dim3(a.kv_heads, (uint32_t)s.tile_slots, s.tile_splits), 64 * TILE_WAVES, 0, st>>>(a, group, w, zeros_of(d_bad), d_bad);
+        k_attend_tile<T, DP><<<dim3((uint32_t)(s.tile_slots * a.kv_heads), 1, s.tile_splits), 64 * TILE_WAVES, 0, st>>>(a, group, w, zeros_of(d_bad), d_bad);
         rc = hipGetLastError();
     }
     return rc;
@@ -670,18 +683,26 @@ AttendShape attend_shape(const she_attend_pages_args &a, uint32_t cus)
     return s;
 }
 
+static size_t few_pieces(const she_attend_pages_args &a, const AttendShape &s)
+{
+    return s.few_splits > 1 ? (size_t)s.few_slots * FEW_ROWS * a.kv_heads * s.few_splits : 0;
+}
+static size_t tile_pieces(const she_attend_pages_args &a, const AttendShape &s)
+{
+    return s.tile_splits > 1 ? (size_t)s.tile_slots * TILE_ROWS * a.kv_heads * s.tile_splits : 0;
+}
+
 size_t attend_scratch(const she_attend_pages_args &a, const AttendShape &s)
 {
-    const uint32_t splits = std::max(s.few_splits, s.tile_splits);
-    return splits <= 1 ? 0 : (size_t)a.tokens * a.q_heads * splits * (a.head * sizeof(float) + sizeof(float2));
+    return (few_pieces(a, s) + tile_pieces(a, s)) * (a.head * sizeof(float) + sizeof(float2));
 }
 
 hipError_t launch_attend_pages(const she_attend_pages_args &a, const AttendShape &s, void *scratch, uint32_t *d_bad, hipStream_t st)
 {
-    const uint32_t splits = std::max(s.few_splits, s.tile_splits);
-    const size_t rows = (size_t)a.tokens * a.q_heads * splits;
-    const Work w{static_cast<float *>(scratch), reinterpret_cast<float2 *>(static_cast<float *>(scratch) + rows * a.head),
-                 s.few_chunk, s.tile_chunk, splits, s.few_most, s.few_each};
+    const size_t few = few_pieces(a, s), tile = tile_pieces(a, s);
+    float *o = static_cast<float *>(scratch);
+    float2 *ml = reinterpret_cast<float2 *>(o + (few + tile) * a.head);
+    const Work w{{o, ml, s.few_splits}, {o + few * a.head, ml + few, s.tile_splits}, s.few_chunk, s.tile_chunk, s.few_most, s.few_each};
     return a.type == SHE_BF16 ? attend<__bf16>(a, s, w, d_bad, st) : attend<_Float16>(a, s, w, d_bad, st);
 }
 

@@ -6,7 +6,8 @@ using namespace she;
 
 namespace {
 
-constexpr uint64_t MOST_TOKENS = 1u << 24, MOST_WIDTH = 1u << 24, MOST_PLACES = 1u << 26;
+// so that no grid has more than 2^32 threads along one axis
+constexpr uint64_t MOST_TOKENS = 1u << 24, MOST_SEGMENTS = 1u << 20, MOST_WIDTH = 1u << 24, MOST_PLACES = 1u << 26, MOST_GROUPS = 1u << 24;
 
 int ready(she_ctx *c)
 {
@@ -47,8 +48,8 @@ template <class Args> int check_adapters(she_ctx *c, const Args &a, const char *
     if (!a.inputs || !a.outputs || !a.adapters || !a.rank) return fail(c, SHE_EINVAL, at + "a size is zero");
     if (a.rank > 512) return fail(c, SHE_ERANGE, at + "rank is at most 512");
     if (a.adapters > 65535) return fail(c, SHE_ERANGE, at + "at most 65535 adapters");
-    if (a.tokens > MOST_TOKENS || a.segments > MOST_TOKENS || a.inputs > MOST_WIDTH || a.outputs > MOST_WIDTH)
-        return fail(c, SHE_ERANGE, at + "tokens, segments and widths are at most 2^24");
+    if (a.tokens > MOST_TOKENS || a.segments > MOST_SEGMENTS || a.inputs > MOST_WIDTH || a.outputs > MOST_WIDTH)
+        return fail(c, SHE_ERANGE, at + "tokens and widths are at most 2^24, segments 2^20");
     if (!a.down || !a.up || !a.scale || (a.segments && (!a.starts || !a.which)) || (a.tokens && !a.x) ||
         (a.tokens && a.base_type != SHE_NO_BASE && !a.base))
         return fail(c, SHE_EINVAL, at + "null argument");
@@ -156,6 +157,7 @@ try {
     int rc = ready(c);
     if (rc) return rc;
     const clear::AttendShape s = clear::attend_shape(a, c->dk.cus);
+    if (s.few_slots > MOST_GROUPS || s.tile_slots * a.kv_heads > MOST_GROUPS) return fail(c, SHE_ERANGE, at + "too many tokens and requests for one call");
     if ((rc = ensure_scratch(c, clear::attend_scratch(a, s)))) return rc;
     HIP_TRY(c, clear::launch_attend_pages(a, s, c->clear.scratch, c->clear.d_bad, c->stream));
     return SHE_OK;

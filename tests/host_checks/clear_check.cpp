@@ -16,7 +16,7 @@ QkGradShape qk_grad_shape(const she_qk_rotate_grad_args &, uint32_t) { return {}
 size_t qk_grad_scratch(const QkGradShape &, uint32_t) { return wanted; }
 size_t adapters_scratch(const she_adapters_args &) { return wanted; }
 size_t adapters_grad_scratch(const she_adapters_grad_args &) { return wanted; }
-AttendShape attend_shape(const she_attend_pages_args &, uint32_t) { return {}; }
+AttendShape attend_shape(const she_attend_pages_args &a, uint32_t) { AttendShape s{}; s.few_slots = a.requests; return s; }
 size_t attend_scratch(const she_attend_pages_args &, const AttendShape &) { return wanted; }
 hipError_t launch_qk_rotate(const she_qk_rotate_args &, const QkShape &, uint32_t *, hipStream_t) { return launched(); }
 hipError_t launch_qk_rotate_grad(const she_qk_rotate_grad_args &, const QkGradShape &, void *, uint32_t *, hipStream_t) { return launched(); }
@@ -62,7 +62,7 @@ int main()
     EXPECT(she_adapters, a, SHE_ERANGE, a.rank = 513);
     EXPECT(she_adapters, a, SHE_ERANGE, a.adapters = 65536);
     EXPECT(she_adapters, a, SHE_ERANGE, a.tokens = (1u << 24) + 1);
-    EXPECT(she_adapters, a, SHE_ERANGE, a.segments = 1u << 31);
+    EXPECT(she_adapters, a, SHE_ERANGE, a.segments = (1u << 20) + 1);
     EXPECT(she_adapters, a, SHE_ERANGE, a.outputs = 1u << 30);
     EXPECT(she_adapters, a, SHE_EINVAL, a.x = nullptr);
     EXPECT(she_adapters, a, SHE_EINVAL, a.down = nullptr);
@@ -134,6 +134,7 @@ int main()
     EXPECT(she_attend_pages, t, SHE_EINVAL, a.head = 264);
     EXPECT(she_attend_pages, t, SHE_EINVAL, a.page_size = 0);
     EXPECT(she_attend_pages, t, SHE_ERANGE, a.table_width = 1u << 23);
+    EXPECT(she_attend_pages, t, SHE_ERANGE, a.requests = (1u << 24) + 1);
     EXPECT(she_attend_pages, t, SHE_EINVAL, a.q = (char *)a.q + 8);
     EXPECT(she_attend_pages, t, SHE_EINVAL, a.page_head = 60);
     EXPECT(she_attend_pages, t, SHE_EINVAL, a.out_token = 252);
