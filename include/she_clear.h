@@ -11,8 +11,10 @@
  *  - Strides count elements; the last axis of every array is contiguous.  An array's rows may be views of a wider one.
  *  - A call enqueues its work on the context's stream and returns without waiting for it (like she_eval_gates_device).
  *    Arrays must stay valid until the stream has passed it.
- *  - Scratch belongs to the context and grows on demand: a call that needs more than any before it waits for the stream and
- *    allocates, so a caller that captures a graph runs each shape once before.
+ *  - Scratch belongs to the context and grows on demand, at least to twice its size; what it was before stays until she_free, so
+ *    that captured graphs remain good.  A call that would have to allocate while its stream is captured is refused (SHE_ENOMEM):
+ *    run it once before.  All calls of a context share the scratch: those on one stream are safe, and replays of a graph count as
+ *    calls.
  *  - What the host can see is checked (SHE_EINVAL, SHE_ERANGE).  Ids in device arrays are checked by the kernels: one that is
  *    out of its range is left out, as each call says, never followed, and counted (she_clear_bad_ids).
  *  - Sums, softmax statistics and norms are held in 32 bits; results are rounded once, to nearest.

@@ -1,4 +1,6 @@
 // The clear side of split inference in the C ABI (declared in include/she_clear.h): checks of arguments, scratch, launches.
+#include <algorithm>
+
 #include "clear_internal.h"
 #include "she_ctx.h"
 
@@ -9,9 +11,20 @@ namespace {
 // so that no grid has more than 2^32 threads along one axis
 constexpr uint64_t MOST_TOKENS = 1u << 24, MOST_SEGMENTS = 1u << 20, MOST_WIDTH = 1u << 24, MOST_PLACES = 1u << 26, MOST_GROUPS = 1u << 24;
 
+// Allocating would break a capture: the error says so before it does.
+int may_allocate(she_ctx *c)
+{
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    HIP_TRY(c, hipStreamIsCapturing(c->stream, &status));
+    if (status == hipStreamCaptureStatusNone) return SHE_OK;
+    return fail(c, SHE_ENOMEM, "this call needs more scratch than any before it: run it once before it is captured");
+}
+
 int ready(she_ctx *c)
 {
     if (c->clear.d_bad) return SHE_OK;
+    int code = may_allocate(c);
+    if (code) return code;
     HIP_TRY(c, hipMalloc((void **)&c->clear.d_bad, clear::COUNTERS * sizeof(uint32_t)));
     hipError_t rc = hipMemset(c->clear.d_bad, 0, clear::COUNTERS * sizeof(uint32_t));
     if (rc == hipSuccess) rc = hipStreamSynchronize(nullptr);
@@ -26,11 +39,13 @@ int ready(she_ctx *c)
 int ensure_scratch(she_ctx *c, size_t bytes)
 {
     if (bytes <= c->clear.bytes) return SHE_OK;
-    HIP_TRY(c, hipStreamSynchronize(c->stream));
-    hipFree(c->clear.scratch);
-    c->clear.scratch = nullptr; c->clear.bytes = 0;
-    bytes += bytes / 4;
-    HIP_TRY(c, hipMalloc(&c->clear.scratch, bytes));
+    int code = may_allocate(c);
+    if (code) return code;
+    c->clear.blocks.reserve(c->clear.blocks.size() + 1);
+    bytes = std::max(bytes, 2 * c->clear.bytes);
+    void *block = nullptr;
+    HIP_TRY(c, hipMalloc(&block, bytes));
+    c->clear.blocks.push_back(block);
     c->clear.bytes = bytes;
     return SHE_OK;
 }
@@ -82,7 +97,7 @@ try {
     if (!a.tokens || !a.segments) return SHE_OK;
     if (!a.out) return fail(c, SHE_EINVAL, "she_adapters: null argument");
     if ((rc = ready(c)) || (rc = ensure_scratch(c, clear::adapters_scratch(a)))) return rc;
-    HIP_TRY(c, clear::launch_adapters(a, c->clear.scratch, c->clear.d_bad, c->dk.cus, c->stream));
+    HIP_TRY(c, clear::launch_adapters(a, c->clear.scratch(), c->clear.d_bad, c->dk.cus, c->stream));
     return SHE_OK;
 } SHE_NOTHROW(c)
 
@@ -96,7 +111,7 @@ try {
     if (a.base_type == SHE_I32) return fail(c, SHE_EINVAL, "she_adapters_grad: base_type must be SHE_NO_BASE, the type or SHE_F32");
     if (!a.ddown || !a.dup || (a.tokens && (!a.dy || !a.dx))) return fail(c, SHE_EINVAL, "she_adapters_grad: null argument");
     if ((rc = ready(c)) || (rc = ensure_scratch(c, clear::adapters_grad_scratch(a)))) return rc;
-    HIP_TRY(c, clear::launch_adapters_grad(a, c->clear.scratch, c->clear.d_bad, c->dk.cus, c->stream));
+    HIP_TRY(c, clear::launch_adapters_grad(a, c->clear.scratch(), c->clear.d_bad, c->dk.cus, c->stream));
     return SHE_OK;
 } SHE_NOTHROW(c)
 
@@ -131,7 +146,7 @@ try {
     if ((rc = ready(c))) return rc;
     const clear::QkGradShape s = clear::qk_grad_shape(a, c->dk.cus);
     if ((rc = ensure_scratch(c, clear::qk_grad_scratch(s, a.head)))) return rc;
-    HIP_TRY(c, clear::launch_qk_rotate_grad(a, s, c->clear.scratch, c->clear.d_bad, c->stream));
+    HIP_TRY(c, clear::launch_qk_rotate_grad(a, s, c->clear.scratch(), c->clear.d_bad, c->stream));
     return SHE_OK;
 } SHE_NOTHROW(c)
 
@@ -159,7 +174,7 @@ try {
     const clear::AttendShape s = clear::attend_shape(a, c->dk.cus);
     if (s.few_slots > MOST_GROUPS || s.tile_slots * a.kv_heads > MOST_GROUPS) return fail(c, SHE_ERANGE, at + "too many tokens and requests for one call");
     if ((rc = ensure_scratch(c, clear::attend_scratch(a, s)))) return rc;
-    HIP_TRY(c, clear::launch_attend_pages(a, s, c->clear.scratch, c->clear.d_bad, c->stream));
+    HIP_TRY(c, clear::launch_attend_pages(a, s, c->clear.scratch(), c->clear.d_bad, c->stream));
     return SHE_OK;
 } SHE_NOTHROW(c)
 

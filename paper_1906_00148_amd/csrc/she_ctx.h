@@ -30,10 +30,18 @@ struct LeveledPools {         // leveled mode: TRGSW selectors (spectral form) a
     hipEvent_t around[2] = {nullptr, nullptr};   // recorded around a level's kernel
 };
 struct ClearWork {            // the clear side's scratch (she_clear.h); freed with the context
-    void *scratch = nullptr;
-    size_t bytes = 0;
+    // The last block is the one in use.  Those before it stay: work under way, and graphs that a caller has captured, may use them.
+    std::vector<void *> blocks;
+    size_t bytes = 0;               // of the last block, at least twice the one before
     uint32_t *d_bad = nullptr;      // ids out of range that its kernels have met, and a unit of zeros (clear::COUNTERS words)
-    ~ClearWork() { hipFree(scratch); hipFree(d_bad); }
+    ClearWork() = default;
+    ClearWork(const ClearWork &) = delete;
+    ~ClearWork()
+    {
+        for (void *b : blocks) hipFree(b);
+        hipFree(d_bad);
+    }
+    void *scratch() const { return blocks.empty() ? nullptr : blocks.back(); }
 };
 // Layer operators recorded between she_defer_begin and she_defer_run: one netlist for all of them, so that the
 // scheduler can overlap the tail of one operator with the head of the next.

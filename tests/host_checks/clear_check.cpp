@@ -25,6 +25,9 @@ hipError_t launch_adapters_grad(const she_adapters_grad_args &, void *, uint32_t
 hipError_t launch_attend_pages(const she_attend_pages_args &, const AttendShape &, void *, uint32_t *, hipStream_t) { return launched(); }
 }}
 
+static hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
+extern "C" hipError_t hipStreamIsCapturing(hipStream_t, hipStreamCaptureStatus *status) { *status = capturing; return hipSuccess; }
+
 static she_ctx *c;
 template <class A> static void expect(int (*call)(she_ctx *, const A *), const A &good, int code, const char *what, void (*change)(A &))
 {
@@ -146,16 +149,30 @@ int main()
     CHECK(she_attend_pages(c, &t) == SHE_OK && !launches, "no tokens\n");
     t.tokens = 2;
 
+    // while the stream is captured, a call that would allocate is refused
+    capturing = hipStreamCaptureStatusActive;
+    wanted = 500;
+    CHECK(she_attend_pages(c, &t) == SHE_ENOMEM, "a capture with scratch to allocate\n");
+    wanted = 0;
+    CHECK(she_attend_pages(c, &t) == SHE_OK, "a capture without\n");
+    capturing = hipStreamCaptureStatusNone;
+
     // scratch grows once, is used again, and a call that gets none says so and leaves nothing behind
     wanted = 1000;
     CHECK(she_attend_pages(c, &t) == SHE_OK, "scratch\n");
     const size_t held = fake::held;
     CHECK(she_attend_pages(c, &t) == SHE_OK && fake::held == held, "scratch is allocated again\n");
+    capturing = hipStreamCaptureStatusActive;
+    CHECK(she_attend_pages(c, &t) == SHE_OK && fake::held == held, "a capture within the scratch\n");
+    capturing = hipStreamCaptureStatusNone;
     wanted = 5000;
     fake::limit = fake::held;
     CHECK(she_attend_pages(c, &t) == SHE_ENOMEM && hipGetLastError() == hipSuccess, "no memory\n");
     fake::limit = ~(size_t)0;
-    CHECK(she_attend_pages(c, &t) == SHE_OK && fake::held > held, "memory again\n");
+    bool freed = false;
+    fake::on_free = [&](const char *, size_t) { freed = true; };
+    CHECK(she_attend_pages(c, &t) == SHE_OK && fake::held > held && !freed, "memory again, or the old block is gone\n");
+    fake::on_free = nullptr;
     she_free(c);
     CHECK(fake::held == 0, "%zu bytes are still held\n", fake::held);
     std::printf("failures %d\n", failures);

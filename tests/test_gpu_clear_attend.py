@@ -209,3 +209,26 @@ def test_refusals(ctx):
     huge = torch.zeros(1, 1, 2, 264, dtype=BF16, device="cuda")
     refused(-1, q=torch.zeros(3, 4, 264, dtype=BF16, device="cuda"), k_pages=huge, v_pages=huge)
     refused(-4, table=torch.zeros(2, (1 << 22) + 1, dtype=torch.int32, device="cuda"))
+
+
+def test_a_capture_never_allocates_and_outlives_the_scratch_it_had():
+    small, large = inputs(BF16, [1], [1500], 4, 1, 128, 16), inputs(BF16, [1, 1], [60000, 300], 8, 8, 128, 64)
+    side = torch.cuda.Stream()
+    with she.Context(she.TOY, 14, 64) as c:
+        c.set_stream(side.cuda_stream)
+        want = c.attend_pages(**small)                            # the cut rows' pieces need scratch
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            with pytest.raises(she.SheError) as e:
+                c.attend_pages(**large)
+            assert e.value.code == -2
+            got = c.attend_pages(**small)
+        c.attend_pages(**large)                                   # grows it
+        torch.cuda.synchronize()
+        junk = torch.randn(1 << 20, device="cuda")                # whatever is allocated next
+        for _ in range(3):
+            got.zero_()
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(got, want) and bool(torch.isfinite(junk).all())
