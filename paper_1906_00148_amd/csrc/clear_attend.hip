@@ -155,6 +155,8 @@ __device__ void attend_row(const she_attend_pages_args &a, uint32_t group, const
     }
 }
 
+// Bound by memory: 64 single tokens over 1 to 16384 places (8 key heads of 128, 2.1 GB) 426 us, 5.0 TB/s, and 11 to join their pieces.
+//
 // Few rows: every wavefront walks places of its own, 32 a step, four steps of the workgroup side by side, straight from memory.  Lane
 // l reads d = 32 s + 8 (l/16) .. of the key of place l%16 for the scores, and EL elements from EL (l%16) on of the values of the
 // eight places that its scores belong to, whole rows over 16 lanes; the eight rows are transposed in registers.
@@ -333,6 +335,12 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
     }
 }
 
+// Bound by what a wavefront does one after the other: 2048 tokens over 32768 places (32 / 8 heads of 128, bf16) 1080 us, 987 TFLOP/s
+// where a product of 8192^3 reaches 1279.  The matrix units are busy for 45 % of the cycles and the vector units for as many; taken
+// out for a timing, the softmax was worth 11 %, the second product 23 % and the tiles' loads 17 %.  Tried and slower: the next
+// step's scores beside a step's softmax (two forms), raised priority around the matrix instructions, pieces for more workgroups.
+// Eight wavefronts on 256 rows gain 3 % there and lose a third where a window makes the tiles' edges count.
+//
 // Many rows: a workgroup has TILE_ROWS of them, 32 a wavefront, and steps through the places STEP at a time with both tiles of the step
 // in LDS, twice over, so that the next step's are on their way while this one's are used.  The matrix instructions are 32 x 32 x 16:
 // lane l has row l%32 of the tile, and of every 32 places the scores of 8 (i/4) + 4 (l/32) + i%4.  The second product's operand is
