@@ -40,15 +40,13 @@ struct Work {
     Pieces few, tile;
     uint32_t few_chunk, tile_chunk;
     uint32_t few_most;                   // rows that a request has at most to be k_attend_few's
-    uint32_t few_each;                   // slots of every request there; 0: they are found by find_piece
 };
 __device__ inline Piece few_piece(const she_attend_pages_args &a, uint32_t group, const Work &w)
 {
-    if (!w.few_each) return find_piece(a.starts, a.requests, a.tokens, group, FEW_ROWS, blockIdx.x);
-    const int r = blockIdx.x / w.few_each;
+    if (w.few_most > FEW_ROWS) return find_piece(a.starts, a.requests, a.tokens, group, FEW_ROWS, blockIdx.x);
+    const int r = blockIdx.x;            // requests of a single tile at most: a slot each
     const int64_t b = bounded_start(a.starts, r, a.tokens) * group, e = bounded_start(a.starts, r + 1, a.tokens) * group;
-    const int index = blockIdx.x % w.few_each;
-    return Piece{b + (int64_t)index * FEW_ROWS < e ? r : -1, index, b, e};
+    return Piece{b < e ? r : -1, 0, b, e};
 }
 
 // A tile of rows and the places that any of them attends to.
@@ -673,15 +671,22 @@ AttendShape attend_shape(const she_attend_pages_args &a, uint32_t cus)
     const uint64_t group = a.q_heads / a.kv_heads, longest = std::min<uint64_t>((uint64_t)a.table_width * a.page_size, 0x7FFFFFFF);
     const uint64_t rows = a.tokens * group;
     if (!cus) cus = 1;
-    // Requests of few rows go to k_attend_few and the others to k_attend_tile.  The lengths are on the device; the host knows that
-    // there is one request, or that they have a token each on average, and leaves the other kernel out.
-    s.few_most = a.requests == 1 ? (rows <= 64 ? 0x7FFFFFFF : 0) : a.tokens <= a.requests ? 0x7FFFFFFF : 2 * FEW_ROWS;
-    s.few_each = s.few_most == 0x7FFFFFFF ? 0 : s.few_most / FEW_ROWS;
-    s.few_slots = s.few_most == 0x7FFFFFFF ? rows / FEW_ROWS + a.requests : (uint64_t)a.requests * s.few_each;
-    s.tile_slots = s.few_most == 0x7FFFFFFF ? 0 : rows / TILE_ROWS + a.requests;
     // places of a span at most: a window's, those that the tile's later tokens see further, and those before it down to a multiple of 32
     const auto span = [&](uint64_t tile) { return a.window ? std::min<uint64_t>(longest, (uint64_t)a.window + tile + 31) : longest; };
     const uint64_t few_span = span(FEW_ROWS), tile_span = span(TILE_ROWS);
+    // Requests of few rows (a token's query heads of one key head are rows) go to k_attend_few and the others to k_attend_tile, which
+    // computes 128 rows whether they are there or not.  Measured with 32 query and 8 key heads of 128 in bf16, either kernel alone, us:
+    //    one request     8 rows    16       32       64      128            16 requests   8 rows     16        32        64
+    //    1000 places    14, 23   15, 23   16, 23   15, 23   19, 25          1000 places   24, 28    29, 28    35, 31    52, 35
+    //    8000           16, 26   22, 27   26, 29   39, 29   54, 31          8000         108, 111  150, 115  176, 119  313, 133
+    //    32768          33, 45   41, 45   54, 46  109, 49  170, 57
+    // A single request is the first kernel's up to 16 rows, and further up to 2^18 rows x places.  Of several, those of a tile of it
+    // are (tokens of one request and chunks of others are often in one call, and a launch costs more than the difference), and
+    // all where the host knows that they have a token each on average: the lengths are on the device.  A kernel without rows is not launched.
+    const bool few_alone = a.requests == 1 ? rows <= FEW_ROWS || rows * few_span <= 1u << 18 : a.tokens <= a.requests;
+    s.few_most = few_alone ? 0x7FFFFFFF : a.requests > 1 && group <= FEW_ROWS ? FEW_ROWS : 0;
+    s.few_slots = few_alone ? rows / FEW_ROWS + a.requests : s.few_most ? a.requests : 0;
+    s.tile_slots = few_alone ? 0 : rows / TILE_ROWS + a.requests;
     // Pieces for two workgroups per compute unit: shorter ones (for eight) cost more to join than they gain, 128 us and not 78 for a
     // token over 32768 places, 84 and 76 for the mixed step.
     s.few_chunk = (uint32_t)std::min<uint64_t>(MOST_CHUNK, std::max<uint64_t>(256, ceil_div(s.few_slots * a.kv_heads * few_span / (2 * cus), 128) * 128));
@@ -710,7 +715,7 @@ hipError_t launch_attend_pages(const she_attend_pages_args &a, const AttendShape
     const size_t few = few_pieces(a, s), tile = tile_pieces(a, s);
     float *o = static_cast<float *>(scratch);
     float2 *ml = reinterpret_cast<float2 *>(o + (few + tile) * a.head);
-    const Work w{{o, ml, s.few_splits}, {o + few * a.head, ml + few, s.tile_splits}, s.few_chunk, s.tile_chunk, s.few_most, s.few_each};
+    const Work w{{o, ml, s.few_splits}, {o + few * a.head, ml + few, s.tile_splits}, s.few_chunk, s.tile_chunk, s.few_most};
     return a.type == SHE_BF16 ? attend<__bf16>(a, s, w, d_bad, st) : attend<_Float16>(a, s, w, d_bad, st);
 }
 

@@ -46,7 +46,7 @@ struct AttendShape {
     uint64_t few_slots, tile_slots;      // tiles of rows, at most, of either kernel; 0: it is not launched
     uint32_t few_chunk, tile_chunk;      // places of the cache that a workgroup walks
     uint32_t few_splits, tile_splits;    // workgroups that share a row's places at most
-    uint32_t few_most, few_each;         // rows of a request that the first kernel takes, slots that it has for each
+    uint32_t few_most;                   // rows of a request that the first kernel takes
 };
 AttendShape attend_shape(const she_attend_pages_args &a, uint32_t cus);
 size_t attend_scratch(const she_attend_pages_args &a, const AttendShape &s);
