@@ -609,7 +609,8 @@ Hidden take_hidden(Room &room, uint32_t slots, uint32_t rows, uint32_t chunks, b
     h.unscale = room.take<float>((size_t)slots * chunks);
     return h;
 }
-// Backward, a workgroup sums eight tiles a wavefront (four: 80 us of gradients over 8192 tokens and not 74), and more where an adapter would else be shared by more than 16.
+// Backward, a workgroup sums eight tiles a wavefront (four: 80 us of gradients over 8192 tokens and not 74), and more where an adapter
+// would else be shared by more than 16.
 template <class Args> Segments segments_of(const Args &a)
 {
     Segments s{a.starts, a.which, a.ranks, a.scale, a.tokens, a.segments, a.adapters, a.rank};

@@ -119,7 +119,7 @@ def rotate_grad(dy, x, w, cos, sin, positions, eps, interleaved):
     dx = r * (w * g - u * (w * g * u).mean(-1, keepdim=True))
     size = r * (w.abs() * gs + u.abs() * (w.abs() * gs * u.abs()).mean(-1, keepdim=True))
     unit = (2 * D + 40) * F32
-    # a weight's sum: over the steps of a wavefront, its lanes, and the workgroups' sums sixteen at a time
+    # a weight's sum: over the steps of a wavefront, its lanes, and the workgroups' sums eight at a time
     chain = D / 2 + 24 + 256
     return ((torch.where(ok, dx, 0.0), torch.where(ok, size * unit, 0.0)),
             ((g * u * ok).sum((0, 1)), (gs * u.abs() * ok).sum((0, 1)) * chain * F32))

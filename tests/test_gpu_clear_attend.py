@@ -62,6 +62,15 @@ def test_long_caches_that_workgroups_share(ctx, dtype, news, lengths):
     assert torch.equal(got, ctx.attend_pages(**a))
 
 
+@pytest.mark.parametrize("Hq,Hkv", [(16, 1), (17, 1), (40, 2), (33, 1)])
+@pytest.mark.parametrize("news", [[1], [9], [1, 1, 1], [1, 0, 5, 1], [2, 30, 1]])
+def test_many_query_heads_for_a_key_head(ctx, Hq, Hkv, news):
+    """A token alone has more rows than a tile of the kernel for few rows, or just as many."""
+    a = inputs(BF16, news, [700 + 60 * i for i in range(len(news))], Hq, Hkv, 64, 16)
+    for window in (0, 90):
+        compare(ctx, a, BF16, window)
+
+
 @pytest.mark.parametrize("window", [0, 50])
 def test_peaked_and_flat_weights(ctx, window):
     for spread in (30.0, 0.0):
