@@ -31,22 +31,11 @@ struct Pieces {
     float *o;                            // [..][head]
     float2 *ml;
     uint32_t splits;
+    uint32_t chunk;                      // places of a piece
 };
 __device__ inline size_t pieces_at(const Pieces &p, uint32_t kv_heads, size_t slot, int tile_rows, int row, int kv_head)
 {
     return ((slot * tile_rows + row) * kv_heads + kv_head) * p.splits;
-}
-struct Work {
-    Pieces few, tile;
-    uint32_t few_chunk, tile_chunk;
-    uint32_t few_most;                   // rows that a request has at most to be k_attend_few's
-};
-__device__ inline Piece few_piece(const she_attend_pages_args &a, uint32_t group, const Work &w)
-{
-    if (w.few_most > FEW_ROWS) return find_piece(a.starts, a.requests, a.tokens, group, FEW_ROWS, blockIdx.x);
-    const int r = blockIdx.x;            // requests of a single tile at most: a slot each
-    const int64_t b = bounded_start(a.starts, r, a.tokens) * group, e = bounded_start(a.starts, r + 1, a.tokens) * group;
-    return Piece{b < e ? r : -1, 0, b, e};
 }
 
 // A tile of rows and the places that any of them attends to.
@@ -153,13 +142,14 @@ __device__ void attend_row(const she_attend_pages_args &a, uint32_t group, const
     }
 }
 
-// Bound by memory: 64 single tokens over 1 to 16384 places (8 key heads of 128, 2.1 GB) 426 us, 5.0 TB/s, and 11 to join their pieces.
+// For small calls, where latencies add up: a token over 197 places (2 key heads of 64) 6.9 us, 16 tokens over 1000 (8 of 128) 21 us; but
+// it reaches the memory's rate too: 64 tokens over 1 to 16384 places (2.1 GB) 426 us, 5.0 TB/s.
 //
 // Few rows: every wavefront walks places of its own, 32 a step, four steps of the workgroup side by side, straight from memory.  Lane
 // l reads d = 32 s + 8 (l/16) .. of the key of place l%16 for the scores, and EL elements from EL (l%16) on of the values of the
 // eight places that its scores belong to, whole rows over 16 lanes; the eight rows are transposed in registers.
 template <class T, int DP>
-__global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_few(she_attend_pages_args a, uint32_t group, Work w, uint32_t *d_bad)
+__global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_few(she_attend_pages_args a, uint32_t group, Pieces pieces, uint32_t *d_bad)
 {
     constexpr int EL = DP == 64 ? 4 : 8, NB = DP == 256 ? 2 : 1, KS = DP / 32;
     __shared__ int64_t rows[MOST_CHUNK];
@@ -168,11 +158,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
     __shared__ int any_bad, any_special;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, quarter = lane >> 4;
     const int kv_head = blockIdx.y, D = (int)a.head;
-    const Piece piece = few_piece(a, group, w);
-    if (piece.segment < 0 || piece.last - piece.first > w.few_most) return;
-    const Span sp = span_of<FEW_ROWS>(a, group, piece, piece.index * FEW_ROWS, w.few_chunk);
+    const Piece piece = find_piece(a.starts, a.requests, a.tokens, group, FEW_ROWS, blockIdx.x);
+    if (piece.segment < 0) return;
+    const Span sp = span_of<FEW_ROWS>(a, group, piece, piece.index * FEW_ROWS, pieces.chunk);
     if ((int)blockIdx.z >= max(sp.parts, 1)) return;
-    const int from = sp.from + (int)blockIdx.z * (int)w.few_chunk, count = sp.parts ? min((int)w.few_chunk, sp.to - from) : 0;
+    const int from = sp.from + (int)blockIdx.z * (int)pieces.chunk, count = sp.parts ? min((int)pieces.chunk, sp.to - from) : 0;
     if (tid == 0) any_bad = any_special = 0;
     __syncthreads();
     look_up(a, sp.request, kv_head, from, count, rows, &any_bad, d_bad);
@@ -297,7 +287,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
     __syncthreads();
     if (any_special) {
         for (int r = wave; r < sp.rows; r += FEW_WAVES)
-            attend_row<T>(a, group, w.few, pieces_at(w.few, a.kv_heads, blockIdx.x, FEW_ROWS, r, kv_head) + blockIdx.z, sp, kv_head, sp.row + r, from, from + count);
+            attend_row<T>(a, group, pieces, pieces_at(pieces, a.kv_heads, blockIdx.x, FEW_ROWS, r, kv_head) + blockIdx.z, sp, kv_head, sp.row + r, from, from + count);
         return;
     }
     constexpr int EACH = DP / 16;                                 // elements of a row that a thread joins
@@ -325,11 +315,11 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
         for (int i = 0; i < EACH; i++)
             if (d0 + i < D) to[i] = (T)(o[i] * inv);
     } else {
-        const size_t at = pieces_at(w.few, a.kv_heads, blockIdx.x, FEW_ROWS, r, kv_head) + blockIdx.z;
-        if (d0 == 0) w.few.ml[at] = float2{top, sum};
+        const size_t at = pieces_at(pieces, a.kv_heads, blockIdx.x, FEW_ROWS, r, kv_head) + blockIdx.z;
+        if (d0 == 0) pieces.ml[at] = float2{top, sum};
 #pragma unroll
         for (int i = 0; i < EACH; i++)
-            if (d0 + i < D) w.few.o[at * D + d0 + i] = o[i];
+            if (d0 + i < D) pieces.o[at * D + d0 + i] = o[i];
     }
 }
 
@@ -337,6 +327,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
 // where a product of 8192^3 reaches 1279.  The matrix units are busy for 45 % of the cycles and the vector units for as many; taken
 // out for a timing, the softmax was worth 11 %, the second product 23 % and the tiles' loads 17 %.  Tried and slower: the next
 // step's scores beside a step's softmax (two forms), raised priority around the matrix instructions, pieces for more workgroups.
+// 24 requests of up to 700 tokens, half of them single (16 heads of 64, f16, a window of 1024): 54 us, most of it in the same steps.
 // Eight wavefronts on 256 rows gain 3 % there and lose a third where a window makes the tiles' edges count.
 //
 // Many rows: a workgroup has TILE_ROWS of them, 32 a wavefront, and steps through the places STEP at a time with both tiles of the step
@@ -356,7 +347,7 @@ template <int DP> __device__ inline int value_unit(int place, int unit)
 }
 
 template <class T, int DP>
-__global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_tile(she_attend_pages_args a, uint32_t group, Work w, const void *zeros, uint32_t *d_bad)
+__global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_tile(she_attend_pages_args a, uint32_t group, Pieces pieces, const void *zeros, uint32_t *d_bad)
 {
     constexpr int UNITS = DP / 8, KS = DP / 16, DB = DP / 32, BLOCK = 4 * STEP;      // places that are looked up together
     constexpr int EACH = STEP * UNITS / (64 * TILE_WAVES);                           // units of either tile that a thread brings
@@ -369,10 +360,10 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
     const int kv_head = blockIdx.x % a.kv_heads, D = (int)a.head;
     const uint32_t slot = gridDim.x / a.kv_heads - 1 - blockIdx.x / a.kv_heads;
     const Piece piece = find_piece(a.starts, a.requests, a.tokens, group, TILE_ROWS, slot);
-    if (piece.segment < 0 || piece.last - piece.first <= w.few_most) return;
-    const Span sp = span_of<TILE_ROWS>(a, group, piece, piece.index * TILE_ROWS, w.tile_chunk);
+    if (piece.segment < 0) return;
+    const Span sp = span_of<TILE_ROWS>(a, group, piece, piece.index * TILE_ROWS, pieces.chunk);
     if ((int)blockIdx.z >= max(sp.parts, 1)) return;
-    const int from = sp.from + (int)(blockIdx.z * w.tile_chunk), count = sp.parts ? min((int)w.tile_chunk, sp.to - from) : 0;
+    const int from = sp.from + (int)(blockIdx.z * pieces.chunk), count = sp.parts ? min((int)pieces.chunk, sp.to - from) : 0;
     const int steps = (count + STEP - 1) / STEP;
 
     // this lane's row, and what the wavefront's rows attend to
@@ -468,7 +459,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
 #pragma unroll
                 for (int k = 0; k < KS; k++) s[t] = mfma32(*reinterpret_cast<const x8<T> *>(keys + t * 32 * DP * 2 + (key_at ^ k * 32)), q[k], s[t]);
             }
-                const bool masked = gone || p0 + STEP - 1 > high_min || p0 < low_max || step * STEP + STEP > count;
+            const bool masked = gone || p0 + STEP - 1 > high_min || p0 < low_max || step * STEP + STEP > count;
             if (__builtin_expect(masked, 0)) {
                 const int from_here = p0 + 4 * half, most = high - from_here, least = low - from_here;
                 const uint64_t out = gone >> 4 * half;
@@ -507,7 +498,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
                     l += v;
                     p[t * 2 + i / 8][i % 8] = (T)v;
                 }
-                // V^T of the 32 elements from 32 b on and the sixteen places from 16 k on, in the scores' order
+            // V^T of the 32 elements from 32 b on and the sixteen places from 16 k on, in the scores' order
             auto columns = [&](int b, int k) {
                 u32x4 v;
 #pragma unroll
@@ -531,15 +522,15 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
 
     if (__ballot(special)) {
         for (int row = first_here; row <= last_here; row++)
-            attend_row<T>(a, group, w.tile, pieces_at(w.tile, a.kv_heads, slot, TILE_ROWS, row - sp.row, kv_head) + blockIdx.z, sp, kv_head, row, from, from + count);
+            attend_row<T>(a, group, pieces, pieces_at(pieces, a.kv_heads, slot, TILE_ROWS, row - sp.row, kv_head) + blockIdx.z, sp, kv_head, row, from, from + count);
         return;
     }
     l += __shfl_xor(l, 32);
     if (first_here + col > last_row) return;
     const int64_t token = sp.token0 + my_token;
-    const size_t at = pieces_at(w.tile, a.kv_heads, slot, TILE_ROWS, my_row - sp.row, kv_head) + blockIdx.z;
+    const size_t at = pieces_at(pieces, a.kv_heads, slot, TILE_ROWS, my_row - sp.row, kv_head) + blockIdx.z;
     const float inv = sp.parts > 1 ? 1.0f : l == 0 ? 0.0f : 1.0f / l;
-    if (sp.parts > 1 && half == 0) w.tile.ml[at] = float2{m, l};
+    if (sp.parts > 1 && half == 0) pieces.ml[at] = float2{m, l};
 #pragma unroll
     for (int b = 0; b < DB; b++)
 #pragma unroll
@@ -547,7 +538,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
             const int d = b * 32 + 2 * i + 4 * half;
             if (d >= D) continue;
             if (sp.parts > 1) {
-                *reinterpret_cast<f32x4 *>(w.tile.o + at * D + d) = f32x4{acc[b][i], acc[b][i + 1], acc[b][i + 2], acc[b][i + 3]};
+                *reinterpret_cast<f32x4 *>(pieces.o + at * D + d) = f32x4{acc[b][i], acc[b][i + 1], acc[b][i + 2], acc[b][i + 3]};
             } else {
                 T *to = (T *)a.out + token * a.out_token + my_head * a.out_head + d;
                 T v[4];
@@ -558,9 +549,11 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
         }
 }
 
-// Rows that were cut, `each` of a tile a workgroup: four, or one where there may be many pieces.  Up to JOIN_AHEAD pieces are a
-// wavefront's work; more are shared out among all four, a row after the other.  Pieces are requested JOIN_AHEAD at a time.  A token
-// over 32768 places, 4 rows of 64 pieces at 8 key heads, takes 32 us so, 43 with four rows a workgroup and 78 with a row a wavefront.
+// Rows that were cut, `each` of a tile a workgroup.  Up to JOIN_AHEAD pieces are a wavefront's work, and a workgroup of the tile kernel's
+// has sixteen rows then (with four, 99 and not 82 us for the whole call of 4063 tokens in two pieces at 16 heads of 64); more are
+// shared out among all four wavefronts, a row after the other, four rows a workgroup or, of many pieces, one.  Pieces are requested
+// JOIN_AHEAD at a time.  A token over 32768 places, 4 rows of 64 pieces at 8 key heads, takes 32 us so, 43 with four rows a
+// workgroup and 78 with a row a wavefront.
 constexpr int JOIN_AHEAD = 4;
 template <class T>
 __device__ inline void join_row(const she_attend_pages_args &a, const Pieces &w, size_t at, int parts, int from, int by, float &sum, float o[4])
@@ -592,19 +585,17 @@ __device__ inline void join_row(const she_attend_pages_args &a, const Pieces &w,
         }
     }
 }
-template <class T, bool TILES>
-__global__ __launch_bounds__(256) void k_attend_join(she_attend_pages_args a, uint32_t group, Work w, int each)
+template <class T, int ROWS>
+__global__ __launch_bounds__(256) void k_attend_join(she_attend_pages_args a, uint32_t group, Pieces pieces, int each)
 {
-    constexpr int ROWS = TILES ? TILE_ROWS : FEW_ROWS;
     __shared__ float sums[4], joined[4][256];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = (int)a.head;
-    const Piece piece = TILES ? find_piece(a.starts, a.requests, a.tokens, group, TILE_ROWS, blockIdx.x) : few_piece(a, group, w);
-    if (piece.segment < 0 || (piece.last - piece.first > w.few_most) != TILES) return;
+    const Piece piece = find_piece(a.starts, a.requests, a.tokens, group, ROWS, blockIdx.x);
+    if (piece.segment < 0) return;
     const int64_t first = piece.first + (int64_t)piece.index * ROWS + blockIdx.z * each;
     if (first >= piece.last) return;
-    const int parts = span_of<ROWS>(a, group, piece, piece.index * ROWS, TILES ? w.tile_chunk : w.few_chunk).parts;
+    const int parts = span_of<ROWS>(a, group, piece, piece.index * ROWS, pieces.chunk).parts;
     if (parts <= 1) return;
-    const Pieces &pieces = TILES ? w.tile : w.few;
     const int rows = (int)min((int64_t)each, piece.last - first);
     for (int r = parts <= JOIN_AHEAD ? wave : 0; r < rows; r += parts <= JOIN_AHEAD ? 4 : 1) {
         const int64_t row = first + r, token = row / group;
@@ -631,36 +622,28 @@ __global__ __launch_bounds__(256) void k_attend_join(she_attend_pages_args a, ui
     }
 }
 
-template <class T, int DP> hipError_t attend_rows(const she_attend_pages_args &a, const AttendShape &s, const Work &w, uint32_t *d_bad, hipStream_t st)
+template <class T, int DP> hipError_t attend_rows(const she_attend_pages_args &a, const AttendShape &s, const Pieces &pieces, uint32_t *d_bad, hipStream_t st)
 {
-    const uint32_t group = a.q_heads / a.kv_heads;
-    hipError_t rc = hipSuccess;
-    if (s.few_slots) {
-        k_attend_few<T, DP><<<dim3((uint32_t)s.few_slots, a.kv_heads, s.few_splits), 64 * FEW_WAVES, 0, st>>>(a, group, w, d_bad);
-        rc = hipGetLastError();
-    }
-    if (rc == hipSuccess && s.tile_slots) {
-        k_attend_tile<T, DP><<<dim3((uint32_t)(s.tile_slots * a.kv_heads), 1, s.tile_splits), 64 * TILE_WAVES, 0, st>>>(a, group, w, zeros_of(d_bad), d_bad);
-        rc = hipGetLastError();
-    }
-    return rc;
+    const uint32_t group = a.q_heads / a.kv_heads, slots = (uint32_t)s.slots;
+    if (s.few)
+        k_attend_few<T, DP><<<dim3(slots, a.kv_heads, s.splits), 64 * FEW_WAVES, 0, st>>>(a, group, pieces, d_bad);
+    else
+        k_attend_tile<T, DP><<<dim3(slots * a.kv_heads, 1, s.splits), 64 * TILE_WAVES, 0, st>>>(a, group, pieces, zeros_of(d_bad), d_bad);
+    return hipGetLastError();
 }
 
-template <class T> hipError_t attend(const she_attend_pages_args &a, const AttendShape &s, const Work &w, uint32_t *d_bad, hipStream_t st)
+template <class T> hipError_t attend(const she_attend_pages_args &a, const AttendShape &s, const Pieces &pieces, uint32_t *d_bad, hipStream_t st)
 {
-    hipError_t rc = a.head <= 64 ? attend_rows<T, 64>(a, s, w, d_bad, st) : a.head <= 128 ? attend_rows<T, 128>(a, s, w, d_bad, st)
-                                                                                          : attend_rows<T, 256>(a, s, w, d_bad, st);
-    const uint32_t group = a.q_heads / a.kv_heads;
-    if (rc == hipSuccess && s.few_slots && s.few_splits > 1) {
-        const int each = s.few_splits > 4 * JOIN_AHEAD ? 1 : 4;
-        k_attend_join<T, false><<<dim3((uint32_t)s.few_slots, a.kv_heads, FEW_ROWS / each), 256, 0, st>>>(a, group, w, each);
-        rc = hipGetLastError();
-    }
-    if (rc == hipSuccess && s.tile_slots && s.tile_splits > 1) {
-        k_attend_join<T, true><<<dim3((uint32_t)s.tile_slots, a.kv_heads, TILE_ROWS / 4), 256, 0, st>>>(a, group, w, 4);
-        rc = hipGetLastError();
-    }
-    return rc;
+    const hipError_t rc = a.head <= 64 ? attend_rows<T, 64>(a, s, pieces, d_bad, st) : a.head <= 128 ? attend_rows<T, 128>(a, s, pieces, d_bad, st)
+                                                                                                     : attend_rows<T, 256>(a, s, pieces, d_bad, st);
+    if (rc != hipSuccess || s.splits == 1) return rc;
+    const uint32_t group = a.q_heads / a.kv_heads, slots = (uint32_t)s.slots;
+    const int each = s.few && s.splits > 4 * JOIN_AHEAD ? 1 : s.few || s.splits > JOIN_AHEAD ? 4 : 16;
+    if (s.few)
+        k_attend_join<T, FEW_ROWS><<<dim3(slots, a.kv_heads, FEW_ROWS / each), 256, 0, st>>>(a, group, pieces, each);
+    else
+        k_attend_join<T, TILE_ROWS><<<dim3(slots, a.kv_heads, TILE_ROWS / each), 256, 0, st>>>(a, group, pieces, each);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -671,52 +654,68 @@ AttendShape attend_shape(const she_attend_pages_args &a, uint32_t cus)
     const uint64_t group = a.q_heads / a.kv_heads, longest = std::min<uint64_t>((uint64_t)a.table_width * a.page_size, 0x7FFFFFFF);
     const uint64_t rows = a.tokens * group;
     if (!cus) cus = 1;
-    // places of a span at most: a window's, those that the tile's later tokens see further, and those before it down to a multiple of 32
+    // places of a tile at most: a window's, those that its later tokens see further, and those before it down to a multiple of 32
     const auto span = [&](uint64_t tile) { return a.window ? std::min<uint64_t>(longest, (uint64_t)a.window + tile + 31) : longest; };
-    const uint64_t few_span = span(FEW_ROWS), tile_span = span(TILE_ROWS);
-    // Requests of few rows (a token's query heads of one key head are rows) go to k_attend_few and the others to k_attend_tile, which
-    // computes 128 rows whether they are there or not.  Measured with 32 query and 8 key heads of 128 in bf16, either kernel alone, us:
-    //    one request     8 rows    16       32       64      128            16 requests   8 rows     16        32        64
-    //    1000 places    14, 23   15, 23   16, 23   15, 23   19, 25          1000 places   24, 28    29, 28    35, 31    52, 35
-    //    8000           16, 26   22, 27   26, 29   39, 29   54, 31          8000         108, 111  150, 115  176, 119  313, 133
-    //    32768          33, 45   41, 45   54, 46  109, 49  170, 57
-    // A single request is the first kernel's up to 16 rows, and further up to 2^18 rows x places.  Of several, those of a tile of it
-    // are (tokens of one request and chunks of others are often in one call, and a launch costs more than the difference), and
-    // all where the host knows that they have a token each on average: the lengths are on the device.  A kernel without rows is not launched.
-    const bool few_alone = a.requests == 1 ? rows <= FEW_ROWS || rows * few_span <= 1u << 18 : a.tokens <= a.requests;
-    s.few_most = few_alone ? 0x7FFFFFFF : a.requests > 1 && group <= FEW_ROWS ? FEW_ROWS : 0;
-    s.few_slots = few_alone ? rows / FEW_ROWS + a.requests : s.few_most ? a.requests : 0;
-    s.tile_slots = few_alone ? 0 : rows / TILE_ROWS + a.requests;
-    // Pieces for two workgroups per compute unit: shorter ones (for eight) cost more to join than they gain, 128 us and not 78 for a
-    // token over 32768 places, 84 and 76 for the mixed step.
-    s.few_chunk = (uint32_t)std::min<uint64_t>(MOST_CHUNK, std::max<uint64_t>(256, ceil_div(s.few_slots * a.kv_heads * few_span / (2 * cus), 128) * 128));
-    s.few_splits = s.few_slots ? (uint32_t)std::max<uint64_t>(1, ceil_div(few_span, s.few_chunk)) : 1;
-    s.tile_chunk = (uint32_t)std::max<uint64_t>(512, ceil_div(s.tile_slots * a.kv_heads * tile_span / (2 * cus), STEP) * STEP);
-    s.tile_splits = s.tile_slots ? (uint32_t)std::max<uint64_t>(1, ceil_div(tile_span, s.tile_chunk)) : 1;
+    // One of the two kernels takes all of a call.  k_attend_tile computes 128 rows whether they are there or not, and k_attend_few reads
+    // the places once for every 16 rows.  Either measured (few, tile; 8 key heads of 128, bf16; us; rows of each request at a key head):
+    //    one request:    8 rows    16       32       64      128          16 requests:   4 rows     16        32        64
+    //    1000 places    14, 23   15, 23   16, 23   15, 23   19, 25         500 places   17, 19    20, 20
+    //    8000           16, 26   22, 27   26, 29   39, 29   54, 31        1000                    29, 28    35, 31    52, 35
+    //    32768          33, 45   41, 45   54, 46  109, 49  170, 57        4000          53, 55    75, 58
+    //                                                                    16384         221, 222  286, 219
+    // Where the work is small the first kernel's short way counts.  It also has single tokens of up to 8 rows, whose caches may have
+    // different lengths: its small pieces even them out (200 tokens over 1 to 3000 places 237, 274; 64 over 1 to 16384 430, 428).
+    s.few = rows * span(FEW_ROWS) <= 1u << 18 || (a.tokens <= a.requests && group <= FEW_ROWS / 2);
+    const uint64_t tile = s.few ? FEW_ROWS : TILE_ROWS, places = span(tile);
+    s.slots = a.requests == 1 ? ceil_div(rows, tile) : rows / tile + a.requests;
+    if (s.few) {
+        // Pieces for two workgroups per compute unit: shorter ones (for eight) cost more to join than they gain, 128 us and not 78 for
+        // a token over 32768 places when every row was joined by one wavefront.
+        const uint64_t share = ceil_div(s.slots * a.kv_heads * places / (2 * cus), 128) * 128;
+        s.chunk = (uint32_t)std::min<uint64_t>(MOST_CHUNK, std::max<uint64_t>(256, share));
+        s.splits = (uint32_t)std::max<uint64_t>(1, ceil_div(places, s.chunk));
+        return s;
+    }
+    // How many tiles there will be: every request has one, and its last is half full on average.
+    const uint64_t groups = std::max<uint64_t>({1, s.slots - a.requests / 2, std::min<uint64_t>(a.requests, a.tokens)}) * a.kv_heads;
+    // Workgroups that run at once, and pieces that make `rounds` rounds of them: the fewest places one after the other, where a workgroup
+    // costs as much as 256 of them beside its own.  Pieces are written and read again, 8 bytes an element of every row where a place is
+    // 4, at a quarter of the rate, and a launch more is 128 places.  So tiles of many rows stay whole (24 requests of up to 700 tokens,
+    // 16 heads of 64, a window of 1024: 54 us, 82 in two pieces), and few tiles over many places are cut until all compute units have
+    // work (64 tokens and one of 100 more over 16384 places each: 1021 us whole, 840 in five pieces).  Single tokens' lengths may
+    // differ: half the places on average, and a whole piece at the end.
+    const uint64_t at_once = cus * (a.head <= 64 ? 3 : a.head <= 128 ? 2 : 1);
+    uint64_t best = ~0ull;
+    for (uint64_t rounds = 1; rounds <= 8; rounds++) {
+        const uint64_t parts = std::max<uint64_t>(1, rounds * at_once / groups);
+        const uint64_t chunk = std::max<uint64_t>(512, ceil_div(ceil_div(places, parts), STEP) * STEP);
+        const uint64_t splits = std::max<uint64_t>(1, ceil_div(places, chunk)), longest_piece = std::min(chunk, places);
+        uint64_t cost = ceil_div(groups * splits, at_once) * (longest_piece + 256);
+        if (a.requests > 1 && a.tokens <= a.requests) cost += groups * (places + (splits + 1) * 256) / (2 * at_once) + longest_piece;
+        if (splits > 1) cost += 128 + 8 * rows * a.kv_heads * splits / at_once;
+        if (cost >= best) continue;
+        best = cost;
+        s.chunk = (uint32_t)chunk;
+        s.splits = (uint32_t)splits;
+    }
     return s;
 }
 
-static size_t few_pieces(const she_attend_pages_args &a, const AttendShape &s)
+static size_t pieces_of(const she_attend_pages_args &a, const AttendShape &s)
 {
-    return s.few_splits > 1 ? (size_t)s.few_slots * FEW_ROWS * a.kv_heads * s.few_splits : 0;
-}
-static size_t tile_pieces(const she_attend_pages_args &a, const AttendShape &s)
-{
-    return s.tile_splits > 1 ? (size_t)s.tile_slots * TILE_ROWS * a.kv_heads * s.tile_splits : 0;
+    return s.splits > 1 ? (size_t)s.slots * (s.few ? FEW_ROWS : TILE_ROWS) * a.kv_heads * s.splits : 0;
 }
 
 size_t attend_scratch(const she_attend_pages_args &a, const AttendShape &s)
 {
-    return (few_pieces(a, s) + tile_pieces(a, s)) * (a.head * sizeof(float) + sizeof(float2));
+    return pieces_of(a, s) * (a.head * sizeof(float) + sizeof(float2));
 }
 
 hipError_t launch_attend_pages(const she_attend_pages_args &a, const AttendShape &s, void *scratch, uint32_t *d_bad, hipStream_t st)
 {
-    const size_t few = few_pieces(a, s), tile = tile_pieces(a, s);
     float *o = static_cast<float *>(scratch);
-    float2 *ml = reinterpret_cast<float2 *>(o + (few + tile) * a.head);
-    const Work w{{o, ml, s.few_splits}, {o + few * a.head, ml + few, s.tile_splits}, s.few_chunk, s.tile_chunk, s.few_most};
-    return a.type == SHE_BF16 ? attend<__bf16>(a, s, w, d_bad, st) : attend<_Float16>(a, s, w, d_bad, st);
+    const Pieces pieces{o, reinterpret_cast<float2 *>(o + pieces_of(a, s) * a.head), s.splits, s.chunk};
+    return a.type == SHE_BF16 ? attend<__bf16>(a, s, pieces, d_bad, st) : attend<_Float16>(a, s, pieces, d_bad, st);
 }
 
 }}  // namespace she::clear

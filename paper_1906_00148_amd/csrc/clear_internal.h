@@ -43,10 +43,10 @@ hipError_t launch_adapters_grad(const she_adapters_grad_args &a, void *scratch, 
 
 // ---- attention
 struct AttendShape {
-    uint64_t few_slots, tile_slots;      // tiles of rows, at most, of either kernel; 0: it is not launched
-    uint32_t few_chunk, tile_chunk;      // places of the cache that a workgroup walks
-    uint32_t few_splits, tile_splits;    // workgroups that share a row's places at most
-    uint32_t few_most;                   // rows of a request that the first kernel takes
+    bool few;                            // the kernel for few rows, and not that for many
+    uint64_t slots;                      // tiles of rows, at most
+    uint32_t chunk;                      // places of the cache that a workgroup walks
+    uint32_t splits;                     // workgroups that share a tile's places, at most
 };
 AttendShape attend_shape(const she_attend_pages_args &a, uint32_t cus);
 size_t attend_scratch(const she_attend_pages_args &a, const AttendShape &s);

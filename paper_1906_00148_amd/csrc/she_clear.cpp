@@ -172,7 +172,7 @@ try {
     int rc = ready(c);
     if (rc) return rc;
     const clear::AttendShape s = clear::attend_shape(a, c->dk.cus);
-    if (s.few_slots > MOST_GROUPS || s.tile_slots * a.kv_heads > MOST_GROUPS) return fail(c, SHE_ERANGE, at + "too many tokens and requests for one call");
+    if ((s.few ? s.slots : s.slots * a.kv_heads) > MOST_GROUPS) return fail(c, SHE_ERANGE, at + "too many tokens and requests for one call");
     if ((rc = ensure_scratch(c, clear::attend_scratch(a, s)))) return rc;
     HIP_TRY(c, clear::launch_attend_pages(a, s, c->clear.scratch(), c->clear.d_bad, c->stream));
     return SHE_OK;

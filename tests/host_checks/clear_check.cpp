@@ -16,7 +16,7 @@ QkGradShape qk_grad_shape(const she_qk_rotate_grad_args &, uint32_t) { return {}
 size_t qk_grad_scratch(const QkGradShape &, uint32_t) { return wanted; }
 size_t adapters_scratch(const she_adapters_args &) { return wanted; }
 size_t adapters_grad_scratch(const she_adapters_grad_args &) { return wanted; }
-AttendShape attend_shape(const she_attend_pages_args &a, uint32_t) { AttendShape s{}; s.few_slots = a.requests; return s; }
+AttendShape attend_shape(const she_attend_pages_args &a, uint32_t) { AttendShape s{}; s.slots = a.requests; return s; }
 size_t attend_scratch(const she_attend_pages_args &, const AttendShape &) { return wanted; }
 hipError_t launch_qk_rotate(const she_qk_rotate_args &, const QkShape &, uint32_t *, hipStream_t) { return launched(); }
 hipError_t launch_qk_rotate_grad(const she_qk_rotate_grad_args &, const QkGradShape &, void *, uint32_t *, hipStream_t) { return launched(); }
