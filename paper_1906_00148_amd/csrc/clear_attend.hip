@@ -142,7 +142,7 @@ __device__ void attend_row(const she_attend_pages_args &a, uint32_t group, const
     }
 }
 
-// For small calls, where latencies add up: a token over 197 places (2 key heads of 64) 6.9 us, 16 tokens over 1000 (8 of 128) 21 us; but
+// For small calls, where latencies add up: a token over 197 places (2 key heads of 64) 6.4 us, 16 tokens over 1000 (8 of 128) 21 us; but
 // it reaches the memory's rate too: 64 tokens over 1 to 16384 places (2.1 GB) 426 us, 5.0 TB/s.
 //
 // Few rows: every wavefront walks places of its own, 32 a step, four steps of the workgroup side by side, straight from memory.  Lane
@@ -327,7 +327,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
 // where a product of 8192^3 reaches 1279.  The matrix units are busy for 45 % of the cycles and the vector units for as many; taken
 // out for a timing, the softmax was worth 11 %, the second product 23 % and the tiles' loads 17 %.  Tried and slower: the next
 // step's scores beside a step's softmax (two forms), raised priority around the matrix instructions, pieces for more workgroups.
-// 24 requests of up to 700 tokens, half of them single (16 heads of 64, f16, a window of 1024): 54 us, most of it in the same steps.
+// 24 requests of up to 700 tokens, half of them single (16 heads of 64, f16, a window of 1024): 57 us, most of it in the same steps.
 // Eight wavefronts on 256 rows gain 3 % there and lose a third where a window makes the tiles' edges count.
 //
 // Many rows: a workgroup has TILE_ROWS of them, 32 a wavefront, and steps through the places STEP at a time with both tiles of the step
@@ -681,7 +681,7 @@ AttendShape attend_shape(const she_attend_pages_args &a, uint32_t cus)
     // Workgroups that run at once, and pieces that make `rounds` rounds of them: the fewest places one after the other, where a workgroup
     // costs as much as 256 of them beside its own.  Pieces are written and read again, 8 bytes an element of every row where a place is
     // 4, at a quarter of the rate, and a launch more is 128 places.  So tiles of many rows stay whole (24 requests of up to 700 tokens,
-    // 16 heads of 64, a window of 1024: 54 us, 82 in two pieces), and few tiles over many places are cut until all compute units have
+    // 16 heads of 64, a window of 1024: 57 us, 82 in two pieces), and few tiles over many places are cut until all compute units have
     // work (64 tokens and one of 100 more over 16384 places each: 1021 us whole, 840 in five pieces).  Single tokens' lengths may
     // differ: half the places on average, and a whole piece at the end.
     const uint64_t at_once = cus * (a.head <= 64 ? 3 : a.head <= 128 ? 2 : 1);
