@@ -353,7 +353,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
     constexpr int EACH = STEP * UNITS / (64 * TILE_WAVES);                           // units of either tile that a thread brings
     __shared__ __align__(16) T even_keys[STEP * DP], even_values[STEP * DP], odd_keys[STEP * DP], odd_values[STEP * DP];
     __shared__ int64_t rows[2][BLOCK];
-    __shared__ uint64_t missing[2][BLOCK / 64];                                      // places that their page id keeps out
+    __shared__ uint64_t missing[2][BLOCK / 64];                                      // places that their page id or the table's end keeps out
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
     // A key head's tiles are one XCD's where there are eight of them: neighbouring workgroups have different heads.  Late tokens have
     // most to attend to: they come first.
@@ -386,7 +386,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
     auto keep_rows = [&](int b, int page) {
         const int i = b * BLOCK + tid;
         rows[b & 1][tid] = page < 0 ? -1 : page * a.page_stride + (int64_t)((uint32_t)(from + i) % a.page_size) * a.slot_stride + kv_head * a.page_head;
-        const uint64_t out = __ballot(page < 0 && i < count);
+        const uint64_t out = __ballot(page < 0);                                     // from `count` on too: a row may reach beyond the table
         if (lane == 0) missing[b & 1][wave] = out;
     };
     // a step's tiles on their way into LDS: a wavefront's 64 units lie side by side there, so each lane picks the one that belongs in
