@@ -13,7 +13,6 @@
 // Masks: a place that no row of the tile attends to is not read at all.  A place that some rows attend to and others do not has weight
 // 0 for the others, which a matrix instruction multiplies with the value all the same.  So where some of such places' values are
 // infinite or NaN, the tile's rows are done again, one by one and over the places that they attend to alone.
-#include <algorithm>
 #include <type_traits>
 
 #include "clear_device.h"
@@ -22,8 +21,7 @@
 namespace she { namespace clear {
 namespace {
 
-constexpr int FEW_ROWS = 16, FEW_WAVES = 4, MOST_CHUNK = 2048;
-constexpr int TILE_WAVES = 4, TILE_ROWS = 32 * TILE_WAVES, STEP = 64;   // rows of a workgroup, places of a step
+constexpr int FEW_WAVES = 4, TILE_WAVES = TILE_ROWS / 32;
 constexpr float LOG2E = 1.4426950408889634f;
 
 // What is left behind of the pieces of cut rows, by tile: [slots][rows of a tile][kv_heads][splits].
@@ -648,73 +646,10 @@ template <class T> hipError_t attend(const she_attend_pages_args &a, const Atten
 
 }  // namespace
 
-AttendShape attend_shape(const she_attend_pages_args &a, uint32_t cus)
-{
-    AttendShape s{};
-    const uint64_t group = a.q_heads / a.kv_heads, longest = std::min<uint64_t>((uint64_t)a.table_width * a.page_size, 0x7FFFFFFF);
-    const uint64_t rows = a.tokens * group;
-    if (!cus) cus = 1;
-    // places of a tile at most: a window's, those that its later tokens see further, and those before it down to a multiple of 32
-    const auto span = [&](uint64_t tile) { return a.window ? std::min<uint64_t>(longest, (uint64_t)a.window + tile + 31) : longest; };
-    // One of the two kernels takes all of a call.  k_attend_tile computes 128 rows whether they are there or not, and k_attend_few reads
-    // the places once for every 16 rows.  Either measured (few, tile; 8 key heads of 128, bf16; us; rows of each request at a key head):
-    //    one request:    8 rows    16       32       64      128          16 requests:   4 rows     16        32        64
-    //    1000 places    14, 23   15, 23   16, 23   15, 23   19, 25         500 places   17, 19    20, 20
-    //    8000           16, 26   22, 27   26, 29   39, 29   54, 31        1000                    29, 28    35, 31    52, 35
-    //    32768          33, 45   41, 45   54, 46  109, 49  170, 57        4000          53, 55    75, 58
-    //                                                                    16384         221, 222  286, 219
-    // Where the work is small the first kernel's short way counts.  It also has single tokens of up to 8 rows, whose caches may have
-    // different lengths: its small pieces even them out (200 tokens over 1 to 3000 places 237, 274; 64 over 1 to 16384 430, 428).
-    s.few = rows * span(FEW_ROWS) <= 1u << 18 || (a.tokens <= a.requests && group <= FEW_ROWS / 2);
-    const uint64_t tile = s.few ? FEW_ROWS : TILE_ROWS, places = span(tile);
-    s.slots = a.requests == 1 ? ceil_div(rows, tile) : rows / tile + a.requests;
-    if (s.few) {
-        // Pieces for two workgroups per compute unit: shorter ones (for eight) cost more to join than they gain, 128 us and not 78 for
-        // a token over 32768 places when every row was joined by one wavefront.
-        const uint64_t share = ceil_div(s.slots * a.kv_heads * places / (2 * cus), 128) * 128;
-        s.chunk = (uint32_t)std::min<uint64_t>(MOST_CHUNK, std::max<uint64_t>(256, share));
-        s.splits = (uint32_t)std::max<uint64_t>(1, ceil_div(places, s.chunk));
-        return s;
-    }
-    // How many tiles there will be: every request has one, and its last is half full on average.
-    const uint64_t groups = std::max<uint64_t>({1, s.slots - a.requests / 2, std::min<uint64_t>(a.requests, a.tokens)}) * a.kv_heads;
-    // Workgroups that run at once, and pieces that make `rounds` rounds of them: the fewest places one after the other, where a workgroup
-    // costs as much as 256 of them beside its own.  Pieces are written and read again, 8 bytes an element of every row where a place is
-    // 4, at a quarter of the rate, and a launch more is 128 places.  So tiles of many rows stay whole (24 requests of up to 700 tokens,
-    // 16 heads of 64, a window of 1024: 57 us, 82 in two pieces), and few tiles over many places are cut until all compute units have
-    // work (64 tokens and one of 100 more over 16384 places each: 1021 us whole, 840 in five pieces).  Single tokens' lengths may
-    // differ: half the places on average, and a whole piece at the end.
-    const uint64_t at_once = cus * (a.head <= 64 ? 3 : a.head <= 128 ? 2 : 1);
-    uint64_t best = ~0ull;
-    for (uint64_t rounds = 1; rounds <= 8; rounds++) {
-        const uint64_t parts = std::max<uint64_t>(1, rounds * at_once / groups);
-        const uint64_t chunk = std::max<uint64_t>(512, ceil_div(ceil_div(places, parts), STEP) * STEP);
-        const uint64_t splits = std::max<uint64_t>(1, ceil_div(places, chunk)), longest_piece = std::min(chunk, places);
-        uint64_t cost = ceil_div(groups * splits, at_once) * (longest_piece + 256);
-        if (a.requests > 1 && a.tokens <= a.requests) cost += groups * (places + (splits + 1) * 256) / (2 * at_once) + longest_piece;
-        if (splits > 1) cost += 128 + 8 * rows * a.kv_heads * splits / at_once;
-        if (cost >= best) continue;
-        best = cost;
-        s.chunk = (uint32_t)chunk;
-        s.splits = (uint32_t)splits;
-    }
-    return s;
-}
-
-static size_t pieces_of(const she_attend_pages_args &a, const AttendShape &s)
-{
-    return s.splits > 1 ? (size_t)s.slots * (s.few ? FEW_ROWS : TILE_ROWS) * a.kv_heads * s.splits : 0;
-}
-
-size_t attend_scratch(const she_attend_pages_args &a, const AttendShape &s)
-{
-    return pieces_of(a, s) * (a.head * sizeof(float) + sizeof(float2));
-}
-
 hipError_t launch_attend_pages(const she_attend_pages_args &a, const AttendShape &s, void *scratch, uint32_t *d_bad, hipStream_t st)
 {
     float *o = static_cast<float *>(scratch);
-    const Pieces pieces{o, reinterpret_cast<float2 *>(o + pieces_of(a, s) * a.head), s.splits, s.chunk};
+    const Pieces pieces{o, reinterpret_cast<float2 *>(o + attend_pieces(a, s) * a.head), s.splits, s.chunk};
     return a.type == SHE_BF16 ? attend<__bf16>(a, s, pieces, d_bad, st) : attend<_Float16>(a, s, pieces, d_bad, st);
 }
 

@@ -42,6 +42,8 @@ hipError_t launch_adapters(const she_adapters_args &a, void *scratch, uint32_t *
 hipError_t launch_adapters_grad(const she_adapters_grad_args &a, void *scratch, uint32_t *d_bad, uint32_t cus, hipStream_t st);
 
 // ---- attention
+// Rows of a workgroup of either kernel, places that k_attend_few looks up together at most, places of a step of k_attend_tile.
+constexpr int FEW_ROWS = 16, TILE_ROWS = 128, MOST_CHUNK = 2048, STEP = 64;
 struct AttendShape {
     bool few;                            // the kernel for few rows, and not that for many
     uint64_t slots;                      // tiles of rows, at most
@@ -49,6 +51,7 @@ struct AttendShape {
     uint32_t splits;                     // workgroups that share a tile's places, at most
 };
 AttendShape attend_shape(const she_attend_pages_args &a, uint32_t cus);
+size_t attend_pieces(const she_attend_pages_args &a, const AttendShape &s);      // rows of pieces that wait to be joined
 size_t attend_scratch(const she_attend_pages_args &a, const AttendShape &s);
 hipError_t launch_attend_pages(const she_attend_pages_args &a, const AttendShape &s, void *scratch, uint32_t *d_bad, hipStream_t st);
 
