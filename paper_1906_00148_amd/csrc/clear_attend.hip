@@ -24,17 +24,13 @@ namespace {
 constexpr int FEW_WAVES = 4, TILE_WAVES = TILE_ROWS / 32;
 constexpr float LOG2E = 1.4426950408889634f;
 
-// What is left behind of the pieces of cut rows, by tile: [slots][rows of a tile][kv_heads][splits].
+// What is left behind of the pieces of cut rows: [rows of all requests][kv_heads][splits].
 struct Pieces {
     float *o;                            // [..][head]
     float2 *ml;
     uint32_t splits;
-    uint32_t chunk;                      // places of a piece
+    uint32_t chunk;                      // places of a piece, unless a tile has more than `splits` such pieces
 };
-__device__ inline size_t pieces_at(const Pieces &p, uint32_t kv_heads, size_t slot, int tile_rows, int row, int kv_head)
-{
-    return ((slot * tile_rows + row) * kv_heads + kv_head) * p.splits;
-}
 
 // A tile of rows and the places that any of them attends to.
 struct Span {
@@ -43,9 +39,13 @@ struct Span {
     int64_t token0;                      // the request's first token
     int first;                           // place of the request's first new token (negative: its length is short of them)
     int from, to;                        // places, `from` a multiple of 32; none if to <= from
-    int parts;                           // pieces that they are cut into
+    int chunk, parts;                    // places of a piece, pieces that they are cut into
 };
-template <int ROWS> __device__ inline Span span_of(const she_attend_pages_args &a, uint32_t group, const Piece &p, int row, uint32_t chunk)
+__device__ inline size_t pieces_at(const Pieces &p, uint32_t kv_heads, uint32_t group, const Span &s, int row, int kv_head)
+{
+    return ((size_t)(s.token0 * group + row) * kv_heads + kv_head) * p.splits;
+}
+template <int ROWS> __device__ inline Span span_of(const she_attend_pages_args &a, uint32_t group, const Piece &p, int row, const Pieces &pieces)
 {
     Span s{};
     s.request = p.segment;
@@ -61,7 +61,11 @@ template <int ROWS> __device__ inline Span span_of(const she_attend_pages_args &
     const int64_t low = a.window ? (int64_t)p0 - (int64_t)a.window + 1 : 0;
     s.from = (int)max(low, (int64_t)0) & ~31;
     s.to = (int)min((int64_t)p1 + 1, room);
-    s.parts = s.to > s.from ? (int)(((uint32_t)(s.to - s.from) + chunk - 1) / chunk) : 0;
+    const uint32_t places = s.to > s.from ? s.to - s.from : 0;
+    uint32_t chunk = pieces.chunk;
+    if (places > (uint64_t)pieces.splits * chunk) chunk = ((places + pieces.splits - 1) / pieces.splits + 127) & ~127u;
+    s.chunk = (int)chunk;
+    s.parts = (int)((places + chunk - 1) / chunk);
     return s;
 }
 
@@ -158,12 +162,12 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
     const int kv_head = blockIdx.y, D = (int)a.head;
     const Piece piece = find_piece(a.starts, a.requests, a.tokens, group, FEW_ROWS, blockIdx.x);
     if (piece.segment < 0) return;
-    const Span sp = span_of<FEW_ROWS>(a, group, piece, piece.index * FEW_ROWS, pieces.chunk);
+    const Span sp = span_of<FEW_ROWS>(a, group, piece, piece.index * FEW_ROWS, pieces);
     if ((int)blockIdx.z >= max(sp.parts, 1)) return;
-    const int from = sp.from + (int)blockIdx.z * (int)pieces.chunk, count = sp.parts ? min((int)pieces.chunk, sp.to - from) : 0;
+    const int from = sp.from + (int)blockIdx.z * sp.chunk, count = sp.parts ? min(sp.chunk, sp.to - from) : 0;
     if (tid == 0) any_bad = any_special = 0;
     __syncthreads();
-    look_up(a, sp.request, kv_head, from, count, rows, &any_bad, d_bad);
+    look_up(a, sp.request, kv_head, from, min(count, MOST_CHUNK), rows, &any_bad, d_bad);
 
     // this lane's row
     const int my_row = min(sp.row + col, sp.row + sp.rows - 1), my_token = my_row / (int)group, my_head = kv_head * (int)group + my_row % (int)group;
@@ -183,15 +187,23 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
 #pragma unroll
         for (int e = 0; e < EL; e++) acc[b][e] = f32x4{0, 0, 0, 0};
     __syncthreads();
-    const bool unsafe = any_bad != 0;
+    bool unsafe = any_bad != 0;
     bool special = false;                                         // infinite or NaN values where not all rows attend
 
-    for (int k0 = wave * 32; k0 < count; k0 += FEW_WAVES * 32) {
+    for (int base = 0; base < count; base += FEW_WAVES * 32) {
+        if (base && base % MOST_CHUNK == 0) {
+            __syncthreads();                                      // the rows that were looked up before have been read
+            look_up(a, sp.request, kv_head, from + base, min(count - base, MOST_CHUNK), rows, &any_bad, d_bad);
+            __syncthreads();
+            unsafe = any_bad != 0;
+        }
+        const int k0 = base + wave * 32, r0 = k0 % MOST_CHUNK - k0;
+        if (k0 >= count) break;
         u32x4 kraw[2][KS];
 #pragma unroll
         for (int t = 0; t < 2; t++) {
             const int i = k0 + t * 16 + col;
-            const int64_t row = i < count ? rows[i] : -1;
+            const int64_t row = i < count ? rows[i + r0] : -1;
             const T *p = (const T *)a.k_pages + (row < 0 ? 0 : row) + quarter * 8;
 #pragma unroll
             for (int s = 0; s < KS; s++) kraw[t][s] = load8<T, true>(p + s * 32, row < 0 ? 0 : D - (s * 32 + quarter * 8));
@@ -201,7 +213,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
 #pragma unroll
         for (int e = 0; e < 8; e++) {
             const int i = k0 + (e < 4 ? 0 : 16) + quarter * 4 + (e & 3);
-            const int64_t row = i < count ? rows[i] : -1;
+            const int64_t row = i < count ? rows[i + r0] : -1;
             there |= row < 0 ? 0u : 1u << e;
 #pragma unroll
             for (int b = 0; b < NB; b++) {
@@ -285,7 +297,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
     __syncthreads();
     if (any_special) {
         for (int r = wave; r < sp.rows; r += FEW_WAVES)
-            attend_row<T>(a, group, pieces, pieces_at(pieces, a.kv_heads, blockIdx.x, FEW_ROWS, r, kv_head) + blockIdx.z, sp, kv_head, sp.row + r, from, from + count);
+            attend_row<T>(a, group, pieces, pieces_at(pieces, a.kv_heads, group, sp, sp.row + r, kv_head) + blockIdx.z, sp, kv_head, sp.row + r, from, from + count);
         return;
     }
     constexpr int EACH = DP / 16;                                 // elements of a row that a thread joins
@@ -313,7 +325,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
         for (int i = 0; i < EACH; i++)
             if (d0 + i < D) to[i] = (T)(o[i] * inv);
     } else {
-        const size_t at = pieces_at(pieces, a.kv_heads, blockIdx.x, FEW_ROWS, r, kv_head) + blockIdx.z;
+        const size_t at = pieces_at(pieces, a.kv_heads, group, sp, row, kv_head) + blockIdx.z;
         if (d0 == 0) pieces.ml[at] = float2{top, sum};
 #pragma unroll
         for (int i = 0; i < EACH; i++)
@@ -359,9 +371,9 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
     const uint32_t slot = gridDim.x / a.kv_heads - 1 - blockIdx.x / a.kv_heads;
     const Piece piece = find_piece(a.starts, a.requests, a.tokens, group, TILE_ROWS, slot);
     if (piece.segment < 0) return;
-    const Span sp = span_of<TILE_ROWS>(a, group, piece, piece.index * TILE_ROWS, pieces.chunk);
+    const Span sp = span_of<TILE_ROWS>(a, group, piece, piece.index * TILE_ROWS, pieces);
     if ((int)blockIdx.z >= max(sp.parts, 1)) return;
-    const int from = sp.from + (int)(blockIdx.z * pieces.chunk), count = sp.parts ? min((int)pieces.chunk, sp.to - from) : 0;
+    const int from = sp.from + (int)blockIdx.z * sp.chunk, count = sp.parts ? min(sp.chunk, sp.to - from) : 0;
     const int steps = (count + STEP - 1) / STEP;
 
     // this lane's row, and what the wavefront's rows attend to
@@ -520,13 +532,13 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
 
     if (__ballot(special)) {
         for (int row = first_here; row <= last_here; row++)
-            attend_row<T>(a, group, pieces, pieces_at(pieces, a.kv_heads, slot, TILE_ROWS, row - sp.row, kv_head) + blockIdx.z, sp, kv_head, row, from, from + count);
+            attend_row<T>(a, group, pieces, pieces_at(pieces, a.kv_heads, group, sp, row, kv_head) + blockIdx.z, sp, kv_head, row, from, from + count);
         return;
     }
     l += __shfl_xor(l, 32);
     if (first_here + col > last_row) return;
     const int64_t token = sp.token0 + my_token;
-    const size_t at = pieces_at(pieces, a.kv_heads, slot, TILE_ROWS, my_row - sp.row, kv_head) + blockIdx.z;
+    const size_t at = pieces_at(pieces, a.kv_heads, group, sp, my_row, kv_head) + blockIdx.z;
     const float inv = sp.parts > 1 ? 1.0f : l == 0 ? 0.0f : 1.0f / l;
     if (sp.parts > 1 && half == 0) pieces.ml[at] = float2{m, l};
 #pragma unroll
@@ -592,13 +604,13 @@ __global__ __launch_bounds__(256) void k_attend_join(she_attend_pages_args a, ui
     if (piece.segment < 0) return;
     const int64_t first = piece.first + (int64_t)piece.index * ROWS + blockIdx.z * each;
     if (first >= piece.last) return;
-    const int parts = span_of<ROWS>(a, group, piece, piece.index * ROWS, pieces.chunk).parts;
+    const Span sp = span_of<ROWS>(a, group, piece, piece.index * ROWS, pieces);
+    const int parts = sp.parts, rows = (int)min((int64_t)each, piece.last - first);
     if (parts <= 1) return;
-    const int rows = (int)min((int64_t)each, piece.last - first);
     for (int r = parts <= JOIN_AHEAD ? wave : 0; r < rows; r += parts <= JOIN_AHEAD ? 4 : 1) {
         const int64_t row = first + r, token = row / group;
         const int head = blockIdx.y * (int)group + (int)(row % group);
-        const size_t at = pieces_at(pieces, a.kv_heads, blockIdx.x, ROWS, blockIdx.z * each + r, blockIdx.y);
+        const size_t at = pieces_at(pieces, a.kv_heads, group, sp, sp.row + (int)blockIdx.z * each + r, blockIdx.y);
         T *to = (T *)a.out + token * a.out_token + head * a.out_head;
         float sum, o[4];
         if (parts <= JOIN_AHEAD) {

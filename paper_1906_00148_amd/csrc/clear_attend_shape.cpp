@@ -30,7 +30,11 @@ AttendShape attend_shape(const she_attend_pages_args &a, uint32_t cus)
         // a token over 32768 places when every row was joined by one wavefront.
         const uint64_t share = ceil_div(s.slots * a.kv_heads * places / (2 * cus), 128) * 128;
         s.chunk = (uint32_t)std::min<uint64_t>(MOST_CHUNK, std::max<uint64_t>(256, share));
-        s.splits = (uint32_t)std::max<uint64_t>(1, ceil_div(places, s.chunk));
+        // Up to sixteen workgroups for each that runs at once, or eight pieces, even the requests' lengths out.  A table of more
+        // places than such pieces have, as wide as a context that few requests fill, does not make scratch for more of them: a
+        // request that does fill it has longer pieces.
+        const uint64_t most = std::max<uint64_t>(8, ceil_div(16 * 2 * cus, s.slots * a.kv_heads));
+        s.splits = (uint32_t)std::max<uint64_t>(1, std::min(most, ceil_div(places, s.chunk)));
         return s;
     }
     // How many tiles there will be: every request has one, and its last is half full on average.
@@ -60,7 +64,7 @@ AttendShape attend_shape(const she_attend_pages_args &a, uint32_t cus)
 
 size_t attend_pieces(const she_attend_pages_args &a, const AttendShape &s)
 {
-    return s.splits > 1 ? (size_t)s.slots * (s.few ? FEW_ROWS : TILE_ROWS) * a.kv_heads * s.splits : 0;
+    return s.splits > 1 ? (size_t)a.tokens * a.q_heads * s.splits : 0;
 }
 
 size_t attend_scratch(const she_attend_pages_args &a, const AttendShape &s)
