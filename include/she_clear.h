@@ -143,8 +143,9 @@ int she_qk_rotate_grad(she_ctx *ctx, const she_qk_rotate_grad_args *args);
  * attends to the places max(0, p - window + 1) .. p (window = 0: all from 0 on), place u of request r being slot u % page_size
  * of page table[r][u / page_size]:
  *   out = sum_u softmax_u(scale * q . k_u) v_u,  query head h reading key head h / (q_heads / kv_heads).
- * A token that attends to nothing gets zeros.  Places whose page id is outside [0, pages) are attended to by nobody, and counted;
- * so are, uncounted, places that the table has no column for.  What the slots of such places hold, of places beyond the length and
+ * A token that attends to nothing gets zeros.  Places whose page id is outside [0, pages) are attended to by nobody, and counted
+ * where a token's window has them (the pages that every window has passed may be gone); so are, uncounted, places that the table has
+ * no column for.  What the slots of such places hold, of places beyond the length and
  * of places that a token does not attend to, infinities and NaN too, has no part in its result.  starts is ascending from 0 to
  * `tokens`.  At most 2^26 places (table_width * page_size). */
 typedef struct {

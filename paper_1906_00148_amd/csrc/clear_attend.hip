@@ -38,7 +38,8 @@ struct Span {
     int row, rows;                       // first row in the request, rows of the tile
     int64_t token0;                      // the request's first token
     int first;                           // place of the request's first new token (negative: its length is short of them)
-    int from, to;                        // places, `from` a multiple of 32; none if to <= from
+    int low;                             // the first place that any row attends to
+    int from, to;                        // places to walk, `from` down from `low` to a multiple of 32; none if to <= from
     int chunk, parts;                    // places of a piece, pieces that they are cut into
 };
 __device__ inline size_t pieces_at(const Pieces &p, uint32_t kv_heads, uint32_t group, const Span &s, int row, int kv_head)
@@ -59,7 +60,8 @@ template <int ROWS> __device__ inline Span span_of(const she_attend_pages_args &
     s.first = length - news;
     const int p0 = s.first + row / (int)group, p1 = s.first + (row + s.rows - 1) / (int)group;
     const int64_t low = a.window ? (int64_t)p0 - (int64_t)a.window + 1 : 0;
-    s.from = (int)max(low, (int64_t)0) & ~31;
+    s.low = (int)max(low, (int64_t)0);
+    s.from = s.low & ~31;
     s.to = (int)min((int64_t)p1 + 1, room);
     const uint32_t places = s.to > s.from ? s.to - s.from : 0;
     uint32_t chunk = pieces.chunk;
@@ -69,17 +71,24 @@ template <int ROWS> __device__ inline Span span_of(const she_attend_pages_args &
     return s;
 }
 
-// Where the rows of the places [from, from + count) start, -1 for those that their page id keeps out; returns whether any is.
-__device__ inline void look_up(const she_attend_pages_args &a, int request, int kv_head, int from, int count, int64_t *rows, int *any_bad, uint32_t *d_bad)
+// Whether place `place`, whose page id is out of range and slot in_page, stands for that page in the count: its first place that is
+// attended to here.  Pages that end before a window may be gone.
+__device__ inline bool counts(const Span &s, int place, int in_page, bool first)
+{
+    return place >= s.low && (in_page == 0 || place == s.low || first);
+}
+
+// Where the rows of the places [from, from + count) start, -1 for those that their page id keeps out; *any_bad: some that is attended to.
+__device__ inline void look_up(const she_attend_pages_args &a, const Span &s, int kv_head, int from, int count, int64_t *rows, int *any_bad, uint32_t *d_bad)
 {
     for (int i = threadIdx.x; i < count; i += blockDim.x) {
         const uint32_t place = from + i, column = place / a.page_size, in_page = place - column * a.page_size;
-        const int32_t page = a.table[request * a.table_stride + column];
+        const int32_t page = a.table[s.request * a.table_stride + column];
         const bool good = page >= 0 && (uint32_t)page < a.pages;
         rows[i] = good ? page * a.page_stride + in_page * a.slot_stride + kv_head * a.page_head : -1;
-        if (!good) {
+        if (!good && (int)place >= s.low) {
             *any_bad = 1;
-            if (in_page == 0 || i == 0) count_bad(d_bad);
+            if (counts(s, place, in_page, i == 0)) count_bad(d_bad);
         }
     }
 }
@@ -167,7 +176,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
     const int from = sp.from + (int)blockIdx.z * sp.chunk, count = sp.parts ? min(sp.chunk, sp.to - from) : 0;
     if (tid == 0) any_bad = any_special = 0;
     __syncthreads();
-    look_up(a, sp.request, kv_head, from, min(count, MOST_CHUNK), rows, &any_bad, d_bad);
+    look_up(a, sp, kv_head, from, min(count, MOST_CHUNK), rows, &any_bad, d_bad);
 
     // this lane's row
     const int my_row = min(sp.row + col, sp.row + sp.rows - 1), my_token = my_row / (int)group, my_head = kv_head * (int)group + my_row % (int)group;
@@ -193,7 +202,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
     for (int base = 0; base < count; base += FEW_WAVES * 32) {
         if (base && base % MOST_CHUNK == 0) {
             __syncthreads();                                      // the rows that were looked up before have been read
-            look_up(a, sp.request, kv_head, from + base, min(count - base, MOST_CHUNK), rows, &any_bad, d_bad);
+            look_up(a, sp, kv_head, from + base, min(count - base, MOST_CHUNK), rows, &any_bad, d_bad);
             __syncthreads();
             unsafe = any_bad != 0;
         }
@@ -390,7 +399,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
         if (i >= count) return -1;
         const int32_t page = a.table[sp.request * a.table_stride + (uint32_t)(from + i) / a.page_size];
         if (page >= 0 && (uint32_t)page < a.pages) return (int)page;
-        if ((uint32_t)(from + i) % a.page_size == 0 || i == 0) count_bad(d_bad);
+        if (counts(sp, from + i, (uint32_t)(from + i) % a.page_size, i == 0)) count_bad(d_bad);
         return -1;
     };
     auto keep_rows = [&](int b, int page) {

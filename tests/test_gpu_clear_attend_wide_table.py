@@ -40,3 +40,20 @@ def test_what_is_missing_or_not_finite_in_a_later_block(ctx):
     a["v_pages"][int(a["table"][77, 15])] = float("nan")          # places 960 to 1023, and up to 1030 of the first 32 that are read
     a["v_pages"][int(a["table"][77, 16]), :7] = float("nan")
     compare(ctx, a, torch.bfloat16, 40001 - 1031)
+
+
+@pytest.mark.parametrize("page", [1, 16, 24])
+@pytest.mark.parametrize("news,lengths,heads,window", [([1, 1], [700, 95], (4, 2), 50), ([3, 1], [700, 96], (4, 2), 60), ([700, 800], [1000, 1333], (8, 1), 75)])
+def test_pages_that_a_window_has_passed_may_be_gone(ctx, page, news, lengths, heads, window):
+    """A cache that gives back the pages that no token of a window reaches, as soon as it can: none of their ids is counted, the first one
+    that a token does reach is.  Single tokens, a few, and many (the kernel for tiles of rows)."""
+    a = inputs(torch.bfloat16, news, lengths, *heads, 64, page)
+    want = ctx.attend_pages(**a, window=window)
+    first = [max(0, length - n - window + 1) // page for n, length in zip(news, lengths)]       # the first page that is needed
+    for r, n in enumerate(first):
+        a["table"][r, :n] = -1
+    ctx.clear_bad_ids()
+    assert torch.equal(ctx.attend_pages(**a, window=window), want) and ctx.clear_bad_ids() == 0
+    a["table"][0, first[0]] = -1
+    compare(ctx, a, torch.bfloat16, window)
+    assert ctx.clear_bad_ids() > 0
