@@ -170,7 +170,7 @@ typedef struct {
 int she_attend_pages(she_ctx *ctx, const she_attend_pages_args *args);
 
 /* Ids out of range that the kernels of this context's clear calls have left out since the last reset (several for one id, where
- * several workgroups meet it).  Waits for the stream. */
+ * several workgroups meet it).  Waits for the stream; refused while that is captured (SHE_EINVAL). */
 int she_clear_bad_ids(she_ctx *ctx, uint64_t *count, int reset);
 
 #ifdef __cplusplus

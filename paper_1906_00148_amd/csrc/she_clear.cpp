@@ -184,10 +184,16 @@ try {
     if (!count) return fail(c, SHE_EINVAL, "null argument");
     *count = 0;
     if (!c->clear.d_bad) return SHE_OK;
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    HIP_TRY(c, hipStreamIsCapturing(c->stream, &status));
+    if (status != hipStreamCaptureStatusNone) return fail(c, SHE_EINVAL, "she_clear_bad_ids: the stream is captured and cannot be waited for");
     uint32_t n = 0;
     HIP_TRY(c, hipStreamSynchronize(c->stream));
     HIP_TRY(c, hipMemcpy(&n, c->clear.d_bad, sizeof(n), hipMemcpyDeviceToHost));
-    if (reset) HIP_TRY(c, hipMemset(c->clear.d_bad, 0, sizeof(n)));
+    if (reset) {                         // on the stream whose next kernel counts, which need not wait for the default one
+        HIP_TRY(c, hipMemsetAsync(c->clear.d_bad, 0, sizeof(n), c->stream));
+        HIP_TRY(c, hipStreamSynchronize(c->stream));
+    }
     *count = n;
     return SHE_OK;
 } SHE_NOTHROW(c)
