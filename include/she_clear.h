@@ -173,6 +173,9 @@ int she_attend_pages(she_ctx *ctx, const she_attend_pages_args *args);
  * several workgroups meet it).  Waits for the stream; refused while that is captured (SHE_EINVAL). */
 int she_clear_bad_ids(she_ctx *ctx, uint64_t *count, int reset);
 
+/* The HIP device that the context's arrays are on: the one that was current at she_keygen.  -1 for NULL. */
+int she_clear_device(const she_ctx *ctx);
+
 #ifdef __cplusplus
 }
 #endif

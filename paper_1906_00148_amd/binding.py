@@ -259,9 +259,9 @@ class Context(clear.Calls):
         self._h = h
         self._pool_tensor = None
         self._stream = 0
-        import torch
-        self._device = torch.cuda.current_device()                # the one that she_keygen has taken
+        self._device = self._L.she_clear_device(h)
         if use_torch_pool:
+            import torch
             nbytes = self._L.she_pool_bytes(self._h)
             self._pool_tensor = torch.zeros(nbytes // 4, dtype=torch.int32, device="cuda")
             self._check(self._L.she_bind_pool(self._h, C.c_void_p(self._pool_tensor.data_ptr()), nbytes))

@@ -10,9 +10,19 @@ from __future__ import annotations
 import ctypes as C
 import struct
 
-import torch
-
 EINVAL = -1
+
+
+class _Later:
+    """Stands for torch until something of it is used: what a Context does on ciphertexts alone needs none."""
+
+    def __getattr__(self, name):
+        global torch
+        import torch
+        return getattr(torch, name)
+
+
+torch = _Later()
 
 
 class SheError(RuntimeError):
@@ -62,7 +72,8 @@ _ATTEND_PAGES = _Layout("she_attend_pages_args", [
 LAYOUTS = [_ADAPTERS, _ADAPTERS_GRAD, _QK_ROTATE, _QK_ROTATE_GRAD, _ATTEND_PAGES]
 
 SIGNATURES = {**{layout.name[:-len("_args")]: (C.c_int, [C.c_void_p, C.c_char_p]) for layout in LAYOUTS},
-              "she_clear_bad_ids": (C.c_int, [C.c_void_p, C.POINTER(C.c_uint64), C.c_int])}
+              "she_clear_bad_ids": (C.c_int, [C.c_void_p, C.POINTER(C.c_uint64), C.c_int]),
+              "she_clear_device": (C.c_int, [C.c_void_p])}
 
 _NO_BASE, _F32, _I32 = -1, 2, 3
 

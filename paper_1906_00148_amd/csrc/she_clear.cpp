@@ -198,4 +198,6 @@ try {
     return SHE_OK;
 } SHE_NOTHROW(c)
 
+int she_clear_device(const she_ctx *c) { return c ? c->device : -1; }
+
 }  // extern "C"
