@@ -9,6 +9,7 @@
  * Conventions beside those of she.h:
  *  - Every pointer inside an argument struct is a DEVICE pointer; the struct itself is read before the call returns.
  *  - Strides count elements; the last axis of every array is contiguous.  An array's rows may be views of a wider one.
+ *  - The context's device (she_clear_device) has to be the current one (SHE_EINVAL).
  *  - A call enqueues its work on the context's stream and returns without waiting for it (like she_eval_gates_device).
  *    Arrays must stay valid until the stream has passed it.
  *  - Scratch belongs to the context and grows on demand, at least to twice its size; what it was before stays until she_free, so

@@ -1,7 +1,7 @@
 """The clear side of split inference on torch tensors (argument marshalling only; include/she_clear.h has the definitions).
 
 `Calls` is the part of a Context that runs between a decryption and the next encryption: adapters beside a shared projection,
-norms and rotation of queries and keys, attention over a paged cache.  Tensors are on the context's GPU, in bfloat16 or float16 where
+norms and rotation of queries and keys, attention over a paged cache.  Tensors are on the context's GPU (refused elsewhere), in bfloat16 or float16 where
 nothing else is said, with a contiguous last axis; their other strides are free.  Work is enqueued on the context's stream: when
 torch's current stream is another one, that work waits for it and it waits for the work.
 """
@@ -90,30 +90,30 @@ def _half(t, name):
     _refuse(f"{name} must be bfloat16 or float16, not {t.dtype}")
 
 
-def _see(t, name, dtype, shape):
+def _see(t, name, dtype, shape, device):
     """A tensor's address and strides; refuses one of another type, shape or place, or without a contiguous last axis."""
     strides = t.stride()
-    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or (strides[-1] != 1 and shape[-1] > 1):
-        _refuse_tensor(t, name, dtype, shape)
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or (strides[-1] != 1 and shape[-1] > 1):
+        _refuse_tensor(t, name, dtype, shape, device)
     return t.data_ptr(), strides
 
 
-def _refuse_tensor(t, name, dtype, shape):
+def _refuse_tensor(t, name, dtype, shape, device):
     if t.dtype is not dtype:
         _refuse(f"{name} must be {dtype}, not {t.dtype}")
     if t.shape != shape:
         _refuse(f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
-    if not t.is_cuda:
-        _refuse(f"{name} must be on the GPU")
+    if t.get_device() != device:
+        _refuse(f"{name} must be on the context's GPU, cuda:{device}, not {t.device}")
     _refuse(f"{name} must be contiguous{' along its last axis' if len(shape) > 1 else ''}")
 
 
-def _line(t, name, dtype, size):
+def _line(t, name, dtype, size, device):
     """The address of a vector that a kernel reads densely; None: a null pointer."""
     if t is None:
         return 0
-    if t.dtype is not dtype or t.shape != (size,) or not t.is_cuda or not t.is_contiguous():
-        _refuse_tensor(t, name, dtype, (size,))
+    if t.dtype is not dtype or t.shape != (size,) or t.get_device() != device or not t.is_contiguous():
+        _refuse_tensor(t, name, dtype, (size,), device)
     return t.data_ptr()
 
 
@@ -121,7 +121,10 @@ class Calls:
     """Mixed into Context."""
 
     def _call(self, fn, args):
-        """Runs a call on the context's stream, ordered with torch's current stream where that is another one."""
+        """Runs a call on the context's GPU and stream, ordered with torch's current stream there where that is another one."""
+        if torch._C._cuda_getDevice() != self._device:
+            with torch.cuda.device(self._device):
+                return self._call(fn, args)
         if torch._C._cuda_getCurrentRawStream(self._device) == self._stream:
             rc = fn(self._h, args)
             if rc:
@@ -143,64 +146,65 @@ class Calls:
         x [tokens, inputs]; down [adapters, rank, inputs], up [adapters, rank, outputs]; starts [segments + 1], which [segments],
         ranks [adapters] or None: int32; scale [adapters] float32; base [tokens, outputs] of x's type, float32, or int32 sums times
         step [outputs] float32, or None.  Returns out [tokens, outputs]; base itself may be given for it."""
-        ty, dtype = _half(x, "x"), x.dtype
+        ty, dtype, dev = _half(x, "x"), x.dtype, self._device
         (T, K), (A, r, N) = x.shape, up.shape
         S = which.shape[0]
-        x_at, xs = _see(x, "x", dtype, (T, K))
-        down_at, ds = _see(down, "down", dtype, (A, r, K))
-        up_at, us = _see(up, "up", dtype, (A, r, N))
-        kind, base_at, base_stride = self._base(base, dtype, ty, (T, N))
+        x_at, xs = _see(x, "x", dtype, (T, K), dev)
+        down_at, ds = _see(down, "down", dtype, (A, r, K), dev)
+        up_at, us = _see(up, "up", dtype, (A, r, N), dev)
+        kind, base_at, base_stride = self._base(base, dtype, ty, (T, N), dev)
         if step is not None and kind != _I32:
             _refuse("step belongs to int32 sums")
         if out is None:
             out = torch.empty(T, N, dtype=dtype, device=x.device)
             out_at, out_stride = out.data_ptr(), N
         else:
-            out_at, (out_stride, _) = _see(out, "out", dtype, (T, N))
+            out_at, (out_stride, _) = _see(out, "out", dtype, (T, N), dev)
         self._call(self._L.she_adapters, _ADAPTERS.pack(
-            ty, kind, T, K, N, A, r, S, x_at, xs[0], down_at, ds[0], ds[1], up_at, us[0], us[1], _line(starts, "starts", torch.int32, S + 1),
-            _line(which, "which", torch.int32, S), _line(ranks, "ranks", torch.int32, A), _line(scale, "scale", torch.float32, A),
-            base_at, base_stride, _line(step, "step", torch.float32, N), out_at, out_stride))
+            ty, kind, T, K, N, A, r, S, x_at, xs[0], down_at, ds[0], ds[1], up_at, us[0], us[1], _line(starts, "starts", torch.int32, S + 1, dev),
+            _line(which, "which", torch.int32, S, dev), _line(ranks, "ranks", torch.int32, A, dev), _line(scale, "scale", torch.float32, A, dev),
+            base_at, base_stride, _line(step, "step", torch.float32, N, dev), out_at, out_stride))
         return out
 
     @staticmethod
-    def _base(base, dtype, ty, shape):
+    def _base(base, dtype, ty, shape, dev):
         if base is None:
             return _NO_BASE, 0, 0
         kind = {dtype: ty, torch.float32: _F32, torch.int32: _I32}.get(base.dtype)
         if kind is None:
             _refuse(f"base must be {dtype}, float32 or int32, not {base.dtype}")
-        at, strides = _see(base, "base", base.dtype, shape)
+        at, strides = _see(base, "base", base.dtype, shape, dev)
         return kind, at, strides[0]
 
     def adapters_grad(self, dy, x, down, up, starts, which, scale, ranks=None, base=None):
         """Gradients of `adapters` for dy [tokens, outputs]: (dx, ddown, dup), dx with `base` (the gradient that reaches x through the
         projection itself, of x's type or float32) added to it."""
-        ty, dtype = _half(x, "x"), x.dtype
+        ty, dtype, dev = _half(x, "x"), x.dtype, self._device
         (T, K), (A, r, N) = x.shape, up.shape
         S = which.shape[0]
-        dy_at, dys = _see(dy, "dy", dtype, (T, N))
-        x_at, xs = _see(x, "x", dtype, (T, K))
-        down_at, ds = _see(down, "down", dtype, (A, r, K))
-        up_at, us = _see(up, "up", dtype, (A, r, N))
-        kind, base_at, base_stride = self._base(base, dtype, ty, (T, K))
+        dy_at, dys = _see(dy, "dy", dtype, (T, N), dev)
+        x_at, xs = _see(x, "x", dtype, (T, K), dev)
+        down_at, ds = _see(down, "down", dtype, (A, r, K), dev)
+        up_at, us = _see(up, "up", dtype, (A, r, N), dev)
+        kind, base_at, base_stride = self._base(base, dtype, ty, (T, K), dev)
+        lines = (_line(starts, "starts", torch.int32, S + 1, dev), _line(which, "which", torch.int32, S, dev),
+                 _line(ranks, "ranks", torch.int32, A, dev), _line(scale, "scale", torch.float32, A, dev))
         dx, ddown, dup = (torch.empty(shape, dtype=dtype, device=x.device) for shape in ((T, K), (A, r, K), (A, r, N)))
         self._call(self._L.she_adapters_grad, _ADAPTERS_GRAD.pack(
-            ty, kind, T, K, N, A, r, S, dy_at, dys[0], x_at, xs[0], down_at, ds[0], ds[1], up_at, us[0], us[1],
-            _line(starts, "starts", torch.int32, S + 1), _line(which, "which", torch.int32, S), _line(ranks, "ranks", torch.int32, A),
-            _line(scale, "scale", torch.float32, A), base_at, base_stride, dx.data_ptr(), K, ddown.data_ptr(), dup.data_ptr()))
+            ty, kind, T, K, N, A, r, S, dy_at, dys[0], x_at, xs[0], down_at, ds[0], ds[1], up_at, us[0], us[1], *lines,
+            base_at, base_stride, dx.data_ptr(), K, ddown.data_ptr(), dup.data_ptr()))
         return dx, ddown, dup
 
     @staticmethod
-    def _rotation(q, k, wq, wk, cos, sin, positions):
+    def _rotation(q, k, wq, wk, cos, sin, positions, dev):
         """What the three calls on queries and keys have in common, checked: type, sizes, addresses and strides."""
         ty, dtype = _half(q, "q"), q.dtype
         (T, Hq, D), Hkv = q.shape, k.shape[1]
         P, half = cos.shape
-        q_at, qs = _see(q, "q", dtype, (T, Hq, D))
-        k_at, ks = _see(k, "k", dtype, (T, Hkv, D))
-        tables = (_line(wq, "wq", torch.float32, D), _line(wk, "wk", torch.float32, D), _see(cos, "cos", torch.float32, (P, half))[0],
-                  _see(sin, "sin", torch.float32, (P, half))[0], _line(positions, "positions", torch.int32, T))
+        q_at, qs = _see(q, "q", dtype, (T, Hq, D), dev)
+        k_at, ks = _see(k, "k", dtype, (T, Hkv, D), dev)
+        tables = (_line(wq, "wq", torch.float32, D, dev), _line(wk, "wk", torch.float32, D, dev), _see(cos, "cos", torch.float32, (P, half), dev)[0],
+                  _see(sin, "sin", torch.float32, (P, half), dev)[0], _line(positions, "positions", torch.int32, T, dev))
         if not (cos.is_contiguous() and sin.is_contiguous()):
             _refuse("cos and sin must be contiguous")
         return ty, dtype, (T, Hq, Hkv, D, 2 * half, P), (q_at, k_at), (qs[0], qs[1], ks[0], ks[1]), tables
@@ -209,11 +213,12 @@ class Calls:
         """Norm of every head of q [tokens, q_heads, head] and k [tokens, kv_heads, head] with the weights wq, wk [head] float32 (or
         None), and the rotation by cos, sin [places, rot / 2] float32 at positions [tokens] int32.  Returns (q', k'); out: a pair
         for them, which may be (q, k)."""
-        ty, dtype, (T, Hq, Hkv, D, rot, P), at, strides, tables = self._rotation(q, k, wq, wk, cos, sin, positions)
+        dev = self._device
+        ty, dtype, (T, Hq, Hkv, D, rot, P), at, strides, tables = self._rotation(q, k, wq, wk, cos, sin, positions, dev)
         if out is None:
             out = torch.empty(T, Hq, D, dtype=dtype, device=q.device), torch.empty(T, Hkv, D, dtype=dtype, device=q.device)
-        q_out, qs = _see(out[0], "out", dtype, (T, Hq, D))
-        k_out, ks = _see(out[1], "out", dtype, (T, Hkv, D))
+        q_out, qs = _see(out[0], "out", dtype, (T, Hq, D), dev)
+        k_out, ks = _see(out[1], "out", dtype, (T, Hkv, D), dev)
         self._call(self._L.she_qk_rotate, _QK_ROTATE.pack(
             ty, bool(interleaved), T, Hq, Hkv, D, rot, P, eps, *at, 0, *strides, 0, 0, *tables, q_out, k_out, qs[0], qs[1], ks[0], ks[1],
             0, 0, 0, 0, 0, 0, 0, 0))
@@ -222,32 +227,34 @@ class Calls:
     def qk_rotate_append(self, q, k, v, wq, wk, cos, sin, positions, k_pages, v_pages, slots, eps=1e-6, interleaved=False, out=None):
         """qk_rotate whose keys, with the values v [tokens, kv_heads, head], go to the places slots [tokens] int64 (-1: nowhere) of
         k_pages, v_pages [pages, page_size, kv_heads, head].  Returns q'."""
-        ty, dtype, (T, Hq, Hkv, D, rot, P), at, strides, tables = self._rotation(q, k, wq, wk, cos, sin, positions)
-        v_at, vs = _see(v, "v", dtype, (T, Hkv, D))
-        pages_at, pages, size = self._pages(k_pages, v_pages, dtype, Hkv, D)
+        dev = self._device
+        ty, dtype, (T, Hq, Hkv, D, rot, P), at, strides, tables = self._rotation(q, k, wq, wk, cos, sin, positions, dev)
+        v_at, vs = _see(v, "v", dtype, (T, Hkv, D), dev)
+        pages_at, pages, size = self._pages(k_pages, v_pages, dtype, Hkv, D, dev)
         if out is None:
             out = torch.empty(T, Hq, D, dtype=dtype, device=q.device)
-        q_out, qs = _see(out, "out", dtype, (T, Hq, D))
+        q_out, qs = _see(out, "out", dtype, (T, Hq, D), dev)
         self._call(self._L.she_qk_rotate, _QK_ROTATE.pack(
             ty, bool(interleaved), T, Hq, Hkv, D, rot, P, eps, *at, v_at, *strides, vs[0], vs[1], *tables, q_out, 0, qs[0], qs[1], 0, 0,
-            *pages_at, pages, size, _line(slots, "slots", torch.int64, T)))
+            *pages_at, pages, size, _line(slots, "slots", torch.int64, T, dev)))
         return out
 
     @staticmethod
-    def _pages(k_pages, v_pages, dtype, Hkv, D):
+    def _pages(k_pages, v_pages, dtype, Hkv, D, dev):
         """(addresses and strides, pages, page size)"""
         pages, size = k_pages.shape[:2]
-        k_at, strides = _see(k_pages, "k_pages", dtype, (pages, size, Hkv, D))
-        v_at, other = _see(v_pages, "v_pages", dtype, (pages, size, Hkv, D))
+        k_at, strides = _see(k_pages, "k_pages", dtype, (pages, size, Hkv, D), dev)
+        v_at, other = _see(v_pages, "v_pages", dtype, (pages, size, Hkv, D), dev)
         if strides != other:
             _refuse("k_pages and v_pages must have the same strides")
         return (k_at, v_at, strides[0], strides[1], strides[2]), pages, size
 
     def qk_rotate_grad(self, dq_out, dk_out, q, k, wq, wk, cos, sin, positions, eps=1e-6, interleaved=False):
         """Gradients of qk_rotate: (dq, dk, dwq, dwk), the weights' in float32."""
-        ty, dtype, (T, Hq, Hkv, D, rot, P), at, strides, tables = self._rotation(q, k, wq, wk, cos, sin, positions)
-        dq_at, dqs = _see(dq_out, "dq_out", dtype, (T, Hq, D))
-        dk_at, dks = _see(dk_out, "dk_out", dtype, (T, Hkv, D))
+        dev = self._device
+        ty, dtype, (T, Hq, Hkv, D, rot, P), at, strides, tables = self._rotation(q, k, wq, wk, cos, sin, positions, dev)
+        dq_at, dqs = _see(dq_out, "dq_out", dtype, (T, Hq, D), dev)
+        dk_at, dks = _see(dk_out, "dk_out", dtype, (T, Hkv, D), dev)
         dq, dk = (torch.empty(T, h, D, dtype=dtype, device=q.device) for h in (Hq, Hkv))
         dw = torch.empty(2, D, dtype=torch.float32, device=q.device)
         dw_at = dw.data_ptr()
@@ -260,27 +267,28 @@ class Calls:
         """Attention of the new tokens q [tokens, q_heads, head] of every request, starts [requests + 1] int32, over its lengths
         [requests] int32 places in k_pages, v_pages [pages, page_size, kv_heads, head], found through table [requests, width] int32;
         causal, and over the last `window` places alone if that is not 0.  scale: head ** -0.5 if None.  Returns out like q."""
-        ty, dtype = _half(q, "q"), q.dtype
+        ty, dtype, dev = _half(q, "q"), q.dtype, self._device
         T, Hq, D = q.shape
         Hkv = k_pages.shape[2]
         R, width = table.shape
-        q_at, qs = _see(q, "q", dtype, (T, Hq, D))
-        pages_at, pages, size = self._pages(k_pages, v_pages, dtype, Hkv, D)
-        table_at, ts = _see(table, "table", torch.int32, (R, width))
+        q_at, qs = _see(q, "q", dtype, (T, Hq, D), dev)
+        pages_at, pages, size = self._pages(k_pages, v_pages, dtype, Hkv, D, dev)
+        table_at, ts = _see(table, "table", torch.int32, (R, width), dev)
         if not 0 <= window < 1 << 32:
             _refuse("window must be a number of places")
         if out is None:
             out = torch.empty(T, Hq, D, dtype=dtype, device=q.device)
             out_at, out_token, out_head = out.data_ptr(), Hq * D, D
         else:
-            out_at, (out_token, out_head, _) = _see(out, "out", dtype, (T, Hq, D))
+            out_at, (out_token, out_head, _) = _see(out, "out", dtype, (T, Hq, D), dev)
         self._call(self._L.she_attend_pages, _ATTEND_PAGES.pack(
             ty, T, R, Hq, Hkv, D, window, D ** -0.5 if scale is None else scale, q_at, qs[0], qs[1], *pages_at, pages, size, table_at, ts[0],
-            width, _line(starts, "starts", torch.int32, R + 1), _line(lengths, "lengths", torch.int32, R), out_at, out_token, out_head))
+            width, _line(starts, "starts", torch.int32, R + 1, dev), _line(lengths, "lengths", torch.int32, R, dev), out_at, out_token, out_head))
         return out
 
     def clear_bad_ids(self, reset: bool = True) -> int:
         """Ids out of range in device arrays that these calls have left out since the last reset; waits for the stream."""
         n = C.c_uint64(0)
-        self._check(self._L.she_clear_bad_ids(self._h, C.byref(n), int(reset)))
+        with torch.cuda.device(self._device):
+            self._check(self._L.she_clear_bad_ids(self._h, C.byref(n), int(reset)))
         return n.value

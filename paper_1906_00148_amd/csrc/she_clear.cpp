@@ -20,11 +20,20 @@ int may_allocate(she_ctx *c)
     return fail(c, SHE_ENOMEM, "this call needs more scratch than any before it: run it once before it is captured");
 }
 
+// Launches go to the current device, and the default stream is another one on each.
+int on_device(she_ctx *c)
+{
+    int now = -1;
+    HIP_TRY(c, hipGetDevice(&now));
+    if (now == c->device) return SHE_OK;
+    return fail(c, SHE_EINVAL, "the current device is " + std::to_string(now) + ", the context is on " + std::to_string(c->device));
+}
+
 int ready(she_ctx *c)
 {
-    if (c->clear.d_bad) return SHE_OK;
-    int code = may_allocate(c);
-    if (code) return code;
+    int code = on_device(c);
+    if (code || c->clear.d_bad) return code;
+    if ((code = may_allocate(c))) return code;
     HIP_TRY(c, hipMalloc((void **)&c->clear.d_bad, clear::COUNTERS * sizeof(uint32_t)));
     hipError_t rc = hipMemset(c->clear.d_bad, 0, clear::COUNTERS * sizeof(uint32_t));
     if (rc == hipSuccess) rc = hipStreamSynchronize(nullptr);
@@ -184,6 +193,7 @@ try {
     if (!count) return fail(c, SHE_EINVAL, "null argument");
     *count = 0;
     if (!c->clear.d_bad) return SHE_OK;
+    if (int code = on_device(c)) return code;
     hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
     HIP_TRY(c, hipStreamIsCapturing(c->stream, &status));
     if (status != hipStreamCaptureStatusNone) return fail(c, SHE_EINVAL, "she_clear_bad_ids: the stream is captured and cannot be waited for");
