@@ -1,9 +1,10 @@
 """The clear side of split inference on torch tensors (argument marshalling only; include/she_clear.h has the definitions).
 
 `Calls` is the part of a Context that runs between a decryption and the next encryption: adapters beside a shared projection,
-norms and rotation of queries and keys, attention over a paged cache.  Tensors are on the context's GPU (refused elsewhere), in bfloat16 or float16 where
-nothing else is said, with a contiguous last axis; their other strides are free.  Work is enqueued on the context's stream: when
-torch's current stream is another one, that work waits for it and it waits for the work.
+norms and rotation of queries and keys, attention over a paged cache.  Tensors are on the context's GPU (refused elsewhere), in
+bfloat16 or float16 where nothing else is said, with a contiguous last axis; their other strides are free.  Gradients have calls of
+their own: backward through a result raises, and what a call writes into (out, pages) counts as changed in place.  Work is enqueued
+on the context's stream: when torch's current stream is another one, that work waits for it and it waits for the work.
 """
 from __future__ import annotations
 
@@ -82,12 +83,14 @@ def _refuse(text):
     raise SheError(EINVAL, text)
 
 
-def _half(t, name):
-    if t.dtype is torch.bfloat16:
-        return 0
-    if t.dtype is torch.float16:
-        return 1
-    _refuse(f"{name} must be bfloat16 or float16, not {t.dtype}")
+def _first(t, name, device):
+    """Of the tensor that decides a call's type: that type, torch's name of it, its shape, address and strides."""
+    dtype, shape, strides = t.dtype, t.shape, t.stride()
+    if dtype is not torch.bfloat16 and dtype is not torch.float16:
+        _refuse(f"{name} must be bfloat16 or float16, not {dtype}")
+    if t.get_device() != device or (strides[-1] != 1 and shape[-1] > 1):
+        _refuse_tensor(t, name, dtype, shape, device)
+    return int(dtype is torch.float16), dtype, shape, t.data_ptr(), strides
 
 
 def _see(t, name, dtype, shape, device):
@@ -117,16 +120,36 @@ def _line(t, name, dtype, size, device):
     return t.data_ptr()
 
 
+_unrecorded = None
+
+
+def _barred(result, instead, *inputs):
+    """`result`, through which backward raises: a gradient of the inputs would get lost there."""
+    global _unrecorded
+    if _unrecorded is None:
+        class Unrecorded(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, result, instead, *inputs):
+                ctx.instead = instead
+                return result.detach()
+
+            @staticmethod
+            def backward(ctx, *_):
+                _refuse(f"this call's gradient is not recorded: {ctx.instead}")
+        _unrecorded = Unrecorded
+    return _unrecorded.apply(result, instead, *inputs)
+
+
 class Calls:
     """Mixed into Context."""
 
     def _call(self, fn, args):
         """Runs a call on the context's GPU and stream, ordered with torch's current stream there where that is another one."""
-        if torch._C._cuda_getDevice() != self._device:
-            with torch.cuda.device(self._device):
-                return self._call(fn, args)
         if torch._C._cuda_getCurrentRawStream(self._device) == self._stream:
             rc = fn(self._h, args)
+            if rc and torch._C._cuda_getDevice() != self._device:  # refused for that reason, if not for another
+                with torch.cuda.device(self._device):
+                    rc = fn(self._h, args)
             if rc:
                 self._check(rc)
             return
@@ -136,7 +159,8 @@ class Calls:
         mine = torch.cuda.ExternalStream(self._stream, self._device) if self._stream else torch.cuda.default_stream(self._device)
         mine.wait_stream(current)
         try:
-            self._check(fn(self._h, args))
+            with torch.cuda.device(self._device):
+                self._check(fn(self._h, args))
         finally:
             current.wait_stream(mine)
 
@@ -146,16 +170,17 @@ class Calls:
         x [tokens, inputs]; down [adapters, rank, inputs], up [adapters, rank, outputs]; starts [segments + 1], which [segments],
         ranks [adapters] or None: int32; scale [adapters] float32; base [tokens, outputs] of x's type, float32, or int32 sums times
         step [outputs] float32, or None.  Returns out [tokens, outputs]; base itself may be given for it."""
-        ty, dtype, dev = _half(x, "x"), x.dtype, self._device
-        (T, K), (A, r, N) = x.shape, up.shape
+        dev = self._device
+        ty, dtype, (T, K), x_at, xs = _first(x, "x", dev)
+        A, r, N = up.shape
         S = which.shape[0]
-        x_at, xs = _see(x, "x", dtype, (T, K), dev)
         down_at, ds = _see(down, "down", dtype, (A, r, K), dev)
         up_at, us = _see(up, "up", dtype, (A, r, N), dev)
         kind, base_at, base_stride = self._base(base, dtype, ty, (T, N), dev)
         if step is not None and kind != _I32:
             _refuse("step belongs to int32 sums")
-        if out is None:
+        given = out is not None
+        if not given:
             out = torch.empty(T, N, dtype=dtype, device=x.device)
             out_at, out_stride = out.data_ptr(), N
         else:
@@ -164,50 +189,66 @@ class Calls:
             ty, kind, T, K, N, A, r, S, x_at, xs[0], down_at, ds[0], ds[1], up_at, us[0], us[1], _line(starts, "starts", torch.int32, S + 1, dev),
             _line(which, "which", torch.int32, S, dev), _line(ranks, "ranks", torch.int32, A, dev), _line(scale, "scale", torch.float32, A, dev),
             base_at, base_stride, _line(step, "step", torch.float32, N, dev), out_at, out_stride))
+        if given:
+            torch.autograd.graph.increment_version(out)
+        if torch.is_grad_enabled() and (x.requires_grad or down.requires_grad or up.requires_grad or scale.requires_grad or
+                                        base is not None and base.requires_grad or step is not None and step.requires_grad):
+            return _barred(out, "use adapters_grad", x, down, up, scale, base, step)
         return out
 
     @staticmethod
     def _base(base, dtype, ty, shape, dev):
         if base is None:
             return _NO_BASE, 0, 0
-        kind = {dtype: ty, torch.float32: _F32, torch.int32: _I32}.get(base.dtype)
+        its = base.dtype
+        kind = ty if its is dtype else _F32 if its is torch.float32 else _I32 if its is torch.int32 else None
         if kind is None:
-            _refuse(f"base must be {dtype}, float32 or int32, not {base.dtype}")
-        at, strides = _see(base, "base", base.dtype, shape, dev)
+            _refuse(f"base must be {dtype}, float32 or int32, not {its}")
+        at, strides = _see(base, "base", its, shape, dev)
         return kind, at, strides[0]
 
     def adapters_grad(self, dy, x, down, up, starts, which, scale, ranks=None, base=None):
         """Gradients of `adapters` for dy [tokens, outputs]: (dx, ddown, dup), dx with `base` (the gradient that reaches x through the
         projection itself, of x's type or float32) added to it."""
-        ty, dtype, dev = _half(x, "x"), x.dtype, self._device
-        (T, K), (A, r, N) = x.shape, up.shape
+        dev = self._device
+        ty, dtype, (T, K), x_at, xs = _first(x, "x", dev)
+        A, r, N = up.shape
         S = which.shape[0]
         dy_at, dys = _see(dy, "dy", dtype, (T, N), dev)
-        x_at, xs = _see(x, "x", dtype, (T, K), dev)
         down_at, ds = _see(down, "down", dtype, (A, r, K), dev)
         up_at, us = _see(up, "up", dtype, (A, r, N), dev)
         kind, base_at, base_stride = self._base(base, dtype, ty, (T, K), dev)
         lines = (_line(starts, "starts", torch.int32, S + 1, dev), _line(which, "which", torch.int32, S, dev),
                  _line(ranks, "ranks", torch.int32, A, dev), _line(scale, "scale", torch.float32, A, dev))
-        dx, ddown, dup = (torch.empty(shape, dtype=dtype, device=x.device) for shape in ((T, K), (A, r, K), (A, r, N)))
+        at = x.device
+        dx, ddown = torch.empty(T, K, dtype=dtype, device=at), torch.empty(A, r, K, dtype=dtype, device=at)
+        dup = torch.empty(A, r, N, dtype=dtype, device=at)
         self._call(self._L.she_adapters_grad, _ADAPTERS_GRAD.pack(
             ty, kind, T, K, N, A, r, S, dy_at, dys[0], x_at, xs[0], down_at, ds[0], ds[1], up_at, us[0], us[1], *lines,
             base_at, base_stride, dx.data_ptr(), K, ddown.data_ptr(), dup.data_ptr()))
+        if torch.is_grad_enabled() and (dy.requires_grad or x.requires_grad or down.requires_grad or up.requires_grad or
+                                        scale.requires_grad or base is not None and base.requires_grad):
+            return tuple(_barred(t, "there is no second one", dy, x, down, up, scale, base) for t in (dx, ddown, dup))
         return dx, ddown, dup
 
     @staticmethod
     def _rotation(q, k, wq, wk, cos, sin, positions, dev):
         """What the three calls on queries and keys have in common, checked: type, sizes, addresses and strides."""
-        ty, dtype = _half(q, "q"), q.dtype
-        (T, Hq, D), Hkv = q.shape, k.shape[1]
+        ty, dtype, (T, Hq, D), q_at, qs = _first(q, "q", dev)
+        Hkv = k.shape[1]
         P, half = cos.shape
-        q_at, qs = _see(q, "q", dtype, (T, Hq, D), dev)
         k_at, ks = _see(k, "k", dtype, (T, Hkv, D), dev)
-        tables = (_line(wq, "wq", torch.float32, D, dev), _line(wk, "wk", torch.float32, D, dev), _see(cos, "cos", torch.float32, (P, half), dev)[0],
-                  _see(sin, "sin", torch.float32, (P, half), dev)[0], _line(positions, "positions", torch.int32, T, dev))
-        if not (cos.is_contiguous() and sin.is_contiguous()):
+        f32, table = torch.float32, (P, half)
+        (c_at, cs), (s_at, ss) = _see(cos, "cos", f32, table, dev), _see(sin, "sin", f32, table, dev)
+        if not (cs[0] == ss[0] == half or cos.is_contiguous() and sin.is_contiguous()):
             _refuse("cos and sin must be contiguous")
+        tables = _line(wq, "wq", f32, D, dev), _line(wk, "wk", f32, D, dev), c_at, s_at, _line(positions, "positions", torch.int32, T, dev)
         return ty, dtype, (T, Hq, Hkv, D, 2 * half, P), (q_at, k_at), (qs[0], qs[1], ks[0], ks[1]), tables
+
+    @staticmethod
+    def _rotation_wanted(q, k, wq, wk, cos, sin):
+        return (q.requires_grad or k.requires_grad or wq is not None and wq.requires_grad or wk is not None and wk.requires_grad or
+                cos.requires_grad or sin.requires_grad)
 
     def qk_rotate(self, q, k, wq, wk, cos, sin, positions, eps=1e-6, interleaved=False, out=None):
         """Norm of every head of q [tokens, q_heads, head] and k [tokens, kv_heads, head] with the weights wq, wk [head] float32 (or
@@ -215,13 +256,18 @@ class Calls:
         for them, which may be (q, k)."""
         dev = self._device
         ty, dtype, (T, Hq, Hkv, D, rot, P), at, strides, tables = self._rotation(q, k, wq, wk, cos, sin, positions, dev)
-        if out is None:
+        given = out is not None
+        if not given:
             out = torch.empty(T, Hq, D, dtype=dtype, device=q.device), torch.empty(T, Hkv, D, dtype=dtype, device=q.device)
         q_out, qs = _see(out[0], "out", dtype, (T, Hq, D), dev)
         k_out, ks = _see(out[1], "out", dtype, (T, Hkv, D), dev)
         self._call(self._L.she_qk_rotate, _QK_ROTATE.pack(
             ty, bool(interleaved), T, Hq, Hkv, D, rot, P, eps, *at, 0, *strides, 0, 0, *tables, q_out, k_out, qs[0], qs[1], ks[0], ks[1],
             0, 0, 0, 0, 0, 0, 0, 0))
+        if given:
+            torch.autograd.graph.increment_version((out[0], out[1]))
+        if torch.is_grad_enabled() and self._rotation_wanted(q, k, wq, wk, cos, sin):
+            return tuple(_barred(t, "use qk_rotate_grad", q, k, wq, wk, cos, sin) for t in (out[0], out[1]))
         return out[0], out[1]
 
     def qk_rotate_append(self, q, k, v, wq, wk, cos, sin, positions, k_pages, v_pages, slots, eps=1e-6, interleaved=False, out=None):
@@ -231,12 +277,16 @@ class Calls:
         ty, dtype, (T, Hq, Hkv, D, rot, P), at, strides, tables = self._rotation(q, k, wq, wk, cos, sin, positions, dev)
         v_at, vs = _see(v, "v", dtype, (T, Hkv, D), dev)
         pages_at, pages, size = self._pages(k_pages, v_pages, dtype, Hkv, D, dev)
+        written = (k_pages, v_pages) if out is None else (k_pages, v_pages, out)
         if out is None:
             out = torch.empty(T, Hq, D, dtype=dtype, device=q.device)
         q_out, qs = _see(out, "out", dtype, (T, Hq, D), dev)
         self._call(self._L.she_qk_rotate, _QK_ROTATE.pack(
             ty, bool(interleaved), T, Hq, Hkv, D, rot, P, eps, *at, v_at, *strides, vs[0], vs[1], *tables, q_out, 0, qs[0], qs[1], 0, 0,
             *pages_at, pages, size, _line(slots, "slots", torch.int64, T, dev)))
+        torch.autograd.graph.increment_version(written)
+        if torch.is_grad_enabled() and (v.requires_grad or self._rotation_wanted(q, k, wq, wk, cos, sin)):
+            return _barred(out, "a cache is for inference", q, k, v, wq, wk, cos, sin)
         return out
 
     @staticmethod
@@ -261,22 +311,24 @@ class Calls:
         self._call(self._L.she_qk_rotate_grad, _QK_ROTATE_GRAD.pack(
             ty, bool(interleaved), T, Hq, Hkv, D, rot, P, eps, dq_at, dk_at, dqs[0], dqs[1], dks[0], dks[1], *at, *strides, *tables,
             dq.data_ptr(), dk.data_ptr(), Hq * D, D, Hkv * D, D, dw_at, dw_at + 4 * D))
+        if torch.is_grad_enabled() and (dq_out.requires_grad or dk_out.requires_grad or self._rotation_wanted(q, k, wq, wk, cos, sin)):
+            return tuple(_barred(t, "there is no second one", dq_out, dk_out, q, k, wq, wk, cos, sin) for t in (dq, dk, dw[0], dw[1]))
         return dq, dk, dw[0], dw[1]
 
     def attend_pages(self, q, k_pages, v_pages, table, starts, lengths, scale=None, window=0, out=None):
         """Attention of the new tokens q [tokens, q_heads, head] of every request, starts [requests + 1] int32, over its lengths
         [requests] int32 places in k_pages, v_pages [pages, page_size, kv_heads, head], found through table [requests, width] int32;
         causal, and over the last `window` places alone if that is not 0.  scale: head ** -0.5 if None.  Returns out like q."""
-        ty, dtype, dev = _half(q, "q"), q.dtype, self._device
-        T, Hq, D = q.shape
+        dev = self._device
+        ty, dtype, (T, Hq, D), q_at, qs = _first(q, "q", dev)
         Hkv = k_pages.shape[2]
         R, width = table.shape
-        q_at, qs = _see(q, "q", dtype, (T, Hq, D), dev)
         pages_at, pages, size = self._pages(k_pages, v_pages, dtype, Hkv, D, dev)
         table_at, ts = _see(table, "table", torch.int32, (R, width), dev)
         if not 0 <= window < 1 << 32:
             _refuse("window must be a number of places")
-        if out is None:
+        given = out is not None
+        if not given:
             out = torch.empty(T, Hq, D, dtype=dtype, device=q.device)
             out_at, out_token, out_head = out.data_ptr(), Hq * D, D
         else:
@@ -284,6 +336,10 @@ class Calls:
         self._call(self._L.she_attend_pages, _ATTEND_PAGES.pack(
             ty, T, R, Hq, Hkv, D, window, D ** -0.5 if scale is None else scale, q_at, qs[0], qs[1], *pages_at, pages, size, table_at, ts[0],
             width, _line(starts, "starts", torch.int32, R + 1, dev), _line(lengths, "lengths", torch.int32, R, dev), out_at, out_token, out_head))
+        if given:
+            torch.autograd.graph.increment_version(out)
+        if torch.is_grad_enabled() and (q.requires_grad or k_pages.requires_grad or v_pages.requires_grad):
+            return _barred(out, "a cache is for inference", q, k_pages, v_pages)
         return out
 
     def clear_bad_ids(self, reset: bool = True) -> int:
