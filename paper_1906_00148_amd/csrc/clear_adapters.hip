@@ -454,6 +454,10 @@ __device__ inline Share share_of(const Segments &s, int a)
     return Share{(uint32_t)__builtin_amdgcn_readfirstlane(before), (uint32_t)__builtin_amdgcn_readfirstlane(own)};
 }
 
+// Where the sums of an adapter that has several begin.  It has more than `share` tiles then, and ceil(own / share) sums are at most
+// floor(2 own / share): no place is another adapter's, and 2 tiles / share places do for all of them, however many adapters there are.
+__device__ inline uint32_t place_of(const Segments &s, const Share &mine) { return (uint32_t)(2ull * mine.before / s.share); }
+
 struct Outer {
     Rows x;
     uint32_t width;
@@ -463,8 +467,7 @@ struct Outer {
 };
 
 // One adapter, SPAN columns, up to CHUNK ranks, and `share` of its tiles: the wavefronts take every eighth and are summed in LDS.
-// An adapter of more tiles has several such sums, in places of their own (as many before them as lower adapters can need), which
-// k_adapter_sum adds in order.
+// An adapter of more tiles has several such sums, in places of their own, which k_adapter_sum adds in order.
 template <class T, bool WIDE, int RT>
 __global__ __launch_bounds__(64 * OUTER_WAVES) void k_adapter_outer(Outer job0, Outer job1, Segments s, uint32_t spans0)
 {
@@ -536,7 +539,7 @@ __global__ __launch_bounds__(64 * OUTER_WAVES) void k_adapter_outer(Outer job0, 
         }
     }
 
-    const size_t place = mine.before / s.share + a + z;
+    const size_t place = place_of(s, mine) + z;
     if (parts > 1 && place >= s.places) return;        // only where starts is not ascending
     const uint32_t rank = rank_of(s, a);
 #pragma unroll
@@ -575,8 +578,8 @@ template <class T> __global__ __launch_bounds__(256) void k_adapter_sum(Outer jo
     const int a = blockIdx.y;
     const Share mine = share_of(s, a);
     const uint32_t parts = min((mine.own + s.share - 1) / s.share, s.most);
-    if (parts <= 1 || mine.before / s.share + a + parts > s.places) return;
-    const size_t each = (size_t)s.rank * job.width, first = (size_t)(mine.before / s.share + a) * each;
+    if (parts <= 1 || place_of(s, mine) + parts > s.places) return;
+    const size_t each = (size_t)s.rank * job.width, first = (size_t)place_of(s, mine) * each;
     for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < each; i += (size_t)gridDim.x * 256) {
         float v = 0;
         for (uint32_t z = 0; z < parts; z++) v += job.partial[first + z * each + i];
@@ -619,7 +622,7 @@ template <class Args> Segments segments_of(const Args &a)
     const uint32_t tiles = slots_of(a.tokens, a.segments);
     s.share = std::max<uint32_t>(8 * OUTER_WAVES, (uint32_t)ceil_div(tiles, 16));
     s.most = (uint32_t)std::max<uint64_t>(1, ceil_div(tiles, s.share));
-    s.places = s.most > 1 ? tiles / s.share + a.adapters : 0;
+    s.places = s.most > 1 ? 2 * tiles / s.share : 0;
     return s;
 }
 
