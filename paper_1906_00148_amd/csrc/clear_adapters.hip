@@ -10,8 +10,10 @@
 // registers, one byte permutation a word of two elements, which makes the operands of eight matrix instructions.
 //
 // h is held in 32 bits while it is summed and handed on as two numbers of the type, the rounded value and what the rounding left
-// (17 bits of it in bf16, 22 in f16), each with a product of its own: as good as 32 bits beside results of 8 or 11.  In f16 a tile's h
-// is scaled by a power of two first, so that the range of the type does not matter.
+// (17 bits of it in bf16, 22 in f16), each with a product of its own: as good as 32 bits beside results of 8 or 11.  In f16 h is
+// scaled by a power of two first, one for each token (and 64 ranks) where tokens are the rows of the result, one for each rank (and the
+// 32 tokens of a tile) where ranks are.  So a number of h that is more than 2^16 below the largest of its token, or of its rank in
+// the tile, is held to 2^-38 of that largest one; no token's result depends on the tokens beside it.
 //
 // Bound by memory: x, base and the adapters are read, and the result written, once; a tile's h is a few KB.  Backward, x and dy are
 // read twice, the second time from the memory-side cache if they fit it.
@@ -38,7 +40,7 @@ constexpr int OUTER_WAVES = 8;
 struct Hidden {
     uint16_t *by_token[2];               // [slots][TILE / 16][rows / 8][16 tokens][8 ranks]
     uint16_t *by_rank[2];                // [slots][rows / 16][TILE / 8][16 ranks][8 tokens]
-    float *unscale;                      // [slots][chunks]: f16, what a tile's values are to be multiplied by
+    float *token_by, *rank_by;           // f16, what they are to be multiplied by: [slots][chunks][TILE], [slots][rows]
 };
 __device__ inline size_t by_token_at(size_t slot, int t, int j, uint32_t rows)
 {
@@ -102,13 +104,23 @@ __device__ inline Tile tile_of(const Segments &s, const Piece &p, uint32_t *d_ba
     return t;
 }
 
+// The power of two that brings `top` to f16's upper range, 2^13 .. 2^14, and its inverse; not beyond what brings 2^-100 there.
+struct Power {
+    float by, back;
+};
+__device__ inline Power power_for(float top)
+{
+    const uint32_t e = top > 0 ? max(__float_as_uint(top) >> 23, 27u) : 127u;        // biased: 2^(e - 127) <= top
+    return Power{__uint_as_float((127 + 127 + 13 - e) << 23), __uint_as_float((e - 13) << 23)};
+}
+
 // One tile, up to CHUNK ranks (RT tiles of 16) of it from r0 on: the wavefronts share the width out and are
-// summed in LDS.  keep(j, t, value, rest) gets every number; returns what they are to be multiplied by.
-template <class T, bool WIDE, int RT, int WAVES, class Keep>
-__device__ inline float hidden_values(const Rows &rows, const Matrix &matrix, const Segments &s, const Tile &tile, uint32_t r0, Keep keep)
+// summed in LDS.  keep(j, t, v, token, rank) gets every number, and in f16 its token's power of two and, with RANKS, its rank's.
+template <class T, bool WIDE, int RT, int WAVES, bool RANKS, class Keep>
+__device__ inline void hidden_values(const Rows &rows, const Matrix &matrix, const Segments &s, const Tile &tile, uint32_t r0, Keep keep)
 {
     __shared__ float part[WAVES][RT * 16][TILE];
-    __shared__ float tops[WAVES];
+    __shared__ float tops[WAVES][TILE];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, quarter = lane >> 4;
     const uint32_t K = matrix.width;
     const T *x[2], *w[RT];
@@ -162,7 +174,7 @@ __device__ inline float hidden_values(const Rows &rows, const Matrix &matrix, co
 
     constexpr int VALUES = RT * 16 * TILE, EACH = (VALUES + 64 * WAVES - 1) / (64 * WAVES);
     const float scale = s.scale[tile.adapter];
-    float v[EACH], top = 0, by = 1, unscale = 1;
+    float v[EACH], top = 0;
 #pragma unroll
     for (int e = 0; e < EACH; e++) {
         const int n = e * 64 * WAVES + tid;
@@ -175,27 +187,28 @@ __device__ inline float hidden_values(const Rows &rows, const Matrix &matrix, co
         v[e] = n % TILE < tile.live && r0 + n / TILE < tile.rank ? v[e] * scale : 0.0f;
         if (fabsf(v[e]) < __builtin_inff()) top = fmaxf(top, fabsf(v[e]));
     }
-    if constexpr (std::is_same<T, _Float16>::value) {
-#pragma unroll
-        for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
-        if (lane == 0) tops[wave] = top;
+    Power token{1, 1};
+    if constexpr (std::is_same<T, _Float16>::value) {        // all of a thread's numbers are of token tid % TILE
+        top = fmaxf(top, __shfl_xor(top, TILE));
+        if (lane < TILE) tops[wave][lane] = top;
         __syncthreads();
         top = 0;
 #pragma unroll
-        for (int k = 0; k < WAVES; k++) top = fmaxf(top, tops[k]);
-        const int e = top > 0 ? min(max(ilogbf(top), -100), 120) : 0;          // the largest becomes 2^13 .. 2^14
-        by = ldexpf(1.0f, 13 - e);
-        unscale = ldexpf(1.0f, e - 13);
+        for (int k = 0; k < WAVES; k++) top = fmaxf(top, tops[k][tid % TILE]);
+        token = power_for(top);
     }
 #pragma unroll
     for (int e = 0; e < EACH; e++) {
         const int n = e * 64 * WAVES + tid, j = r0 + n / TILE;
-        if (n >= VALUES || (uint32_t)j >= s.rows) continue;
-        uint16_t value, rest;
-        split<T>(v[e] * by, value, rest);
-        keep(j, n % TILE, value, rest);
+        Power rank{1, 1};
+        if constexpr (RANKS && std::is_same<T, _Float16>::value) {
+            float most = fabsf(v[e]) < __builtin_inff() ? fabsf(v[e]) : 0.0f;
+#pragma unroll
+            for (int m = 1; m < TILE; m *= 2) most = fmaxf(most, __shfl_xor(most, m));
+            rank = power_for(most);
+        }
+        if (n < VALUES && (uint32_t)j < s.rows) keep(j, n % TILE, v[e], token, rank);
     }
-    return unscale;
 }
 
 struct Down {
@@ -204,7 +217,8 @@ struct Down {
     Hidden h;
 };
 
-template <class T, bool WIDE, int RT, int WAVES>
+// RANKS: by_rank is wanted of every job, and by_token of those that have room for it; else by_token alone.
+template <class T, bool WIDE, int RT, int WAVES, bool RANKS>
 __global__ __launch_bounds__(64 * WAVES) void k_adapter_down(Down job0, Down job1, Segments s, uint32_t *d_bad)
 {
     const Down &job = blockIdx.z ? job1 : job0;
@@ -213,19 +227,24 @@ __global__ __launch_bounds__(64 * WAVES) void k_adapter_down(Down job0, Down job
     if (piece.segment < 0) return;
     const Tile tile = tile_of(s, piece, threadIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && piece.index == 0 ? d_bad : nullptr);
     if (tile.adapter < 0) return;
-    const float unscale = hidden_values<T, WIDE, RT, WAVES>(job.x, job.w, s, tile, r0, [&](int j, int t, uint16_t value, uint16_t rest) {
+    hidden_values<T, WIDE, RT, WAVES, RANKS>(job.x, job.w, s, tile, r0, [&](int j, int t, float v, Power token, Power rank) {
+        constexpr bool F16 = std::is_same<T, _Float16>::value;
+        uint16_t value, rest;
         if (job.h.by_token[0]) {
             const size_t at = by_token_at(slot, t, j, s.rows);
+            split<T>(v * token.by, value, rest);
             job.h.by_token[0][at] = value;
             job.h.by_token[1][at] = rest;
+            if (F16 && j == (int)r0) job.h.token_by[((size_t)slot * s.chunks + blockIdx.y) * TILE + t] = token.back;
         }
-        if (job.h.by_rank[0]) {
+        if constexpr (RANKS) {
             const size_t at = by_rank_at(slot, j, t, s.rows);
+            split<T>(v * rank.by, value, rest);
             job.h.by_rank[0][at] = value;
             job.h.by_rank[1][at] = rest;
+            if (F16 && t == 0) job.h.rank_by[(size_t)slot * s.rows + j] = rank.back;
         }
     });
-    if (threadIdx.x == 0 && std::is_same<T, _Float16>::value) job.h.unscale[(size_t)slot * s.chunks + blockIdx.y] = unscale;
 }
 
 struct Up {
@@ -296,7 +315,8 @@ template <class T> __device__ inline void base_numbers(const Up &u, const BaseWo
     }
 }
 
-// Sixteen tokens from `first` on, `live` of them: their bases; and `by` times acc[m] added to the lane's output m, and written.
+// Sixteen tokens from `first` on, `live` of them: their bases; and by(i) times acc[m][i] added to the lane's output m of its token i,
+// and written.
 template <class T, bool WIDE> __device__ inline void load_bases(const Up &u, int64_t first, int live, uint32_t n_first, BaseWords base[4])
 {
     const uint32_t n = lane_output(n_first);
@@ -307,7 +327,7 @@ template <class T, bool WIDE> __device__ inline void load_bases(const Up &u, int
         base[i] = load_base<T, WIDE>(u, first + (there ? lane_token(i) : 0), there ? n : 0, there ? count : 0);
     }
 }
-template <class T, bool WIDE> __device__ inline void write_outputs(const Up &u, int64_t first, int live, uint32_t n_first, const BaseWords base[4], const f32x4 acc[8], float by)
+template <class T, bool WIDE, class By> __device__ inline void write_outputs(const Up &u, int64_t first, int live, uint32_t n_first, const BaseWords base[4], const f32x4 acc[8], By by)
 {
     const uint32_t n = lane_output(n_first);
     const int count = (int)u.w.width - (int)n;
@@ -319,15 +339,16 @@ template <class T, bool WIDE> __device__ inline void write_outputs(const Up &u, 
     for (int i = 0; i < 4; i++) {
         if (lane_token(i) >= live) break;
         float v[8];
+        const float times = by(i);
         base_numbers<T>(u, base[i], step, v);
 #pragma unroll
-        for (int m = 0; m < 8; m++) v[m] = fmaf(acc[m][i], by, v[m]);
+        for (int m = 0; m < 8; m++) v[m] = fmaf(acc[m][i], times, v[m]);
         store_quads<T, WIDE>((T *)u.out + (first + lane_token(i)) * u.out_stride + n, pack<T>(v), count, count - 64);
     }
 }
 
-// A wavefront: SPAN outputs of one tile, 32 ranks a step.  CHUNKS: several chunks of ranks whose tiles' powers of two (f16) differ,
-// summed apart.
+// A wavefront: SPAN outputs of one tile, 32 ranks a step.  CHUNKS: several chunks of ranks whose powers of two (f16) differ, summed
+// apart.
 template <class T, bool WIDE, bool CHUNKS>
 __global__ __launch_bounds__(64 * UP_WAVES, WIDE && !CHUNKS ? 3 : 1) void k_adapter_up(Up u, Segments s)
 {
@@ -337,6 +358,10 @@ __global__ __launch_bounds__(64 * UP_WAVES, WIDE && !CHUNKS ? 3 : 1) void k_adap
     const Piece piece = find_piece(s.starts, s.segments, s.tokens, 1, TILE, slot);
     if (piece.segment < 0) return;
     const Tile tile = tile_of(s, piece, nullptr);
+    // what the sums of the lane's tokens are to be multiplied by
+    const auto back_of = [&](int c, uint32_t chunk) {
+        return *reinterpret_cast<const f32x4 *>(u.h.token_by + ((size_t)slot * s.chunks + chunk) * TILE + c * 16 + lane_token(0));
+    };
     f32x4 acc[2][8], total[CHUNKS ? 2 : 1][8];
 #pragma unroll
     for (int c = 0; c < 2; c++) {
@@ -364,23 +389,24 @@ __global__ __launch_bounds__(64 * UP_WAVES, WIDE && !CHUNKS ? 3 : 1) void k_adap
                 acc[c][m] = mfma16(h[c][1], cols[m], acc[c][m]);
             }
         if constexpr (CHUNKS) {
-            const float unscale = u.h.unscale[(size_t)slot * s.chunks + j0 / CHUNK];
 #pragma unroll
-            for (int m = 0; m < 8; m++)
+            for (int c = 0; c < 2; c++) {
+                const f32x4 back = back_of(c, j0 / CHUNK);
 #pragma unroll
-                for (int c = 0; c < 2; c++) {
-                    total[c][m] += acc[c][m] * unscale;
+                for (int m = 0; m < 8; m++) {
+                    total[c][m] += acc[c][m] * back;
                     acc[c][m] = f32x4{0, 0, 0, 0};
                 }
+            }
         }
     }
     BaseWords base[2][4];
 #pragma unroll
     for (int c = 0; c < 2; c++) load_bases<T, WIDE>(u, tile.first + c * 16, tile.live - c * 16, n_first, base[c]);
-    const float unscale = std::is_same<T, _Float16>::value && !CHUNKS && tile.rank ? u.h.unscale[(size_t)slot * s.chunks] : 1.0f;
 #pragma unroll
     for (int c = 0; c < 2; c++) {
-        write_outputs<T, WIDE>(u, tile.first + c * 16, tile.live - c * 16, n_first, base[c], CHUNKS ? total[CHUNKS ? c : 0] : acc[c], unscale);
+        const f32x4 back = std::is_same<T, _Float16>::value && !CHUNKS && tile.rank ? back_of(c, 0) : f32x4{1, 1, 1, 1};
+        write_outputs<T, WIDE>(u, tile.first + c * 16, tile.live - c * 16, n_first, base[c], CHUNKS ? total[CHUNKS ? c : 0] : acc[c], [&](int i) { return back[i]; });
     }
 }
 
@@ -391,16 +417,16 @@ template <class T, bool WIDE, int RT>
 __global__ __launch_bounds__(64 * STEP_WAVES) void k_adapter_step(Rows x, Matrix w_down, Up u, Segments s, uint32_t *d_bad)
 {
     __shared__ __align__(16) uint16_t h[2][TILE][RT * 16];
+    __shared__ __align__(16) float back[TILE];
     const int wave = threadIdx.x >> 6, col = threadIdx.x & 15, quarter = threadIdx.x >> 4 & 3;
     const Piece piece = find_piece(s.starts, s.segments, s.tokens, 1, TILE, blockIdx.x);
     if (piece.segment < 0) return;
     const Tile tile = tile_of(s, piece, threadIdx.x == 0 && blockIdx.y == 0 && piece.index == 0 ? d_bad : nullptr);
     const uint32_t n_first = (blockIdx.y * STEP_WAVES + wave) * SPAN;
-    float unscale = 1;
     if (tile.adapter >= 0) {
-        unscale = hidden_values<T, WIDE, RT, STEP_WAVES>(x, w_down, s, tile, 0, [&](int j, int t, uint16_t value, uint16_t rest) {
-            h[0][t][j] = value;
-            h[1][t][j] = rest;
+        hidden_values<T, WIDE, RT, STEP_WAVES, false>(x, w_down, s, tile, 0, [&](int j, int t, float v, Power token, Power) {
+            split<T>(v * token.by, h[0][t][j], h[1][t][j]);
+            if (std::is_same<T, _Float16>::value && j == 0) back[t] = token.back;
         });
         __syncthreads();
     }
@@ -426,7 +452,10 @@ __global__ __launch_bounds__(64 * STEP_WAVES) void k_adapter_step(Rows x, Matrix
                 acc[m] = mfma16(hv[1], cols[m], acc[m]);
             }
         }
-        write_outputs<T, WIDE>(u, tile.first + c * 16, tile.live - c * 16, n_first, base, acc, std::is_same<T, _Float16>::value ? unscale : 1.0f);
+        write_outputs<T, WIDE>(u, tile.first + c * 16, tile.live - c * 16, n_first, base, acc, [&](int i) {
+            // read when it is needed: there is no register to keep it in
+            return std::is_same<T, _Float16>::value && some ? *(volatile const float *)&back[c * 16 + lane_token(i)] : 1.0f;
+        });
     }
 }
 
@@ -519,7 +548,14 @@ __global__ __launch_bounds__(64 * OUTER_WAVES) void k_adapter_outer(Outer job0, 
                                                       : u32x4{0, 0, 0, 0});
                     }
                 transpose8<T, 8>(raw, cols);
-                const float unscale = std::is_same<T, _Float16>::value ? job.h.unscale[slot * s.chunks + chunk] : 1.0f;
+                f32x4 back[RT];                           // of the lane's ranks in the results
+                if constexpr (std::is_same<T, _Float16>::value) {
+#pragma unroll
+                    for (int r = 0; r < RT; r++) {
+                        const uint32_t j = r0 + r * 16 + quarter * 4;
+                        back[r] = j < s.rows ? *reinterpret_cast<const f32x4 *>(job.h.rank_by + slot * s.rows + j) : f32x4{0, 0, 0, 0};
+                    }
+                }
 #pragma unroll
                 for (int m = 0; m < 8; m++)
 #pragma unroll
@@ -528,7 +564,7 @@ __global__ __launch_bounds__(64 * OUTER_WAVES) void k_adapter_outer(Outer job0, 
                             f32x4 v = mfma16(h[r][0], cols[m], f32x4{0, 0, 0, 0});
                             v = mfma16(h[r][1], cols[m], v);
 #pragma unroll
-                            for (int k = 0; k < 4; k++) acc[m][r][k] = fmaf(v[k], unscale, acc[m][r][k]);
+                            for (int k = 0; k < 4; k++) acc[m][r][k] = fmaf(v[k], back[r][k], acc[m][r][k]);
                         } else {
                             acc[m][r] = mfma16(h[r][0], cols[m], acc[m][r]);
                             acc[m][r] = mfma16(h[r][1], cols[m], acc[m][r]);
@@ -609,7 +645,8 @@ Hidden take_hidden(Room &room, uint32_t slots, uint32_t rows, uint32_t chunks, b
         if (by_token) h.by_token[p] = room.take<uint16_t>(n);
         if (by_rank) h.by_rank[p] = room.take<uint16_t>(n);
     }
-    h.unscale = room.take<float>((size_t)slots * chunks);
+    if (by_token) h.token_by = room.take<float>((size_t)slots * chunks * TILE);
+    if (by_rank) h.rank_by = room.take<float>((size_t)slots * rows);
     return h;
 }
 // Backward, a workgroup sums eight tiles a wavefront (four: 80 us of gradients over 8192 tokens and not 74), and more where an adapter
@@ -626,12 +663,12 @@ template <class Args> Segments segments_of(const Args &a)
     return s;
 }
 
-template <class T, bool WIDE> hipError_t down(const Down &d0, const Down &d1, int jobs, const Segments &s, uint32_t *d_bad, hipStream_t st)
+template <class T, bool WIDE, bool RANKS> hipError_t down(const Down &d0, const Down &d1, int jobs, const Segments &s, uint32_t *d_bad, hipStream_t st)
 {
     const dim3 grid(slots_of(s.tokens, s.segments), s.chunks, jobs);
-    if (s.rank <= 16) k_adapter_down<T, WIDE, 1, 16><<<grid, 1024, 0, st>>>(d0, d1, s, d_bad);
-    else if (s.rank <= 32) k_adapter_down<T, WIDE, 2, 16><<<grid, 1024, 0, st>>>(d0, d1, s, d_bad);
-    else k_adapter_down<T, WIDE, 4, 8><<<grid, 512, 0, st>>>(d0, d1, s, d_bad);
+    if (s.rank <= 16) k_adapter_down<T, WIDE, 1, 16, RANKS><<<grid, 1024, 0, st>>>(d0, d1, s, d_bad);
+    else if (s.rank <= 32) k_adapter_down<T, WIDE, 2, 16, RANKS><<<grid, 1024, 0, st>>>(d0, d1, s, d_bad);
+    else k_adapter_down<T, WIDE, 4, 8, RANKS><<<grid, 512, 0, st>>>(d0, d1, s, d_bad);
     return hipGetLastError();
 }
 template <class T, bool WIDE> hipError_t up(const Up &u, const Segments &s, hipStream_t st)
@@ -692,7 +729,7 @@ template <class T> hipError_t forward(const she_adapters_args &a, void *scratch,
         else k_adapter_step<T, true, 2><<<grid, 64 * STEP_WAVES, 0, st>>>(d.x, d.w, u, s, d_bad);
         return hipGetLastError();
     }
-    hipError_t rc = wide_down ? down<T, true>(d, d, 1, s, d_bad, st) : down<T, false>(d, d, 1, s, d_bad, st);
+    hipError_t rc = wide_down ? down<T, true, false>(d, d, 1, s, d_bad, st) : down<T, false, false>(d, d, 1, s, d_bad, st);
     if (rc == hipSuccess) rc = wide_up ? up<T, true>(u, s, st) : up<T, false>(u, s, st);
     return rc;
 }
@@ -711,7 +748,7 @@ template <class T> hipError_t backward(const she_adapters_grad_args &a, void *sc
     const Down d0{x, w_down, r.h}, d1{dy, w_up, r.g};
     const Up u{w_down, r.g, a.base, a.base_stride, nullptr, a.base_type, a.dx, a.dx_stride};
     hipError_t rc = !slots_of(a.tokens, a.segments) ? hipSuccess
-                  : wide ? down<T, true>(d0, d1, 2, s, d_bad, st) : down<T, false>(d0, d1, 2, s, d_bad, st);
+                  : wide ? down<T, true, true>(d0, d1, 2, s, d_bad, st) : down<T, false, true>(d0, d1, 2, s, d_bad, st);
     if (rc != hipSuccess) return rc;
     if (slots_of(a.tokens, a.segments))
         rc = wide_down && on16(a.base) && on16(a.dx) && (a.base_stride | a.dx_stride) % 8 == 0 ? up<T, true>(u, s, st) : up<T, false>(u, s, st);
