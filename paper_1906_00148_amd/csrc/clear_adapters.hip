@@ -89,6 +89,11 @@ template <class T> __device__ inline void split(float v, uint16_t &value, uint16
     rest = __builtin_bit_cast(uint16_t, (T)(fabsf(left) < __builtin_inff() ? left : 0.0f));
 }
 
+template <class T> __device__ inline float whole(uint16_t value, uint16_t rest)
+{
+    return (float)__builtin_bit_cast(T, value) + (float)__builtin_bit_cast(T, rest);
+}
+
 struct Tile {                            // the tokens [first, first + live) of a segment whose adapter is `adapter` (-1: none)
     int adapter, live;
     int64_t first;
@@ -247,6 +252,19 @@ __global__ __launch_bounds__(64 * WAVES) void k_adapter_down(Down job0, Down job
     });
 }
 
+// An infinity in an operand that h is multiplied with is to be multiplied with h as a whole: the products with value and rest may have
+// opposite signs, or the rest may be 0, and their sum NaN.  So sums that are not finite are done again, one by one (write_one_by_one,
+// sum_one).
+template <int N> __device__ inline bool all_finite(const f32x4 (&acc)[N])
+{
+    float v = 0;
+#pragma unroll
+    for (int n = 0; n < N; n++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) v = fmaf(acc[n][i], 0.0f, v);
+    return v == 0;
+}
+
 struct Up {
     Matrix w;
     Hidden h;
@@ -347,6 +365,24 @@ template <class T, bool WIDE, class By> __device__ inline void write_outputs(con
     }
 }
 
+// The same where sums are not finite: element by element, with hidden(t, j) for the hidden value of token t of the sixteen.
+template <class T, class Value> __device__ inline void write_one_by_one(const Up &u, const Tile &tile, int64_t first, int live, uint32_t n_first, Value hidden)
+{
+#pragma unroll 1
+    for (int e = 0; e < 32; e++) {
+        const int t = lane_token(e & 3);
+        const uint32_t n = lane_output(n_first) + e / 16 * 64 + e / 4 % 4;
+        if (t >= live || n >= u.w.width) continue;
+        const T *w = (const T *)u.w.p + (int64_t)tile.adapter * u.w.adapter + n;
+        float sum = 0;
+        for (uint32_t j = 0; j < tile.rank; j++) sum = fmaf(hidden(t, (int)j), (float)w[(int64_t)j * u.w.row], sum);
+        const int64_t at = (first + t) * u.base_stride + n;
+        const float base = u.base_type == SHE_NO_BASE ? 0.0f : u.base_type == SHE_F32 ? ((const float *)u.base)[at]
+                           : u.base_type == SHE_I32   ? (float)((const int32_t *)u.base)[at] * (u.step ? u.step[n] : 1.0f) : (float)((const T *)u.base)[at];
+        ((T *)u.out)[(first + t) * u.out_stride + n] = (T)(base + sum);
+    }
+}
+
 // A wavefront: SPAN outputs of one tile, 32 ranks a step.  CHUNKS: several chunks of ranks whose powers of two (f16) differ, summed
 // apart.
 template <class T, bool WIDE, bool CHUNKS>
@@ -405,6 +441,14 @@ __global__ __launch_bounds__(64 * UP_WAVES, WIDE && !CHUNKS ? 3 : 1) void k_adap
     for (int c = 0; c < 2; c++) load_bases<T, WIDE>(u, tile.first + c * 16, tile.live - c * 16, n_first, base[c]);
 #pragma unroll
     for (int c = 0; c < 2; c++) {
+        if (__ballot(!all_finite(CHUNKS ? total[CHUNKS ? c : 0] : acc[c]))) {
+            write_one_by_one<T>(u, tile, tile.first + c * 16, tile.live - c * 16, n_first, [&](int t, int j) {
+                const size_t at = by_token_at(slot, c * 16 + t, j, s.rows);
+                const float by = std::is_same<T, _Float16>::value ? u.h.token_by[((size_t)slot * s.chunks + j / CHUNK) * TILE + c * 16 + t] : 1.0f;
+                return whole<T>(u.h.by_token[0][at], u.h.by_token[1][at]) * by;
+            });
+            continue;
+        }
         const f32x4 back = std::is_same<T, _Float16>::value && !CHUNKS && tile.rank ? back_of(c, 0) : f32x4{1, 1, 1, 1};
         write_outputs<T, WIDE>(u, tile.first + c * 16, tile.live - c * 16, n_first, base[c], CHUNKS ? total[CHUNKS ? c : 0] : acc[c], [&](int i) { return back[i]; });
     }
@@ -452,6 +496,12 @@ __global__ __launch_bounds__(64 * STEP_WAVES) void k_adapter_step(Rows x, Matrix
                 acc[m] = mfma16(hv[1], cols[m], acc[m]);
             }
         }
+        if (__ballot(!all_finite(acc))) {
+            write_one_by_one<T>(u, tile, tile.first + c * 16, tile.live - c * 16, n_first, [&](int t, int j) {
+                return whole<T>(h[0][c * 16 + t][j], h[1][c * 16 + t][j]) * (std::is_same<T, _Float16>::value ? back[c * 16 + t] : 1.0f);
+            });
+            continue;
+        }
         write_outputs<T, WIDE>(u, tile.first + c * 16, tile.live - c * 16, n_first, base, acc, [&](int i) {
             // read when it is needed: there is no register to keep it in
             return std::is_same<T, _Float16>::value && some ? *(volatile const float *)&back[c * 16 + lane_token(i)] : 1.0f;
@@ -494,6 +544,29 @@ struct Outer {
     void *out;                           // [adapters][rank][width]
     float *partial;                      // [places][rank][width]
 };
+
+// d[j][k] over the adapter's tiles [from, to), by one thread.
+template <class T> __device__ float sum_one(const Outer &job, const Segments &s, int a, uint32_t from, uint32_t to, uint32_t j, uint32_t k)
+{
+    float sum = 0;
+    uint32_t seen = 0;
+    for (uint32_t seg = 0; seg < s.segments && seen < to; seg++) {
+        if (s.which[seg] != a) continue;
+        const int64_t first = bounded_start(s.starts, (int)seg, s.tokens), last = bounded_start(s.starts, (int)seg + 1, s.tokens);
+        const uint32_t n = tiles_of(s, seg);
+        for (uint32_t i = seen < from ? from - seen : 0; i < n && seen + i < to; i++) {
+            const size_t slot = (size_t)(first / TILE + seg) + i;
+            const float by = std::is_same<T, _Float16>::value ? job.h.rank_by[slot * s.rows + j] : 1.0f;
+            const int64_t t0 = first + (int64_t)i * TILE;
+            for (int t = 0; t < TILE && t0 + t < last; t++) {
+                const size_t at = by_rank_at(slot, j, t, s.rows);
+                sum = fmaf(whole<T>(job.h.by_rank[0][at], job.h.by_rank[1][at]) * by, (float)((const T *)job.x.p)[(t0 + t) * job.x.stride + k], sum);
+            }
+        }
+        seen += n;
+    }
+    return sum;
+}
 
 // One adapter, SPAN columns, up to CHUNK ranks, and `share` of its tiles: the wavefronts take every eighth and are summed in LDS.
 // An adapter of more tiles has several such sums, in places of their own, which k_adapter_sum adds in order.
@@ -595,6 +668,13 @@ __global__ __launch_bounds__(64 * OUTER_WAVES) void k_adapter_outer(Outer job0, 
 #pragma unroll
             for (int w = 0; w < OUTER_WAVES; w++) v += *reinterpret_cast<const f32x4 *>(&part[w][n / (SPAN / 4)][n % (SPAN / 4) * 4]);
             if (j >= rank) v = f32x4{0, 0, 0, 0};
+            if (__builtin_expect(!all_finite<1>({v}), 0)) {
+#pragma unroll 1
+                for (uint32_t i = 0; i < 4 && k + i < job.width; i++) {
+                    const float again = sum_one<T>(job, s, a, from, to, j, k + i);
+                    for (uint32_t m = 0; m < 4; m++) v[m] = m == i ? again : v[m];
+                }
+            }
             if (parts > 1) {
                 float *p = job.partial + (place * s.rank + j) * job.width + k;
                 for (int i = 0; i < 4; i++)
