@@ -370,6 +370,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
 {
     constexpr int UNITS = DP / 8, KS = DP / 16, DB = DP / 32, BLOCK = 4 * STEP;      // places that are looked up together
     constexpr int EACH = STEP * UNITS / (64 * TILE_WAVES);                           // units of either tile that a thread brings
+    constexpr float LEAD = std::is_same<T, __bf16>::value ? 8.0f : 0.0f;
     __shared__ __align__(16) T even_keys[STEP * DP], even_values[STEP * DP], odd_keys[STEP * DP], odd_values[STEP * DP];
     __shared__ int64_t rows[2][BLOCK];
     __shared__ uint64_t missing[2][BLOCK / 64];                                      // places that their page id or the table's end keeps out
@@ -497,9 +498,10 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
 #pragma unroll
                 for (int i = 0; i < 16; i++) top = fmaxf(top, s[t][i]);
             top = other_half_max(top) * scale;
-            // the reference need not be the top itself: it is raised where a weight would exceed 2^8
-            if (__builtin_expect(__ballot(top > m + 8.0f) != 0, 0)) {
-                const float to = fmaxf(m, top), ref = to == -__builtin_inff() ? 0.0f : to, alpha = __builtin_amdgcn_exp2f(m - ref);
+            // The reference need not be the top itself: it is raised where a top exceeds it by 8.  In bf16, whose largest numbers are
+            // f32's, it is raised to 8 above the top, so that no weight is more than 1; f16's smallest weights need the room instead.
+            if (__builtin_expect(__ballot(top > m + (8.0f - LEAD)) != 0, 0)) {
+                const float to = top > m ? top + LEAD : m, ref = to == -__builtin_inff() ? 0.0f : to, alpha = __builtin_amdgcn_exp2f(m - ref);
                 m = to;
                 l *= alpha;
 #pragma unroll

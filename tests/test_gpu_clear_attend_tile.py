@@ -30,6 +30,7 @@ LONG = [([80, 1], [5000, 777], 8, 1, 64, 32, 0), ([300], [2300], 4, 2, 128, 16, 
 # where values or keys are not finite
 SPECIAL = [([470, 1], [500, 90], 16, 2, 128, 16, 0), ([470, 1], [500, 90], 16, 2, 128, 16, 25), ([1, 500], [100, 1400], 16, 2, 64, 16, 20),
            ([470], [470], 16, 2, 256, 16, 60), ([130], [2600], 4, 2, 128, 16, 0), ([40, 300], [1200, 2000], 4, 2, 80, 16, 1100)]
+LARGE = [200], [264], 8, 1, 64, 16
 NOTHING = [400, 300, 1, 200], [300, 0, 1, 700], 8, 2, 64, 16
 
 
@@ -40,7 +41,7 @@ def calls():
     out = [call(*c) for c in BEYOND_THE_TABLE]
     out += [call(*MIXED, *h, page, None, window) for h in HEADS for page, window in WINDOWS]
     out += [call(*c[:6], None, c[6]) for c in LONG + SPECIAL]
-    out += [call(*NOTHING), call(*NOTHING, 19), call(*MIXED, 8, 1, 64, 16, None, 50), call(*MIXED, 6, 3, 64, 16), call(*MIXED, 8, 8, 128, 64)]
+    out += [call(*LARGE), call(*NOTHING), call(*NOTHING, 19), call(*MIXED, 8, 1, 64, 16, None, 50), call(*MIXED, 6, 3, 64, 16), call(*MIXED, 8, 8, 128, 64)]
     return out
 
 
@@ -150,3 +151,15 @@ def test_a_cache_beyond_four_giga_elements(ctx):
     k[far], v[far] = a["k_pages"], a["v_pages"]
     b = dict(a, k_pages=k, v_pages=v, table=torch.where(a["table"] >= 0, far[a["table"].clamp(min=0).long()], -1).int())
     assert torch.equal(ctx.attend_pages(**b), compare(ctx, a, BF16))
+
+
+def test_values_near_the_largest_of_bf16(ctx):
+    """Weighted sums that 32 bits hold if no weight is more than 1: values of 2^120, scores that rise by 6.9 bits once a row is under way."""
+    a = inputs(BF16, *LARGE)
+    a["q"].zero_()
+    a["q"][..., 0] = 1
+    a["k_pages"].zero_()
+    a["v_pages"].copy_(torch.where(a["v_pages"].isnan(), a["v_pages"], a["v_pages"].sign() * 2.0 ** 120))
+    for page in a["table"][0, 4:17]:
+        a["k_pages"][int(page), :, :, 0] = 4.8
+    compare(ctx, dict(a, scale=1.0), BF16)
