@@ -7,8 +7,10 @@
 //
 // Scores are taken transposed, S^T = K Q^T, so that the lanes' results are the operands of the second product O^T = V^T P^T as they
 // lie: a lane's scores of one row become eight places of one column, if V's rows are taken in the same order.  The softmax is the
-// running one: a top m and a sum l per row in 32 bits, weights exp2(s - m) with log2(e) in the scale.  The weights are rounded to the
-// type for the second product (their sum is not): an error of the size of the result's own rounding.
+// running one: a top m and a sum l per row in 32 bits, weights exp2(s - m) with log2(e) in the scale.  k_attend_few, which waits for
+// memory, takes the second product with the weights as two numbers of the type, the rounded value and the rest, so that nothing but the
+// result's own rounding shows.  k_attend_tile rounds the weights to the type (their sum is not): an error of the size of the result's
+// own rounding, 0.0024 and not 0.0017 of a result in bf16; with two numbers 2048 tokens over 32768 places take 1434 us and not 1065.
 //
 // Masks: a place that no row of the tile attends to is not read at all.  A place that some rows attend to and others do not has weight
 // 0 for the others, which a matrix instruction multiplies with the value all the same.  So where some of such places' values are
@@ -258,13 +260,14 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
         top = fmaxf(top, __shfl_xor(top, 32));
         const float ref = top == -__builtin_inff() ? 0.0f : top, alpha = __builtin_amdgcn_exp2f(m - ref);
         m = top;
-        x8<T> p;
+        x8<T> p, rest;
         float sum = 0;
 #pragma unroll
         for (int e = 0; e < 8; e++) {
             const float v = __builtin_amdgcn_exp2f(s[e] - ref);
             sum += v;
             p[e] = (T)v;
+            rest[e] = (T)(v - (float)p[e]);
         }
         l = fmaf(l, alpha, sum);
         if (__ballot(alpha != 1.0f)) {
@@ -286,7 +289,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
             x8<T> v[EL];
             transpose8<T, EL>(vraw[b], v);
 #pragma unroll
-            for (int e = 0; e < EL; e++) acc[b][e] = mfma16(v[e], p, acc[b][e]);
+            for (int e = 0; e < EL; e++) acc[b][e] = mfma16(v[e], p, mfma16(v[e], rest, acc[b][e]));
         }
     }
     if (special) any_special = 1;
