@@ -18,9 +18,10 @@
 // Bound by memory: x, base and the adapters are read, and the result written, once; a tile's h is a few KB.  Backward, x and dy are
 // read twice, the second time from the memory-side cache if they fit it.
 //
-// Measured: 4099 tokens of 4096 -> 6144, rank 64, f16 with sums as base: 18 us for h (136 workgroups, each with all of its adapter)
-// and 34 for the result (157 MB).  Backward, 8192 tokens of 4096 -> 4096, rank 32, bf16: 25 us for both hidden values (134 MB), 20
-// for dx (67 MB written), 24 + 5 for the matrices' gradients.  96 requests of a token, rank 16, 4096 -> 4096: 13 us in one launch.
+// Measured, on inputs that do not repeat: 4099 tokens of 4096 -> 6144, rank 64, f16 with sums as base: 23 us for h (136 workgroups, each
+// with all of its adapter) and 45 for the result (157 MB).  Backward, 8192 tokens of 4096 -> 4096, rank 32, bf16: 34 us for both hidden
+// values (134 MB), 21 for dx (67 MB written), 26 + 6 for the matrices' gradients.  96 requests of a token, rank 16, 4096 -> 4096: 13 us
+// in one launch.
 #include <algorithm>
 #include <type_traits>
 
@@ -729,7 +730,7 @@ Hidden take_hidden(Room &room, uint32_t slots, uint32_t rows, uint32_t chunks, b
     if (by_rank) h.rank_by = room.take<float>((size_t)slots * rows);
     return h;
 }
-// Backward, a workgroup sums eight tiles a wavefront (four: 80 us of gradients over 8192 tokens and not 74), and more where an adapter
+// Backward, a workgroup sums eight tiles a wavefront (four: 80 and not 74 us for 8192 tokens, on one input again and again), and more where an adapter
 // would else be shared by more than 16.
 template <class Args> Segments segments_of(const Args &a)
 {

@@ -155,8 +155,8 @@ __device__ void attend_row(const she_attend_pages_args &a, uint32_t group, const
     }
 }
 
-// For small calls, where latencies add up: a token over 197 places (2 key heads of 64) 6.4 us, 16 tokens over 1000 (8 of 128) 21 us; but
-// it reaches the memory's rate too: 64 tokens over 1 to 16384 places (2.1 GB) 426 us, 5.0 TB/s.
+// For small calls, where latencies add up: a token over 197 places (2 key heads of 64) 6.8 us, 16 tokens over 1000 (8 of 128) 21 us; but
+// it reaches the memory's rate too: 64 tokens over 1 to 16384 places (2.1 GB) 425 us, 5.0 TB/s.
 //
 // Few rows: every wavefront walks places of its own, 32 a step, four steps of the workgroup side by side, straight from memory.  Lane
 // l reads d = 32 s + 8 (l/16) .. of the key of place l%16 for the scores, and EL elements from EL (l%16) on of the values of the
@@ -345,11 +345,13 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
     }
 }
 
-// Bound by what a wavefront does one after the other: 2048 tokens over 32768 places (32 / 8 heads of 128, bf16) 1080 us, 987 TFLOP/s
-// where a product of 8192^3 reaches 1279.  The matrix units are busy for 45 % of the cycles and the vector units for as many; taken
+// Bound by what a wavefront does one after the other: 2048 tokens over 32768 places (32 / 8 heads of 128, bf16) 1066 us, 1000 TFLOP/s
+// where a product of 8192^3 reaches 1279 (946 on another card).  The matrix units are busy for 45 % of the cycles and the vector units for as many; taken
 // out for a timing, the softmax was worth 11 %, the second product 23 % and the tiles' loads 17 %.  Tried and slower: the next
 // step's scores beside a step's softmax (two forms), raised priority around the matrix instructions, pieces for more workgroups.
-// 24 requests of up to 700 tokens, half of them single (16 heads of 64, f16, a window of 1024): 57 us, most of it in the same steps.
+// 24 requests of up to 700 tokens, half of them single (16 heads of 64, f16, a window of 1024): 56 us, most of it in the same steps.
+// Heads of 64, 96, 192 and 256 over those 32768 places: 737, 742, 551 and 713 TFLOP/s (192 is computed as 256, with one workgroup per
+// compute unit).
 // Eight wavefronts on 256 rows gain 3 % there and lose a third where a window makes the tiles' edges count.
 //
 // Many rows: a workgroup has TILE_ROWS of them, 32 a wavefront, and steps through the places STEP at a time with both tiles of the step
@@ -576,8 +578,8 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
 // Rows that were cut, `each` of a tile a workgroup.  Up to JOIN_AHEAD pieces are a wavefront's work, and a workgroup of the tile kernel's
 // has sixteen rows then (with four, 99 and not 82 us for the whole call of 4063 tokens in two pieces at 16 heads of 64); more are
 // shared out among all four wavefronts, a row after the other, four rows a workgroup or, of many pieces, one.  Pieces are requested
-// JOIN_AHEAD at a time.  A token over 32768 places, 4 rows of 64 pieces at 8 key heads, takes 32 us so, 43 with four rows a
-// workgroup and 78 with a row a wavefront.
+// JOIN_AHEAD at a time.  A token over 32768 places, 4 rows of 64 pieces at 8 key heads, takes 33 us so on one input again and again (38 on
+// others in turn), 43 with four rows a workgroup and 78 with a row a wavefront.
 constexpr int JOIN_AHEAD = 4;
 template <class T>
 __device__ inline void join_row(const she_attend_pages_args &a, const Pieces &w, size_t at, int parts, int from, int by, float &sum, float o[4])

@@ -16,12 +16,12 @@ AttendShape attend_shape(const she_attend_pages_args &a, uint32_t cus)
     // One of the two kernels takes all of a call.  k_attend_tile computes 128 rows whether they are there or not, and k_attend_few reads
     // the places once for every 16 rows.  Either measured (few, tile; 8 key heads of 128, bf16; us; rows of each request at a key head):
     //    one request:    8 rows    16       32       64      128          16 requests:   4 rows     16        32        64
-    //    1000 places    14, 23   15, 23   16, 23   15, 23   19, 25         500 places   17, 19    20, 20
-    //    8000           16, 26   22, 27   26, 29   39, 29   54, 31        1000                    29, 28    35, 31    52, 35
-    //    32768          33, 45   41, 45   54, 46  109, 49  170, 57        4000          53, 55    75, 58
-    //                                                                    16384         221, 222  286, 219
+    //    1000 places    13, 23   13, 25   13, 25   15, 26   17, 28         500 places   17, 20    20, 20    24, 20    30, 20
+    //    8000           17, 26   18, 26   23, 27   38, 28   57, 30        1000          21, 24    28, 30    34, 30    52, 35
+    //    32768          38, 50   40, 51   56, 52   99, 54  172, 59        4000          64, 67    86, 65    92, 66   179, 90
+    //                                                                    16384         226, 218  294, 209  325, 211  634, 293
     // Where the work is small the first kernel's short way counts.  It also has single tokens of up to 8 rows, whose caches may have
-    // different lengths: its small pieces even them out (200 tokens over 1 to 3000 places 237, 274; 64 over 1 to 16384 430, 428).
+    // different lengths: its small pieces even them out (200 tokens over 1 to 3000 places 245, 268; 64 over 1 to 16384 421, 429).
     s.few = rows * span(FEW_ROWS) <= 1u << 18 || (a.tokens <= a.requests && group <= FEW_ROWS / 2);
     const uint64_t tile = s.few ? FEW_ROWS : TILE_ROWS, places = span(tile);
     s.slots = a.requests == 1 ? ceil_div(rows, tile) : rows / tile + a.requests;

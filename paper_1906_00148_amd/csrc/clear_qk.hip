@@ -9,7 +9,7 @@
 // for all the heads that it does.  Bound by memory: every element is read and written once.
 //
 // Measured: 16383 tokens of 64 heads of 80 (f16, ten of sixteen lanes busy) 79 us, 4.3 TB/s of the 4.9 that a large copy reaches;
-// backward, 8192 tokens of 40 heads of 128 (bf16) 59 us, 4.3 TB/s, and 4.8 us for the weights' sums.
+// backward, 8192 tokens of 40 heads of 128 (bf16) 63 us, 4.1 TB/s, and 4.6 us for the weights' sums.
 #include <algorithm>
 #include <type_traits>
 
