@@ -30,10 +30,12 @@ AttendShape attend_shape(const she_attend_pages_args &a, uint32_t cus)
         // a token over 32768 places when every row was joined by one wavefront.
         const uint64_t share = ceil_div(s.slots * a.kv_heads * places / (2 * cus), 128) * 128;
         s.chunk = (uint32_t)std::min<uint64_t>(MOST_CHUNK, std::max<uint64_t>(256, share));
-        // Up to sixteen workgroups for each that runs at once, or eight pieces, even the requests' lengths out.  A table of more
-        // places than such pieces have, as wide as a context that few requests fill, does not make scratch for more of them: a
-        // request that does fill it has longer pieces.
-        const uint64_t most = std::max<uint64_t>(8, ceil_div(16 * 2 * cus, s.slots * a.kv_heads));
+        // Up to 32 workgroups for each that runs at once, or eight pieces, even the requests' lengths out.  A table of more places than
+        // such pieces have, as wide as a context that few requests fill, does not make scratch and workgroups for more of them: a
+        // request that does fill it has longer pieces.  Tables of 131072 places, 8 key heads of 128, in us with a piece for every 2048
+        // places, at most 16 workgroups, and 32: one request of 131000 places among 63 of up to 300 841, 915, 855, among 1023 4003,
+        // 2160, 2170; 1024 of up to 300 2222, 432, 431; 64 of up to 60000 1503, 1476, 1484.
+        const uint64_t most = std::max<uint64_t>(8, ceil_div(32 * 2 * cus, s.slots * a.kv_heads));
         s.splits = (uint32_t)std::max<uint64_t>(1, std::min(most, ceil_div(places, s.chunk)));
         return s;
     }

@@ -9,7 +9,7 @@ from test_gpu_clear_attend import compare, inputs
 pytestmark = pytest.mark.gpu
 REQUESTS, HEADS, PAGE = 136, 8, 64
 LENGTHS = [(37 * i) % 300 + 1 for i in range(REQUESTS)]
-LENGTHS[5], LENGTHS[77], LENGTHS[130] = 17000, 40001, 16385
+LENGTHS[5], LENGTHS[77], LENGTHS[130] = 31000, 40001, 16385
 
 
 @pytest.fixture(scope="module")
@@ -30,9 +30,9 @@ def test_long_requests_among_short_ones(ctx, dtype, window):
 
 
 def test_what_is_missing_or_not_finite_in_a_later_block(ctx):
-    """Places 3000 and 7000 of the long request's first pieces, and its last places."""
+    """Places after the 2048 that are looked up first, in the first piece of the long request and in the third."""
     a = inputs(torch.bfloat16, [1] * REQUESTS, LENGTHS, HEADS, HEADS, 64, PAGE)
-    a["table"][77, 3000 // PAGE] = -1
+    a["table"][77, 2500 // PAGE] = a["table"][77, 7600 // PAGE] = -1
     ctx.clear_bad_ids()
     compare(ctx, a, torch.bfloat16)
     assert ctx.clear_bad_ids() > 0

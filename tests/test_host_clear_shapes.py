@@ -41,7 +41,7 @@ def test_scratch_follows_the_rows_and_not_the_table(shapes):
         got = shapes([(T, T, 32, 8, 128, 0, w // 16, 16) for w in widths])
         for w, (kernel, tiles, chunk, pieces, scratch) in zip(widths, got):
             assert kernel == "few" and scratch == (T * 32 * pieces * (128 + 2) * 4 if pieces > 1 else 0), (T, w)
-            assert pieces <= max(8, 16 * 512 // (tiles * 8) + 1)
+            assert pieces <= max(8, 32 * 512 // (tiles * 8) + 1)
             # pieces of a full table end on time: no fewer of them than the table's places in pieces of 2048, up to eight
             assert pieces >= min(8, w // 2048)
         # tables of up to 16384 places are cut as finely as places that are looked up together allow
