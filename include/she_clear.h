@@ -4,7 +4,8 @@
  * In split inference the projections whose weights a server shares among its clients are evaluated on ciphertexts
  * (she_shift_acc; Section 3.2 of arXiv 1906.00148), and the client runs what lies between a decryption and the next
  * encryption itself, on plain numbers: its own low-rank adapters beside such a projection, the norms and the rotation of
- * queries and keys, and the attention of new tokens over its cache.  These calls are that part for a decoder block.
+ * queries and keys, the places of new tokens in its cache, their attention over it, and the choice of the next token.  These calls
+ * are that part for a decoder block and what a step of generation needs around it.
  *
  * Conventions beside those of she.h:
  *  - Every pointer inside an argument struct is a DEVICE pointer; the struct itself is read before the call returns.
@@ -169,6 +170,59 @@ typedef struct {
     int64_t out_token, out_head;
 } she_attend_pages_args;
 int she_attend_pages(she_ctx *ctx, const she_attend_pages_args *args);
+
+/* Places in a paged cache for the new tokens of a step, worked out from the requests' lengths on the GPU: the starts, lengths,
+ * positions, slots and table that she_qk_rotate and she_attend_pages read.  Request r has cached[r] places and gets news[r] more:
+ *   starts[r+1] = min(starts[r] + news[r], tokens), starts[0] = 0;  lengths[r] = cached[r] + starts[r+1] - starts[r];
+ * its columns of the table from ceil(cached[r] / page_size) up to ceil(lengths[r] / page_size), which it has not yet, get pages off
+ * the list `free`, from its entry taken[0] on, request by request and column by column; taken_out[0] is the entry after the last.
+ * Token starts[r] + i has place u = cached[r] + i: position before[r] + u and slot table[r][u / page_size] * page_size +
+ * u % page_size.  A token gets slot -1, and is counted, where the list is at its end (that column gets -1, as it does from an id
+ * outside [0, pages) in the list), where the page that its request has already is outside [0, pages), and where the table has no
+ * column for it.  The tokens from starts[requests] on are the padding of a batch: position 0, slot -1, not counted.  Other columns are
+ * left as they are.  Numbers below 0 in cached, news, taken and before count as 0, and positions end at 2^31 - 1.  lengths may be
+ * cached, taken_out may be taken; no other two arrays may share memory. */
+typedef struct {
+    uint32_t requests, tokens;           /* tokens: the room in positions and slots */
+    uint32_t pages, page_size, table_width, free_count;
+    const int32_t *cached, *news;        /* [requests] */
+    const int32_t *before;               /* [requests]: places before a request's own, as of a shared prefix; NULL: none */
+    const int32_t *free;                 /* [free_count] */
+    const int32_t *taken;                /* [1] */
+    int32_t *table;                      /* [requests][table_width] */
+    int64_t table_stride;
+    int32_t *starts;                     /* [requests + 1] */
+    int32_t *lengths;                    /* [requests] */
+    int32_t *positions;                  /* [tokens] */
+    int64_t *slots;                      /* [tokens] */
+    int32_t *taken_out;                  /* [1] */
+} she_plan_pages_args;
+int she_plan_pages(she_ctx *ctx, const she_plan_pages_args *args);
+
+/* The next token of every row of logits.  A logit is an element of `type`, or with SHE_I32 a projection's decrypted sum times step[i]
+ * (NULL: 1), as a number of 32 bits; NaN counts as -infinity.  With x_i = logit_i / temperature, the weight of token i is
+ * exp(x_i - max x).  Kept are the top_k largest (of equals the lower index first), of these the shortest head in that order whose
+ * weight reaches top_p of theirs, and of these the tokens with a weight of at least min_p.  The token is the first, by index, at
+ * which the running weight of the kept tokens exceeds uniform times their whole weight; probs is its share of that weight.
+ * top_k < 1, top_p >= 1 or NaN, and min_p <= 0 or NaN keep all, and the likeliest token is kept in any case.  A temperature of 0 (or
+ * below, or NaN) takes the largest logit of lowest index with probability 1, and so does +infinity, shared equally by all that have
+ * it where the temperature is above 0.  A row without a logit above -infinity gets token -1, probability 0.  uniform is taken as at
+ * least 0 (NaN too) and at most 1 - 2^-24.  Weights are held to 2^-44 of the largest and their sums are exact. */
+typedef struct {
+    int32_t type;                        /* SHE_BF16, SHE_F16, SHE_F32 or SHE_I32 */
+    uint32_t rows, vocab;                /* vocab at most 2^20 */
+    const void *logits;                  /* [rows][vocab] */
+    int64_t row_stride;
+    const float *step;                   /* [vocab], with SHE_I32 */
+    const float *uniform;                /* [rows] */
+    const float *temperature;            /* [rows]; NULL: 1 */
+    const int32_t *top_k;                /* [rows]; NULL: all */
+    const float *top_p;                  /* [rows]; NULL: 1 */
+    const float *min_p;                  /* [rows]; NULL: 0 */
+    int32_t *tokens;                     /* [rows] */
+    float *probs;                        /* [rows]; may be NULL */
+} she_sample_args;
+int she_sample(she_ctx *ctx, const she_sample_args *args);
 
 /* Ids out of range that the kernels of this context's clear calls have left out since the last reset (several for one id, where
  * several workgroups meet it).  Waits for the stream; refused while that is captured (SHE_EINVAL). */

@@ -8,7 +8,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libshe_hip.so")
 SOURCES = ["she_kernels.hip", "she_api.cpp", "she_host.cpp", "she_circuits.cpp", "she_leveled.cpp", "she_clear.cpp",
-           "clear_attend_shape.cpp", "clear_qk.hip", "clear_adapters.hip", "clear_attend.hip"]
+           "she_clear_step.cpp", "clear_plan.hip", "clear_sample.hip", "clear_attend_shape.cpp", "clear_qk.hip", "clear_adapters.hip", "clear_attend.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

@@ -70,7 +70,12 @@ _ATTEND_PAGES = _Layout("she_attend_pages_args", [
     ("i", "type"), ("I", "tokens requests q_heads kv_heads head window"), ("f", "scale"), ("P", "q"), ("q", "q_token q_head"),
     ("P", "k_pages v_pages"), ("q", "page_stride slot_stride page_head"), ("I", "pages page_size"), ("P", "table"),
     ("q", "table_stride"), ("I", "table_width"), ("P", "starts lengths out"), ("q", "out_token out_head")])
-LAYOUTS = [_ADAPTERS, _ADAPTERS_GRAD, _QK_ROTATE, _QK_ROTATE_GRAD, _ATTEND_PAGES]
+_PLAN_PAGES = _Layout("she_plan_pages_args", [
+    ("I", "requests tokens pages page_size table_width free_count"), ("P", "cached news before free taken table"), ("q", "table_stride"),
+    ("P", "starts lengths positions slots taken_out")])
+_SAMPLE = _Layout("she_sample_args", [
+    ("i", "type"), ("I", "rows vocab"), ("P", "logits"), ("q", "row_stride"), ("P", "step uniform temperature top_k top_p min_p tokens probs")])
+LAYOUTS = [_ADAPTERS, _ADAPTERS_GRAD, _QK_ROTATE, _QK_ROTATE_GRAD, _ATTEND_PAGES, _PLAN_PAGES, _SAMPLE]
 
 SIGNATURES = {**{layout.name[:-len("_args")]: (C.c_int, [C.c_void_p, C.c_char_p]) for layout in LAYOUTS},
               "she_clear_bad_ids": (C.c_int, [C.c_void_p, C.POINTER(C.c_uint64), C.c_int]),
@@ -341,6 +346,62 @@ class Calls:
         if torch.is_grad_enabled() and (q.requires_grad or k_pages.requires_grad or v_pages.requires_grad):
             return _barred(out, "a cache is for inference", q, k_pages, v_pages)
         return out
+
+    def plan_pages(self, cached, news, table, free, taken, tokens, pages, page_size, before=None, out=None):
+        """The places of a step's new tokens in a paged cache: request r has cached[r] places and gets news[r] more, [requests] int32;
+        new pages come off the list free [entries] int32 from its entry taken[0] on, [1] int32, and into table [requests, width] int32.
+        `tokens` is the room for tokens, of which those behind the last request's are padding; pages and page_size are the cache's;
+        before [requests] int32: places before a request's own, which its positions count.  Returns (starts [requests + 1], lengths
+        [requests], positions [tokens] int32, slots [tokens] int64, taken [1]); out: these five, where lengths may be cached and
+        taken may be taken."""
+        dev, i32 = self._device, torch.int32
+        R, width = table.shape
+        F = free.shape[0]
+        if not (0 <= tokens < 1 << 31 and 0 <= pages < 1 << 31 and 0 < page_size < 1 << 31):
+            _refuse("tokens, pages and page_size must be sizes")
+        table_at, ts = _see(table, "table", i32, (R, width), dev)
+        inputs = (_line(cached, "cached", i32, R, dev), _line(news, "news", i32, R, dev), _line(before, "before", i32, R, dev),
+                  _line(free, "free", i32, F, dev), _line(taken, "taken", i32, 1, dev))
+        given = out is not None
+        if not given:
+            numbers = torch.empty(2 * R + tokens + 2, dtype=i32, device=table.device)
+            out = (*numbers.split((R + 1, R, tokens, 1)), torch.empty(tokens, dtype=torch.int64, device=table.device))
+            out = out[0], out[1], out[2], out[4], out[3]
+        starts, lengths, positions, slots, now = out
+        self._call(self._L.she_plan_pages, _PLAN_PAGES.pack(
+            R, tokens, pages, page_size, width, F, *inputs, table_at, ts[0], _line(starts, "starts", i32, R + 1, dev),
+            _line(lengths, "lengths", i32, R, dev), _line(positions, "positions", i32, tokens, dev),
+            _line(slots, "slots", torch.int64, tokens, dev), _line(now, "taken", i32, 1, dev)))
+        torch.autograd.graph.increment_version((table, *out) if given else table)
+        return out
+
+    def sample(self, logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, step=None, out=None):
+        """The next token of every row of logits [rows, vocab], in bfloat16, float16, float32, or int32 sums times step [vocab] float32:
+        the first whose running weight among the kept ones exceeds uniform [rows] float32 of theirs.  temperature, top_p, min_p [rows]
+        float32 and top_k [rows] int32: each row's own settings, or None.  Returns (tokens [rows] int32, -1 for a row without a
+        logit above -infinity; probs [rows] float32, the token's share); out: a pair for them."""
+        dev = self._device
+        kind = {torch.bfloat16: 0, torch.float16: 1, torch.float32: _F32, torch.int32: _I32}.get(logits.dtype)
+        if kind is None:
+            _refuse(f"logits must be bfloat16, float16, float32 or int32, not {logits.dtype}")
+        if step is not None and kind != _I32:
+            _refuse("step belongs to int32 sums")
+        rows, vocab = logits.shape
+        at, strides = _see(logits, "logits", logits.dtype, (rows, vocab), dev)
+        f32 = torch.float32
+        settings = (_line(step, "step", f32, vocab, dev), _line(uniform, "uniform", f32, rows, dev), _line(temperature, "temperature", f32, rows, dev),
+                    _line(top_k, "top_k", torch.int32, rows, dev), _line(top_p, "top_p", f32, rows, dev), _line(min_p, "min_p", f32, rows, dev))
+        given = out is not None
+        if not given:
+            out = torch.empty(rows, dtype=torch.int32, device=logits.device), torch.empty(rows, dtype=f32, device=logits.device)
+        self._call(self._L.she_sample, _SAMPLE.pack(kind, rows, vocab, at, strides[0], *settings, _line(out[0], "tokens", torch.int32, rows, dev),
+                                                    _line(out[1], "probs", f32, rows, dev)))
+        if given:
+            torch.autograd.graph.increment_version((out[0], out[1]))
+        if torch.is_grad_enabled() and (logits.requires_grad or step is not None and step.requires_grad or
+                                        temperature is not None and temperature.requires_grad):
+            return out[0], _barred(out[1], "sampling is for inference", logits, step, temperature)
+        return out[0], out[1]
 
     def clear_bad_ids(self, reset: bool = True) -> int:
         """Ids out of range in device arrays that these calls have left out since the last reset; waits for the stream."""

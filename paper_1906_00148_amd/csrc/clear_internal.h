@@ -55,4 +55,14 @@ size_t attend_pieces(const she_attend_pages_args &a, const AttendShape &s);     
 size_t attend_scratch(const she_attend_pages_args &a, const AttendShape &s);
 hipError_t launch_attend_pages(const she_attend_pages_args &a, const AttendShape &s, void *scratch, uint32_t *d_bad, hipStream_t st);
 
+// ---- places of a step's new tokens
+constexpr uint32_t PLAN_REQUESTS = 4096;             // requests that one workgroup scans at once
+// Whether one workgroup does all of a call: its requests and tokens are few.
+inline bool plan_few(const she_plan_pages_args &a) { return a.requests <= PLAN_REQUESTS && a.tokens <= 4096; }
+size_t plan_scratch(const she_plan_pages_args &a);
+hipError_t launch_plan_pages(const she_plan_pages_args &a, void *scratch, uint32_t *d_bad, hipStream_t st);
+
+// ---- the next token
+hipError_t launch_sample(const she_sample_args &a, uint32_t cus, hipStream_t st);
+
 }}  // namespace she::clear

@@ -1,15 +1,12 @@
 // The clear side of split inference in the C ABI (declared in include/she_clear.h): checks of arguments, scratch, launches.
 #include <algorithm>
 
-#include "clear_internal.h"
-#include "she_ctx.h"
+#include "clear_host.h"
 
 using namespace she;
+using namespace she::clear;
 
 namespace {
-
-// so that no grid has more than 2^32 threads along one axis
-constexpr uint64_t MOST_TOKENS = 1u << 24, MOST_SEGMENTS = 1u << 20, MOST_WIDTH = 1u << 24, MOST_PLACES = 1u << 26, MOST_GROUPS = 1u << 24;
 
 // Allocating would break a capture: the error says so before it does.
 int may_allocate(she_ctx *c)
@@ -28,6 +25,10 @@ int on_device(she_ctx *c)
     if (now == c->device) return SHE_OK;
     return fail(c, SHE_EINVAL, "the current device is " + std::to_string(now) + ", the context is on " + std::to_string(c->device));
 }
+
+}  // namespace
+
+namespace she { namespace clear {
 
 int ready(she_ctx *c)
 {
@@ -59,8 +60,9 @@ int ensure_scratch(she_ctx *c, size_t bytes)
     return SHE_OK;
 }
 
-bool half_type(int32_t t) { return t == SHE_BF16 || t == SHE_F16; }
-bool on16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+}}  // namespace she::clear
+
+namespace {
 
 // what both directions of the adapters have in common
 template <class Args> int check_adapters(she_ctx *c, const Args &a, const char *name)

@@ -1,0 +1,46 @@
+// What a step of generation needs around its block, in the C ABI (declared in include/she_clear.h): checks of arguments, scratch, launches.
+#include "clear_host.h"
+
+using namespace she;
+using namespace she::clear;
+
+extern "C" {
+
+int she_plan_pages(she_ctx *c, const she_plan_pages_args *args)
+try {
+    if (!c) return SHE_EINVAL;
+    if (!args) return fail(c, SHE_EINVAL, "null argument");
+    const she_plan_pages_args a = *args;
+    const std::string at = "she_plan_pages: ";
+    if (!a.page_size) return fail(c, SHE_EINVAL, at + "a size is zero");
+    if (a.requests > MOST_SEGMENTS || a.tokens > MOST_TOKENS || a.page_size > MOST_PLACES || a.pages > 0x7FFFFFFF || a.free_count > 0x7FFFFFFF ||
+        (uint64_t)a.table_width * a.page_size > MOST_PLACES)
+        return fail(c, SHE_ERANGE, at + "at most 2^20 requests, 2^24 tokens, 2^26 places of a request and 2^31 pages");
+    if (!a.taken || !a.taken_out || !a.starts || (a.requests && (!a.cached || !a.news || !a.lengths)) || (a.tokens && (!a.positions || !a.slots)) ||
+        (a.requests && a.table_width && !a.table) || (a.free_count && !a.free))
+        return fail(c, SHE_EINVAL, at + "null argument");
+    int rc;
+    if ((rc = ready(c)) || (rc = ensure_scratch(c, plan_scratch(a)))) return rc;
+    HIP_TRY(c, launch_plan_pages(a, c->clear.scratch(), c->clear.d_bad, c->stream));
+    return SHE_OK;
+} SHE_NOTHROW(c)
+
+int she_sample(she_ctx *c, const she_sample_args *args)
+try {
+    if (!c) return SHE_EINVAL;
+    if (!args) return fail(c, SHE_EINVAL, "null argument");
+    const she_sample_args a = *args;
+    const std::string at = "she_sample: ";
+    if (!half_type(a.type) && a.type != SHE_F32 && a.type != SHE_I32) return fail(c, SHE_EINVAL, at + "type must be SHE_BF16, SHE_F16, SHE_F32 or SHE_I32");
+    if (!a.vocab) return fail(c, SHE_EINVAL, at + "a size is zero");
+    if (a.vocab > 1u << 20 || a.rows > 1u << 20) return fail(c, SHE_ERANGE, at + "rows and vocab are at most 2^20");
+    if (!a.rows) return SHE_OK;
+    if (!a.logits || !a.uniform || !a.tokens) return fail(c, SHE_EINVAL, at + "null argument");
+    if (a.step && a.type != SHE_I32) return fail(c, SHE_EINVAL, at + "step belongs to SHE_I32");
+    const int rc = ready(c);
+    if (rc) return rc;
+    HIP_TRY(c, launch_sample(a, c->dk.cus, c->stream));
+    return SHE_OK;
+} SHE_NOTHROW(c)
+
+}  // extern "C"
