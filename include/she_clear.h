@@ -199,6 +199,39 @@ typedef struct {
 } she_plan_pages_args;
 int she_plan_pages(she_ctx *ctx, const she_plan_pages_args *args);
 
+/* she_attend_pages for requests that begin with the same text, whose places are in the cache once and are read once for all of
+ * them.  The requests [prefix_requests[g], prefix_requests[g+1]) have the prefix g of prefix_lengths[g] places, place u being slot
+ * u % page_size of page prefix_table[g][u / page_size]; prefix_requests is ascending, and requests outside all of it have no prefix.
+ * lengths, starts and table are the requests' own places, which follow the prefix on pages of their own: new token i of n stands at
+ * p = lengths[r] - n + i of them and attends to its own places 0 .. p and to the whole prefix; with a window, to the last `window`
+ * of the row of both.  A token with p < 0 attends to nothing and gets zeros.  Page ids out of range, places without a column and
+ * what lies in places that are not attended to: as in she_attend_pages.  At most 2^26 places of a prefix and of a request. */
+typedef struct {
+    int32_t type;                        /* SHE_BF16 or SHE_F16 */
+    uint32_t tokens, requests, q_heads, kv_heads;
+    uint32_t head;                       /* a multiple of 8, at most 256 */
+    uint32_t window;
+    float scale;
+    const void *q;                       /* [tokens][q_heads][head]; rows start on 16 bytes */
+    int64_t q_token, q_head;
+    const void *k_pages, *v_pages;       /* [pages][page_size][kv_heads][head], strides shared by both; rows start on 16 bytes */
+    int64_t page_stride, slot_stride, page_head;
+    uint32_t pages, page_size;
+    const int32_t *table;                /* [requests][table_width] */
+    int64_t table_stride;
+    uint32_t table_width;
+    uint32_t prefixes, prefix_width;
+    const int32_t *starts;               /* [requests + 1] */
+    const int32_t *lengths;              /* [requests] */
+    const int32_t *prefix_table;         /* [prefixes][prefix_width] */
+    int64_t prefix_stride;
+    const int32_t *prefix_requests;      /* [prefixes + 1] */
+    const int32_t *prefix_lengths;       /* [prefixes] */
+    void *out;                           /* [tokens][q_heads][head]; rows start on 16 bytes */
+    int64_t out_token, out_head;
+} she_attend_shared_args;
+int she_attend_shared(she_ctx *ctx, const she_attend_shared_args *args);
+
 /* The next token of every row of logits.  A logit is an element of `type`, or with SHE_I32 a projection's decrypted sum times step[i]
  * (NULL: 1), as a number of 32 bits; NaN counts as -infinity.  With x_i = logit_i / temperature, the weight of token i is
  * exp(x_i - max x).  Kept are the top_k largest (of equals the lower index first), of these the shortest head in that order whose

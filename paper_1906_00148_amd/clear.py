@@ -73,9 +73,14 @@ _ATTEND_PAGES = _Layout("she_attend_pages_args", [
 _PLAN_PAGES = _Layout("she_plan_pages_args", [
     ("I", "requests tokens pages page_size table_width free_count"), ("P", "cached news before free taken table"), ("q", "table_stride"),
     ("P", "starts lengths positions slots taken_out")])
+_ATTEND_SHARED = _Layout("she_attend_shared_args", [
+    ("i", "type"), ("I", "tokens requests q_heads kv_heads head window"), ("f", "scale"), ("P", "q"), ("q", "q_token q_head"),
+    ("P", "k_pages v_pages"), ("q", "page_stride slot_stride page_head"), ("I", "pages page_size"), ("P", "table"),
+    ("q", "table_stride"), ("I", "table_width prefixes prefix_width"), ("P", "starts lengths prefix_table"), ("q", "prefix_stride"),
+    ("P", "prefix_requests prefix_lengths out"), ("q", "out_token out_head")])
 _SAMPLE = _Layout("she_sample_args", [
     ("i", "type"), ("I", "rows vocab"), ("P", "logits"), ("q", "row_stride"), ("P", "step uniform temperature top_k top_p min_p tokens probs")])
-LAYOUTS = [_ADAPTERS, _ADAPTERS_GRAD, _QK_ROTATE, _QK_ROTATE_GRAD, _ATTEND_PAGES, _PLAN_PAGES, _SAMPLE]
+LAYOUTS = [_ADAPTERS, _ADAPTERS_GRAD, _QK_ROTATE, _QK_ROTATE_GRAD, _ATTEND_PAGES, _PLAN_PAGES, _ATTEND_SHARED, _SAMPLE]
 
 SIGNATURES = {**{layout.name[:-len("_args")]: (C.c_int, [C.c_void_p, C.c_char_p]) for layout in LAYOUTS},
               "she_clear_bad_ids": (C.c_int, [C.c_void_p, C.POINTER(C.c_uint64), C.c_int]),
@@ -373,6 +378,38 @@ class Calls:
             _line(lengths, "lengths", i32, R, dev), _line(positions, "positions", i32, tokens, dev),
             _line(slots, "slots", torch.int64, tokens, dev), _line(now, "taken", i32, 1, dev)))
         torch.autograd.graph.increment_version((table, *out) if given else table)
+        return out
+
+    def attend_shared(self, q, k_pages, v_pages, table, starts, lengths, prefix_table, prefix_requests, prefix_lengths, scale=None, window=0,
+                      out=None):
+        """attend_pages for requests that begin with the same text: the requests from prefix_requests[g] up to prefix_requests[g + 1]
+        ([prefixes + 1] int32) attend to the prefix_lengths[g] places ([prefixes] int32) found through prefix_table [prefixes, width]
+        int32, which are read once for all of them, and then to their own, of which table, starts and lengths tell.  A window
+        counts both.  Returns out like q."""
+        dev = self._device
+        ty, dtype, (T, Hq, D), q_at, qs = _first(q, "q", dev)
+        Hkv = k_pages.shape[2]
+        (R, width), (G, prefix_width) = table.shape, prefix_table.shape
+        pages_at, pages, size = self._pages(k_pages, v_pages, dtype, Hkv, D, dev)
+        i32 = torch.int32
+        table_at, ts = _see(table, "table", i32, (R, width), dev)
+        prefix_at, ps = _see(prefix_table, "prefix_table", i32, (G, prefix_width), dev)
+        if not 0 <= window < 1 << 32:
+            _refuse("window must be a number of places")
+        given = out is not None
+        if not given:
+            out = torch.empty(T, Hq, D, dtype=dtype, device=q.device)
+            out_at, out_token, out_head = out.data_ptr(), Hq * D, D
+        else:
+            out_at, (out_token, out_head, _) = _see(out, "out", dtype, (T, Hq, D), dev)
+        self._call(self._L.she_attend_shared, _ATTEND_SHARED.pack(
+            ty, T, R, Hq, Hkv, D, window, D ** -0.5 if scale is None else scale, q_at, qs[0], qs[1], *pages_at, pages, size, table_at, ts[0],
+            width, G, prefix_width, _line(starts, "starts", i32, R + 1, dev), _line(lengths, "lengths", i32, R, dev), prefix_at, ps[0],
+            _line(prefix_requests, "prefix_requests", i32, G + 1, dev), _line(prefix_lengths, "prefix_lengths", i32, G, dev), out_at, out_token, out_head))
+        if given:
+            torch.autograd.graph.increment_version(out)
+        if torch.is_grad_enabled() and (q.requires_grad or k_pages.requires_grad or v_pages.requires_grad):
+            return _barred(out, "a cache is for inference", q, k_pages, v_pages)
         return out
 
     def sample(self, logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None, step=None, out=None):

@@ -26,13 +26,30 @@ namespace {
 constexpr int FEW_WAVES = 4, TILE_WAVES = TILE_ROWS / 32;
 constexpr float LOG2E = 1.4426950408889634f;
 
+// What a kernel walks: a call's requests, or in a call with shared prefixes these, each as a request of all tokens that have it, or what
+// the requests have behind them.
+enum Walk { REQUESTS, PREFIXES, BEHIND };
+
 // What is left behind of the pieces of cut rows: [rows of all requests][kv_heads][splits].
 struct Pieces {
     float *o;                            // [..][head]
     float2 *ml;
     uint32_t splits;
-    uint32_t chunk;                      // places of a piece, unless a tile has more than `splits` such pieces
+    uint32_t first, most;                // of these, the ones of this walk
+    uint32_t chunk;                      // places of a piece, unless a tile has more than `most` such pieces
 };
+
+// What the walk over prefixes knows of the requests: its own arguments have prefixes for requests.
+struct Owners {
+    const int32_t *requests;             // [prefixes + 1]
+    const int32_t *prefix_lengths;       // [prefixes]
+    const int32_t *lengths;              // [count]
+    uint32_t count, prefixes, prefix_width;
+};
+__device__ inline int owner_start(const Owners &w, int g)
+{
+    return min(max(w.requests[g], 0), (int)w.count);
+}
 
 // A tile of rows and the places that any of them attends to.
 struct Span {
@@ -48,7 +65,23 @@ __device__ inline size_t pieces_at(const Pieces &p, uint32_t kv_heads, uint32_t 
 {
     return ((size_t)(s.token0 * group + row) * kv_heads + kv_head) * p.splits;
 }
-template <int ROWS> __device__ inline Span span_of(const she_attend_pages_args &a, uint32_t group, const Piece &p, int row, const Pieces &pieces)
+// A prefix's places are cut alike for all of its tiles, into as many pieces as there may be.
+__device__ inline uint32_t prefix_chunk(uint32_t places, const Pieces &pieces)
+{
+    return max(pieces.chunk, ((places + pieces.most - 1) / pieces.most + 63) & ~63u);
+}
+__device__ inline int prefix_places(const she_attend_pages_args &a, int length, uint32_t width)
+{
+    return (int)min((int64_t)max(length, 0), (int64_t)width * a.page_size);
+}
+template <Walk WALK> __device__ inline Piece tile_of(const she_attend_pages_args &a, const Owners &owners, uint32_t group, uint32_t tile, uint32_t slot)
+{
+    if constexpr (WALK == PREFIXES)
+        return find_piece_by([&](int g) { return bounded_start(a.starts, owner_start(owners, g), a.tokens); }, a.requests, group, tile, slot);
+    else
+        return find_piece(a.starts, a.requests, a.tokens, group, tile, slot);
+}
+template <int ROWS, Walk WALK> __device__ inline Span span_of(const she_attend_pages_args &a, uint32_t group, const Piece &p, int row, const Pieces &pieces)
 {
     Span s{};
     s.request = p.segment;
@@ -59,6 +92,13 @@ template <int ROWS> __device__ inline Span span_of(const she_attend_pages_args &
     s.row = row;
     s.rows = min(ROWS, all - row);
     s.token0 = p.first / group;
+    if constexpr (WALK == PREFIXES) {
+        s.to = prefix_places(a, length, a.table_width);
+        s.first = s.to - 1;                                       // a token's window is looked up apart
+        s.chunk = (int)prefix_chunk(s.to, pieces);
+        s.parts = (s.to + s.chunk - 1) / s.chunk;
+        return s;
+    }
     s.first = length - news;
     const int p0 = s.first + row / (int)group, p1 = s.first + (row + s.rows - 1) / (int)group;
     const int64_t low = a.window ? (int64_t)p0 - (int64_t)a.window + 1 : 0;
@@ -67,10 +107,36 @@ template <int ROWS> __device__ inline Span span_of(const she_attend_pages_args &
     s.to = (int)min((int64_t)p1 + 1, room);
     const uint32_t places = s.to > s.from ? s.to - s.from : 0;
     uint32_t chunk = pieces.chunk;
-    if (places > (uint64_t)pieces.splits * chunk) chunk = ((places + pieces.splits - 1) / pieces.splits + 127) & ~127u;
+    if (places > (uint64_t)pieces.most * chunk) chunk = ((places + pieces.most - 1) / pieces.most + 127) & ~127u;
     s.chunk = (int)chunk;
     s.parts = (int)((places + chunk - 1) / chunk);
     return s;
+}
+
+// The places that a row of a tile attends to, from low to high.  In the walk over prefixes the request's own length says where its window
+// reaches back to.
+struct Reach {
+    int low, high;
+};
+template <Walk WALK> __device__ inline Reach reach_of(const she_attend_pages_args &a, const Owners &owners, uint32_t group, const Span &s, int row)
+{
+    Reach w{0, s.first};
+    if constexpr (WALK == PREFIXES) {
+        if (!a.window) return w;
+        const int64_t token = s.token0 + row / (int)group;
+        int r = owner_start(owners, s.request), end = owner_start(owners, s.request + 1);
+        while (end - r > 1) {
+            const int mid = (r + end) / 2;
+            if (bounded_start(a.starts, mid, a.tokens) <= token) r = mid;
+            else end = mid;
+        }
+        const int64_t place = (int64_t)max(owners.lengths[r], 0) - (bounded_start(a.starts, r + 1, a.tokens) - token);
+        w.low = (int)min(max(max(a.lengths[s.request], 0) + place - (int64_t)a.window + 1, (int64_t)0), (int64_t)s.to);
+    } else {
+        w.high = s.first + row / (int)group;
+        if (a.window) w.low = (int)max((int64_t)w.high - (int64_t)a.window + 1, (int64_t)0);
+    }
+    return w;
 }
 
 // Whether place `place`, whose page id is out of range and slot in_page, stands for that page in the count: its first place that is
@@ -107,16 +173,15 @@ template <class T> __device__ inline bool has_special(u32x4 v)
 // One row over those of the places [from, to) that it attends to, its piece `part`, by one wavefront: scores with a place a lane, sums with elements on
 // the lanes.  Writes the row's result, or its piece's.
 template <class T>
-__device__ void attend_row(const she_attend_pages_args &a, uint32_t group, const Pieces &pieces, size_t part, const Span &sp, int kv_head, int row, int from, int to)
+__device__ void attend_row(const she_attend_pages_args &a, uint32_t group, const Pieces &pieces, bool cut, size_t part, const Span &sp, int kv_head, int row, Reach reach, int from, int to)
 {
     const int lane = threadIdx.x & 63, D = (int)a.head;
     const int64_t token = sp.token0 + row / (int)group;
-    const int head = kv_head * (int)group + row % (int)group, high = sp.first + row / (int)group;
-    const int low = a.window ? (int)max((int64_t)high - (int64_t)a.window + 1, (int64_t)0) : 0;
+    const int head = kv_head * (int)group + row % (int)group;
     const T *q = (const T *)a.q + token * a.q_token + head * a.q_head;
     float top = -__builtin_inff(), sum = 0, o[4] = {0, 0, 0, 0};
-    to = min(to, high + 1);
-    for (int first = max(from, low); first < to; first += 64) {
+    to = min(to, reach.high + 1);
+    for (int first = max(from, reach.low); first < to; first += 64) {
         const int place = first + lane;
         const int32_t page = place < to ? a.table[sp.request * a.table_stride + (uint32_t)place / a.page_size] : -1;
         const bool there = page >= 0 && (uint32_t)page < a.pages;
@@ -145,12 +210,12 @@ __device__ void attend_row(const she_attend_pages_args &a, uint32_t group, const
                 if (lane + 64 * i < D) o[i] = fmaf(weight, (float)v[lane + 64 * i], o[i]);
         }
     }
-    const float inv = sp.parts > 1 ? 1.0f : sum == 0 ? 0.0f : 1.0f / sum;
-    if (sp.parts > 1 && lane == 0) pieces.ml[part] = float2{top, sum};
+    const float inv = cut ? 1.0f : sum == 0 ? 0.0f : 1.0f / sum;
+    if (cut && lane == 0) pieces.ml[part] = float2{top, sum};
     for (int i = 0; i < 4; i++) {
         const int d = lane + 64 * i;
         if (d >= D) continue;
-        if (sp.parts > 1) pieces.o[part * D + d] = o[i];
+        if (cut) pieces.o[part * D + d] = o[i];
         else ((T *)a.out)[token * a.out_token + head * a.out_head + d] = (T)(o[i] * inv);
     }
 }
@@ -161,8 +226,8 @@ __device__ void attend_row(const she_attend_pages_args &a, uint32_t group, const
 // Few rows: every wavefront walks places of its own, 32 a step, four steps of the workgroup side by side, straight from memory.  Lane
 // l reads d = 32 s + 8 (l/16) .. of the key of place l%16 for the scores, and EL elements from EL (l%16) on of the values of the
 // eight places that its scores belong to, whole rows over 16 lanes; the eight rows are transposed in registers.
-template <class T, int DP>
-__global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_few(she_attend_pages_args a, uint32_t group, Pieces pieces, uint32_t *d_bad)
+template <class T, int DP, Walk WALK>
+__global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_few(she_attend_pages_args a, uint32_t group, Pieces pieces, Owners owners, uint32_t *d_bad)
 {
     constexpr int EL = DP == 64 ? 4 : 8, NB = DP == 256 ? 2 : 1, KS = DP / 32;
     __shared__ int64_t rows[MOST_CHUNK];
@@ -171,19 +236,40 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
     __shared__ int any_bad, any_special;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, quarter = lane >> 4;
     const int kv_head = blockIdx.y, D = (int)a.head;
-    const Piece piece = find_piece(a.starts, a.requests, a.tokens, group, FEW_ROWS, blockIdx.x);
+    const Piece piece = tile_of<WALK>(a, owners, group, FEW_ROWS, blockIdx.x);
     if (piece.segment < 0) return;
-    const Span sp = span_of<FEW_ROWS>(a, group, piece, piece.index * FEW_ROWS, pieces);
-    if ((int)blockIdx.z >= max(sp.parts, 1)) return;
-    const int from = sp.from + (int)blockIdx.z * sp.chunk, count = sp.parts ? min(sp.chunk, sp.to - from) : 0;
-    if (tid == 0) any_bad = any_special = 0;
-    __syncthreads();
-    look_up(a, sp, kv_head, from, min(count, MOST_CHUNK), rows, &any_bad, d_bad);
+    Span sp = span_of<FEW_ROWS, WALK>(a, group, piece, piece.index * FEW_ROWS, pieces);
+    if ((int)blockIdx.z >= max(sp.parts, WALK == REQUESTS ? 1 : 0)) return;
+    const bool cut = WALK != REQUESTS || sp.parts > 1;
+    const uint32_t part = pieces.first + blockIdx.z;
+    int from = sp.from + (int)blockIdx.z * sp.chunk, count = sp.parts ? min(sp.chunk, sp.to - from) : 0;
 
     // this lane's row
     const int my_row = min(sp.row + col, sp.row + sp.rows - 1), my_token = my_row / (int)group, my_head = kv_head * (int)group + my_row % (int)group;
-    const int high = sp.first + my_token, low = a.window ? (int)max((int64_t)high - (int64_t)a.window + 1, (int64_t)0) : 0;
-    const int high_min = sp.first + sp.row / (int)group, low_max = a.window ? (int)max((int64_t)sp.first + (sp.row + sp.rows - 1) / (int)group - (int64_t)a.window + 1, (int64_t)0) : 0;
+    const Reach mine = reach_of<WALK>(a, owners, group, sp, my_row);
+    const int high = mine.high, low = mine.low;
+    int high_min = sp.first, low_max = 0;
+    if constexpr (WALK == PREFIXES) {
+        if (a.window) {                                           // requests in any order: the earliest and the latest place of the rows
+            int low_min = low;
+            low_max = low;
+#pragma unroll
+            for (int m = 1; m < 16; m *= 2) {
+                low_min = min(low_min, __shfl_xor(low_min, m));
+                low_max = max(low_max, __shfl_xor(low_max, m));
+            }
+            sp.low = low_min;
+            const int end = from + count;
+            from = max(from, low_min & ~31);
+            count = max(end - from, 0);
+        }
+    } else {
+        high_min = sp.first + sp.row / (int)group;
+        low_max = a.window ? (int)max((int64_t)sp.first + (sp.row + sp.rows - 1) / (int)group - (int64_t)a.window + 1, (int64_t)0) : 0;
+    }
+    if (tid == 0) any_bad = any_special = 0;
+    __syncthreads();
+    look_up(a, sp, kv_head, from, min(count, MOST_CHUNK), rows, &any_bad, d_bad);
     x8<T> q[KS];
     {
         const T *p = (const T *)a.q + (sp.token0 + my_token) * a.q_token + my_head * a.q_head + quarter * 8;
@@ -309,7 +395,8 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
     __syncthreads();
     if (any_special) {
         for (int r = wave; r < sp.rows; r += FEW_WAVES)
-            attend_row<T>(a, group, pieces, pieces_at(pieces, a.kv_heads, group, sp, sp.row + r, kv_head) + blockIdx.z, sp, kv_head, sp.row + r, from, from + count);
+            attend_row<T>(a, group, pieces, cut, pieces_at(pieces, a.kv_heads, group, sp, sp.row + r, kv_head) + part, sp, kv_head, sp.row + r,
+                          Reach{__shfl(low, r), __shfl(high, r)}, from, from + count);
         return;
     }
     constexpr int EACH = DP / 16;                                 // elements of a row that a thread joins
@@ -330,14 +417,14 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
     const int row = sp.row + r;
     const int64_t token = sp.token0 + row / (int)group;
     const int head = kv_head * (int)group + row % (int)group;
-    if (sp.parts <= 1) {
+    if (!cut) {
         const float inv = sum == 0 ? 0.0f : 1.0f / sum;
         T *to = (T *)a.out + token * a.out_token + head * a.out_head + d0;
 #pragma unroll
         for (int i = 0; i < EACH; i++)
             if (d0 + i < D) to[i] = (T)(o[i] * inv);
     } else {
-        const size_t at = pieces_at(pieces, a.kv_heads, group, sp, row, kv_head) + blockIdx.z;
+        const size_t at = pieces_at(pieces, a.kv_heads, group, sp, row, kv_head) + part;
         if (d0 == 0) pieces.ml[at] = float2{top, sum};
 #pragma unroll
         for (int i = 0; i < EACH; i++)
@@ -370,8 +457,8 @@ template <int DP> __device__ inline int value_unit(int place, int unit)
     return unit ^ (DP == 64 ? ((place >> 1) & 3) << 1 : (place & 7) << 1);
 }
 
-template <class T, int DP>
-__global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_tile(she_attend_pages_args a, uint32_t group, Pieces pieces, const void *zeros, uint32_t *d_bad)
+template <class T, int DP, Walk WALK>
+__global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_tile(she_attend_pages_args a, uint32_t group, Pieces pieces, Owners owners, const void *zeros, uint32_t *d_bad)
 {
     constexpr int UNITS = DP / 8, KS = DP / 16, DB = DP / 32, BLOCK = 4 * STEP;      // places that are looked up together
     constexpr int EACH = STEP * UNITS / (64 * TILE_WAVES);                           // units of either tile that a thread brings
@@ -384,20 +471,43 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
     // most to attend to: they come first.
     const int kv_head = blockIdx.x % a.kv_heads, D = (int)a.head;
     const uint32_t slot = gridDim.x / a.kv_heads - 1 - blockIdx.x / a.kv_heads;
-    const Piece piece = find_piece(a.starts, a.requests, a.tokens, group, TILE_ROWS, slot);
+    const Piece piece = tile_of<WALK>(a, owners, group, TILE_ROWS, slot);
     if (piece.segment < 0) return;
-    const Span sp = span_of<TILE_ROWS>(a, group, piece, piece.index * TILE_ROWS, pieces);
-    if ((int)blockIdx.z >= max(sp.parts, 1)) return;
-    const int from = sp.from + (int)blockIdx.z * sp.chunk, count = sp.parts ? min(sp.chunk, sp.to - from) : 0;
-    const int steps = (count + STEP - 1) / STEP;
+    Span sp = span_of<TILE_ROWS, WALK>(a, group, piece, piece.index * TILE_ROWS, pieces);
+    if ((int)blockIdx.z >= max(sp.parts, WALK == REQUESTS ? 1 : 0)) return;
+    const bool cut = WALK != REQUESTS || sp.parts > 1;
+    const uint32_t part = pieces.first + blockIdx.z;
+    int from = sp.from + (int)blockIdx.z * sp.chunk, count = sp.parts ? min(sp.chunk, sp.to - from) : 0;
 
     // this lane's row, and what the wavefront's rows attend to
     const int last_row = sp.row + sp.rows - 1, first_here = sp.row + wave * 32, last_here = min(first_here + 31, last_row);
     const int my_row = min(first_here + col, last_row), my_token = my_row / (int)group, my_head = kv_head * (int)group + my_row % (int)group;
-    const int64_t reach = a.window ? (int64_t)a.window - 1 : (int64_t)1 << 40;
-    const int high = sp.first + my_token, low = (int)max(high - reach, (int64_t)0);
-    const int high_min = sp.first + min(first_here, last_row) / (int)group, high_max = sp.first + last_here / (int)group;
-    const int low_min = (int)max(high_min - reach, (int64_t)0), low_max = (int)max(high_max - reach, (int64_t)0);
+    int high, low, high_min, high_max, low_min, low_max;
+    if constexpr (WALK == PREFIXES) {
+        const Reach mine = reach_of<WALK>(a, owners, group, sp, my_row);
+        high = high_min = high_max = mine.high;
+        low = low_min = low_max = mine.low;
+        if (a.window) {                                           // requests in any order: the earliest and the latest place of the rows
+            __shared__ int lows[TILE_WAVES];
+#pragma unroll
+            for (int m = 1; m < 32; m *= 2) {
+                low_min = min(low_min, __shfl_xor(low_min, m));
+                low_max = max(low_max, __shfl_xor(low_max, m));
+            }
+            if (lane == 0) lows[wave] = low_min;
+            __syncthreads();
+            for (int k = 0; k < TILE_WAVES; k++) sp.low = k ? min(sp.low, lows[k]) : lows[k];
+            const int end = from + count;
+            from = max(from, sp.low & ~31);
+            count = max(end - from, 0);
+        }
+    } else {
+        const int64_t reach = a.window ? (int64_t)a.window - 1 : (int64_t)1 << 40;
+        high = sp.first + my_token, low = (int)max(high - reach, (int64_t)0);
+        high_min = sp.first + min(first_here, last_row) / (int)group, high_max = sp.first + last_here / (int)group;
+        low_min = (int)max(high_min - reach, (int64_t)0), low_max = (int)max(high_max - reach, (int64_t)0);
+    }
+    const int steps = (count + STEP - 1) / STEP;
 
     // the rows of a block of places: thread tid has place BLOCK * b + tid, a wavefront a step
     auto page_of = [&](int b) {
@@ -548,22 +658,23 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
 
     if (__ballot(special)) {
         for (int row = first_here; row <= last_here; row++)
-            attend_row<T>(a, group, pieces, pieces_at(pieces, a.kv_heads, group, sp, row, kv_head) + blockIdx.z, sp, kv_head, row, from, from + count);
+            attend_row<T>(a, group, pieces, cut, pieces_at(pieces, a.kv_heads, group, sp, row, kv_head) + part, sp, kv_head, row,
+                          Reach{__shfl(low, row - first_here), __shfl(high, row - first_here)}, from, from + count);
         return;
     }
     l += __shfl_xor(l, 32);
     if (first_here + col > last_row) return;
     const int64_t token = sp.token0 + my_token;
-    const size_t at = pieces_at(pieces, a.kv_heads, group, sp, my_row, kv_head) + blockIdx.z;
-    const float inv = sp.parts > 1 ? 1.0f : l == 0 ? 0.0f : 1.0f / l;
-    if (sp.parts > 1 && half == 0) pieces.ml[at] = float2{m, l};
+    const size_t at = pieces_at(pieces, a.kv_heads, group, sp, my_row, kv_head) + part;
+    const float inv = cut ? 1.0f : l == 0 ? 0.0f : 1.0f / l;
+    if (cut && half == 0) pieces.ml[at] = float2{m, l};
 #pragma unroll
     for (int b = 0; b < DB; b++)
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
             const int d = b * 32 + 2 * i + 4 * half;
             if (d >= D) continue;
-            if (sp.parts > 1) {
+            if (cut) {
                 *reinterpret_cast<f32x4 *>(pieces.o + at * D + d) = f32x4{acc[b][i], acc[b][i + 1], acc[b][i + 2], acc[b][i + 3]};
             } else {
                 T *to = (T *)a.out + token * a.out_token + my_head * a.out_head + d;
@@ -581,12 +692,17 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
 // JOIN_AHEAD at a time.  A token over 32768 places, 4 rows of 64 pieces at 8 key heads, takes 33 us so on one input again and again (38 on
 // others in turn), 43 with four rows a workgroup and 78 with a row a wavefront.
 constexpr int JOIN_AHEAD = 4;
+// A row's pieces in order: the first `near` one after the other, and the others `gap` further on.
+struct Order {
+    int parts, near, gap;
+    __device__ size_t operator[](int k) const { return (size_t)(k + (k >= near ? gap : 0)); }
+};
 template <class T>
-__device__ inline void join_row(const she_attend_pages_args &a, const Pieces &w, size_t at, int parts, int from, int by, float &sum, float o[4])
+__device__ inline void join_row(const she_attend_pages_args &a, const Pieces &w, size_t at, const Order &order, int from, int by, float &sum, float o[4])
 {
-    const int lane = threadIdx.x & 63, D = (int)a.head;
+    const int lane = threadIdx.x & 63, D = (int)a.head, parts = order.parts;
     float top = -__builtin_inff();
-    for (int k = lane; k < parts; k += 64) top = fmaxf(top, w.ml[at + k].x);
+    for (int k = lane; k < parts; k += 64) top = fmaxf(top, w.ml[at + order[k]].x);
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
     sum = 0;
@@ -598,9 +714,9 @@ __device__ inline void join_row(const she_attend_pages_args &a, const Pieces &w,
 #pragma unroll
         for (int e = 0; e < JOIN_AHEAD; e++) {
             const int k = k0 + by * e;
-            ml[e] = k < parts ? w.ml[at + k] : float2{-__builtin_inff(), 0};
+            ml[e] = k < parts ? w.ml[at + order[k]] : float2{-__builtin_inff(), 0};
 #pragma unroll
-            for (int i = 0; i < 4; i++) v[e][i] = k < parts && lane + 64 * i < D ? w.o[(at + k) * D + lane + 64 * i] : 0.0f;
+            for (int i = 0; i < 4; i++) v[e][i] = k < parts && lane + 64 * i < D ? w.o[(at + order[k]) * D + lane + 64 * i] : 0.0f;
         }
 #pragma unroll
         for (int e = 0; e < JOIN_AHEAD; e++) {
@@ -611,8 +727,23 @@ __device__ inline void join_row(const she_attend_pages_args &a, const Pieces &w,
         }
     }
 }
-template <class T, int ROWS>
-__global__ __launch_bounds__(256) void k_attend_join(she_attend_pages_args a, uint32_t group, Pieces pieces, int each)
+// The pieces of the prefix that request r has, none if it has none.
+__device__ inline int prefix_parts(const she_attend_pages_args &a, const Owners &owners, const Pieces &prefix, int r)
+{
+    const int lane = threadIdx.x & 63;
+    int found = 0;
+    for (uint32_t g0 = 0; g0 < owners.prefixes; g0 += 64) {
+        const bool before = g0 + lane < owners.prefixes && owner_start(owners, (int)g0 + lane) <= r;
+        const int n = __popcll(__ballot(before));
+        found += n;
+        if (n < 64) break;
+    }
+    if (!found || r >= owner_start(owners, found)) return 0;
+    const int places = prefix_places(a, owners.prefix_lengths[found - 1], owners.prefix_width);
+    return places ? (places - 1) / (int)prefix_chunk(places, prefix) + 1 : 0;
+}
+template <class T, int ROWS, Walk WALK>
+__global__ __launch_bounds__(256) void k_attend_join(she_attend_pages_args a, uint32_t group, Pieces pieces, Pieces prefix, Owners owners, int each)
 {
     __shared__ float sums[4], joined[4][256];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = (int)a.head;
@@ -620,23 +751,33 @@ __global__ __launch_bounds__(256) void k_attend_join(she_attend_pages_args a, ui
     if (piece.segment < 0) return;
     const int64_t first = piece.first + (int64_t)piece.index * ROWS + blockIdx.z * each;
     if (first >= piece.last) return;
-    const Span sp = span_of<ROWS>(a, group, piece, piece.index * ROWS, pieces);
-    const int parts = sp.parts, rows = (int)min((int64_t)each, piece.last - first);
-    if (parts <= 1) return;
-    for (int r = parts <= JOIN_AHEAD ? wave : 0; r < rows; r += parts <= JOIN_AHEAD ? 4 : 1) {
+    const Span sp = span_of<ROWS, WALK>(a, group, piece, piece.index * ROWS, pieces);
+    const int rows = (int)min((int64_t)each, piece.last - first);
+    Order order{sp.parts, sp.parts, 0};
+    if constexpr (WALK == REQUESTS) {
+        if (order.parts <= 1) return;
+    } else {
+        order.near = prefix_parts(a, owners, prefix, piece.segment);
+        order.parts += order.near;
+        order.gap = (int)pieces.first - order.near;
+    }
+    const bool few = order.parts <= JOIN_AHEAD;
+    for (int r = few ? wave : 0; r < rows; r += few ? 4 : 1) {
         const int64_t row = first + r, token = row / group;
-        const int head = blockIdx.y * (int)group + (int)(row % group);
-        const size_t at = pieces_at(pieces, a.kv_heads, group, sp, sp.row + (int)blockIdx.z * each + r, blockIdx.y);
+        const int head = blockIdx.y * (int)group + (int)(row % group), in_request = sp.row + (int)blockIdx.z * each + r;
+        const size_t at = pieces_at(pieces, a.kv_heads, group, sp, in_request, blockIdx.y);
         T *to = (T *)a.out + token * a.out_token + head * a.out_head;
+        // behind a prefix, a token without a place of its own attends to nothing
+        const bool none = WALK == BEHIND && sp.first + in_request / (int)group < 0;
         float sum, o[4];
-        if (parts <= JOIN_AHEAD) {
-            join_row<T>(a, pieces, at, parts, 0, 1, sum, o);
+        if (few) {
+            join_row<T>(a, pieces, at, order, 0, 1, sum, o);
 #pragma unroll
             for (int i = 0; i < 4; i++)
-                if (lane + 64 * i < D) to[lane + 64 * i] = (T)(o[i] * (sum == 0 ? 0.0f : 1.0f / sum));
+                if (lane + 64 * i < D) to[lane + 64 * i] = none ? (T)0.0f : (T)(o[i] * (sum == 0 ? 0.0f : 1.0f / sum));
             continue;
         }
-        join_row<T>(a, pieces, at, parts, wave, 4, sum, o);
+        join_row<T>(a, pieces, at, order, wave, 4, sum, o);
         if (r) __syncthreads();
         if (lane == 0) sums[wave] = sum;
 #pragma unroll
@@ -644,32 +785,54 @@ __global__ __launch_bounds__(256) void k_attend_join(she_attend_pages_args a, ui
         __syncthreads();
         const int d = threadIdx.x;
         sum = sums[0] + sums[1] + sums[2] + sums[3];
-        if (d < D) to[d] = (T)((joined[0][d] + joined[1][d] + joined[2][d] + joined[3][d]) * (sum == 0 ? 0.0f : 1.0f / sum));
+        if (d < D) to[d] = none ? (T)0.0f : (T)((joined[0][d] + joined[1][d] + joined[2][d] + joined[3][d]) * (sum == 0 ? 0.0f : 1.0f / sum));
     }
 }
 
-template <class T, int DP> hipError_t attend_rows(const she_attend_pages_args &a, const AttendShape &s, const Pieces &pieces, uint32_t *d_bad, hipStream_t st)
+template <class T, int DP, Walk WALK>
+hipError_t walk(const she_attend_pages_args &a, const AttendShape &s, const Pieces &pieces, const Owners &owners, uint32_t *d_bad, hipStream_t st)
 {
     const uint32_t group = a.q_heads / a.kv_heads, slots = (uint32_t)s.slots;
     if (s.few)
-        k_attend_few<T, DP><<<dim3(slots, a.kv_heads, s.splits), 64 * FEW_WAVES, 0, st>>>(a, group, pieces, d_bad);
+        k_attend_few<T, DP, WALK><<<dim3(slots, a.kv_heads, s.splits), 64 * FEW_WAVES, 0, st>>>(a, group, pieces, owners, d_bad);
     else
-        k_attend_tile<T, DP><<<dim3(slots * a.kv_heads, 1, s.splits), 64 * TILE_WAVES, 0, st>>>(a, group, pieces, zeros_of(d_bad), d_bad);
+        k_attend_tile<T, DP, WALK><<<dim3(slots * a.kv_heads, 1, s.splits), 64 * TILE_WAVES, 0, st>>>(a, group, pieces, owners, zeros_of(d_bad), d_bad);
+    return hipGetLastError();
+}
+template <class T, Walk WALK>
+hipError_t walk(const she_attend_pages_args &a, const AttendShape &s, const Pieces &pieces, const Owners &owners, uint32_t *d_bad, hipStream_t st)
+{
+    return a.head <= 64 ? walk<T, 64, WALK>(a, s, pieces, owners, d_bad, st) : a.head <= 128 ? walk<T, 128, WALK>(a, s, pieces, owners, d_bad, st)
+                                                                                            : walk<T, 256, WALK>(a, s, pieces, owners, d_bad, st);
+}
+template <class T, Walk WALK>
+hipError_t join(const she_attend_pages_args &a, const AttendShape &s, uint32_t most, const Pieces &pieces, const Pieces &prefix, const Owners &owners, hipStream_t st)
+{
+    const uint32_t group = a.q_heads / a.kv_heads, slots = (uint32_t)s.slots;
+    const int each = s.few && most > 4 * JOIN_AHEAD ? 1 : s.few || most > JOIN_AHEAD ? 4 : 16;
+    if (s.few)
+        k_attend_join<T, FEW_ROWS, WALK><<<dim3(slots, a.kv_heads, FEW_ROWS / each), 256, 0, st>>>(a, group, pieces, prefix, owners, each);
+    else
+        k_attend_join<T, TILE_ROWS, WALK><<<dim3(slots, a.kv_heads, TILE_ROWS / each), 256, 0, st>>>(a, group, pieces, prefix, owners, each);
     return hipGetLastError();
 }
 
 template <class T> hipError_t attend(const she_attend_pages_args &a, const AttendShape &s, const Pieces &pieces, uint32_t *d_bad, hipStream_t st)
 {
-    const hipError_t rc = a.head <= 64 ? attend_rows<T, 64>(a, s, pieces, d_bad, st) : a.head <= 128 ? attend_rows<T, 128>(a, s, pieces, d_bad, st)
-                                                                                                     : attend_rows<T, 256>(a, s, pieces, d_bad, st);
+    const hipError_t rc = walk<T, REQUESTS>(a, s, pieces, Owners{}, d_bad, st);
     if (rc != hipSuccess || s.splits == 1) return rc;
-    const uint32_t group = a.q_heads / a.kv_heads, slots = (uint32_t)s.slots;
-    const int each = s.few && s.splits > 4 * JOIN_AHEAD ? 1 : s.few || s.splits > JOIN_AHEAD ? 4 : 16;
-    if (s.few)
-        k_attend_join<T, FEW_ROWS><<<dim3(slots, a.kv_heads, FEW_ROWS / each), 256, 0, st>>>(a, group, pieces, each);
-    else
-        k_attend_join<T, TILE_ROWS><<<dim3(slots, a.kv_heads, TILE_ROWS / each), 256, 0, st>>>(a, group, pieces, each);
-    return hipGetLastError();
+    return join<T, REQUESTS>(a, s, s.splits, pieces, Pieces{}, Owners{}, st);
+}
+
+template <class T>
+hipError_t attend_shared(const she_attend_pages_args &of_prefixes, const she_attend_pages_args &behind, const SharedShape &s, const Pieces &prefix, const Pieces &pieces,
+                         const Owners &owners, uint32_t *d_bad, hipStream_t st)
+{
+    hipError_t rc = hipSuccess;
+    if (owners.prefixes) rc = walk<T, PREFIXES>(of_prefixes, s.prefix, prefix, owners, d_bad, st);
+    if (rc == hipSuccess) rc = walk<T, BEHIND>(behind, s.behind, pieces, owners, d_bad, st);
+    if (rc == hipSuccess) rc = join<T, BEHIND>(behind, s.behind, prefix.splits, pieces, prefix, owners, st);
+    return rc;
 }
 
 }  // namespace
@@ -677,8 +840,19 @@ template <class T> hipError_t attend(const she_attend_pages_args &a, const Atten
 hipError_t launch_attend_pages(const she_attend_pages_args &a, const AttendShape &s, void *scratch, uint32_t *d_bad, hipStream_t st)
 {
     float *o = static_cast<float *>(scratch);
-    const Pieces pieces{o, reinterpret_cast<float2 *>(o + attend_pieces(a, s) * a.head), s.splits, s.chunk};
+    const Pieces pieces{o, reinterpret_cast<float2 *>(o + attend_pieces(a, s) * a.head), s.splits, 0, s.splits, s.chunk};
     return a.type == SHE_BF16 ? attend<__bf16>(a, s, pieces, d_bad, st) : attend<_Float16>(a, s, pieces, d_bad, st);
+}
+
+hipError_t launch_attend_shared(const she_attend_shared_args &a, const SharedShape &s, void *scratch, uint32_t *d_bad, hipStream_t st)
+{
+    float *o = static_cast<float *>(scratch);
+    const uint32_t splits = s.prefix.splits + s.behind.splits;
+    float2 *ml = reinterpret_cast<float2 *>(o + (size_t)a.tokens * a.q_heads * splits * a.head);
+    const Pieces prefix{o, ml, splits, 0, s.prefix.splits, s.prefix.chunk}, pieces{o, ml, splits, s.prefix.splits, s.behind.splits, s.behind.chunk};
+    const Owners owners{a.prefix_requests, a.prefix_lengths, a.lengths, a.requests, a.prefixes, a.prefix_width};
+    return a.type == SHE_BF16 ? attend_shared<__bf16>(shared_prefixes(a), shared_behind(a), s, prefix, pieces, owners, d_bad, st)
+                              : attend_shared<_Float16>(shared_prefixes(a), shared_behind(a), s, prefix, pieces, owners, d_bad, st);
 }
 
 }}  // namespace she::clear

@@ -74,4 +74,71 @@ size_t attend_scratch(const she_attend_pages_args &a, const AttendShape &s)
     return attend_pieces(a, s) * (a.head * sizeof(float) + sizeof(float2));
 }
 
+she_attend_pages_args shared_behind(const she_attend_shared_args &a)
+{
+    she_attend_pages_args b{};
+    b.type = a.type;
+    b.tokens = a.tokens;
+    b.requests = a.requests;
+    b.q_heads = a.q_heads;
+    b.kv_heads = a.kv_heads;
+    b.head = a.head;
+    b.window = a.window;
+    b.scale = a.scale;
+    b.q = a.q;
+    b.q_token = a.q_token;
+    b.q_head = a.q_head;
+    b.k_pages = a.k_pages;
+    b.v_pages = a.v_pages;
+    b.page_stride = a.page_stride;
+    b.slot_stride = a.slot_stride;
+    b.page_head = a.page_head;
+    b.pages = a.pages;
+    b.page_size = a.page_size;
+    b.table = a.table;
+    b.table_stride = a.table_stride;
+    b.table_width = a.table_width;
+    b.starts = a.starts;
+    b.lengths = a.lengths;
+    b.out = a.out;
+    b.out_token = a.out_token;
+    b.out_head = a.out_head;
+    return b;
+}
+
+she_attend_pages_args shared_prefixes(const she_attend_shared_args &a)
+{
+    she_attend_pages_args b = shared_behind(a);
+    b.requests = a.prefixes;
+    b.table = a.prefix_table;
+    b.table_stride = a.prefix_stride;
+    b.table_width = a.prefix_width;
+    b.lengths = a.prefix_lengths;
+    return b;
+}
+
+SharedShape shared_shape(const she_attend_shared_args &a, uint32_t cus)
+{
+    SharedShape s{};
+    s.behind = attend_shape(shared_behind(a), cus);
+    if (!cus) cus = 1;
+    const uint64_t group = a.q_heads / a.kv_heads, rows = a.tokens * group, places = (uint64_t)a.prefix_width * a.page_size;
+    if (!a.prefixes) return s;
+    // rows of a prefix: the host knows their average
+    const uint64_t each = ceil_div(rows, a.prefixes);
+    s.prefix.few = each <= FEW_ROWS || each * places <= 1u << 18;
+    const uint64_t tile = s.prefix.few ? FEW_ROWS : TILE_ROWS;
+    s.prefix.slots = a.prefixes == 1 ? ceil_div(rows, tile) : rows / tile + a.prefixes;
+    const uint64_t at_once = s.prefix.few ? 2 * cus : cus * (a.head <= 64 ? 3 : a.head <= 128 ? 2 : 1);
+    const uint64_t tiles = a.prefixes * ceil_div(each, tile) * a.kv_heads;
+    s.prefix.chunk = s.prefix.few ? 256 : 512;
+    s.prefix.splits = (uint32_t)std::max<uint64_t>(1, std::min(ceil_div(places, s.prefix.chunk), at_once / tiles));
+    return s;
+}
+
+size_t shared_scratch(const she_attend_shared_args &a, const SharedShape &s)
+{
+    return (size_t)a.tokens * a.q_heads * (s.prefix.splits + s.behind.splits) * (a.head * sizeof(float) + sizeof(float2));
+}
+
 }}  // namespace she::clear

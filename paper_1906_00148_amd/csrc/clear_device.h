@@ -180,13 +180,14 @@ __device__ inline int64_t bounded_start(const int32_t *starts, int s, uint32_t t
     const int32_t v = starts[s];
     return v < 0 ? 0 : (uint32_t)v > tokens ? tokens : v;
 }
-__device__ inline Piece find_piece(const int32_t *starts, uint32_t segments, uint32_t tokens, uint32_t scale, uint32_t tile, uint32_t slot)
+// `start_of(s)`: where segment s starts, inside [0, tokens] whatever it is read from.
+template <class F> __device__ inline Piece find_piece_by(F start_of, uint32_t segments, uint32_t scale, uint32_t tile, uint32_t slot)
 {
     const int lane = threadIdx.x & 63;
     int found = 0;
     for (uint32_t s0 = 0; s0 < segments; s0 += 64) {
         const uint32_t s = s0 + lane;
-        const bool before = s < segments && bounded_start(starts, (int)s, tokens) * scale / tile + s <= slot;
+        const bool before = s < segments && start_of((int)s) * scale / tile + s <= slot;
         const int n = __popcll(__ballot(before));
         found += n;
         if (n < 64) break;
@@ -194,7 +195,7 @@ __device__ inline Piece find_piece(const int32_t *starts, uint32_t segments, uin
     Piece p{-1, 0, 0, 0};
     if (!found) return p;
     const int s = __builtin_amdgcn_readfirstlane(found - 1);
-    const int64_t a = bounded_start(starts, s, tokens), b = bounded_start(starts, s + 1, tokens);
+    const int64_t a = start_of(s), b = start_of(s + 1);
     const int64_t index = (int64_t)slot - (a * scale / tile + s);
     if (b > a && index >= 0 && index * tile < (b - a) * scale) {
         p.segment = s;
@@ -203,6 +204,10 @@ __device__ inline Piece find_piece(const int32_t *starts, uint32_t segments, uin
         p.last = b * scale;
     }
     return p;
+}
+__device__ inline Piece find_piece(const int32_t *starts, uint32_t segments, uint32_t tokens, uint32_t scale, uint32_t tile, uint32_t slot)
+{
+    return find_piece_by([=](int s) { return bounded_start(starts, s, tokens); }, segments, scale, tile, slot);
 }
 
 }}  // namespace she::clear

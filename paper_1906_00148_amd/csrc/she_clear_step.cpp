@@ -25,6 +25,37 @@ try {
     return SHE_OK;
 } SHE_NOTHROW(c)
 
+int she_attend_shared(she_ctx *c, const she_attend_shared_args *args)
+try {
+    if (!c) return SHE_EINVAL;
+    if (!args) return fail(c, SHE_EINVAL, "null argument");
+    const she_attend_shared_args a = *args;
+    const std::string at = "she_attend_shared: ";
+    if (!half_type(a.type)) return fail(c, SHE_EINVAL, at + "type must be SHE_BF16 or SHE_F16");
+    if (!a.q_heads || !a.kv_heads || !a.head || !a.page_size) return fail(c, SHE_EINVAL, at + "a size is zero");
+    if (a.q_heads % a.kv_heads) return fail(c, SHE_EINVAL, at + "q_heads must be a multiple of kv_heads");
+    if (a.head % 8 || a.head > 256) return fail(c, SHE_EINVAL, at + "head must be a multiple of 8, at most 256");
+    if (a.q_heads > 65535 || a.tokens > MOST_TOKENS || a.requests > MOST_TOKENS || a.prefixes > MOST_SEGMENTS ||
+        (uint64_t)a.table_width * a.page_size > MOST_PLACES || (uint64_t)a.prefix_width * a.page_size > MOST_PLACES ||
+        (uint64_t)a.tokens * (a.q_heads / a.kv_heads) > 0x7FFFFFFF)
+        return fail(c, SHE_ERANGE, at + "at most 2^24 tokens and requests, 2^20 prefixes, 65535 heads, 2^26 places of a request or prefix and 2^31 rows of a key head");
+    if (!a.tokens || !a.requests) return SHE_OK;
+    if (!a.q || !a.out || !a.starts || !a.lengths || (a.table_width && !a.table) || (a.prefixes && (!a.prefix_requests || !a.prefix_lengths)) ||
+        (a.prefixes && a.prefix_width && !a.prefix_table) || ((a.table_width || (a.prefixes && a.prefix_width)) && (!a.k_pages || !a.v_pages)))
+        return fail(c, SHE_EINVAL, at + "null argument");
+    if (!on16(a.q) || !on16(a.k_pages) || !on16(a.v_pages) || !on16(a.out) ||
+        (a.q_token | a.q_head | a.page_stride | a.slot_stride | a.page_head | a.out_token | a.out_head) % 8)
+        return fail(c, SHE_EINVAL, at + "rows must start on 16 bytes");
+    int rc = ready(c);
+    if (rc) return rc;
+    const SharedShape s = shared_shape(a, c->dk.cus);
+    for (const AttendShape &w : {s.prefix, s.behind})
+        if ((w.few ? w.slots : w.slots * a.kv_heads) > MOST_GROUPS) return fail(c, SHE_ERANGE, at + "too many tokens and requests for one call");
+    if ((rc = ensure_scratch(c, shared_scratch(a, s)))) return rc;
+    HIP_TRY(c, launch_attend_shared(a, s, c->clear.scratch(), c->clear.d_bad, c->stream));
+    return SHE_OK;
+} SHE_NOTHROW(c)
+
 int she_sample(she_ctx *c, const she_sample_args *args)
 try {
     if (!c) return SHE_EINVAL;

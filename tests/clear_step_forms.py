@@ -5,6 +5,8 @@ from itertools import accumulate
 import numpy as np
 import torch
 
+import clear_forms as C
+
 F32 = 2.0 ** -24
 LAST = 2 ** 31 - 1
 
@@ -76,3 +78,47 @@ def sample(logits, uniform, temperature=None, top_k=None, top_p=None, min_p=None
     got = [sample_row(x[r], float(uniform[r]), *(v[r] for v in settings)) for r in range(rows)]
     probs = torch.tensor([p for _, p in got], dtype=torch.float64)
     return torch.tensor([t for t, _ in got], dtype=torch.int32), probs, probs * (F32 + 2.0 ** -50 + vocab * 2.0 ** -44) + 2.0 ** -149
+
+
+def shared(q, k_pages, v_pages, table, starts, lengths, prefix_table, prefix_requests, prefix_lengths, scale, window=0):
+    """(out, bound), with the bound of clear_forms.attend.  Only what a token attends to is looked at."""
+    dtype = q.dtype
+    T, Hq, D = q.shape
+    pages, size, Hkv = k_pages.shape[:3]
+    q, k_pages, v_pages = C.cpu(q), C.cpu(k_pages), C.cpu(v_pages)
+    starts, lengths, ranges, prefixes = (t.tolist() for t in (starts, lengths, prefix_requests, prefix_lengths))
+    table, prefix_table = table.tolist(), prefix_table.tolist()
+    out, bound = torch.zeros(T, Hq, D, dtype=torch.float64), torch.zeros(T, Hq, D, dtype=torch.float64)
+
+    def there(row, count):
+        return [(u, row[u // size], u % size) for u in range(min(count, len(row) * size)) if 0 <= row[u // size] < pages]
+    for r, length in enumerate(lengths):
+        b, e = starts[r], starts[r + 1]
+        if e <= b:
+            continue
+        g = next((g for g in range(len(prefixes)) if ranges[g] <= r < ranges[g + 1]), None)
+        P = 0 if g is None else max(prefixes[g], 0)
+        found = ([] if g is None else there(prefix_table[g], P)) + [(P + u, page, slot) for u, page, slot in there(table[r], length)]
+        place, page, slot = (torch.tensor([f[i] for f in found], dtype=torch.long) for i in range(3))
+        k, v = k_pages[page, slot], v_pages[page, slot]                                # [places, Hkv, D]
+        for t in range(b, e):
+            p = length - (e - b) + (t - b)
+            if p < 0:
+                continue
+            mine = place <= P + p
+            if window:
+                mine &= place > P + p - window
+            if not mine.any():
+                continue
+            km = k[mine].repeat_interleave(Hq // Hkv, 1).transpose(0, 1)               # [Hq, n, D]
+            vm = v[mine].repeat_interleave(Hq // Hkv, 1).transpose(0, 1)
+            s = scale * (km @ q[t][:, :, None])[..., 0]
+            w = torch.softmax(s, -1)
+            out[t] = (w[:, None] @ vm)[:, 0]
+            ds = (D + 8) * F32 * (abs(scale) * (km.abs() @ q[t].abs()[:, :, None])[..., 0]).amax(-1) + 4 * F32 * s.abs().amax(-1)
+            n = mine.sum().item()
+            unit = C.UNIT[dtype] + 2 * ds + (2 * n + 32) * F32
+            bound[t] = unit[:, None] * (w[:, None] @ vm.abs())[:, 0]
+            if dtype is torch.float16:
+                bound[t] += 2.0 ** -25 * vm.abs().sum(1)
+    return out, bound

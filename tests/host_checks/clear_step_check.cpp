@@ -12,6 +12,9 @@ static hipError_t launched() { launches++; return fake::step(); }
 namespace she { namespace clear {
 size_t plan_scratch(const she_plan_pages_args &) { return wanted; }
 hipError_t launch_plan_pages(const she_plan_pages_args &, void *, uint32_t *, hipStream_t) { return launched(); }
+SharedShape shared_shape(const she_attend_shared_args &a, uint32_t) { SharedShape s{}; s.prefix.slots = a.prefixes; s.behind.slots = a.requests; return s; }
+size_t shared_scratch(const she_attend_shared_args &, const SharedShape &) { return wanted; }
+hipError_t launch_attend_shared(const she_attend_shared_args &, const SharedShape &, void *, uint32_t *, hipStream_t) { return launched(); }
 hipError_t launch_sample(const she_sample_args &, uint32_t, hipStream_t) { return launched(); }
 }}
 
@@ -88,14 +91,52 @@ int main()
     s.rows = 3;
     CHECK(she_sample(c, nullptr) == SHE_EINVAL && she_sample(nullptr, &s) == SHE_EINVAL, "null struct or context\n");
 
+    she_attend_shared_args t{};
+    t.type = SHE_F16; t.tokens = 2; t.requests = 1; t.q_heads = 4; t.kv_heads = 2; t.head = 64; t.page_size = 16; t.pages = 4; t.table_width = 3;
+    t.prefixes = 1; t.prefix_width = 5; t.q = t.k_pages = t.v_pages = t.out = mem;
+    t.table = t.starts = t.lengths = t.prefix_table = t.prefix_requests = t.prefix_lengths = ints;
+    t.q_token = t.out_token = 256; t.q_head = t.out_head = t.page_head = 64; t.slot_stride = 128; t.page_stride = 2048;
+    EXPECT(she_attend_shared, t, SHE_OK, (void)a);
+    EXPECT(she_attend_shared, t, SHE_OK, a.table_width = 0; a.table = nullptr);
+    EXPECT(she_attend_shared, t, SHE_OK, a.prefix_width = 0; a.prefix_table = nullptr);
+    EXPECT(she_attend_shared, t, SHE_OK, a.prefixes = 0; a.prefix_table = a.prefix_requests = a.prefix_lengths = nullptr);
+    EXPECT(she_attend_shared, t, SHE_OK, a.prefix_width = a.table_width = 0; a.prefix_table = a.table = nullptr; a.k_pages = a.v_pages = nullptr);
+    EXPECT(she_attend_shared, t, SHE_EINVAL, a.type = SHE_F32);
+    EXPECT(she_attend_shared, t, SHE_EINVAL, a.q_heads = 5);
+    EXPECT(she_attend_shared, t, SHE_EINVAL, a.kv_heads = 0);
+    EXPECT(she_attend_shared, t, SHE_EINVAL, a.head = 60);
+    EXPECT(she_attend_shared, t, SHE_EINVAL, a.head = 264);
+    EXPECT(she_attend_shared, t, SHE_EINVAL, a.page_size = 0);
+    EXPECT(she_attend_shared, t, SHE_ERANGE, a.table_width = 1u << 23);
+    EXPECT(she_attend_shared, t, SHE_ERANGE, a.prefix_width = 1u << 23);
+    EXPECT(she_attend_shared, t, SHE_ERANGE, a.requests = (1u << 24) + 1);
+    EXPECT(she_attend_shared, t, SHE_ERANGE, a.prefixes = (1u << 20) + 1);
+    EXPECT(she_attend_shared, t, SHE_ERANGE, a.tokens = 1u << 24; a.q_heads = 1024);
+    EXPECT(she_attend_shared, t, SHE_EINVAL, a.q = (char *)a.q + 8);
+    EXPECT(she_attend_shared, t, SHE_EINVAL, a.page_head = 60);
+    EXPECT(she_attend_shared, t, SHE_EINVAL, a.out_token = 252);
+    EXPECT(she_attend_shared, t, SHE_EINVAL, a.lengths = nullptr);
+    EXPECT(she_attend_shared, t, SHE_EINVAL, a.starts = nullptr);
+    EXPECT(she_attend_shared, t, SHE_EINVAL, a.table = nullptr);
+    EXPECT(she_attend_shared, t, SHE_EINVAL, a.prefix_table = nullptr);
+    EXPECT(she_attend_shared, t, SHE_EINVAL, a.prefix_requests = nullptr);
+    EXPECT(she_attend_shared, t, SHE_EINVAL, a.prefix_lengths = nullptr);
+    EXPECT(she_attend_shared, t, SHE_EINVAL, a.v_pages = nullptr);
+    EXPECT(she_attend_shared, t, SHE_EINVAL, a.out = nullptr);
+    launches = 0;
+    t.tokens = 0;
+    CHECK(she_attend_shared(c, &t) == SHE_OK && !launches, "no tokens\n");
+    t.tokens = 2;
+    CHECK(she_attend_shared(c, nullptr) == SHE_EINVAL && she_attend_shared(nullptr, &t) == SHE_EINVAL, "null struct or context\n");
+
     // while the stream is captured, a call that would allocate is refused
     capturing = hipStreamCaptureStatusActive;
     wanted = 500;
-    CHECK(she_plan_pages(c, &p) == SHE_ENOMEM, "a capture with scratch to allocate\n");
+    CHECK(she_plan_pages(c, &p) == SHE_ENOMEM && she_attend_shared(c, &t) == SHE_ENOMEM, "a capture with scratch to allocate\n");
     capturing = hipStreamCaptureStatusNone;
     CHECK(she_plan_pages(c, &p) == SHE_OK, "scratch\n");
     capturing = hipStreamCaptureStatusActive;
-    CHECK(she_plan_pages(c, &p) == SHE_OK && she_sample(c, &s) == SHE_OK, "a capture within the scratch\n");
+    CHECK(she_plan_pages(c, &p) == SHE_OK && she_attend_shared(c, &t) == SHE_OK && she_sample(c, &s) == SHE_OK, "a capture within the scratch\n");
     capturing = hipStreamCaptureStatusNone;
     she_free(c);
     CHECK(fake::held == 0, "%zu bytes are still held\n", fake::held);
