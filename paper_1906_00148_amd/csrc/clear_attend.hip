@@ -15,6 +15,7 @@
 // Masks: a place that no row of the tile attends to is not read at all.  A place that some rows attend to and others do not has weight
 // 0 for the others, which a matrix instruction multiplies with the value all the same.  So where some of such places' values are
 // infinite or NaN, the tile's rows are done again, one by one and over the places that they attend to alone.
+#include <algorithm>
 #include <type_traits>
 
 #include "clear_device.h"
@@ -26,9 +27,12 @@ namespace {
 constexpr int FEW_WAVES = 4, TILE_WAVES = TILE_ROWS / 32;
 constexpr float LOG2E = 1.4426950408889634f;
 
-// What a kernel walks: a call's requests, or in a call with shared prefixes these, each as a request of all tokens that have it, or what
-// the requests have behind them.
-enum Walk { REQUESTS, PREFIXES, BEHIND };
+// What a kernel walks: a call's requests; or in a call with shared prefixes these, each as a request of all tokens that have it, or what
+// the requests have behind them, or both as one, where a request has so many rows that sharing saves nothing.
+enum Walk { REQUESTS, PREFIXES, BEHIND, WHOLE };
+// The first and the last of them write results, or pieces where a tile is cut; the others, which are joined, pieces only, all of them.
+constexpr bool joined_with_another(Walk walk) { return walk == PREFIXES || walk == BEHIND; }
+constexpr float NOTHING = -1;            // in place of a sum: a token that attends to nothing at all, prefix or not
 
 // What is left behind of the pieces of cut rows: [rows of all requests][kv_heads][splits].
 struct Pieces {
@@ -39,16 +43,36 @@ struct Pieces {
     uint32_t chunk;                      // places of a piece, unless a tile has more than `most` such pieces
 };
 
-// What the walk over prefixes knows of the requests: its own arguments have prefixes for requests.
+// What a call with shared prefixes has beside the arguments of a walk: over prefixes these have prefixes for requests, otherwise the requests.
 struct Owners {
     const int32_t *requests;             // [prefixes + 1]
     const int32_t *prefix_lengths;       // [prefixes]
     const int32_t *lengths;              // [count]
+    const int32_t *prefix_table;
+    int64_t prefix_stride;
     uint32_t count, prefixes, prefix_width;
 };
 __device__ inline int owner_start(const Owners &w, int g)
 {
     return min(max(w.requests[g], 0), (int)w.count);
+}
+// The prefix of request r, or -1.
+__device__ inline int prefix_of(const Owners &owners, int r)
+{
+    const int lane = threadIdx.x & 63;
+    int found = 0;
+    for (uint32_t g0 = 0; g0 < owners.prefixes; g0 += 64) {
+        const bool before = g0 + lane < owners.prefixes && owner_start(owners, (int)g0 + lane) <= r;
+        const int n = __popcll(__ballot(before));
+        found += n;
+        if (n < 64) break;
+    }
+    return __builtin_amdgcn_readfirstlane(found && r < owner_start(owners, found) ? found - 1 : -1);
+}
+// Of a prefix's places, those that its table has a column for.
+__device__ inline int prefix_places(const she_attend_pages_args &a, int length, uint32_t width)
+{
+    return (int)min((int64_t)max(length, 0), (int64_t)width * a.page_size);
 }
 
 // A tile of rows and the places that any of them attends to.
@@ -60,19 +84,12 @@ struct Span {
     int low;                             // the first place that any row attends to
     int from, to;                        // places to walk, `from` down from `low` to a multiple of 32; none if to <= from
     int chunk, parts;                    // places of a piece, pieces that they are cut into
+    int prefix, own;                     // WHOLE: the prefix (-1: none), and the first place behind it
+    int64_t missing;                     // WHOLE, PREFIXES: places of the prefix that have no column
 };
 __device__ inline size_t pieces_at(const Pieces &p, uint32_t kv_heads, uint32_t group, const Span &s, int row, int kv_head)
 {
     return ((size_t)(s.token0 * group + row) * kv_heads + kv_head) * p.splits;
-}
-// A prefix's places are cut alike for all of its tiles, into as many pieces as there may be.
-__device__ inline uint32_t prefix_chunk(uint32_t places, const Pieces &pieces)
-{
-    return max(pieces.chunk, ((places + pieces.most - 1) / pieces.most + 63) & ~63u);
-}
-__device__ inline int prefix_places(const she_attend_pages_args &a, int length, uint32_t width)
-{
-    return (int)min((int64_t)max(length, 0), (int64_t)width * a.page_size);
 }
 template <Walk WALK> __device__ inline Piece tile_of(const she_attend_pages_args &a, const Owners &owners, uint32_t group, uint32_t tile, uint32_t slot)
 {
@@ -81,30 +98,46 @@ template <Walk WALK> __device__ inline Piece tile_of(const she_attend_pages_args
     else
         return find_piece(a.starts, a.requests, a.tokens, group, tile, slot);
 }
-template <int ROWS, Walk WALK> __device__ inline Span span_of(const she_attend_pages_args &a, uint32_t group, const Piece &p, int row, const Pieces &pieces)
+template <int ROWS, Walk WALK>
+__device__ inline Span span_of(const she_attend_pages_args &a, const Owners &owners, uint32_t group, const Piece &p, int row, const Pieces &pieces)
 {
     Span s{};
     s.request = p.segment;
     if (p.segment < 0) return s;
     const int all = (int)(p.last - p.first), news = all / (int)group;
-    const int64_t room = (int64_t)a.table_width * a.page_size;
+    int64_t room = (int64_t)a.table_width * a.page_size;
     const int length = max(a.lengths[p.segment], 0);
     s.row = row;
     s.rows = min(ROWS, all - row);
     s.token0 = p.first / group;
     if constexpr (WALK == PREFIXES) {
+        // cut alike for all of a prefix's tiles
         s.to = prefix_places(a, length, a.table_width);
+        s.missing = length - s.to;
         s.first = s.to - 1;                                       // a token's window is looked up apart
-        s.chunk = (int)prefix_chunk(s.to, pieces);
-        s.parts = (s.to + s.chunk - 1) / s.chunk;
+        s.chunk = (int)max(pieces.chunk, (((uint32_t)s.to + pieces.most - 1) / pieces.most + 63) & ~63u);
+        s.parts = s.to ? (s.to - 1) / s.chunk + 1 : 0;
         return s;
     }
     s.first = length - news;
-    const int p0 = s.first + row / (int)group, p1 = s.first + (row + s.rows - 1) / (int)group;
-    const int64_t low = a.window ? (int64_t)p0 - (int64_t)a.window + 1 : 0;
+    if constexpr (WALK == WHOLE) {
+        s.prefix = prefix_of(owners, p.segment);
+        if (s.prefix >= 0) {
+            const int places = max(owners.prefix_lengths[s.prefix], 0);
+            s.own = prefix_places(a, places, owners.prefix_width);
+            s.missing = places - s.own;
+        }
+        room += s.own;
+    }
+    const int p0 = WALK == WHOLE ? max(s.first + row / (int)group, 0) : s.first + row / (int)group, p1 = s.first + (row + s.rows - 1) / (int)group;
+    int64_t low = a.window ? (int64_t)p0 - (int64_t)a.window + 1 : WALK == WHOLE ? -(int64_t)0x7FFFFFFF : 0, to = (int64_t)p1 + 1;
+    if constexpr (WALK == WHOLE) {
+        low = p1 < 0 ? 0 : low >= 0 ? s.own + low : min(low + s.missing + s.own, (int64_t)s.own);
+        to = p1 < 0 ? 0 : s.own + to;
+    }
     s.low = (int)max(low, (int64_t)0);
     s.from = s.low & ~31;
-    s.to = (int)min((int64_t)p1 + 1, room);
+    s.to = (int)min(to, room);
     const uint32_t places = s.to > s.from ? s.to - s.from : 0;
     uint32_t chunk = pieces.chunk;
     if (places > (uint64_t)pieces.most * chunk) chunk = ((places + pieces.most - 1) / pieces.most + 127) & ~127u;
@@ -113,8 +146,25 @@ template <int ROWS, Walk WALK> __device__ inline Span span_of(const she_attend_p
     return s;
 }
 
+// Of a walk that is joined with another: the piece z of the tile's rows is none, and if `alone`, nor are those of a prefix.  Returns whether
+// there is nothing more to do.
+template <Walk WALK>
+__device__ inline bool leave_none(const she_attend_pages_args &a, const Owners &owners, uint32_t group, const Pieces &pieces, const Span &s, int kv_head, int z)
+{
+    if (WALK == BEHIND && z == 0) {
+        if (prefix_of(owners, s.request) < 0)
+            for (uint32_t i = threadIdx.x; i < s.rows * pieces.first; i += blockDim.x)
+                pieces.ml[pieces_at(pieces, a.kv_heads, group, s, s.row + (int)(i / pieces.first), kv_head) + i % pieces.first] = float2{-__builtin_inff(), 0};
+        return false;
+    }
+    if (z < s.parts) return false;
+    for (int i = threadIdx.x; i < s.rows; i += blockDim.x)
+        pieces.ml[pieces_at(pieces, a.kv_heads, group, s, s.row + i, kv_head) + pieces.first + z] = float2{-__builtin_inff(), 0};
+    return true;
+}
+
 // The places that a row of a tile attends to, from low to high.  In the walk over prefixes the request's own length says where its window
-// reaches back to.
+// reaches back to.  With a prefix before them, tokens without a place of their own attend to nothing.
 struct Reach {
     int low, high;
 };
@@ -131,12 +181,36 @@ template <Walk WALK> __device__ inline Reach reach_of(const she_attend_pages_arg
             else end = mid;
         }
         const int64_t place = (int64_t)max(owners.lengths[r], 0) - (bounded_start(a.starts, r + 1, a.tokens) - token);
-        w.low = (int)min(max(max(a.lengths[s.request], 0) + place - (int64_t)a.window + 1, (int64_t)0), (int64_t)s.to);
+        w.low = (int)min(max(s.to + s.missing + place - (int64_t)a.window + 1, (int64_t)0), (int64_t)s.to);
     } else {
-        w.high = s.first + row / (int)group;
-        if (a.window) w.low = (int)max((int64_t)w.high - (int64_t)a.window + 1, (int64_t)0);
+        const int place = s.first + row / (int)group;
+        w.high = place;
+        const int64_t low = (int64_t)place - (int64_t)a.window + 1;
+        if constexpr (WALK == WHOLE) {
+            if (place < 0) return Reach{0, -1};
+            w.high += s.own;
+            if (a.window) w.low = (int)max(low >= 0 ? s.own + low : min(low + s.missing + s.own, (int64_t)s.own), (int64_t)0);
+        } else {
+            if (a.window) w.low = (int)max(low, (int64_t)0);
+        }
     }
     return w;
+}
+
+// The page and slot of a place.  Whether page ids are in range is the caller's to see.
+struct Slot {
+    int32_t page;
+    uint32_t in_page;
+};
+template <Walk WALK> __device__ inline Slot slot_of(const she_attend_pages_args &a, const Owners &owners, const Span &s, uint32_t place)
+{
+    const int32_t *row = a.table + s.request * a.table_stride;
+    if constexpr (WALK == WHOLE) {
+        if (place < (uint32_t)s.own) row = owners.prefix_table + s.prefix * owners.prefix_stride;
+        else place -= s.own;
+    }
+    const uint32_t column = place / a.page_size;
+    return Slot{row[column], place - column * a.page_size};
 }
 
 // Whether place `place`, whose page id is out of range and slot in_page, stands for that page in the count: its first place that is
@@ -147,16 +221,16 @@ __device__ inline bool counts(const Span &s, int place, int in_page, bool first)
 }
 
 // Where the rows of the places [from, from + count) start, -1 for those that their page id keeps out; *any_bad: some that is attended to.
-__device__ inline void look_up(const she_attend_pages_args &a, const Span &s, int kv_head, int from, int count, int64_t *rows, int *any_bad, uint32_t *d_bad)
+template <Walk WALK>
+__device__ inline void look_up(const she_attend_pages_args &a, const Owners &owners, const Span &s, int kv_head, int from, int count, int64_t *rows, int *any_bad, uint32_t *d_bad)
 {
     for (int i = threadIdx.x; i < count; i += blockDim.x) {
-        const uint32_t place = from + i, column = place / a.page_size, in_page = place - column * a.page_size;
-        const int32_t page = a.table[s.request * a.table_stride + column];
-        const bool good = page >= 0 && (uint32_t)page < a.pages;
-        rows[i] = good ? page * a.page_stride + in_page * a.slot_stride + kv_head * a.page_head : -1;
-        if (!good && (int)place >= s.low) {
+        const Slot at = slot_of<WALK>(a, owners, s, from + i);
+        const bool good = at.page >= 0 && (uint32_t)at.page < a.pages;
+        rows[i] = good ? at.page * a.page_stride + at.in_page * a.slot_stride + kv_head * a.page_head : -1;
+        if (!good && from + i >= s.low) {
             *any_bad = 1;
-            if (counts(s, place, in_page, i == 0)) count_bad(d_bad);
+            if (counts(s, from + i, at.in_page, i == 0)) count_bad(d_bad);
         }
     }
 }
@@ -172,8 +246,8 @@ template <class T> __device__ inline bool has_special(u32x4 v)
 
 // One row over those of the places [from, to) that it attends to, its piece `part`, by one wavefront: scores with a place a lane, sums with elements on
 // the lanes.  Writes the row's result, or its piece's.
-template <class T>
-__device__ void attend_row(const she_attend_pages_args &a, uint32_t group, const Pieces &pieces, bool cut, size_t part, const Span &sp, int kv_head, int row, Reach reach, int from, int to)
+template <class T, Walk WALK>
+__device__ void attend_row(const she_attend_pages_args &a, const Owners &owners, uint32_t group, const Pieces &pieces, bool cut, size_t part, const Span &sp, int kv_head, int row, Reach reach, int from, int to)
 {
     const int lane = threadIdx.x & 63, D = (int)a.head;
     const int64_t token = sp.token0 + row / (int)group;
@@ -183,9 +257,9 @@ __device__ void attend_row(const she_attend_pages_args &a, uint32_t group, const
     to = min(to, reach.high + 1);
     for (int first = max(from, reach.low); first < to; first += 64) {
         const int place = first + lane;
-        const int32_t page = place < to ? a.table[sp.request * a.table_stride + (uint32_t)place / a.page_size] : -1;
-        const bool there = page >= 0 && (uint32_t)page < a.pages;
-        const int64_t at = there ? page * a.page_stride + (int64_t)((uint32_t)place % a.page_size) * a.slot_stride + kv_head * a.page_head : 0;
+        const Slot its = place < to ? slot_of<WALK>(a, owners, sp, place) : Slot{-1, 0};
+        const bool there = its.page >= 0 && (uint32_t)its.page < a.pages;
+        const int64_t at = there ? its.page * a.page_stride + (int64_t)its.in_page * a.slot_stride + kv_head * a.page_head : 0;
         float s = 0;
         if (there)
             for (int d = 0; d < D; d += 8) {
@@ -211,7 +285,7 @@ __device__ void attend_row(const she_attend_pages_args &a, uint32_t group, const
         }
     }
     const float inv = cut ? 1.0f : sum == 0 ? 0.0f : 1.0f / sum;
-    if (cut && lane == 0) pieces.ml[part] = float2{top, sum};
+    if (cut && lane == 0) pieces.ml[part] = float2{top, WALK == BEHIND && reach.high < 0 ? NOTHING : sum};
     for (int i = 0; i < 4; i++) {
         const int d = lane + 64 * i;
         if (d >= D) continue;
@@ -226,23 +300,34 @@ __device__ void attend_row(const she_attend_pages_args &a, uint32_t group, const
 // Few rows: every wavefront walks places of its own, 32 a step, four steps of the workgroup side by side, straight from memory.  Lane
 // l reads d = 32 s + 8 (l/16) .. of the key of place l%16 for the scores, and EL elements from EL (l%16) on of the values of the
 // eight places that its scores belong to, whole rows over 16 lanes; the eight rows are transposed in registers.
+template <int DP> struct FewShared {
+    int64_t rows[MOST_CHUNK];
+    float joined[FEW_WAVES][FEW_ROWS][DP];
+    float tops[FEW_WAVES][FEW_ROWS], sums[FEW_WAVES][FEW_ROWS];
+    int any_bad, any_special;
+};
 template <class T, int DP, Walk WALK>
-__global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_few(she_attend_pages_args a, uint32_t group, Pieces pieces, Owners owners, uint32_t *d_bad)
+__device__ __forceinline__ void attend_few(const she_attend_pages_args &a, uint32_t group, const Pieces &pieces, const Owners &owners, uint32_t *d_bad, FewShared<DP> &shared,
+                                           uint32_t slot, int kv_head, int z)
 {
     constexpr int EL = DP == 64 ? 4 : 8, NB = DP == 256 ? 2 : 1, KS = DP / 32;
-    __shared__ int64_t rows[MOST_CHUNK];
-    __shared__ float joined[FEW_WAVES][FEW_ROWS][DP];
-    __shared__ float tops[FEW_WAVES][FEW_ROWS], sums[FEW_WAVES][FEW_ROWS];
-    __shared__ int any_bad, any_special;
+    auto &rows = shared.rows;
+    auto &joined = shared.joined;
+    auto &tops = shared.tops, &sums = shared.sums;
+    int &any_bad = shared.any_bad, &any_special = shared.any_special;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, quarter = lane >> 4;
-    const int kv_head = blockIdx.y, D = (int)a.head;
-    const Piece piece = tile_of<WALK>(a, owners, group, FEW_ROWS, blockIdx.x);
+    const int D = (int)a.head;
+    const Piece piece = tile_of<WALK>(a, owners, group, FEW_ROWS, slot);
     if (piece.segment < 0) return;
-    Span sp = span_of<FEW_ROWS, WALK>(a, group, piece, piece.index * FEW_ROWS, pieces);
-    if ((int)blockIdx.z >= max(sp.parts, WALK == REQUESTS ? 1 : 0)) return;
-    const bool cut = WALK != REQUESTS || sp.parts > 1;
-    const uint32_t part = pieces.first + blockIdx.z;
-    int from = sp.from + (int)blockIdx.z * sp.chunk, count = sp.parts ? min(sp.chunk, sp.to - from) : 0;
+    Span sp = span_of<FEW_ROWS, WALK>(a, owners, group, piece, piece.index * FEW_ROWS, pieces);
+    if constexpr (joined_with_another(WALK)) {
+        if (leave_none<WALK>(a, owners, group, pieces, sp, kv_head, z)) return;
+    } else {
+        if (z >= max(sp.parts, 1)) return;
+    }
+    const bool cut = joined_with_another(WALK) || sp.parts > 1;
+    const uint32_t part = pieces.first + z;
+    int from = sp.from + z * sp.chunk, count = sp.parts ? min(sp.chunk, sp.to - from) : 0;
 
     // this lane's row
     const int my_row = min(sp.row + col, sp.row + sp.rows - 1), my_token = my_row / (int)group, my_head = kv_head * (int)group + my_row % (int)group;
@@ -269,7 +354,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
     }
     if (tid == 0) any_bad = any_special = 0;
     __syncthreads();
-    look_up(a, sp, kv_head, from, min(count, MOST_CHUNK), rows, &any_bad, d_bad);
+    look_up<WALK>(a, owners, sp, kv_head, from, min(count, MOST_CHUNK), rows, &any_bad, d_bad);
     x8<T> q[KS];
     {
         const T *p = (const T *)a.q + (sp.token0 + my_token) * a.q_token + my_head * a.q_head + quarter * 8;
@@ -290,7 +375,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
     for (int base = 0; base < count; base += FEW_WAVES * 32) {
         if (base && base % MOST_CHUNK == 0) {
             __syncthreads();                                      // the rows that were looked up before have been read
-            look_up(a, sp, kv_head, from + base, min(count - base, MOST_CHUNK), rows, &any_bad, d_bad);
+            look_up<WALK>(a, owners, sp, kv_head, from + base, min(count - base, MOST_CHUNK), rows, &any_bad, d_bad);
             __syncthreads();
             unsafe = any_bad != 0;
         }
@@ -395,7 +480,7 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
     __syncthreads();
     if (any_special) {
         for (int r = wave; r < sp.rows; r += FEW_WAVES)
-            attend_row<T>(a, group, pieces, cut, pieces_at(pieces, a.kv_heads, group, sp, sp.row + r, kv_head) + part, sp, kv_head, sp.row + r,
+            attend_row<T, WALK>(a, owners, group, pieces, cut, pieces_at(pieces, a.kv_heads, group, sp, sp.row + r, kv_head) + part, sp, kv_head, sp.row + r,
                           Reach{__shfl(low, r), __shfl(high, r)}, from, from + count);
         return;
     }
@@ -425,11 +510,17 @@ __global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_fe
             if (d0 + i < D) to[i] = (T)(o[i] * inv);
     } else {
         const size_t at = pieces_at(pieces, a.kv_heads, group, sp, row, kv_head) + part;
-        if (d0 == 0) pieces.ml[at] = float2{top, sum};
+        if (d0 == 0) pieces.ml[at] = float2{top, WALK == BEHIND && sp.first + row / (int)group < 0 ? NOTHING : sum};
 #pragma unroll
         for (int i = 0; i < EACH; i++)
             if (d0 + i < D) pieces.o[at * D + d0 + i] = o[i];
     }
+}
+template <class T, int DP, Walk WALK>
+__global__ __launch_bounds__(64 * FEW_WAVES, DP == 256 ? 1 : 2) void k_attend_few(she_attend_pages_args a, uint32_t group, Pieces pieces, Owners owners, uint32_t *d_bad)
+{
+    __shared__ FewShared<DP> shared;
+    attend_few<T, DP, WALK>(a, group, pieces, owners, d_bad, shared, blockIdx.x, (int)blockIdx.y, (int)blockIdx.z);
 }
 
 // Bound by what a wavefront does one after the other: 2048 tokens over 32768 places (32 / 8 heads of 128, bf16) 1066 us, 1000 TFLOP/s
@@ -457,38 +548,51 @@ template <int DP> __device__ inline int value_unit(int place, int unit)
     return unit ^ (DP == 64 ? ((place >> 1) & 3) << 1 : (place & 7) << 1);
 }
 
+constexpr int TILE_BLOCK = 4 * STEP;                                                 // places that are looked up together
+template <class T, int DP> struct alignas(16) TileShared {
+    T even_keys[STEP * DP], even_values[STEP * DP], odd_keys[STEP * DP], odd_values[STEP * DP];
+    int64_t rows[2][TILE_BLOCK];
+    uint64_t missing[2][TILE_BLOCK / 64];                                            // places that their page id or the table's end keeps out
+    int lows[TILE_WAVES];
+};
 template <class T, int DP, Walk WALK>
-__global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_tile(she_attend_pages_args a, uint32_t group, Pieces pieces, Owners owners, const void *zeros, uint32_t *d_bad)
+__device__ __forceinline__ void attend_tile(const she_attend_pages_args &a, uint32_t group, const Pieces &pieces, const Owners &owners, const void *zeros, uint32_t *d_bad,
+                                            TileShared<T, DP> &shared, uint32_t slot, int kv_head, int z)
 {
-    constexpr int UNITS = DP / 8, KS = DP / 16, DB = DP / 32, BLOCK = 4 * STEP;      // places that are looked up together
+    constexpr int UNITS = DP / 8, KS = DP / 16, DB = DP / 32, BLOCK = TILE_BLOCK;
     constexpr int EACH = STEP * UNITS / (64 * TILE_WAVES);                           // units of either tile that a thread brings
     constexpr float LEAD = std::is_same<T, __bf16>::value ? 8.0f : 0.0f;
-    __shared__ __align__(16) T even_keys[STEP * DP], even_values[STEP * DP], odd_keys[STEP * DP], odd_values[STEP * DP];
-    __shared__ int64_t rows[2][BLOCK];
-    __shared__ uint64_t missing[2][BLOCK / 64];                                      // places that their page id or the table's end keeps out
+    T *even_keys = shared.even_keys, *even_values = shared.even_values, *odd_keys = shared.odd_keys, *odd_values = shared.odd_values;
+    auto &rows = shared.rows;
+    auto &missing = shared.missing;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
-    // A key head's tiles are one XCD's where there are eight of them: neighbouring workgroups have different heads.  Late tokens have
-    // most to attend to: they come first.
-    const int kv_head = blockIdx.x % a.kv_heads, D = (int)a.head;
-    const uint32_t slot = gridDim.x / a.kv_heads - 1 - blockIdx.x / a.kv_heads;
+    const int D = (int)a.head;
     const Piece piece = tile_of<WALK>(a, owners, group, TILE_ROWS, slot);
     if (piece.segment < 0) return;
-    Span sp = span_of<TILE_ROWS, WALK>(a, group, piece, piece.index * TILE_ROWS, pieces);
-    if ((int)blockIdx.z >= max(sp.parts, WALK == REQUESTS ? 1 : 0)) return;
-    const bool cut = WALK != REQUESTS || sp.parts > 1;
-    const uint32_t part = pieces.first + blockIdx.z;
-    int from = sp.from + (int)blockIdx.z * sp.chunk, count = sp.parts ? min(sp.chunk, sp.to - from) : 0;
+    Span sp = span_of<TILE_ROWS, WALK>(a, owners, group, piece, piece.index * TILE_ROWS, pieces);
+    if constexpr (joined_with_another(WALK)) {
+        if (leave_none<WALK>(a, owners, group, pieces, sp, kv_head, z)) return;
+    } else {
+        if (z >= max(sp.parts, 1)) return;
+    }
+    const bool cut = joined_with_another(WALK) || sp.parts > 1;
+    const uint32_t part = pieces.first + z;
+    int from = sp.from + z * sp.chunk, count = sp.parts ? min(sp.chunk, sp.to - from) : 0;
 
     // this lane's row, and what the wavefront's rows attend to
     const int last_row = sp.row + sp.rows - 1, first_here = sp.row + wave * 32, last_here = min(first_here + 31, last_row);
     const int my_row = min(first_here + col, last_row), my_token = my_row / (int)group, my_head = kv_head * (int)group + my_row % (int)group;
     int high, low, high_min, high_max, low_min, low_max;
-    if constexpr (WALK == PREFIXES) {
+    if constexpr (WALK == WHOLE) {
+        const Reach mine = reach_of<WALK>(a, owners, group, sp, my_row), least = reach_of<WALK>(a, owners, group, sp, min(first_here, last_row)),
+                    most = reach_of<WALK>(a, owners, group, sp, last_here);
+        high = mine.high, low = mine.low, high_min = least.high, high_max = most.high, low_min = least.low, low_max = most.low;
+    } else if constexpr (WALK == PREFIXES) {
         const Reach mine = reach_of<WALK>(a, owners, group, sp, my_row);
         high = high_min = high_max = mine.high;
         low = low_min = low_max = mine.low;
         if (a.window) {                                           // requests in any order: the earliest and the latest place of the rows
-            __shared__ int lows[TILE_WAVES];
+            auto &lows = shared.lows;
 #pragma unroll
             for (int m = 1; m < 32; m *= 2) {
                 low_min = min(low_min, __shfl_xor(low_min, m));
@@ -512,16 +616,15 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
     // the rows of a block of places: thread tid has place BLOCK * b + tid, a wavefront a step
     auto page_of = [&](int b) {
         const int i = b * BLOCK + tid;
-        if (i >= count) return -1;
-        const int32_t page = a.table[sp.request * a.table_stride + (uint32_t)(from + i) / a.page_size];
-        if (page >= 0 && (uint32_t)page < a.pages) return (int)page;
-        if (counts(sp, from + i, (uint32_t)(from + i) % a.page_size, i == 0)) count_bad(d_bad);
-        return -1;
+        if (i >= count) return Slot{-1, 0};
+        const Slot at = slot_of<WALK>(a, owners, sp, from + i);
+        if (at.page >= 0 && (uint32_t)at.page < a.pages) return at;
+        if (counts(sp, from + i, at.in_page, i == 0)) count_bad(d_bad);
+        return Slot{-1, 0};
     };
-    auto keep_rows = [&](int b, int page) {
-        const int i = b * BLOCK + tid;
-        rows[b & 1][tid] = page < 0 ? -1 : page * a.page_stride + (int64_t)((uint32_t)(from + i) % a.page_size) * a.slot_stride + kv_head * a.page_head;
-        const uint64_t out = __ballot(page < 0);                                     // from `count` on too: a row may reach beyond the table
+    auto keep_rows = [&](int b, Slot at) {
+        rows[b & 1][tid] = at.page < 0 ? -1 : at.page * a.page_stride + (int64_t)at.in_page * a.slot_stride + kv_head * a.page_head;
+        const uint64_t out = __ballot(at.page < 0);                                     // from `count` on too: a row may reach beyond the table
         if (lane == 0) missing[b & 1][wave] = out;
     };
     // a step's tiles on their way into LDS: a wavefront's 64 units lie side by side there, so each lane picks the one that belongs in
@@ -575,7 +678,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
     const int key_at = col * DP * 2 + key_unit<DP>(col, half) * 16;
     const int value_place = half * 4 + (lane & 15) / 4, value_d = (lane & 16) + (lane & 3) * 4;
     const int value_at = value_place * DP * 2 + value_unit<DP>(value_place, value_d / 8) * 16 + value_d % 8 * 2;
-    int page = -1;
+    Slot page{-1, 0};
     bool special = false;                                         // infinite or NaN values where not all rows attend
     auto do_step = [&](int step, const T *key_tile, const T *value_tile, T *next_keys, T *next_values) {
         wait_for_lds_loads();
@@ -658,7 +761,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
 
     if (__ballot(special)) {
         for (int row = first_here; row <= last_here; row++)
-            attend_row<T>(a, group, pieces, cut, pieces_at(pieces, a.kv_heads, group, sp, row, kv_head) + part, sp, kv_head, row,
+            attend_row<T, WALK>(a, owners, group, pieces, cut, pieces_at(pieces, a.kv_heads, group, sp, row, kv_head) + part, sp, kv_head, row,
                           Reach{__shfl(low, row - first_here), __shfl(high, row - first_here)}, from, from + count);
         return;
     }
@@ -667,7 +770,7 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
     const int64_t token = sp.token0 + my_token;
     const size_t at = pieces_at(pieces, a.kv_heads, group, sp, my_row, kv_head) + part;
     const float inv = cut ? 1.0f : l == 0 ? 0.0f : 1.0f / l;
-    if (cut && half == 0) pieces.ml[at] = float2{m, l};
+    if (cut && half == 0) pieces.ml[at] = float2{m, WALK == BEHIND && high < 0 ? NOTHING : l};
 #pragma unroll
     for (int b = 0; b < DB; b++)
 #pragma unroll
@@ -685,6 +788,14 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
             }
         }
 }
+// A key head's tiles are one XCD's where there are eight of them: neighbouring workgroups have different heads.  Late tokens have
+// most to attend to: they come first.
+template <class T, int DP, Walk WALK>
+__global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_tile(she_attend_pages_args a, uint32_t group, Pieces pieces, Owners owners, const void *zeros, uint32_t *d_bad)
+{
+    __shared__ TileShared<T, DP> shared;
+    attend_tile<T, DP, WALK>(a, group, pieces, owners, zeros, d_bad, shared, gridDim.x / a.kv_heads - 1 - blockIdx.x / a.kv_heads, (int)(blockIdx.x % a.kv_heads), (int)blockIdx.z);
+}
 
 // Rows that were cut, `each` of a tile a workgroup.  Up to JOIN_AHEAD pieces are a wavefront's work, and a workgroup of the tile kernel's
 // has sixteen rows then (with four, 99 and not 82 us for the whole call of 4063 tokens in two pieces at 16 heads of 64); more are
@@ -692,17 +803,12 @@ __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_t
 // JOIN_AHEAD at a time.  A token over 32768 places, 4 rows of 64 pieces at 8 key heads, takes 33 us so on one input again and again (38 on
 // others in turn), 43 with four rows a workgroup and 78 with a row a wavefront.
 constexpr int JOIN_AHEAD = 4;
-// A row's pieces in order: the first `near` one after the other, and the others `gap` further on.
-struct Order {
-    int parts, near, gap;
-    __device__ size_t operator[](int k) const { return (size_t)(k + (k >= near ? gap : 0)); }
-};
 template <class T>
-__device__ inline void join_row(const she_attend_pages_args &a, const Pieces &w, size_t at, const Order &order, int from, int by, float &sum, float o[4])
+__device__ inline void join_row(const she_attend_pages_args &a, const Pieces &w, size_t at, int parts, int from, int by, float &sum, float o[4])
 {
-    const int lane = threadIdx.x & 63, D = (int)a.head, parts = order.parts;
+    const int lane = threadIdx.x & 63, D = (int)a.head;
     float top = -__builtin_inff();
-    for (int k = lane; k < parts; k += 64) top = fmaxf(top, w.ml[at + order[k]].x);
+    for (int k = lane; k < parts; k += 64) top = fmaxf(top, w.ml[at + k].x);
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
     sum = 0;
@@ -714,9 +820,9 @@ __device__ inline void join_row(const she_attend_pages_args &a, const Pieces &w,
 #pragma unroll
         for (int e = 0; e < JOIN_AHEAD; e++) {
             const int k = k0 + by * e;
-            ml[e] = k < parts ? w.ml[at + order[k]] : float2{-__builtin_inff(), 0};
+            ml[e] = k < parts ? w.ml[at + k] : float2{-__builtin_inff(), 0};
 #pragma unroll
-            for (int i = 0; i < 4; i++) v[e][i] = k < parts && lane + 64 * i < D ? w.o[(at + order[k]) * D + lane + 64 * i] : 0.0f;
+            for (int i = 0; i < 4; i++) v[e][i] = k < parts && lane + 64 * i < D ? w.o[(at + k) * D + lane + 64 * i] : 0.0f;
         }
 #pragma unroll
         for (int e = 0; e < JOIN_AHEAD; e++) {
@@ -727,23 +833,8 @@ __device__ inline void join_row(const she_attend_pages_args &a, const Pieces &w,
         }
     }
 }
-// The pieces of the prefix that request r has, none if it has none.
-__device__ inline int prefix_parts(const she_attend_pages_args &a, const Owners &owners, const Pieces &prefix, int r)
-{
-    const int lane = threadIdx.x & 63;
-    int found = 0;
-    for (uint32_t g0 = 0; g0 < owners.prefixes; g0 += 64) {
-        const bool before = g0 + lane < owners.prefixes && owner_start(owners, (int)g0 + lane) <= r;
-        const int n = __popcll(__ballot(before));
-        found += n;
-        if (n < 64) break;
-    }
-    if (!found || r >= owner_start(owners, found)) return 0;
-    const int places = prefix_places(a, owners.prefix_lengths[found - 1], owners.prefix_width);
-    return places ? (places - 1) / (int)prefix_chunk(places, prefix) + 1 : 0;
-}
 template <class T, int ROWS, Walk WALK>
-__global__ __launch_bounds__(256) void k_attend_join(she_attend_pages_args a, uint32_t group, Pieces pieces, Pieces prefix, Owners owners, int each)
+__global__ __launch_bounds__(256) void k_attend_join(she_attend_pages_args a, uint32_t group, Pieces pieces, Owners owners, int each)
 {
     __shared__ float sums[4], joined[4][256];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = (int)a.head;
@@ -751,33 +842,23 @@ __global__ __launch_bounds__(256) void k_attend_join(she_attend_pages_args a, ui
     if (piece.segment < 0) return;
     const int64_t first = piece.first + (int64_t)piece.index * ROWS + blockIdx.z * each;
     if (first >= piece.last) return;
-    const Span sp = span_of<ROWS, WALK>(a, group, piece, piece.index * ROWS, pieces);
-    const int rows = (int)min((int64_t)each, piece.last - first);
-    Order order{sp.parts, sp.parts, 0};
-    if constexpr (WALK == REQUESTS) {
-        if (order.parts <= 1) return;
-    } else {
-        order.near = prefix_parts(a, owners, prefix, piece.segment);
-        order.parts += order.near;
-        order.gap = (int)pieces.first - order.near;
-    }
-    const bool few = order.parts <= JOIN_AHEAD;
-    for (int r = few ? wave : 0; r < rows; r += few ? 4 : 1) {
+    const Span sp = span_of<ROWS, WALK>(a, owners, group, piece, piece.index * ROWS, pieces);
+    const int parts = sp.parts, rows = (int)min((int64_t)each, piece.last - first);
+    if (parts <= 1) return;
+    for (int r = parts <= JOIN_AHEAD ? wave : 0; r < rows; r += parts <= JOIN_AHEAD ? 4 : 1) {
         const int64_t row = first + r, token = row / group;
-        const int head = blockIdx.y * (int)group + (int)(row % group), in_request = sp.row + (int)blockIdx.z * each + r;
-        const size_t at = pieces_at(pieces, a.kv_heads, group, sp, in_request, blockIdx.y);
+        const int head = blockIdx.y * (int)group + (int)(row % group);
+        const size_t at = pieces_at(pieces, a.kv_heads, group, sp, sp.row + (int)blockIdx.z * each + r, blockIdx.y);
         T *to = (T *)a.out + token * a.out_token + head * a.out_head;
-        // behind a prefix, a token without a place of its own attends to nothing
-        const bool none = WALK == BEHIND && sp.first + in_request / (int)group < 0;
         float sum, o[4];
-        if (few) {
-            join_row<T>(a, pieces, at, order, 0, 1, sum, o);
+        if (parts <= JOIN_AHEAD) {
+            join_row<T>(a, pieces, at, parts, 0, 1, sum, o);
 #pragma unroll
             for (int i = 0; i < 4; i++)
-                if (lane + 64 * i < D) to[lane + 64 * i] = none ? (T)0.0f : (T)(o[i] * (sum == 0 ? 0.0f : 1.0f / sum));
+                if (lane + 64 * i < D) to[lane + 64 * i] = (T)(o[i] * (sum == 0 ? 0.0f : 1.0f / sum));
             continue;
         }
-        join_row<T>(a, pieces, at, order, wave, 4, sum, o);
+        join_row<T>(a, pieces, at, parts, wave, 4, sum, o);
         if (r) __syncthreads();
         if (lane == 0) sums[wave] = sum;
 #pragma unroll
@@ -785,54 +866,142 @@ __global__ __launch_bounds__(256) void k_attend_join(she_attend_pages_args a, ui
         __syncthreads();
         const int d = threadIdx.x;
         sum = sums[0] + sums[1] + sums[2] + sums[3];
-        if (d < D) to[d] = none ? (T)0.0f : (T)((joined[0][d] + joined[1][d] + joined[2][d] + joined[3][d]) * (sum == 0 ? 0.0f : 1.0f / sum));
+        if (d < D) to[d] = (T)((joined[0][d] + joined[1][d] + joined[2][d] + joined[3][d]) * (sum == 0 ? 0.0f : 1.0f / sum));
     }
 }
 
-template <class T, int DP, Walk WALK>
+// A call with shared prefixes, whose two walks are one launch: while the prefixes' workgroups, of many rows, wait for the matrix units, those
+// of the requests' own places wait for memory.
+template <class T, int DP, bool FEW> struct SharedOf;
+template <class T, int DP> struct SharedOf<T, DP, true> { using Prefix = FewShared<DP>; };
+template <class T, int DP> struct SharedOf<T, DP, false> { using Prefix = TileShared<T, DP>; };
+template <class T, int DP, bool FEW>
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_shared(she_attend_pages_args a, uint32_t group, Pieces prefix, Pieces pieces, Owners owners, const void *zeros,
+                                                                          uint32_t prefix_slots, uint32_t prefix_blocks, uint32_t slots, uint32_t *d_bad)
+{
+    using Prefix = typename SharedOf<T, DP, FEW>::Prefix;
+    __shared__ union {
+        char prefix[sizeof(Prefix)];
+        char behind[sizeof(FewShared<DP>)];
+        int64_t align[2];
+    } shared;
+    if (blockIdx.x < prefix_blocks) {
+        she_attend_pages_args p = a;
+        p.requests = owners.prefixes;
+        p.table = owners.prefix_table;
+        p.table_stride = owners.prefix_stride;
+        p.table_width = owners.prefix_width;
+        p.lengths = owners.prefix_lengths;
+        const uint32_t i = blockIdx.x / a.kv_heads, kv_head = blockIdx.x - i * a.kv_heads, z = i / prefix_slots, slot = i - z * prefix_slots;
+        if constexpr (FEW)
+            attend_few<T, DP, PREFIXES>(p, group, prefix, owners, d_bad, *reinterpret_cast<Prefix *>(shared.prefix), slot, (int)kv_head, (int)z);
+        else
+            attend_tile<T, DP, PREFIXES>(p, group, prefix, owners, zeros, d_bad, *reinterpret_cast<Prefix *>(shared.prefix), slot, (int)kv_head, (int)z);
+    } else {
+        const uint32_t b = blockIdx.x - prefix_blocks, i = b / a.kv_heads, kv_head = b - i * a.kv_heads, z = i / slots, slot = i - z * slots;
+        attend_few<T, DP, BEHIND>(a, group, pieces, owners, d_bad, *reinterpret_cast<FewShared<DP> *>(shared.behind), slot, (int)kv_head, (int)z);
+    }
+}
+
+// Rows of such a call: a workgroup each, in the order of the pieces, in which neighbours have different key heads and a key head's
+// pieces come from the XCD that wrote them, where there are eight of them.  D/4 lanes have a piece's elements, so that 1024 / D pieces are
+// read side by side.
+template <class T> __global__ __launch_bounds__(256) void k_shared_join(she_attend_pages_args a, uint32_t group, Pieces pieces)
+{
+    __shared__ f32x4 joined[256];
+    const int tid = threadIdx.x, lane = tid & 63, D = (int)a.head, lanes = D / 4, sets = 256 / lanes, set = tid / lanes, d = tid % lanes * 4, parts = (int)pieces.splits;
+    const int64_t first = bounded_start(a.starts, 0, a.tokens), last = bounded_start(a.starts, (int)a.requests, a.tokens);
+    for (int64_t row = blockIdx.x; row < (int64_t)a.tokens * a.q_heads; row += gridDim.x) {
+        const int64_t token = row / a.q_heads;
+        const int at_token = (int)(row - token * a.q_heads), kv_head = at_token % (int)a.kv_heads, head = kv_head * (int)group + at_token / (int)a.kv_heads;
+        if (token < first || token >= last) continue;
+        const float2 *ml = pieces.ml + (size_t)row * parts;
+        float top = -__builtin_inff();
+        for (int k = lane; k < parts; k += 64) top = fmaxf(top, ml[k].x);
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
+        const auto factor = [&](float of) { return of == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(of - top); };
+        float sum = 0;
+        for (int k = lane; k < parts; k += 64) sum = fmaf(ml[k].y, factor(ml[k].x), sum);
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) sum += __shfl_xor(sum, m);
+        const bool none = ml[pieces.first].y == NOTHING;
+        f32x4 o{0, 0, 0, 0};
+        if (set < sets && !none) {
+#pragma unroll 4
+            for (int k = set; k < parts; k += sets) {
+                const float f = factor(ml[k].x);
+                const f32x4 v = f == 0 ? f32x4{0, 0, 0, 0} : *reinterpret_cast<const f32x4 *>(pieces.o + ((size_t)row * parts + k) * D + d);
+#pragma unroll
+                for (int i = 0; i < 4; i++) o[i] = fmaf(v[i], f, o[i]);
+            }
+        }
+        joined[tid] = o;
+        __syncthreads();
+        if (tid < D) {
+            float v = 0;
+            for (int k = 0; k < sets; k++) v += joined[k * lanes + tid / 4][tid & 3];
+            ((T *)a.out)[token * a.out_token + head * a.out_head + tid] = none ? (T)0.0f : (T)(v * (sum == 0 ? 0.0f : 1.0f / sum));
+        }
+        __syncthreads();
+    }
+}
+
+// By the padded size of a head.
+template <class F> hipError_t by_head(uint32_t head, F launch)
+{
+    if (head <= 64) launch(std::integral_constant<int, 64>{});
+    else if (head <= 128) launch(std::integral_constant<int, 128>{});
+    else launch(std::integral_constant<int, 256>{});
+    return hipGetLastError();
+}
+
+// A walk that is a launch of its own.
+template <class T, Walk WALK>
 hipError_t walk(const she_attend_pages_args &a, const AttendShape &s, const Pieces &pieces, const Owners &owners, uint32_t *d_bad, hipStream_t st)
 {
     const uint32_t group = a.q_heads / a.kv_heads, slots = (uint32_t)s.slots;
-    if (s.few)
-        k_attend_few<T, DP, WALK><<<dim3(slots, a.kv_heads, s.splits), 64 * FEW_WAVES, 0, st>>>(a, group, pieces, owners, d_bad);
-    else
+    return by_head(a.head, [&](auto size) {
+        constexpr int DP = decltype(size)::value;
+        if constexpr (WALK == REQUESTS)
+            if (s.few) {
+                k_attend_few<T, DP, WALK><<<dim3(slots, a.kv_heads, s.splits), 64 * FEW_WAVES, 0, st>>>(a, group, pieces, owners, d_bad);
+                return;
+            }
         k_attend_tile<T, DP, WALK><<<dim3(slots * a.kv_heads, 1, s.splits), 64 * TILE_WAVES, 0, st>>>(a, group, pieces, owners, zeros_of(d_bad), d_bad);
-    return hipGetLastError();
-}
-template <class T, Walk WALK>
-hipError_t walk(const she_attend_pages_args &a, const AttendShape &s, const Pieces &pieces, const Owners &owners, uint32_t *d_bad, hipStream_t st)
-{
-    return a.head <= 64 ? walk<T, 64, WALK>(a, s, pieces, owners, d_bad, st) : a.head <= 128 ? walk<T, 128, WALK>(a, s, pieces, owners, d_bad, st)
-                                                                                            : walk<T, 256, WALK>(a, s, pieces, owners, d_bad, st);
-}
-template <class T, Walk WALK>
-hipError_t join(const she_attend_pages_args &a, const AttendShape &s, uint32_t most, const Pieces &pieces, const Pieces &prefix, const Owners &owners, hipStream_t st)
-{
-    const uint32_t group = a.q_heads / a.kv_heads, slots = (uint32_t)s.slots;
-    const int each = s.few && most > 4 * JOIN_AHEAD ? 1 : s.few || most > JOIN_AHEAD ? 4 : 16;
-    if (s.few)
-        k_attend_join<T, FEW_ROWS, WALK><<<dim3(slots, a.kv_heads, FEW_ROWS / each), 256, 0, st>>>(a, group, pieces, prefix, owners, each);
-    else
-        k_attend_join<T, TILE_ROWS, WALK><<<dim3(slots, a.kv_heads, TILE_ROWS / each), 256, 0, st>>>(a, group, pieces, prefix, owners, each);
-    return hipGetLastError();
+    });
 }
 
-template <class T> hipError_t attend(const she_attend_pages_args &a, const AttendShape &s, const Pieces &pieces, uint32_t *d_bad, hipStream_t st)
+template <class T, Walk WALK> hipError_t attend(const she_attend_pages_args &a, const AttendShape &s, const Pieces &pieces, const Owners &owners, uint32_t *d_bad, hipStream_t st)
 {
-    const hipError_t rc = walk<T, REQUESTS>(a, s, pieces, Owners{}, d_bad, st);
+    const hipError_t rc = walk<T, WALK>(a, s, pieces, owners, d_bad, st);
     if (rc != hipSuccess || s.splits == 1) return rc;
-    return join<T, REQUESTS>(a, s, s.splits, pieces, Pieces{}, Owners{}, st);
+    const uint32_t group = a.q_heads / a.kv_heads, slots = (uint32_t)s.slots;
+    const int each = s.few && s.splits > 4 * JOIN_AHEAD ? 1 : s.few || s.splits > JOIN_AHEAD ? 4 : 16;
+    if (s.few)
+        k_attend_join<T, FEW_ROWS, WALK><<<dim3(slots, a.kv_heads, FEW_ROWS / each), 256, 0, st>>>(a, group, pieces, owners, each);
+    else
+        k_attend_join<T, TILE_ROWS, WALK><<<dim3(slots, a.kv_heads, TILE_ROWS / each), 256, 0, st>>>(a, group, pieces, owners, each);
+    return hipGetLastError();
 }
 
-template <class T>
-hipError_t attend_shared(const she_attend_pages_args &of_prefixes, const she_attend_pages_args &behind, const SharedShape &s, const Pieces &prefix, const Pieces &pieces,
-                         const Owners &owners, uint32_t *d_bad, hipStream_t st)
+template <class T> hipError_t attend_shared(const she_attend_pages_args &a, const SharedShape &s, const Pieces &prefix, const Pieces &pieces, const Owners &owners, uint32_t *d_bad, hipStream_t st)
 {
+    const uint32_t group = a.q_heads / a.kv_heads, prefix_slots = (uint32_t)s.prefix.slots, prefix_blocks = prefix_slots * a.kv_heads * s.prefix.splits;
+    const uint32_t slots = s.behind.few ? (uint32_t)s.behind.slots : 0, blocks = slots * a.kv_heads * s.behind.splits;
     hipError_t rc = hipSuccess;
-    if (owners.prefixes) rc = walk<T, PREFIXES>(of_prefixes, s.prefix, prefix, owners, d_bad, st);
-    if (rc == hipSuccess) rc = walk<T, BEHIND>(behind, s.behind, pieces, owners, d_bad, st);
-    if (rc == hipSuccess) rc = join<T, BEHIND>(behind, s.behind, prefix.splits, pieces, prefix, owners, st);
-    return rc;
+    if (prefix_blocks + blocks)
+        rc = by_head(a.head, [&](auto size) {
+            constexpr int DP = decltype(size)::value;
+            if (s.prefix.few)
+                k_attend_shared<T, DP, true><<<prefix_blocks + blocks, 256, 0, st>>>(a, group, prefix, pieces, owners, zeros_of(d_bad), prefix_slots, prefix_blocks, slots, d_bad);
+            else
+                k_attend_shared<T, DP, false><<<prefix_blocks + blocks, 256, 0, st>>>(a, group, prefix, pieces, owners, zeros_of(d_bad), prefix_slots, prefix_blocks, slots, d_bad);
+        });
+    if (rc == hipSuccess && !s.behind.few) rc = walk<T, BEHIND>(a, s.behind, pieces, owners, d_bad, st);
+    if (rc != hipSuccess) return rc;
+    k_shared_join<T><<<(uint32_t)std::min<uint64_t>((uint64_t)a.tokens * a.q_heads, 1u << 20), 256, 0, st>>>(a, group, pieces);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -841,18 +1010,22 @@ hipError_t launch_attend_pages(const she_attend_pages_args &a, const AttendShape
 {
     float *o = static_cast<float *>(scratch);
     const Pieces pieces{o, reinterpret_cast<float2 *>(o + attend_pieces(a, s) * a.head), s.splits, 0, s.splits, s.chunk};
-    return a.type == SHE_BF16 ? attend<__bf16>(a, s, pieces, d_bad, st) : attend<_Float16>(a, s, pieces, d_bad, st);
+    return a.type == SHE_BF16 ? attend<__bf16, REQUESTS>(a, s, pieces, Owners{}, d_bad, st) : attend<_Float16, REQUESTS>(a, s, pieces, Owners{}, d_bad, st);
 }
 
-hipError_t launch_attend_shared(const she_attend_shared_args &a, const SharedShape &s, void *scratch, uint32_t *d_bad, hipStream_t st)
+hipError_t launch_attend_shared(const she_attend_shared_args &args, const SharedShape &s, void *scratch, uint32_t *d_bad, hipStream_t st)
 {
+    const she_attend_pages_args a = shared_behind(args);
+    const Owners owners{args.prefix_requests, args.prefix_lengths, a.lengths, args.prefix_table, args.prefix_stride, a.requests, args.prefixes, args.prefix_width};
     float *o = static_cast<float *>(scratch);
+    float2 *ml = reinterpret_cast<float2 *>(o + shared_pieces(args, s) * a.head);
+    if (s.whole) {
+        const Pieces pieces{o, ml, s.behind.splits, 0, s.behind.splits, s.behind.chunk};
+        return a.type == SHE_BF16 ? attend<__bf16, WHOLE>(a, s.behind, pieces, owners, d_bad, st) : attend<_Float16, WHOLE>(a, s.behind, pieces, owners, d_bad, st);
+    }
     const uint32_t splits = s.prefix.splits + s.behind.splits;
-    float2 *ml = reinterpret_cast<float2 *>(o + (size_t)a.tokens * a.q_heads * splits * a.head);
     const Pieces prefix{o, ml, splits, 0, s.prefix.splits, s.prefix.chunk}, pieces{o, ml, splits, s.prefix.splits, s.behind.splits, s.behind.chunk};
-    const Owners owners{a.prefix_requests, a.prefix_lengths, a.lengths, a.requests, a.prefixes, a.prefix_width};
-    return a.type == SHE_BF16 ? attend_shared<__bf16>(shared_prefixes(a), shared_behind(a), s, prefix, pieces, owners, d_bad, st)
-                              : attend_shared<_Float16>(shared_prefixes(a), shared_behind(a), s, prefix, pieces, owners, d_bad, st);
+    return a.type == SHE_BF16 ? attend_shared<__bf16>(a, s, prefix, pieces, owners, d_bad, st) : attend_shared<_Float16>(a, s, prefix, pieces, owners, d_bad, st);
 }
 
 }}  // namespace she::clear

@@ -106,23 +106,21 @@ she_attend_pages_args shared_behind(const she_attend_shared_args &a)
     return b;
 }
 
-she_attend_pages_args shared_prefixes(const she_attend_shared_args &a)
-{
-    she_attend_pages_args b = shared_behind(a);
-    b.requests = a.prefixes;
-    b.table = a.prefix_table;
-    b.table_stride = a.prefix_stride;
-    b.table_width = a.prefix_width;
-    b.lengths = a.prefix_lengths;
-    return b;
-}
-
 SharedShape shared_shape(const she_attend_shared_args &a, uint32_t cus)
 {
     SharedShape s{};
-    s.behind = attend_shape(shared_behind(a), cus);
-    if (!cus) cus = 1;
     const uint64_t group = a.q_heads / a.kv_heads, rows = a.tokens * group, places = (uint64_t)a.prefix_width * a.page_size;
+    if (!cus) cus = 1;
+    she_attend_pages_args call = shared_behind(a);
+    if (!a.prefixes || rows >= 96ull * a.requests) {
+        s.whole = true;
+        call.table_width += a.prefix_width;
+        s.behind = attend_shape(call, cus);
+        if (!s.behind.few) return s;
+        s = SharedShape{};
+        call.table_width = a.table_width;
+    }
+    s.behind = attend_shape(call, cus);
     if (!a.prefixes) return s;
     // rows of a prefix: the host knows their average
     const uint64_t each = ceil_div(rows, a.prefixes);
@@ -136,9 +134,15 @@ SharedShape shared_shape(const she_attend_shared_args &a, uint32_t cus)
     return s;
 }
 
+size_t shared_pieces(const she_attend_shared_args &a, const SharedShape &s)
+{
+    if (s.whole) return s.behind.splits > 1 ? (size_t)a.tokens * a.q_heads * s.behind.splits : 0;
+    return (size_t)a.tokens * a.q_heads * (s.prefix.splits + s.behind.splits);
+}
+
 size_t shared_scratch(const she_attend_shared_args &a, const SharedShape &s)
 {
-    return (size_t)a.tokens * a.q_heads * (s.prefix.splits + s.behind.splits) * (a.head * sizeof(float) + sizeof(float2));
+    return shared_pieces(a, s) * (a.head * sizeof(float) + sizeof(float2));
 }
 
 }}  // namespace she::clear

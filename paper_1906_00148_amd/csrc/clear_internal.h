@@ -55,14 +55,14 @@ size_t attend_pieces(const she_attend_pages_args &a, const AttendShape &s);     
 size_t attend_scratch(const she_attend_pages_args &a, const AttendShape &s);
 hipError_t launch_attend_pages(const she_attend_pages_args &a, const AttendShape &s, void *scratch, uint32_t *d_bad, hipStream_t st);
 
-// A call with shared prefixes: the walk over these, and the one over what the requests have behind them.
+// A call with shared prefixes: the walk over these, and the one over what the requests have behind them; or each request's over both.
 struct SharedShape {
-    AttendShape prefix, behind;
+    bool whole;                          // `behind` is the walk over both
+    AttendShape prefix, behind;          // either joined with the other, whatever its pieces
 };
-// The two walks as calls of their own: of the prefixes as requests, and of the requests' own places.
-she_attend_pages_args shared_prefixes(const she_attend_shared_args &a);
-she_attend_pages_args shared_behind(const she_attend_shared_args &a);
+she_attend_pages_args shared_behind(const she_attend_shared_args &a);            // the walk over the requests' own places as a call
 SharedShape shared_shape(const she_attend_shared_args &a, uint32_t cus);
+size_t shared_pieces(const she_attend_shared_args &a, const SharedShape &s);     // rows of pieces that wait to be joined
 size_t shared_scratch(const she_attend_shared_args &a, const SharedShape &s);
 hipError_t launch_attend_shared(const she_attend_shared_args &a, const SharedShape &s, void *scratch, uint32_t *d_bad, hipStream_t st);
 

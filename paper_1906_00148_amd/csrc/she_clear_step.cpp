@@ -49,8 +49,8 @@ try {
     int rc = ready(c);
     if (rc) return rc;
     const SharedShape s = shared_shape(a, c->dk.cus);
-    for (const AttendShape &w : {s.prefix, s.behind})
-        if ((w.few ? w.slots : w.slots * a.kv_heads) > MOST_GROUPS) return fail(c, SHE_ERANGE, at + "too many tokens and requests for one call");
+    if (s.prefix.slots * a.kv_heads * s.prefix.splits + s.behind.slots * a.kv_heads * s.behind.splits > MOST_GROUPS)
+        return fail(c, SHE_ERANGE, at + "too many tokens and requests for one call");
     if ((rc = ensure_scratch(c, shared_scratch(a, s)))) return rc;
     HIP_TRY(c, launch_attend_shared(a, s, c->clear.scratch(), c->clear.d_bad, c->stream));
     return SHE_OK;
