@@ -872,19 +872,21 @@ __global__ __launch_bounds__(256) void k_attend_join(she_attend_pages_args a, ui
 
 // A call with shared prefixes, whose two walks are one launch: while the prefixes' workgroups, of many rows, wait for the matrix units, those
 // of the requests' own places wait for memory.
-template <class T, int DP, bool FEW> struct SharedOf;
-template <class T, int DP> struct SharedOf<T, DP, true> { using Prefix = FewShared<DP>; };
-template <class T, int DP> struct SharedOf<T, DP, false> { using Prefix = TileShared<T, DP>; };
-template <class T, int DP, bool FEW>
+template <class T, int DP, bool FEW> using SharedOf = typename std::conditional<FEW, FewShared<DP>, TileShared<T, DP>>::type;
+template <class T, int DP, bool FEW, Walk WALK>
+__device__ __forceinline__ void attend_block(const she_attend_pages_args &a, uint32_t group, const Pieces &pieces, const Owners &owners, const void *zeros, uint32_t *d_bad, char *shared,
+                                             uint32_t slots, uint32_t block)
+{
+    const uint32_t i = block / a.kv_heads, kv_head = block - i * a.kv_heads, z = i / slots, slot = i - z * slots;
+    auto &its = *reinterpret_cast<SharedOf<T, DP, FEW> *>(shared);
+    if constexpr (FEW) attend_few<T, DP, WALK>(a, group, pieces, owners, d_bad, its, slot, (int)kv_head, (int)z);
+    else attend_tile<T, DP, WALK>(a, group, pieces, owners, zeros, d_bad, its, slot, (int)kv_head, (int)z);
+}
+template <class T, int DP, bool PREFIX_FEW, bool FEW>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_shared(she_attend_pages_args a, uint32_t group, Pieces prefix, Pieces pieces, Owners owners, const void *zeros,
                                                                           uint32_t prefix_slots, uint32_t prefix_blocks, uint32_t slots, uint32_t *d_bad)
 {
-    using Prefix = typename SharedOf<T, DP, FEW>::Prefix;
-    __shared__ union {
-        char prefix[sizeof(Prefix)];
-        char behind[sizeof(FewShared<DP>)];
-        int64_t align[2];
-    } shared;
+    __shared__ alignas(16) char shared[std::max(sizeof(SharedOf<T, DP, PREFIX_FEW>), sizeof(SharedOf<T, DP, FEW>))];
     if (blockIdx.x < prefix_blocks) {
         she_attend_pages_args p = a;
         p.requests = owners.prefixes;
@@ -892,26 +894,22 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_shared(she_at
         p.table_stride = owners.prefix_stride;
         p.table_width = owners.prefix_width;
         p.lengths = owners.prefix_lengths;
-        const uint32_t i = blockIdx.x / a.kv_heads, kv_head = blockIdx.x - i * a.kv_heads, z = i / prefix_slots, slot = i - z * prefix_slots;
-        if constexpr (FEW)
-            attend_few<T, DP, PREFIXES>(p, group, prefix, owners, d_bad, *reinterpret_cast<Prefix *>(shared.prefix), slot, (int)kv_head, (int)z);
-        else
-            attend_tile<T, DP, PREFIXES>(p, group, prefix, owners, zeros, d_bad, *reinterpret_cast<Prefix *>(shared.prefix), slot, (int)kv_head, (int)z);
+        attend_block<T, DP, PREFIX_FEW, PREFIXES>(p, group, prefix, owners, zeros, d_bad, shared, prefix_slots, blockIdx.x);
     } else {
-        const uint32_t b = blockIdx.x - prefix_blocks, i = b / a.kv_heads, kv_head = b - i * a.kv_heads, z = i / slots, slot = i - z * slots;
-        attend_few<T, DP, BEHIND>(a, group, pieces, owners, d_bad, *reinterpret_cast<FewShared<DP> *>(shared.behind), slot, (int)kv_head, (int)z);
+        attend_block<T, DP, FEW, BEHIND>(a, group, pieces, owners, zeros, d_bad, shared, slots, blockIdx.x - prefix_blocks);
     }
 }
 
-// Rows of such a call: a workgroup each, in the order of the pieces, in which neighbours have different key heads and a key head's
-// pieces come from the XCD that wrote them, where there are eight of them.  D/4 lanes have a piece's elements, so that 1024 / D pieces are
-// read side by side.
-template <class T> __global__ __launch_bounds__(256) void k_shared_join(she_attend_pages_args a, uint32_t group, Pieces pieces)
+// Rows of such a call, in the order of the pieces: neighbours have different key heads, so that where there are eight a row's pieces come from
+// the XCD that wrote them.  D/4 lanes have a piece's elements, and 4 * `lanes` / D pieces are read side by side by as many threads as
+// have the row: a workgroup for many pieces, a wavefront for few, which then needs no barrier.
+template <class T, int ROW> __global__ __launch_bounds__(256) void k_shared_join(she_attend_pages_args a, uint32_t group, Pieces pieces)
 {
     __shared__ f32x4 joined[256];
-    const int tid = threadIdx.x, lane = tid & 63, D = (int)a.head, lanes = D / 4, sets = 256 / lanes, set = tid / lanes, d = tid % lanes * 4, parts = (int)pieces.splits;
-    const int64_t first = bounded_start(a.starts, 0, a.tokens), last = bounded_start(a.starts, (int)a.requests, a.tokens);
-    for (int64_t row = blockIdx.x; row < (int64_t)a.tokens * a.q_heads; row += gridDim.x) {
+    const int tid = threadIdx.x % ROW, lane = threadIdx.x & 63, D = (int)a.head, lanes = D / 4, sets = ROW / lanes, set = tid / lanes, d = tid % lanes * 4, parts = (int)pieces.splits;
+    f32x4 *mine = joined + (threadIdx.x - tid);
+    const int64_t first = bounded_start(a.starts, 0, a.tokens), last = bounded_start(a.starts, (int)a.requests, a.tokens), rows = (int64_t)a.tokens * a.q_heads;
+    for (int64_t row = (int64_t)blockIdx.x * (256 / ROW) + threadIdx.x / ROW; row < rows; row += (int64_t)gridDim.x * (256 / ROW)) {
         const int64_t token = row / a.q_heads;
         const int at_token = (int)(row - token * a.q_heads), kv_head = at_token % (int)a.kv_heads, head = kv_head * (int)group + at_token / (int)a.kv_heads;
         if (token < first || token >= last) continue;
@@ -926,6 +924,7 @@ template <class T> __global__ __launch_bounds__(256) void k_shared_join(she_atte
 #pragma unroll
         for (int m = 1; m < 64; m *= 2) sum += __shfl_xor(sum, m);
         const bool none = ml[pieces.first].y == NOTHING;
+        const float inv = sum == 0 ? 0.0f : 1.0f / sum;
         f32x4 o{0, 0, 0, 0};
         if (set < sets && !none) {
 #pragma unroll 4
@@ -936,14 +935,16 @@ template <class T> __global__ __launch_bounds__(256) void k_shared_join(she_atte
                 for (int i = 0; i < 4; i++) o[i] = fmaf(v[i], f, o[i]);
             }
         }
-        joined[tid] = o;
-        __syncthreads();
-        if (tid < D) {
+        mine[tid] = o;
+        if constexpr (ROW == 64) wave_lds_fence();
+        else __syncthreads();
+        for (int e = tid; e < D; e += ROW) {
             float v = 0;
-            for (int k = 0; k < sets; k++) v += joined[k * lanes + tid / 4][tid & 3];
-            ((T *)a.out)[token * a.out_token + head * a.out_head + tid] = none ? (T)0.0f : (T)(v * (sum == 0 ? 0.0f : 1.0f / sum));
+            for (int k = 0; k < sets; k++) v += mine[k * lanes + e / 4][e & 3];
+            ((T *)a.out)[token * a.out_token + head * a.out_head + e] = none ? (T)0.0f : (T)(v * inv);
         }
-        __syncthreads();
+        if constexpr (ROW == 64) wave_lds_fence();
+        else __syncthreads();
     }
 }
 
@@ -956,7 +957,6 @@ template <class F> hipError_t by_head(uint32_t head, F launch)
     return hipGetLastError();
 }
 
-// A walk that is a launch of its own.
 template <class T, Walk WALK>
 hipError_t walk(const she_attend_pages_args &a, const AttendShape &s, const Pieces &pieces, const Owners &owners, uint32_t *d_bad, hipStream_t st)
 {
@@ -988,19 +988,18 @@ template <class T, Walk WALK> hipError_t attend(const she_attend_pages_args &a, 
 template <class T> hipError_t attend_shared(const she_attend_pages_args &a, const SharedShape &s, const Pieces &prefix, const Pieces &pieces, const Owners &owners, uint32_t *d_bad, hipStream_t st)
 {
     const uint32_t group = a.q_heads / a.kv_heads, prefix_slots = (uint32_t)s.prefix.slots, prefix_blocks = prefix_slots * a.kv_heads * s.prefix.splits;
-    const uint32_t slots = s.behind.few ? (uint32_t)s.behind.slots : 0, blocks = slots * a.kv_heads * s.behind.splits;
-    hipError_t rc = hipSuccess;
-    if (prefix_blocks + blocks)
-        rc = by_head(a.head, [&](auto size) {
-            constexpr int DP = decltype(size)::value;
-            if (s.prefix.few)
-                k_attend_shared<T, DP, true><<<prefix_blocks + blocks, 256, 0, st>>>(a, group, prefix, pieces, owners, zeros_of(d_bad), prefix_slots, prefix_blocks, slots, d_bad);
-            else
-                k_attend_shared<T, DP, false><<<prefix_blocks + blocks, 256, 0, st>>>(a, group, prefix, pieces, owners, zeros_of(d_bad), prefix_slots, prefix_blocks, slots, d_bad);
-        });
-    if (rc == hipSuccess && !s.behind.few) rc = walk<T, BEHIND>(a, s.behind, pieces, owners, d_bad, st);
+    const uint32_t slots = (uint32_t)s.behind.slots, blocks = prefix_blocks + slots * a.kv_heads * s.behind.splits;
+    const hipError_t rc = by_head(a.head, [&](auto size) {
+        constexpr int DP = decltype(size)::value;
+        const auto launch = [&](auto kernel) { kernel<<<blocks, 256, 0, st>>>(a, group, prefix, pieces, owners, zeros_of(d_bad), prefix_slots, prefix_blocks, slots, d_bad); };
+        if (s.prefix.few) launch(k_attend_shared<T, DP, true, true>);
+        else if (s.behind.few) launch(k_attend_shared<T, DP, false, true>);
+        else launch(k_attend_shared<T, DP, false, false>);
+    });
     if (rc != hipSuccess) return rc;
-    k_shared_join<T><<<(uint32_t)std::min<uint64_t>((uint64_t)a.tokens * a.q_heads, 1u << 20), 256, 0, st>>>(a, group, pieces);
+    const uint64_t rows = (uint64_t)a.tokens * a.q_heads;
+    if (pieces.splits <= 8) k_shared_join<T, 64><<<(uint32_t)std::min<uint64_t>(ceil_div(rows, 4), 1u << 20), 256, 0, st>>>(a, group, pieces);
+    else k_shared_join<T, 256><<<(uint32_t)std::min<uint64_t>(rows, 1u << 20), 256, 0, st>>>(a, group, pieces);
     return hipGetLastError();
 }
 

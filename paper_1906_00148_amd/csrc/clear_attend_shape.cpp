@@ -109,29 +109,48 @@ she_attend_pages_args shared_behind(const she_attend_shared_args &a)
 SharedShape shared_shape(const she_attend_shared_args &a, uint32_t cus)
 {
     SharedShape s{};
-    const uint64_t group = a.q_heads / a.kv_heads, rows = a.tokens * group, places = (uint64_t)a.prefix_width * a.page_size;
     if (!cus) cus = 1;
-    she_attend_pages_args call = shared_behind(a);
-    if (!a.prefixes || rows >= 96ull * a.requests) {
-        s.whole = true;
-        call.table_width += a.prefix_width;
-        s.behind = attend_shape(call, cus);
-        if (!s.behind.few) return s;
-        s = SharedShape{};
-        call.table_width = a.table_width;
-    }
+    const uint64_t group = a.q_heads / a.kv_heads, rows = a.tokens * group, places = (uint64_t)a.prefix_width * a.page_size, own = (uint64_t)a.table_width * a.page_size;
+    const she_attend_pages_args call = shared_behind(a);
     s.behind = attend_shape(call, cus);
     if (!a.prefixes) return s;
     // rows of a prefix: the host knows their average
     const uint64_t each = ceil_div(rows, a.prefixes);
-    s.prefix.few = each <= FEW_ROWS || each * places <= 1u << 18;
+    s.prefix.few = s.behind.few && (each <= FEW_ROWS || each * places <= 1u << 18);
     const uint64_t tile = s.prefix.few ? FEW_ROWS : TILE_ROWS;
     s.prefix.slots = a.prefixes == 1 ? ceil_div(rows, tile) : rows / tile + a.prefixes;
-    const uint64_t at_once = s.prefix.few ? 2 * cus : cus * (a.head <= 64 ? 3 : a.head <= 128 ? 2 : 1);
-    const uint64_t tiles = a.prefixes * ceil_div(each, tile) * a.kv_heads;
     s.prefix.chunk = s.prefix.few ? 256 : 512;
-    s.prefix.splits = (uint32_t)std::max<uint64_t>(1, std::min(ceil_div(places, s.prefix.chunk), at_once / tiles));
-    return s;
+    // Costs in places that a workgroup with a compute unit to itself walks.  It costs as much as 256 of them beside its own, two on a unit take
+    // 1.44 times as long as one, and a row of a piece, written and read again, is a 94th.
+    const uint64_t share = a.head > 128 ? 100 : 72, at_most = std::max<uint64_t>(1, std::min<uint64_t>(64, ceil_div(places, s.prefix.chunk)));
+    const auto time = [&](uint64_t groups, uint64_t walk, uint64_t beside) {
+        return std::max(walk + 256, (ceil_div(groups, cus) * (walk + 256) + beside) * share / 100);
+    };
+    // the requests' own places, of which the host knows the most that there may be: half of them, a tile of few rows at half the price
+    const uint64_t behind = ceil_div(s.behind.slots * a.kv_heads * s.behind.splits, cus) * (own / (2 * s.behind.splits) + 256) / (s.behind.few ? 2 : 1);
+    const uint64_t groups = a.prefixes * ceil_div(each, tile) * a.kv_heads, row = rows * a.kv_heads;
+    uint64_t best = ~0ull;
+    for (uint64_t splits = 1; splits <= at_most; splits++) {
+        const uint64_t c = time(groups * splits, ceil_div(places, splits), behind) + row * (splits + s.behind.splits) / 94;
+        if (c >= best) continue;
+        best = c;
+        s.prefix.splits = (uint32_t)splits;
+    }
+    // Or every request's tiles walk the prefix and its own places as one.
+    if (s.behind.few) return s;
+    const uint64_t tiles = std::max<uint64_t>(rows / TILE_ROWS + a.requests / 2, std::min<uint64_t>(a.requests, a.tokens)) * a.kv_heads;
+    SharedShape w{};
+    w.whole = true;
+    w.behind.slots = a.requests == 1 ? ceil_div(rows, TILE_ROWS) : rows / TILE_ROWS + a.requests;
+    uint64_t least = ~0ull;
+    for (uint64_t splits = 1; splits <= std::max<uint64_t>(1, std::min<uint64_t>(64, ceil_div(places + own, 512))); splits++) {
+        const uint64_t c = time(tiles * splits, ceil_div(places + own / 2, splits), 0) * 5 / 4 + (splits > 1 ? 128 + row * splits / 94 : 0);
+        if (c >= least) continue;
+        least = c;
+        w.behind.splits = (uint32_t)splits;
+        w.behind.chunk = (uint32_t)(ceil_div(ceil_div(places + own, splits), STEP) * STEP);
+    }
+    return least <= best ? w : s;
 }
 
 size_t shared_pieces(const she_attend_shared_args &a, const SharedShape &s)

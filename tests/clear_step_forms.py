@@ -101,24 +101,27 @@ def shared(q, k_pages, v_pages, table, starts, lengths, prefix_table, prefix_req
         found = ([] if g is None else there(prefix_table[g], P)) + [(P + u, page, slot) for u, page, slot in there(table[r], length)]
         place, page, slot = (torch.tensor([f[i] for f in found], dtype=torch.long) for i in range(3))
         k, v = k_pages[page, slot], v_pages[page, slot]                                # [places, Hkv, D]
-        for t in range(b, e):
-            p = length - (e - b) + (t - b)
-            if p < 0:
-                continue
-            mine = place <= P + p
-            if window:
-                mine &= place > P + p - window
+        p = torch.arange(length - (e - b), length)
+        seen = (place <= P + p[:, None]) & (p >= 0)[:, None]
+        if window:
+            seen &= place > P + p[:, None] - window
+        # all tokens at once, or one by one where a place that others attend to is not finite, nor is its product with a weight of 0
+        whole = bool(torch.isfinite(k).all() and torch.isfinite(v).all())
+        for rows in [slice(0, e - b)] if whole else [slice(i, i + 1) for i in range(e - b)]:
+            mine = seen[rows].any(0)
             if not mine.any():
                 continue
-            km = k[mine].repeat_interleave(Hq // Hkv, 1).transpose(0, 1)               # [Hq, n, D]
-            vm = v[mine].repeat_interleave(Hq // Hkv, 1).transpose(0, 1)
-            s = scale * (km @ q[t][:, :, None])[..., 0]
-            w = torch.softmax(s, -1)
-            out[t] = (w[:, None] @ vm)[:, 0]
-            ds = (D + 8) * F32 * (abs(scale) * (km.abs() @ q[t].abs()[:, :, None])[..., 0]).amax(-1) + 4 * F32 * s.abs().amax(-1)
-            n = mine.sum().item()
-            unit = C.UNIT[dtype] + 2 * ds + (2 * n + 32) * F32
-            bound[t] = unit[:, None] * (w[:, None] @ vm.abs())[:, 0]
+            km, vm = (t[mine].repeat_interleave(Hq // Hkv, 1).transpose(0, 1).contiguous() for t in (k, v))        # [Hq, n, D]
+            qm, sees = q[b:e][rows].transpose(0, 1), seen[rows][:, mine]                # [Hq, tokens, D], [tokens, n]
+            some = sees.any(1)[:, None]
+            s = (scale * (qm @ km.mT)).masked_fill(~sees, -np.inf)
+            w = torch.where(some, torch.softmax(s, -1), 0.0)
+            out[b:e][rows] = (w @ vm).transpose(0, 1)
+            most = (abs(scale) * (qm.abs() @ km.abs().mT)).masked_fill(~sees, 0.0).amax(-1)
+            ds = (D + 8) * F32 * most + 4 * F32 * s.masked_fill(~sees, 0.0).abs().amax(-1)
+            unit = C.UNIT[dtype] + 2 * ds + (2 * sees.sum(1) + 32) * F32               # [Hq, tokens]
+            limit = unit[..., None] * (w @ vm.abs())
             if dtype is torch.float16:
-                bound[t] += 2.0 ** -25 * vm.abs().sum(1)
+                limit = limit + 2.0 ** -25 * (sees.double() @ vm.abs())
+            bound[b:e][rows] = limit.transpose(0, 1)
     return out, bound
