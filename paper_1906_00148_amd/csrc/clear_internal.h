@@ -74,6 +74,11 @@ size_t plan_scratch(const she_plan_pages_args &a);
 hipError_t launch_plan_pages(const she_plan_pages_args &a, void *scratch, uint32_t *d_bad, hipStream_t st);
 
 // ---- the next token
-hipError_t launch_sample(const she_sample_args &a, uint32_t cus, hipStream_t st);
+struct SampleShape {
+    uint32_t parts, tiles;               // workgroups that share a row, none if one has all of it at once; tiles of logits of each
+};
+SampleShape sample_shape(const she_sample_args &a, uint32_t cus);
+size_t sample_scratch(const she_sample_args &a, const SampleShape &s);
+hipError_t launch_sample(const she_sample_args &a, const SampleShape &s, void *scratch, hipStream_t st);
 
 }}  // namespace she::clear

@@ -4,21 +4,25 @@
 // adding gives the same.  One is computed in 64-bit floating point, since a draw next to a border shows an error of 32 bits: with
 // y = (logit - max) log2(e) / T in units of 1/256, the nearest whole k and the rest r, it is 2^(k/256) from a table and a power of two,
 // times 2^(r/256) by its series up to the fourth power (the fifth is below 2^-54).  What lies more than 44.5 octaves below the
-// largest has no weight.
+// largest has no weight: it is taken as there, where the weight rounds to 0.
 //
 // The tokens that filters keep are the first of an order, larger logits first and of equals the lower index: all above a logit, and of
-// those equal to it the ones up to an index.  The logit is found by histograms: over y in 32nds of an octave first, then over the
-// bits of the bin's logits until a bin is one value.  top_k counts with ones, top_p with weights.
+// those equal to it the ones up to an index.  Mostly they are few.  Then those that may be among them are picked out, up to a thread of a
+// workgroup each, by a histogram of y in 32nds of an octave: of weights for top_p, which needs all of them anyway; for top_k of the largest of
+// every eight neighbours, since k of these that reach a logit are k logits that do.  Where they are many, the logit is found by
+// histograms over the row, from the 32nds of an octave on to the bits of the bin's logits until a bin is one value.
+#include <algorithm>
+
 #include "clear_device.h"
 #include "clear_internal.h"
 
 namespace she { namespace clear {
 namespace {
 
-constexpr int THREADS = 1024, WAVES = THREADS / 64, TILE = 512, BINS = 2048;
+constexpr int TILE = 512, BINS = 2048, THREADS = 1024, WAVES = THREADS / 64, PART_THREADS = 256;
 constexpr int ONE_AT = 43;                                         // a weight of 1 is 2^43
 constexpr uint64_t ONE = 1ull << ONE_AT;
-constexpr double LOG2E = 1.4426950408889634074, DEAD = -256 * 44.5;
+constexpr double LOG2E = 1.4426950408889634074, LN2 = 0.69314718055994530942, DEAD = -256 * 44.5;
 
 __device__ inline uint32_t key_of(float v)                         // ordered as the numbers are
 {
@@ -27,15 +31,18 @@ __device__ inline uint32_t key_of(float v)                         // ordered as
 }
 __device__ inline float number_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
 
-// Eight logits of a row from `at` on, -infinity beyond its end and for NaN, and no negative zero.
 template <class T> struct Row {
     const T *p;
     const float *step;
     uint32_t vocab;
 };
-template <class T> __device__ inline void load_logits(const Row<T> &row, uint32_t at, float v[8])
+template <class T> __device__ inline Row<T> row_of(const she_sample_args &a, uint32_t r) { return Row<T>{(const T *)a.logits + r * a.row_stride, a.step, a.vocab}; }
+
+// Eight logits of a row from `at` on, NaN beyond its end.
+template <class T> __device__ __forceinline__ void load_logits(const Row<T> &row, uint32_t at, float v[8])
 {
-    const int count = (int)min((int64_t)row.vocab - at, (int64_t)8);
+    const int64_t left = (int64_t)row.vocab - at;                  // any distance, also of a place that no row has
+    const int count = left <= 0 ? 0 : left < 8 ? (int)left : 8;
     if constexpr (sizeof(T) == 2) {
         unpack<T>(load8<T, false>(row.p + at, count), v);
     } else {
@@ -49,12 +56,21 @@ template <class T> __device__ inline void load_logits(const Row<T> &row, uint32_
 #pragma unroll
             for (int i = 0; i < 8; i++) v[i] = raw[i];
         } else {
+            float step[8];
+            if (row.step && count >= 8) {
+                __builtin_memcpy(step, row.step + at, 32);
+            } else {
+                for (int i = 0; i < 8; i++) step[i] = row.step && i < count ? row.step[at + i] : 1.0f;
+            }
+            // one rounding: a sum need not be a number of 32 bits
 #pragma unroll
-            for (int i = 0; i < 8; i++) v[i] = (float)((double)raw[i] * (row.step && i < count ? (double)row.step[at + i] : 1.0));
+            for (int i = 0; i < 8; i++) v[i] = (float)((double)raw[i] * (double)step[i]);
         }
     }
+    if (count < 8) {
 #pragma unroll
-    for (int i = 0; i < 8; i++) v[i] = i < count && v[i] == v[i] ? v[i] + 0.0f : -__builtin_inff();
+        for (int i = 0; i < 8; i++) v[i] = i < count ? v[i] : __builtin_nanf("");
+    }
 }
 
 // 2^(j/256), to which a whole exponent is added in place.
@@ -65,31 +81,48 @@ __device__ inline void make_table(double *table)
 
 // What the logits of a row weigh.
 struct Weights {
-    float top;                           // the largest logit
-    double unit;                         // 256 log2(e) / T
+    float top;                           // the largest logit, 0 where that is infinite
+    bool infinite;                       // it is: then those that are have 0 for a logit, and the others -infinity
+    double unit;                         // 256 log2(e) / T, finite
     const double *table;
 
-    // in units of 1/256 octave, from 0 down; DEAD where there is no weight
-    __device__ double below(float v) const
+    __device__ __forceinline__ Weights(float largest, float temperature, const double *table)
+        : top(largest + 0.0f), infinite(largest == __builtin_inff()), unit(fmin(256 * LOG2E / (double)temperature, 1e300)), table(table)
     {
-        const double s = v == top ? 0.0 : ((double)v - (double)top) * unit;
-        return s >= DEAD ? s : DEAD;                               // NaN, of -infinity at T = infinity, has none either
+        if (infinite) top = 0;
     }
-    __device__ static int nearest(double s) { return __double2loint(s + 6755399441055744.0); }
-    __device__ uint64_t weight(double s) const
+    // a logit as it is compared: no NaN, no negative zero
+    __device__ __forceinline__ float plain(float v) const
     {
-        if (s <= DEAD) return 0;
-        const double shifted = s + 6755399441055744.0;             // 1.5 * 2^52: the nearest whole number is in the low bits
+        if (infinite) return v == __builtin_inff() ? 0.0f : -__builtin_inff();
+        return v == v ? v + 0.0f : -__builtin_inff();
+    }
+    // in units of 1/256 octave, from 0 down to DEAD, which is where NaN goes too
+    __device__ __forceinline__ double below(float v) const
+    {
+        if (infinite) v = v == __builtin_inff() ? 0.0f : -__builtin_inff();
+        return fmax(((double)v - (double)top) * unit, DEAD);
+    }
+    __device__ __forceinline__ double below_plain(float v) const { return fmax(((double)v - (double)top) * unit, DEAD); }
+    __device__ __forceinline__ static int nearest(double s) { return __double2loint(s + 6755399441055744.0); }      // 1.5 * 2^52: the low bits have it
+    __device__ __forceinline__ static int bin(double s) { return -nearest(s) >> 3; }
+    // the weight, with the bits of 512.0 above it
+    __device__ __forceinline__ uint64_t raw_weight(double s) const
+    {
+        constexpr double L = LN2 / 256;
+        const double shifted = s + 6755399441055744.0;
         const int k = __double2loint(shifted);
-        const double r = (s - (shifted - 6755399441055744.0)) * (0.69314718055994530942 / 256);
-        const double f = fma(r * r, fma(r, fma(r, 1.0 / 24, 1.0 / 6), 0.5), r);      // 2^(r/256) - 1
-        const double t = __longlong_as_double(__double_as_longlong(table[k & 255]) + ((int64_t)(k >> 8) << 52));
-        // added to 2^9, whose last bit is 2^-43
-        return (uint64_t)(__double_as_longlong(fma(t, f, t) + 512.0) - __double_as_longlong(512.0));
+        const double r = s - (shifted - 6755399441055744.0);
+        const double f = r * fma(r, fma(r, fma(r, L * L * L * L / 24, L * L * L / 6), L * L / 2), L);       // 2^(r/256) - 1
+        const double t = __longlong_as_double(__double_as_longlong(table[k & 255]) + ((int64_t)(k & ~255) << 44));
+        return (uint64_t)__double_as_longlong(fma(t, f, t) + 512.0);                                       // whose last bit is 2^-43
     }
+    __device__ __forceinline__ uint64_t weight(double s) const { return raw_weight(s) - (uint64_t)__double_as_longlong(512.0); }
 };
+constexpr uint64_t RAW = 0x4080000000000000ull;                    // the bits of 512.0
+constexpr int DEAD_BIN = (int)(256 * 44.5) >> 3;
 
-__device__ inline uint64_t wave_sum(uint64_t v)
+__device__ __forceinline__ uint64_t wave_sum(uint64_t v)
 {
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) v += __shfl_xor(v, m);
@@ -97,7 +130,7 @@ __device__ inline uint64_t wave_sum(uint64_t v)
 }
 
 // f * all for f in [0, 1), rounded down or up and not by way of a shorter number: a border that falls on a token exactly stays there.
-__device__ inline uint64_t share_of(uint64_t all, float f, bool up)
+__device__ __forceinline__ uint64_t share_of(uint64_t all, float f, bool up)
 {
     const uint32_t bits = __float_as_uint(f), e = bits >> 23;
     const uint64_t m = e ? (bits & 0x7FFFFF) | 0x800000 : bits;    // f = m / 2^s, s >= 24
@@ -120,7 +153,7 @@ struct Crossing {
     int bin;
     uint64_t before;
 };
-__device__ inline Crossing find_crossing(const uint64_t *hist, uint64_t target, uint64_t *sums, Crossing *found)
+__device__ __forceinline__ Crossing find_crossing(const uint64_t *hist, uint64_t target, uint64_t *sums, Crossing *found)
 {
     constexpr int EACH = BINS / THREADS;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -152,22 +185,28 @@ __device__ inline Crossing find_crossing(const uint64_t *hist, uint64_t target, 
 // The tokens that are kept: of the logits of `key` those up to index `last`, and all with larger keys.
 struct Kept {
     uint32_t key, last;
-    __device__ bool has(uint32_t k, uint32_t index) const { return k > key || (k == key && index <= last); }
+    __device__ __forceinline__ bool has(uint32_t k, uint32_t index) const { return k > key || (k == key && index <= last); }
 };
 
+struct Candidate {
+    uint64_t order;                      // larger ones come first: the logit's key above the index, turned round
+    uint64_t weight;
+};
 struct Shared {
     uint64_t bins[BINS];                 // a histogram; sums or counts of tiles
     double table[256];
-    uint64_t sums[WAVES];
+    Candidate list[THREADS];
+    uint64_t sums[WAVES], totals[WAVES];
     Crossing found;
     float tops[WAVES];
-    uint32_t where[WAVES], answer;
+    uint32_t where[WAVES], answer, count;
 };
 
-template <class T, class F> __device__ inline void for_all(const Row<T> &row, F f)
+template <class T, class F> __device__ __forceinline__ void for_all(const Row<T> &row, F f)
 {
-    constexpr int AHEAD = 4;
+    constexpr int AHEAD = 2;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll 1
     for (uint32_t at = wave * TILE; at < row.vocab; at += WAVES * TILE * AHEAD) {
         float v[AHEAD][8];
 #pragma unroll
@@ -178,34 +217,34 @@ template <class T, class F> __device__ inline void for_all(const Row<T> &row, F 
             if (at + k * WAVES * TILE < row.vocab) f(at + k * WAVES * TILE + lane * 8, v[k]);
     }
 }
-__device__ inline void clear_bins(Shared &s)
+__device__ __forceinline__ void clear_bins(Shared &s)
 {
     for (int i = threadIdx.x; i < BINS; i += THREADS) s.bins[i] = 0;
     __syncthreads();
 }
 
 // Of what `kept` has, the first of the order whose measure (ones or weights) together reaches `target`; `kept` itself if all does not.
-template <bool COUNT, class T> __device__ inline Kept select(const Row<T> &row, const Weights &w, Kept kept, uint64_t target, Shared &s)
+// `known`: the bins have that histogram already.
+template <bool COUNT, class T> __device__ __forceinline__ Kept select(const Row<T> &row, const Weights &w, Kept kept, uint64_t target, bool known, Shared &s)
 {
     const auto measure = [&](double y) { return COUNT ? 1 : w.weight(y); };
+    if (!known) {
     clear_bins(s);
     for_all(row, [&](uint32_t at, const float v[8]) {
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-            const double y = w.below(v[i]);
-            if (y > DEAD && kept.has(key_of(v[i]), at + i)) atomicAdd((unsigned long long *)&s.bins[-w.nearest(y) >> 3], (unsigned long long)measure(y));
+            const float l = w.plain(v[i]);
+            const double y = w.below_plain(l);
+            if (y > DEAD && kept.has(key_of(l), at + i)) atomicAdd((unsigned long long *)&s.bins[w.bin(y)], (unsigned long long)measure(y));
         }
     });
     __syncthreads();
+    }
     Crossing c = find_crossing(s.bins, target, s.sums, &s.found);
     if (c.bin < 0) return kept;
     const int bin = c.bin;
     // Keys that surround the bin's, so wide that no rounding matters.  (Where unit is 0, all logits are in bin 0.)
-    uint32_t high = key_of(w.top), low = high;
-    if (w.top < __builtin_inff()) {
-        low = key_of((float)((double)w.top - (8 * bin + 8) / w.unit));
-        high = min(high, key_of((float)((double)w.top - (8 * bin - 1) / w.unit)));
-    }
+    uint32_t low = key_of((float)((double)w.top - (8 * bin + 8) / w.unit)), high = min(key_of(w.top), key_of((float)((double)w.top - (8 * bin - 1) / w.unit)));
     target -= c.before;
     for (;;) {
         int shift = 0;
@@ -214,10 +253,11 @@ template <bool COUNT, class T> __device__ inline Kept select(const Row<T> &row, 
         for_all(row, [&](uint32_t at, const float v[8]) {
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                const uint32_t key = key_of(v[i]);
+                const float l = w.plain(v[i]);
+                const uint32_t key = key_of(l);
                 if (key < low || key > high || !kept.has(key, at + i)) continue;
-                const double y = w.below(v[i]);
-                if (y > DEAD && -w.nearest(y) >> 3 == bin) atomicAdd((unsigned long long *)&s.bins[(high - key) >> shift], (unsigned long long)measure(y));
+                const double y = w.below_plain(l);
+                if (y > DEAD && w.bin(y) == bin) atomicAdd((unsigned long long *)&s.bins[(high - key) >> shift], (unsigned long long)measure(y));
             }
         });
         __syncthreads();
@@ -234,14 +274,14 @@ template <bool COUNT, class T> __device__ inline Kept select(const Row<T> &row, 
         break;
     }
     // `low` is the last key that is kept; how many of the tokens that have it are
-    const uint64_t each = measure(w.below(number_of(low))), all = s.bins[c.bin] / each, wanted = (target + each - 1) / each;
+    const uint64_t each = measure(w.below_plain(number_of(low))), all = s.bins[c.bin] / each, wanted = (target + each - 1) / each;
     __syncthreads();
     if (wanted >= all) return Kept{low, low == kept.key ? kept.last : ~0u};
     // the index of the last of them, by tile and then by place
     for_all(row, [&](uint32_t at, const float v[8]) {
         uint32_t here = 0;
 #pragma unroll
-        for (int i = 0; i < 8; i++) here += key_of(v[i]) == low && kept.has(low, at + i);
+        for (int i = 0; i < 8; i++) here += key_of(w.plain(v[i])) == low && kept.has(low, at + i);
         const uint64_t sum = wave_sum(here);
         if ((threadIdx.x & 63) == 0) s.bins[at / TILE] = sum;
     });
@@ -254,7 +294,7 @@ template <bool COUNT, class T> __device__ inline Kept select(const Row<T> &row, 
         load_logits(row, at, v);
         uint32_t here = 0;
 #pragma unroll
-        for (int i = 0; i < 8; i++) here += key_of(v[i]) == low && kept.has(low, at + i);
+        for (int i = 0; i < 8; i++) here += key_of(w.plain(v[i])) == low && kept.has(low, at + i);
         uint32_t run = here;
 #pragma unroll
         for (int m = 1; m < 64; m *= 2) {
@@ -264,7 +304,7 @@ template <bool COUNT, class T> __device__ inline Kept select(const Row<T> &row, 
         uint32_t left = (uint32_t)(wanted - c.before), before = run - here;
 #pragma unroll
         for (int i = 0; i < 8; i++)
-            if (key_of(v[i]) == low && kept.has(low, at + i) && ++before == left) s.answer = at + i;
+            if (key_of(w.plain(v[i])) == low && kept.has(low, at + i) && ++before == left) s.answer = at + i;
     }
     __syncthreads();
     const uint32_t last = s.answer;
@@ -272,13 +312,117 @@ template <bool COUNT, class T> __device__ inline Kept select(const Row<T> &row, 
     return Kept{low, last};
 }
 
-// One workgroup a row.
+// The sum of v over the workgroup.
+__device__ __forceinline__ uint64_t block_sum(uint64_t v, Shared &s)
+{
+    v = wave_sum(v);
+    if ((threadIdx.x & 63) == 0) s.totals[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0;
+    for (int k = 0; k < WAVES; k++) v += s.totals[k];
+    __syncthreads();
+    return v;
+}
+
+struct Settings {
+    float temperature, top_p, uniform;
+    uint32_t top_k;                      // vocab: all
+    uint64_t least;                      // the weight that min_p asks for
+    __device__ __forceinline__ Settings(const she_sample_args &a, uint32_t r) : temperature(a.temperature ? a.temperature[r] : 1.0f), top_p(a.top_p ? a.top_p[r] : 1.0f), uniform(a.uniform[r])
+    {
+        const int32_t k = a.top_k ? a.top_k[r] : 0;
+        top_k = k > 0 && (uint32_t)k < a.vocab ? (uint32_t)k : a.vocab;
+        const float m = a.min_p ? a.min_p[r] : 0.0f;
+        least = m > 0 ? (uint64_t)ceil((double)fminf(m, 1.0f) * (double)ONE) : 0;
+        uniform = uniform > 0 ? fminf(uniform, 1.0f - 0x1p-24f) : 0.0f;
+    }
+    __device__ __forceinline__ uint64_t head(uint64_t all) const { return max(share_of(all, fmaxf(top_p, 0.0f), true), (uint64_t)1); }    // of a whole weight, for top_p below 1
+};
+
+__device__ inline void answer(const she_sample_args &a, uint32_t r, int32_t token, float prob)
+{
+    a.tokens[r] = token;
+    if (a.probs) a.probs[r] = prob;
+}
+// The weight itself, since of a small one few bits are held.
+__device__ __forceinline__ float prob_of(const Weights &w, float logit, uint64_t all) { return (float)(exp2(w.below(logit) / 256) * ((double)ONE / (double)all)); }
+
+// The draw from sums of the kept weights of every tile, in s.bins.
+template <class T> __device__ __forceinline__ void draw_by_tiles(const she_sample_args &a, uint32_t r, const Row<T> &row, const Weights &w, const Settings &set, const Kept &kept, Shared &s)
+{
+    const int lane = threadIdx.x & 63;
+    uint64_t all = 0;
+    for (int i = lane; i < BINS; i += 64) all += s.bins[i];
+    all = wave_sum(all);
+    const uint64_t drawn = share_of(all, set.uniform, false);
+    const Crossing c = find_crossing(s.bins, drawn + 1, s.sums, &s.found);
+    if (threadIdx.x >= 64) return;
+    float v[8];
+    const uint32_t at = c.bin * TILE + lane * 8;
+    load_logits(row, at, v);
+    uint64_t weight[8], here = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const float l = w.plain(v[i]);
+        weight[i] = kept.has(key_of(l), at + i) ? w.weight(w.below_plain(l)) : 0;
+        if (weight[i] < set.least) weight[i] = 0;
+        here += weight[i];
+    }
+    uint64_t run = here;
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) {
+        const uint64_t other = __shfl_up(run, m);
+        if (lane >= m) run += other;
+    }
+    run = run - here + c.before;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        if (run <= drawn && run + weight[i] > drawn) answer(a, r, (int32_t)(at + i), prob_of(w, v[i], all));
+        run += weight[i];
+    }
+}
+
+// The weights that are kept of every tile.
+template <class T> __device__ __forceinline__ void sum_tiles(const Row<T> &row, const Weights &w, const Kept &kept, uint64_t least, Shared &s)
+{
+    for_all(row, [&](uint32_t at, const float v[8]) {
+        uint64_t sum = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float l = w.plain(v[i]);
+            const uint64_t weight = kept.has(key_of(l), at + i) ? w.weight(w.below_plain(l)) : 0;
+            if (weight >= least) sum += weight;
+        }
+        sum = wave_sum(sum);
+        if ((threadIdx.x & 63) == 0) s.bins[at / TILE] = sum;
+    });
+    for (int i = threadIdx.x + (row.vocab + TILE - 1) / TILE; i < BINS; i += THREADS) s.bins[i] = 0;
+    __syncthreads();
+}
+
+// A row of any kind by passes over all of it.  `known`: s.bins has the histogram of all weights, and there is no top_k.
+template <class T> __device__ __forceinline__ void pass_by_pass(const she_sample_args &a, uint32_t r, const Row<T> &row, const Weights &w, const Settings &set, bool known, Shared &s)
+{
+    Kept kept{0, ~0u};
+    if (set.top_k < a.vocab) kept = select<true>(row, w, kept, set.top_k, false, s);
+    if (set.top_p < 1.0f) {
+        if (!known) sum_tiles(row, w, kept, 0, s);
+        uint64_t all = 0;
+        for (int i = threadIdx.x; i < BINS; i += THREADS) all += s.bins[i];
+        all = block_sum(all, s);
+        kept = select<false>(row, w, kept, set.head(all), known, s);
+    }
+    sum_tiles(row, w, kept, set.least, s);
+    draw_by_tiles(a, r, row, w, set, kept, s);
+}
+
+// Rows of few logits: a workgroup each.
 template <class T> __global__ __launch_bounds__(THREADS) void k_sample_rows(she_sample_args a)
 {
     __shared__ Shared s;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t r = blockIdx.x;
-    const Row<T> row{(const T *)a.logits + r * a.row_stride, a.step, a.vocab};
+    const Row<T> row = row_of<T>(a, r);
     make_table(s.table);
 
     // the largest logit, and the first that is as large
@@ -306,90 +450,303 @@ template <class T> __global__ __launch_bounds__(THREADS) void k_sample_rows(she_
     }
     __syncthreads();
     for (int k = 0; k < WAVES; k++) join(s.tops[k], s.where[k]);
-    const float temperature = a.temperature ? a.temperature[r] : 1.0f;
+    const Settings set(a, r);
     const bool none = top == -__builtin_inff();
-    if (none || !(temperature > 0)) {
-        if (threadIdx.x == 0) {
-            a.tokens[r] = none ? -1 : (int32_t)where;
-            if (a.probs) a.probs[r] = none ? 0.0f : 1.0f;
-        }
+    if (none || !(set.temperature > 0)) {
+        if (threadIdx.x == 0) answer(a, r, none ? -1 : (int32_t)where, none ? 0.0f : 1.0f);
         return;
     }
+    pass_by_pass(a, r, row, Weights(top, set.temperature, s.table), set, false, s);
+}
 
-    const Weights w{top, 256 * LOG2E / (double)temperature, s.table};
-    Kept kept{0, ~0u};
-    if (a.top_k && a.top_k[r] > 0 && (uint32_t)a.top_k[r] < a.vocab) kept = select<true>(row, w, kept, (uint64_t)a.top_k[r], s);
-    const float top_p = a.top_p ? a.top_p[r] : 1.0f;
-    const uint32_t tiles = (a.vocab + TILE - 1) / TILE;
-    // the kept weights of every tile
-    const auto sum_tiles = [&](uint64_t least) {
-        for_all(row, [&](uint32_t at, const float v[8]) {
-            uint64_t sum = 0;
+// Larger rows, in three launches.  First a row's parts have the largest logit of every eight neighbours, and their own.
+struct Parts {
+    float2 *tops;                        // [rows][parts]: the largest logit of each part, and the first eight neighbours that have it
+    float *eights;                       // [rows][ceil(vocab / 8)]; null where no filter asks for them
+    uint64_t *bins;                      // [rows][BINS]: the histogram of weights for top_p, or the weights of tiles without a filter
+    uint32_t parts, tiles;               // tiles of a part, a multiple of PART_THREADS * 8 / TILE
+};
+__device__ inline uint32_t eights_of(uint32_t vocab) { return (vocab + 7) / 8; }
+
+template <class T> __global__ __launch_bounds__(PART_THREADS) void k_sample_largest(she_sample_args a, Parts w)
+{
+    constexpr int AHEAD = 4;
+    __shared__ float tops[PART_THREADS / 64];
+    __shared__ uint32_t wheres[PART_THREADS / 64];
+    const uint32_t r = blockIdx.y, part = blockIdx.x;
+    const Row<T> row = row_of<T>(a, r);
+    for (uint32_t i = part * PART_THREADS + threadIdx.x; i < BINS; i += w.parts * PART_THREADS) w.bins[(size_t)r * BINS + i] = 0;
+    const uint32_t first = part * w.tiles * (TILE / 8), last = min(first + w.tiles * (TILE / 8), eights_of(a.vocab));
+    float top = -__builtin_inff();
+    uint32_t where = first;
+    for (uint32_t e0 = first + threadIdx.x; e0 < last; e0 += PART_THREADS * AHEAD) {
+        float v[AHEAD][8];
 #pragma unroll
-            for (int i = 0; i < 8; i++) {
-                if (!kept.has(key_of(v[i]), at + i)) continue;
-                const uint64_t weight = w.weight(w.below(v[i]));
-                if (weight >= least) sum += weight;
+        for (int k = 0; k < AHEAD; k++)
+            if (e0 + k * PART_THREADS < last) load_logits(row, (e0 + k * PART_THREADS) * 8, v[k]);
+#pragma unroll
+        for (int k = 0; k < AHEAD; k++) {
+            const uint32_t e = e0 + k * PART_THREADS;
+            if (e >= last) break;
+            float m = -__builtin_inff();
+#pragma unroll
+            for (int i = 0; i < 8; i++) m = fmaxf(m, v[k][i]);
+            if (w.eights) w.eights[(size_t)r * eights_of(a.vocab) + e] = m;
+            if (m > top) {
+                top = m;
+                where = e;
             }
-            sum = wave_sum(sum);
-            if (lane == 0) s.bins[at / TILE] = sum;
-        });
-        for (int i = threadIdx.x + tiles; i < BINS; i += THREADS) s.bins[i] = 0;
-        __syncthreads();
-        uint64_t all = 0;
-        for (int i = lane; i < BINS; i += 64) all += s.bins[i];
-        return wave_sum(all);
+        }
+    }
+    const auto join = [&](float other, uint32_t place) {
+        if (other > top || (other == top && place < where)) {
+            top = other;
+            where = place;
+        }
     };
-    if (top_p < 1.0f) {
-        const uint64_t all = sum_tiles(0);
-        __syncthreads();
-        kept = select<false>(row, w, kept, max(share_of(all, fmaxf(top_p, 0.0f), true), (uint64_t)1), s);
-    }
-    const float min_p = a.min_p ? a.min_p[r] : 0.0f;
-    const uint64_t least = min_p > 0 ? (uint64_t)ceil((double)fminf(min_p, 1.0f) * (double)ONE) : 0, all = sum_tiles(least);
-    const float u = a.uniform[r];
-    const uint64_t drawn = share_of(all, u > 0 ? fminf(u, 1.0f - 0x1p-24f) : 0.0f, false);
-    const Crossing c = find_crossing(s.bins, drawn + 1, s.sums, &s.found);
-    if (threadIdx.x >= 64) return;
-    float v[8];
-    const uint32_t at = c.bin * TILE + lane * 8;
-    load_logits(row, at, v);
-    uint64_t weight[8], here = 0;
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-        weight[i] = kept.has(key_of(v[i]), at + i) ? w.weight(w.below(v[i])) : 0;
-        if (weight[i] < least) weight[i] = 0;
-        here += weight[i];
+    for (int m = 1; m < 64; m *= 2) join(__shfl_xor(top, m), __shfl_xor(where, m));
+    if ((threadIdx.x & 63) == 0) {
+        tops[threadIdx.x >> 6] = top;
+        wheres[threadIdx.x >> 6] = where;
     }
-    uint64_t run = here;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int k = 1; k < PART_THREADS / 64; k++) join(tops[k], wheres[k]);
+    w.tops[(size_t)r * w.parts + part] = float2{top, __uint_as_float(where)};
+}
+// The largest logit of a row, and the first eight neighbours that have it.  Every wavefront has both.
+__device__ __forceinline__ void largest_of(const Parts &w, uint32_t r, float &top, uint32_t &where)
+{
+    const uint32_t lane = threadIdx.x & 63;
+    const float2 mine = w.tops[(size_t)r * w.parts + min(lane, w.parts - 1)];
+    top = mine.x;
+    where = __float_as_uint(mine.y);
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) {
-        const uint64_t other = __shfl_up(run, m);
-        if (lane >= m) run += other;
-    }
-    run = run - here + c.before;
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-        if (run <= drawn && run + weight[i] > drawn) {
-            a.tokens[r] = (int32_t)(at + i);
-            // the weight itself, since of a small one few bits are held
-            if (a.probs) a.probs[r] = (float)(exp2(w.below(v[i]) / 256) * ((double)ONE / (double)all));
+        const float other = __shfl_xor(top, m);
+        const uint32_t place = __shfl_xor(where, m);
+        if (other > top || (other == top && place < where)) {
+            top = other;
+            where = place;
         }
-        run += weight[i];
     }
+}
+
+// Then the weights of rows without top_k: a histogram for top_p, or their sums over tiles.
+template <class T> __global__ __launch_bounds__(PART_THREADS) void k_sample_weights(she_sample_args a, Parts w)
+{
+    constexpr int AHEAD = 2;
+    __shared__ double table[256];
+    __shared__ uint64_t bins[DEAD_BIN + 1];
+    const uint32_t r = blockIdx.y, part = blockIdx.x;
+    const Settings set(a, r);
+    float top;
+    uint32_t where;
+    largest_of(w, r, top, where);
+    if (top == -__builtin_inff() || !(set.temperature > 0) || set.top_k < a.vocab) return;
+    const Row<T> row = row_of<T>(a, r);
+    const Weights weights(top, set.temperature, table);
+    make_table(table);
+    const bool by_bin = set.top_p < 1.0f;
+    if (by_bin)
+        for (int i = threadIdx.x; i <= DEAD_BIN; i += PART_THREADS) bins[i] = 0;
+    __syncthreads();
+    const uint32_t first = part * w.tiles * (TILE / 8), last = min(first + w.tiles * (TILE / 8), eights_of(a.vocab));
+    const uint64_t least = set.least + RAW;
+    // whole wavefronts stay together: a tile is one's 64 times eight
+    for (uint32_t e0 = first + threadIdx.x; e0 - (threadIdx.x & 63) < last; e0 += PART_THREADS * AHEAD) {
+        float v[AHEAD][8];
+#pragma unroll
+        for (int k = 0; k < AHEAD; k++) load_logits(row, (e0 + k * PART_THREADS) * 8, v[k]);
+#pragma unroll
+        for (int k = 0; k < AHEAD; k++) {
+            const uint32_t e = e0 + k * PART_THREADS;
+            if (e - (threadIdx.x & 63) >= last) break;
+            if (by_bin) {
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const double y = weights.below(v[k][i]);
+                    if (y > DEAD) atomicAdd((unsigned long long *)&bins[weights.bin(y)], (unsigned long long)weights.weight(y));
+                }
+            } else {
+                uint64_t sum = 0;
+#pragma unroll
+                for (int i = 0; i < 8; i++) {
+                    const uint64_t raw = weights.raw_weight(weights.below(v[k][i]));
+                    sum += raw >= least ? raw - RAW : 0;
+                }
+                sum = wave_sum(sum);
+                if ((threadIdx.x & 63) == 0) w.bins[(size_t)r * BINS + e / (TILE / 8)] = sum;
+            }
+        }
+    }
+    if (!by_bin) return;
+    __syncthreads();
+    for (int i = threadIdx.x; i <= DEAD_BIN; i += PART_THREADS)
+        if (bins[i]) atomicAdd((unsigned long long *)&w.bins[(size_t)r * BINS + i], (unsigned long long)bins[i]);
+}
+
+// The tokens of bins up to `bin`, if they are no more than threads: a candidate a thread, in no order.  Returns how many there are.
+template <class T> __device__ __forceinline__ uint32_t pick_out(const Row<T> &row, const Weights &w, const float *eights, int bin, Shared &s)
+{
+    constexpr int AHEAD = 8;
+    if (threadIdx.x == 0) s.count = 0;
+    __syncthreads();
+    const uint32_t all = eights_of(row.vocab);
+    for (uint32_t e0 = threadIdx.x; e0 < all; e0 += THREADS * AHEAD) {
+        float m[AHEAD];
+#pragma unroll
+        for (int k = 0; k < AHEAD; k++) m[k] = e0 + k * THREADS < all ? eights[e0 + k * THREADS] : -__builtin_inff();
+#pragma unroll
+        for (int k = 0; k < AHEAD; k++) {
+            const double y = w.below(m[k]);
+            if (!(y > DEAD) || w.bin(y) > bin || s.count > THREADS) continue;
+            const uint32_t at = (e0 + k * THREADS) * 8;
+            float v[8];
+            load_logits(row, at, v);
+            for (int i = 0; i < 8; i++) {
+                const float l = w.plain(v[i]);
+                const double z = w.below_plain(l);
+                if (!(z > DEAD) || w.bin(z) > bin) continue;
+                const uint32_t n = atomicAdd(&s.count, 1u);
+                if (n < THREADS) s.list[n] = Candidate{(uint64_t)key_of(l) << 32 | (uint32_t)~(at + i), w.weight(z)};
+            }
+        }
+    }
+    __syncthreads();
+    return s.count;
+}
+
+// The draw from `count` candidates; `whole`: the row's weight, which top_p is of where there is no top_k.
+template <class T> __device__ __forceinline__ void draw_by_list(const she_sample_args &a, uint32_t r, const Weights &w, const Settings &set, uint64_t whole, uint32_t count, Shared &s)
+{
+    const uint32_t i = threadIdx.x;
+    const Candidate mine = i < count ? s.list[i] : Candidate{0, 0};
+    uint32_t rank = 0;
+    uint64_t before = 0;
+    if ((i & ~63u) < count)
+        for (uint32_t j = 0; j < count; j++) {
+            const Candidate c = s.list[j];
+            const bool better = c.order > mine.order;
+            rank += better;
+            before += better ? c.weight : 0;
+        }
+    bool kept = i < count && rank < set.top_k;
+    if (set.top_p < 1.0f) {
+        if (set.top_k < a.vocab) whole = block_sum(kept ? mine.weight : 0, s);
+        kept &= before < set.head(whole);
+    }
+    kept &= mine.weight >= set.least;
+    const uint64_t weight = kept ? mine.weight : 0, all = block_sum(weight, s), drawn = share_of(all, set.uniform, false);
+    if (i < count) s.list[i].weight = weight;
+    __syncthreads();
+    if ((i & ~63u) >= count) return;
+    uint64_t run = 0;
+    for (uint32_t j = 0; j < count; j++) {
+        const Candidate c = s.list[j];
+        run += (uint32_t)c.order > (uint32_t)mine.order ? c.weight : 0;       // an earlier index
+    }
+    if (weight && run <= drawn && run + weight > drawn)
+        answer(a, r, (int32_t)~(uint32_t)mine.order, (float)(exp2(w.below_plain(number_of((uint32_t)(mine.order >> 32))) / 256) * ((double)ONE / (double)all)));
+}
+
+// And the rows' answers.
+template <class T> __global__ __launch_bounds__(THREADS) void k_sample_answers(she_sample_args a, Parts parts)
+{
+    __shared__ Shared s;
+    const uint32_t r = blockIdx.x;
+    const Row<T> row = row_of<T>(a, r);
+    const Settings set(a, r);
+    float top;
+    uint32_t where;
+    largest_of(parts, r, top, where);
+    const bool none = top == -__builtin_inff();
+    if (none || !(set.temperature > 0)) {
+        if (threadIdx.x >= 64) return;
+        float v[8];
+        load_logits(row, where * 8, v);
+        if (threadIdx.x) return;
+        int i = 0;
+        while (i < 7 && v[i] != top) i++;
+        answer(a, r, none ? -1 : (int32_t)(where * 8 + i), none ? 0.0f : 1.0f);
+        return;
+    }
+    make_table(s.table);
+    const Weights w(top, set.temperature, s.table);
+    const float *eights = parts.eights + (size_t)r * eights_of(a.vocab);
+    const bool counted = set.top_k < a.vocab, headed = set.top_p < 1.0f;
+    uint64_t all = 0;
+    if (counted) {
+        // the k-th of the eights' largest is no larger than the k-th logit
+        clear_bins(s);
+        for (uint32_t e = threadIdx.x; e < eights_of(a.vocab); e += THREADS) {
+            const double y = w.below(eights[e]);
+            if (y > DEAD) atomicAdd((unsigned long long *)&s.bins[w.bin(y)], 1ull);
+        }
+        __syncthreads();
+    } else {
+        for (int i = threadIdx.x; i < BINS; i += THREADS) all += s.bins[i] = parts.bins[(size_t)r * BINS + i];
+        all = block_sum(all, s);
+        if (!headed) {
+            draw_by_tiles(a, r, row, w, set, Kept{0, ~0u}, s);
+            return;
+        }
+    }
+    const Crossing c = find_crossing(s.bins, counted ? set.top_k : set.head(all), s.sums, &s.found);
+    const uint32_t count = pick_out(row, w, eights, c.bin < 0 ? DEAD_BIN : c.bin, s);
+    if (count <= THREADS) draw_by_list<T>(a, r, w, set, all, count, s);
+    else pass_by_pass(a, r, row, w, set, !counted, s);
+}
+
+template <class T> hipError_t sample(const she_sample_args &a, const SampleShape &s, void *scratch, hipStream_t st)
+{
+    if (!s.parts) {
+        k_sample_rows<T><<<a.rows, THREADS, 0, st>>>(a);
+        return hipGetLastError();
+    }
+    Parts w{};
+    w.bins = static_cast<uint64_t *>(scratch);
+    w.tops = reinterpret_cast<float2 *>(w.bins + (size_t)a.rows * BINS);
+    w.eights = a.top_k || a.top_p ? reinterpret_cast<float *>(w.tops + (size_t)a.rows * s.parts) : nullptr;
+    w.parts = s.parts;
+    w.tiles = s.tiles;
+    k_sample_largest<T><<<dim3(s.parts, a.rows), PART_THREADS, 0, st>>>(a, w);
+    hipError_t rc = hipGetLastError();
+    if (rc != hipSuccess) return rc;
+    k_sample_weights<T><<<dim3(s.parts, a.rows), PART_THREADS, 0, st>>>(a, w);
+    if ((rc = hipGetLastError()) != hipSuccess) return rc;
+    k_sample_answers<T><<<a.rows, THREADS, 0, st>>>(a, w);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_sample(const she_sample_args &a, uint32_t, hipStream_t st)
+SampleShape sample_shape(const she_sample_args &a, uint32_t cus)
+{
+    SampleShape s{0, 0};
+    if (a.vocab <= 8192 || (uint64_t)a.rows * a.vocab > 1u << 30) return s;    // of larger calls the eights are much memory
+    constexpr uint32_t STEP = PART_THREADS * 8;                    // logits that a workgroup of a part has at once
+    const uint64_t steps = ceil_div(a.vocab, STEP), parts = std::max<uint64_t>(1, std::min<uint64_t>({16, steps, ceil_div(8 * cus, a.rows)}));
+    s.tiles = (uint32_t)(ceil_div(steps, parts) * (STEP / TILE));
+    s.parts = (uint32_t)ceil_div(a.vocab, (uint64_t)s.tiles * TILE);
+    return s;
+}
+
+size_t sample_scratch(const she_sample_args &a, const SampleShape &s)
+{
+    if (!s.parts) return 0;
+    return (size_t)a.rows * (BINS * sizeof(uint64_t) + s.parts * sizeof(float2) + (a.top_k || a.top_p ? (a.vocab + 7) / 8 * sizeof(float) : 0));
+}
+
+hipError_t launch_sample(const she_sample_args &a, const SampleShape &s, void *scratch, hipStream_t st)
 {
     switch (a.type) {
-    case SHE_BF16: k_sample_rows<__bf16><<<a.rows, THREADS, 0, st>>>(a); break;
-    case SHE_F16: k_sample_rows<_Float16><<<a.rows, THREADS, 0, st>>>(a); break;
-    case SHE_F32: k_sample_rows<float><<<a.rows, THREADS, 0, st>>>(a); break;
-    default: k_sample_rows<int32_t><<<a.rows, THREADS, 0, st>>>(a); break;
+    case SHE_BF16: return sample<__bf16>(a, s, scratch, st);
+    case SHE_F16: return sample<_Float16>(a, s, scratch, st);
+    case SHE_F32: return sample<float>(a, s, scratch, st);
+    default: return sample<int32_t>(a, s, scratch, st);
     }
-    return hipGetLastError();
 }
 
 }}  // namespace she::clear

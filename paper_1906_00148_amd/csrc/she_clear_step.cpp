@@ -68,9 +68,10 @@ try {
     if (!a.rows) return SHE_OK;
     if (!a.logits || !a.uniform || !a.tokens) return fail(c, SHE_EINVAL, at + "null argument");
     if (a.step && a.type != SHE_I32) return fail(c, SHE_EINVAL, at + "step belongs to SHE_I32");
-    const int rc = ready(c);
-    if (rc) return rc;
-    HIP_TRY(c, launch_sample(a, c->dk.cus, c->stream));
+    const SampleShape s = sample_shape(a, c->dk.cus);
+    int rc;
+    if ((rc = ready(c)) || (rc = ensure_scratch(c, sample_scratch(a, s)))) return rc;
+    HIP_TRY(c, launch_sample(a, s, c->clear.scratch(), c->stream));
     return SHE_OK;
 } SHE_NOTHROW(c)
 

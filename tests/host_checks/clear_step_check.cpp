@@ -15,7 +15,9 @@ hipError_t launch_plan_pages(const she_plan_pages_args &, void *, uint32_t *, hi
 SharedShape shared_shape(const she_attend_shared_args &a, uint32_t) { SharedShape s{}; s.prefix.slots = a.prefixes; s.behind.slots = a.requests; return s; }
 size_t shared_scratch(const she_attend_shared_args &, const SharedShape &) { return wanted; }
 hipError_t launch_attend_shared(const she_attend_shared_args &, const SharedShape &, void *, uint32_t *, hipStream_t) { return launched(); }
-hipError_t launch_sample(const she_sample_args &, uint32_t, hipStream_t) { return launched(); }
+SampleShape sample_shape(const she_sample_args &, uint32_t) { return {}; }
+size_t sample_scratch(const she_sample_args &, const SampleShape &) { return wanted; }
+hipError_t launch_sample(const she_sample_args &, const SampleShape &, void *, hipStream_t) { return launched(); }
 }}
 
 static hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
@@ -132,7 +134,7 @@ int main()
     // while the stream is captured, a call that would allocate is refused
     capturing = hipStreamCaptureStatusActive;
     wanted = 500;
-    CHECK(she_plan_pages(c, &p) == SHE_ENOMEM && she_attend_shared(c, &t) == SHE_ENOMEM, "a capture with scratch to allocate\n");
+    CHECK(she_plan_pages(c, &p) == SHE_ENOMEM && she_attend_shared(c, &t) == SHE_ENOMEM && she_sample(c, &s) == SHE_ENOMEM, "a capture with scratch to allocate\n");
     capturing = hipStreamCaptureStatusNone;
     CHECK(she_plan_pages(c, &p) == SHE_OK, "scratch\n");
     capturing = hipStreamCaptureStatusActive;
