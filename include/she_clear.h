@@ -181,7 +181,7 @@ int she_attend_pages(she_ctx *ctx, const she_attend_pages_args *args);
  * outside [0, pages) in the list), where the page that its request has already is outside [0, pages), and where the table has no
  * column for it.  The tokens from starts[requests] on are the padding of a batch: position 0, slot -1, not counted.  Other columns are
  * left as they are.  Numbers below 0 in cached, news, taken and before count as 0, and positions end at 2^31 - 1.  lengths may be
- * cached, taken_out may be taken; no other two arrays may share memory. */
+ * cached, taken_out may be taken; no other two arrays, and no two rows of the table, may share memory. */
 typedef struct {
     uint32_t requests, tokens;           /* tokens: the room in positions and slots */
     uint32_t pages, page_size, table_width, free_count;

@@ -473,7 +473,7 @@ template <class T> __global__ __launch_bounds__(PART_THREADS) void k_sample_larg
     constexpr int AHEAD = 4;
     __shared__ float tops[PART_THREADS / 64];
     __shared__ uint32_t wheres[PART_THREADS / 64];
-    const uint32_t r = blockIdx.y, part = blockIdx.x;
+    const uint32_t r = blockIdx.x / w.parts, part = blockIdx.x - r * w.parts;         // one axis: another one ends at 65535
     const Row<T> row = row_of<T>(a, r);
     for (uint32_t i = part * PART_THREADS + threadIdx.x; i < BINS; i += w.parts * PART_THREADS) w.bins[(size_t)r * BINS + i] = 0;
     const uint32_t first = part * w.tiles * (TILE / 8), last = min(first + w.tiles * (TILE / 8), eights_of(a.vocab));
@@ -539,7 +539,7 @@ template <class T> __global__ __launch_bounds__(PART_THREADS) void k_sample_weig
     constexpr int AHEAD = 2;
     __shared__ double table[256];
     __shared__ uint64_t bins[DEAD_BIN + 1];
-    const uint32_t r = blockIdx.y, part = blockIdx.x;
+    const uint32_t r = blockIdx.x / w.parts, part = blockIdx.x - r * w.parts;
     const Settings set(a, r);
     float top;
     uint32_t where;
@@ -711,10 +711,10 @@ template <class T> hipError_t sample(const she_sample_args &a, const SampleShape
     w.eights = a.top_k || a.top_p ? reinterpret_cast<float *>(w.tops + (size_t)a.rows * s.parts) : nullptr;
     w.parts = s.parts;
     w.tiles = s.tiles;
-    k_sample_largest<T><<<dim3(s.parts, a.rows), PART_THREADS, 0, st>>>(a, w);
+    k_sample_largest<T><<<a.rows * s.parts, PART_THREADS, 0, st>>>(a, w);
     hipError_t rc = hipGetLastError();
     if (rc != hipSuccess) return rc;
-    k_sample_weights<T><<<dim3(s.parts, a.rows), PART_THREADS, 0, st>>>(a, w);
+    k_sample_weights<T><<<a.rows * s.parts, PART_THREADS, 0, st>>>(a, w);
     if ((rc = hipGetLastError()) != hipSuccess) return rc;
     k_sample_answers<T><<<a.rows, THREADS, 0, st>>>(a, w);
     return hipGetLastError();

@@ -19,6 +19,8 @@ try {
     if (!a.taken || !a.taken_out || !a.starts || (a.requests && (!a.cached || !a.news || !a.lengths)) || (a.tokens && (!a.positions || !a.slots)) ||
         (a.requests && a.table_width && !a.table) || (a.free_count && !a.free))
         return fail(c, SHE_EINVAL, at + "null argument");
+    if (a.requests > 1 && (a.table_stride < 0 ? -(uint64_t)a.table_stride : (uint64_t)a.table_stride) < a.table_width)
+        return fail(c, SHE_EINVAL, at + "rows of the table must not overlap");
     int rc;
     if ((rc = ready(c)) || (rc = ensure_scratch(c, plan_scratch(a)))) return rc;
     HIP_TRY(c, launch_plan_pages(a, c->clear.scratch(), c->clear.d_bad, c->stream));

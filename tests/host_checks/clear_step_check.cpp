@@ -69,6 +69,13 @@ int main()
     EXPECT(she_plan_pages, p, SHE_EINVAL, a.lengths = nullptr);
     EXPECT(she_plan_pages, p, SHE_EINVAL, a.positions = nullptr);
     EXPECT(she_plan_pages, p, SHE_EINVAL, a.slots = nullptr);
+    EXPECT(she_plan_pages, p, SHE_EINVAL, a.table_stride = 3);
+    EXPECT(she_plan_pages, p, SHE_EINVAL, a.table_stride = 0);
+    EXPECT(she_plan_pages, p, SHE_EINVAL, a.table_stride = -3);
+    EXPECT(she_plan_pages, p, SHE_OK, a.table_stride = -4);
+    EXPECT(she_plan_pages, p, SHE_OK, a.table_stride = INT64_MIN);
+    EXPECT(she_plan_pages, p, SHE_OK, a.table_stride = 0; a.requests = 1);
+    EXPECT(she_plan_pages, p, SHE_OK, a.table_stride = 0; a.table_width = 0);
     CHECK(she_plan_pages(c, nullptr) == SHE_EINVAL && she_plan_pages(nullptr, &p) == SHE_EINVAL, "null struct or context\n");
 
     she_sample_args s{};
