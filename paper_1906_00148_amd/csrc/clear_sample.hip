@@ -12,6 +12,7 @@
 // every eight neighbours, since k of these that reach a logit are k logits that do.  Where they are many, the logit is found by
 // histograms over the row, from the 32nds of an octave on to the bits of the bin's logits until a bin is one value.
 #include <algorithm>
+#include <type_traits>
 
 #include "clear_device.h"
 #include "clear_internal.h"
@@ -188,69 +189,182 @@ struct Kept {
     __device__ __forceinline__ bool has(uint32_t k, uint32_t index) const { return k > key || (k == key && index <= last); }
 };
 
-struct Candidate {
-    uint64_t order;                      // larger ones come first: the logit's key above the index, turned round
-    uint64_t weight;
-};
 struct Shared {
     uint64_t bins[BINS];                 // a histogram; sums or counts of tiles
     double table[256];
-    Candidate list[THREADS];
+    uint64_t list[THREADS];              // tokens: the logit's key above the index turned round, so that larger ones come first
     uint64_t sums[WAVES], totals[WAVES];
     Crossing found;
+    Kept cut;
     float tops[WAVES];
-    uint32_t where[WAVES], answer, count;
+    uint32_t where[WAVES], answer, count, eights;
+    uint32_t waiting[WAVES][TILE];       // logits that wait for their weight; places of eights
 };
+__device__ __forceinline__ uint64_t token_of(uint32_t key, uint32_t index) { return (uint64_t)key << 32 | (uint32_t)~index; }
 
-template <class T, class F> __device__ __forceinline__ void for_all(const Row<T> &row, F f)
-{
-    constexpr int AHEAD = 2;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__device__ __host__ inline uint32_t eights_of(uint32_t vocab) { return (vocab + 7) / 8; }
+
+// A row's logits eight by eight: f(index, logits, whether they are there) for whole wavefronts, a tile each.  Eights below `least` need not be there.
+template <class T> struct FromMemory {
+    Row<T> row;
+    const float *eights;                 // the largest of each; may be null
+    template <class F> __device__ __forceinline__ void all(float least, F f) const
+    {
+        constexpr int AHEAD = 4;
+        const uint32_t lane = threadIdx.x & 63, end = eights_of(row.vocab);
 #pragma unroll 1
-    for (uint32_t at = wave * TILE; at < row.vocab; at += WAVES * TILE * AHEAD) {
-        float v[AHEAD][8];
+        for (uint32_t e0 = threadIdx.x; e0 - lane < end; e0 += THREADS * AHEAD) {
+            float v[AHEAD][8];
+            bool there[AHEAD];
 #pragma unroll
-        for (int k = 0; k < AHEAD; k++)
-            if (at + k * WAVES * TILE < row.vocab) load_logits(row, at + k * WAVES * TILE + lane * 8, v[k]);
+            for (int k = 0; k < AHEAD; k++) {
+                const uint32_t e = e0 + k * THREADS;
+                there[k] = e < end && (!eights || eights[e] >= least);
+            }
 #pragma unroll
-        for (int k = 0; k < AHEAD; k++)
-            if (at + k * WAVES * TILE < row.vocab) f(at + k * WAVES * TILE + lane * 8, v[k]);
+            for (int k = 0; k < AHEAD; k++)
+                if (there[k]) load_logits(row, (e0 + k * THREADS) * 8, v[k]);
+#pragma unroll
+            for (int k = 0; k < AHEAD; k++)
+                if (e0 + k * THREADS - lane < end) f((e0 + k * THREADS) * 8, v[k], there[k]);
+        }
     }
-}
+};
+template <class T> struct Held {         // by the workgroup, eight a thread
+    Row<T> row;
+    float v[8];
+    template <class F> __device__ __forceinline__ void all(float, F f) const
+    {
+        if ((threadIdx.x & ~63u) * 8 < row.vocab) f(threadIdx.x * 8, v, true);
+    }
+};
 __device__ __forceinline__ void clear_bins(Shared &s)
 {
     for (int i = threadIdx.x; i < BINS; i += THREADS) s.bins[i] = 0;
     __syncthreads();
 }
 
-// Of what `kept` has, the first of the order whose measure (ones or weights) together reaches `target`; `kept` itself if all does not.
-// `known`: the bins have that histogram already.
-template <bool COUNT, class T> __device__ __forceinline__ Kept select(const Row<T> &row, const Weights &w, Kept kept, uint64_t target, bool known, Shared &s)
+// The running sum of v over the workgroup's threads; `all` gets the last.
+__device__ __forceinline__ uint64_t running_sum(uint64_t v, uint64_t &all, Shared &s)
 {
-    const auto measure = [&](double y) { return COUNT ? 1 : w.weight(y); };
-    if (!known) {
-    clear_bins(s);
-    for_all(row, [&](uint32_t at, const float v[8]) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) {
+        const uint64_t other = __shfl_up(v, m);
+        if (lane >= m) v += other;
+    }
+    if (lane == 63) s.totals[wave] = v;
+    __syncthreads();
+    all = 0;
+#pragma unroll
+    for (int k = 0; k < WAVES; k++) {
+        if (k == wave) v += all;
+        all += s.totals[k];
+    }
+    __syncthreads();
+    return v;
+}
+__device__ __forceinline__ uint64_t block_sum(uint64_t v, Shared &s)
+{
+    v = wave_sum(v);
+    if ((threadIdx.x & 63) == 0) s.totals[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0;
+    for (int k = 0; k < WAVES; k++) v += s.totals[k];
+    __syncthreads();
+    return v;
+}
+
+// The numbers of the threads, the largest first, where those from `count` on have 0: a bitonic sort.
+__device__ __forceinline__ uint64_t sorted(uint64_t v, uint32_t count, Shared &s)
+{
+    const uint32_t i = threadIdx.x;
+#pragma unroll 1
+    for (uint32_t k = 2; k < 2 * count; k *= 2)
+#pragma unroll 1
+        for (uint32_t d = k / 2; d; d /= 2) {
+            uint64_t other;
+            if (d >= 64) {
+                __syncthreads();
+                s.list[i] = v;
+                __syncthreads();
+                other = s.list[i ^ d];
+            } else {
+                other = __shfl_xor(v, (int)d);
+            }
+            if ((((i & d) == 0) == ((i & k) == 0)) != (v > other)) v = other;
+        }
+    return v;
+}
+
+// A logit that is no larger than any of y or more, in units of 1/256 octave.
+__device__ __forceinline__ float least_at(const Weights &w, double y) { return (float)((double)w.top + (y - 1) / w.unit); }
+__device__ __forceinline__ float least_of(const Kept &kept) { return kept.key ? number_of(kept.key) : -__builtin_inff(); }
+
+// Of what `kept` has, the tokens of the bins from `first` to `last`, if they are no more than threads, in no order.  Returns how many there are.
+template <class S> __device__ __forceinline__ uint32_t pick_out(const S &row, const Weights &w, Kept kept, int first, int last, Shared &s)
+{
+    __syncthreads();
+    if (threadIdx.x == 0) s.count = 0;
+    __syncthreads();
+    const float least = least_at(w, -8 * last - 8);
+    row.all(least, [&](uint32_t at, const float v[8], bool there) {
+        if (!there || s.count > THREADS) return;
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             const float l = w.plain(v[i]);
+            if (!(l >= least)) continue;
             const double y = w.below_plain(l);
-            if (y > DEAD && kept.has(key_of(l), at + i)) atomicAdd((unsigned long long *)&s.bins[w.bin(y)], (unsigned long long)measure(y));
+            if (!(y > DEAD) || w.bin(y) > last || w.bin(y) < first || !kept.has(key_of(l), at + i)) continue;
+            const uint32_t n = atomicAdd(&s.count, 1u);
+            if (n < THREADS) s.list[n] = token_of(key_of(l), at + i);
         }
     });
     __syncthreads();
-    }
+    return s.count;
+}
+__device__ __forceinline__ float logit_of(uint64_t token) { return number_of((uint32_t)(token >> 32)); }
+
+// Of what `kept` has, the first of the order whose measure (ones or weights) together reaches `target`; `kept` itself if all does not.
+// No token of a bin behind `bound` is among them.
+template <bool COUNT, class S> __device__ __forceinline__ Kept select(const S &source, const Weights &w, Kept kept, uint64_t target, int bound, Shared &s)
+{
+    const auto &row = source.row;
+    const auto measure = [&](double y) { return COUNT ? 1 : w.weight(y); };
+    const float least = fmaxf(least_of(kept), least_at(w, -8 * bound - 8));
+    clear_bins(s);
+    source.all(least, [&](uint32_t at, const float v[8], bool there) {
+        if (!there) return;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float l = w.plain(v[i]);
+            if (!(l >= least) || !kept.has(key_of(l), at + i)) continue;
+            const double y = w.below_plain(l);
+            if (y > DEAD) atomicAdd((unsigned long long *)&s.bins[w.bin(y)], (unsigned long long)measure(y));
+        }
+    });
+    __syncthreads();
     Crossing c = find_crossing(s.bins, target, s.sums, &s.found);
     if (c.bin < 0) return kept;
     const int bin = c.bin;
+    target -= c.before;
+    const uint32_t count = pick_out(source, w, kept, bin, bin, s);
+    if (count <= THREADS) {
+        const uint64_t token = sorted(threadIdx.x < count ? s.list[threadIdx.x] : 0, count, s), mine = threadIdx.x < count ? measure(w.below_plain(logit_of(token))) : 0;
+        uint64_t all;
+        const uint64_t run = running_sum(mine, all, s);
+        if (run >= target && run - mine < target) s.cut = Kept{(uint32_t)(token >> 32), ~(uint32_t)token};
+        __syncthreads();
+        return s.cut;
+    }
     // Keys that surround the bin's, so wide that no rounding matters.  (Where unit is 0, all logits are in bin 0.)
     uint32_t low = key_of((float)((double)w.top - (8 * bin + 8) / w.unit)), high = min(key_of(w.top), key_of((float)((double)w.top - (8 * bin - 1) / w.unit)));
-    target -= c.before;
     for (;;) {
         int shift = 0;
         while ((high - low) >> shift >= BINS) shift++;
         clear_bins(s);
-        for_all(row, [&](uint32_t at, const float v[8]) {
+        source.all(number_of(low), [&](uint32_t at, const float v[8], bool there) {
+            if (!there) return;
 #pragma unroll
             for (int i = 0; i < 8; i++) {
                 const float l = w.plain(v[i]);
@@ -278,10 +392,10 @@ template <bool COUNT, class T> __device__ __forceinline__ Kept select(const Row<
     __syncthreads();
     if (wanted >= all) return Kept{low, low == kept.key ? kept.last : ~0u};
     // the index of the last of them, by tile and then by place
-    for_all(row, [&](uint32_t at, const float v[8]) {
+    source.all(number_of(low), [&](uint32_t at, const float v[8], bool there) {
         uint32_t here = 0;
 #pragma unroll
-        for (int i = 0; i < 8; i++) here += key_of(w.plain(v[i])) == low && kept.has(low, at + i);
+        for (int i = 0; i < 8; i++) here += there && key_of(w.plain(v[i])) == low && kept.has(low, at + i);
         const uint64_t sum = wave_sum(here);
         if ((threadIdx.x & 63) == 0) s.bins[at / TILE] = sum;
     });
@@ -312,30 +426,21 @@ template <bool COUNT, class T> __device__ __forceinline__ Kept select(const Row<
     return Kept{low, last};
 }
 
-// The sum of v over the workgroup.
-__device__ __forceinline__ uint64_t block_sum(uint64_t v, Shared &s)
-{
-    v = wave_sum(v);
-    if ((threadIdx.x & 63) == 0) s.totals[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = 0;
-    for (int k = 0; k < WAVES; k++) v += s.totals[k];
-    __syncthreads();
-    return v;
-}
-
 struct Settings {
     float temperature, top_p, uniform;
     uint32_t top_k;                      // vocab: all
     uint64_t least;                      // the weight that min_p asks for
+    float share;                         // of the largest: min_p, 0 to 1
     __device__ __forceinline__ Settings(const she_sample_args &a, uint32_t r) : temperature(a.temperature ? a.temperature[r] : 1.0f), top_p(a.top_p ? a.top_p[r] : 1.0f), uniform(a.uniform[r])
     {
         const int32_t k = a.top_k ? a.top_k[r] : 0;
         top_k = k > 0 && (uint32_t)k < a.vocab ? (uint32_t)k : a.vocab;
         const float m = a.min_p ? a.min_p[r] : 0.0f;
-        least = m > 0 ? (uint64_t)ceil((double)fminf(m, 1.0f) * (double)ONE) : 0;
+        share = m > 0 ? fminf(m, 1.0f) : 0.0f;
+        least = (uint64_t)ceil((double)share * (double)ONE);
         uniform = uniform > 0 ? fminf(uniform, 1.0f - 0x1p-24f) : 0.0f;
     }
+    __device__ __forceinline__ float least_logit(const Weights &w) const { return share > 0 ? least_at(w, 256 * log2((double)share)) : -__builtin_inff(); }
     __device__ __forceinline__ uint64_t head(uint64_t all) const { return max(share_of(all, fmaxf(top_p, 0.0f), true), (uint64_t)1); }    // of a whole weight, for top_p below 1
 };
 
@@ -345,7 +450,7 @@ __device__ inline void answer(const she_sample_args &a, uint32_t r, int32_t toke
     if (a.probs) a.probs[r] = prob;
 }
 // The weight itself, since of a small one few bits are held.
-__device__ __forceinline__ float prob_of(const Weights &w, float logit, uint64_t all) { return (float)(exp2(w.below(logit) / 256) * ((double)ONE / (double)all)); }
+__device__ __forceinline__ float prob_of(double y, uint64_t all) { return (float)(exp2(y / 256) * ((double)ONE / (double)all)); }
 
 // The draw from sums of the kept weights of every tile, in s.bins.
 template <class T> __device__ __forceinline__ void draw_by_tiles(const she_sample_args &a, uint32_t r, const Row<T> &row, const Weights &w, const Settings &set, const Kept &kept, Shared &s)
@@ -377,58 +482,142 @@ template <class T> __device__ __forceinline__ void draw_by_tiles(const she_sampl
     run = run - here + c.before;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-        if (run <= drawn && run + weight[i] > drawn) answer(a, r, (int32_t)(at + i), prob_of(w, v[i], all));
+        if (run <= drawn && run + weight[i] > drawn) answer(a, r, (int32_t)(at + i), prob_of(w.below(v[i]), all));
         run += weight[i];
     }
 }
 
-// The weights that are kept of every tile.
-template <class T> __device__ __forceinline__ void sum_tiles(const Row<T> &row, const Weights &w, const Kept &kept, uint64_t least, Shared &s)
+// The weights of a tile's logits, of which a wavefront's lanes hold eight each, `which` a bit for each that counts.  Few do mostly, and a weight is
+// many instructions: they are moved together first.
+__device__ __forceinline__ uint64_t tile_sum(const Weights &w, const float l[8], uint32_t which, uint64_t least, Shared &s)
 {
-    for_all(row, [&](uint32_t at, const float v[8]) {
-        uint64_t sum = 0;
+    const uint32_t lane = threadIdx.x & 63;
+    float *waiting = reinterpret_cast<float *>(s.waiting[threadIdx.x >> 6]);
+    uint32_t count = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        const uint64_t those = __ballot(which >> i & 1);
+        if (which >> i & 1) waiting[count + __builtin_amdgcn_mbcnt_hi((uint32_t)(those >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)those, 0))] = l[i];
+        count += __popcll(those);
+    }
+    wave_lds_fence();
+    uint64_t sum = 0;
+#pragma unroll 2
+    for (uint32_t i = lane; i < count; i += 64) {
+        const uint64_t weight = w.weight(w.below_plain(waiting[i]));
+        if (weight >= least) sum += weight;
+    }
+    wave_lds_fence();
+    return count ? wave_sum(sum) : 0;
+}
+
+// The weights that are kept of every tile.
+template <class S> __device__ __forceinline__ void sum_tiles(const S &source, const Weights &w, const Kept &kept, const Settings &set, bool filtered, Shared &s)
+{
+    const uint64_t least = filtered ? set.least : 0;
+    const float floor = fmaxf(least_of(kept), filtered ? set.least_logit(w) : -__builtin_inff());
+    __syncthreads();
+    source.all(floor, [&](uint32_t at, const float v[8], bool there) {
+        float l[8];
+        uint32_t which = 0;
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-            const float l = w.plain(v[i]);
-            const uint64_t weight = kept.has(key_of(l), at + i) ? w.weight(w.below_plain(l)) : 0;
-            if (weight >= least) sum += weight;
+            l[i] = w.plain(v[i]);
+            which |= (there && l[i] >= floor && kept.has(key_of(l[i]), at + i)) << i;
         }
-        sum = wave_sum(sum);
+        const uint64_t sum = tile_sum(w, l, which, least, s);
         if ((threadIdx.x & 63) == 0) s.bins[at / TILE] = sum;
     });
-    for (int i = threadIdx.x + (row.vocab + TILE - 1) / TILE; i < BINS; i += THREADS) s.bins[i] = 0;
+    for (int i = threadIdx.x + (source.row.vocab + TILE - 1) / TILE; i < BINS; i += THREADS) s.bins[i] = 0;
     __syncthreads();
 }
 
-// A row of any kind by passes over all of it.  `known`: s.bins has the histogram of all weights, and there is no top_k.
-template <class T> __device__ __forceinline__ void pass_by_pass(const she_sample_args &a, uint32_t r, const Row<T> &row, const Weights &w, const Settings &set, bool known, Shared &s)
+// Both for top_p alone, in one pass: with the histogram of all weights in s.bins, the bin that has the border is picked out and the weights above it
+// are summed up.  Returns whether the bin has no more tokens than there are threads; if it has, s.bins is not as it was.
+template <class S> __device__ __forceinline__ bool head_sums(const S &source, const Weights &w, const Settings &set, uint64_t target, Kept &kept, Shared &s)
+{
+    const Crossing c = find_crossing(s.bins, target, s.sums, &s.found);
+    const int bin = c.bin;                                         // there is one: the target is at most all of it
+    target -= c.before;
+    if (threadIdx.x == 0) s.count = 0;
+    clear_bins(s);
+    // logits below `least` are behind the bin, and those above `most` before it
+    const float least = least_at(w, -8 * bin - 8), most = bin ? (float)((double)w.top - (8 * bin - 1) / w.unit) : __builtin_inff(), floor = set.least_logit(w);
+    source.all(fmaxf(least, floor), [&](uint32_t at, const float v[8], bool there) {
+        float l[8];
+        uint32_t which = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            l[i] = w.plain(v[i]);
+            which |= (there && l[i] >= least) << i;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            if (!(which >> i & 1) || l[i] > most) continue;
+            const double y = w.below_plain(l[i]);
+            if (y > DEAD && w.bin(y) < bin) continue;
+            which &= ~(1u << i);
+            if (!(y > DEAD) || w.bin(y) > bin) continue;
+            const uint32_t n = atomicAdd(&s.count, 1u);
+            if (n < THREADS) s.list[n] = token_of(key_of(l[i]), at + i);
+        }
+        const uint64_t sum = tile_sum(w, l, which, set.least, s);
+        if ((threadIdx.x & 63) == 0) s.bins[at / TILE] = sum;
+    });
+    __syncthreads();
+    const uint32_t count = s.count;
+    if (count > THREADS) return false;
+    const uint64_t token = sorted(threadIdx.x < count ? s.list[threadIdx.x] : 0, count, s), mine = threadIdx.x < count ? w.weight(w.below_plain(logit_of(token))) : 0;
+    uint64_t all;
+    const uint64_t before = running_sum(mine, all, s) - mine;
+    const uint32_t index = ~(uint32_t)token;
+    if (threadIdx.x < count && before < target) {
+        if (mine >= set.least) atomicAdd((unsigned long long *)&s.bins[index / TILE], (unsigned long long)mine);
+        if (before + mine >= target) s.cut = Kept{(uint32_t)(token >> 32), index};
+    }
+    __syncthreads();
+    kept = s.cut;
+    return true;
+}
+
+// A row of any kind by passes over all of it.  `known`: s.bins has the histogram of all weights, there is no top_k, and `target` is top_p of
+// them.  `bound`: as in select, of the first filter.
+template <class T, class S> __device__ __forceinline__ void pass_by_pass(const she_sample_args &a, uint32_t r, const S &source, const Weights &w, const Settings &set, bool known, uint64_t target, int bound, Shared &s)
 {
     Kept kept{0, ~0u};
-    if (set.top_k < a.vocab) kept = select<true>(row, w, kept, set.top_k, false, s);
-    if (set.top_p < 1.0f) {
-        if (!known) sum_tiles(row, w, kept, 0, s);
+    if (set.top_k < a.vocab) kept = select<true>(source, w, kept, set.top_k, bound, s);
+    if (known) {
+        if (head_sums(source, w, set, target, kept, s)) {
+            draw_by_tiles(a, r, source.row, w, set, kept, s);
+            return;
+        }
+        kept = select<false>(source, w, kept, target, bound, s);
+    } else if (set.top_p < 1.0f) {
+        sum_tiles(source, w, kept, set, false, s);
         uint64_t all = 0;
         for (int i = threadIdx.x; i < BINS; i += THREADS) all += s.bins[i];
         all = block_sum(all, s);
-        kept = select<false>(row, w, kept, set.head(all), known, s);
+        kept = select<false>(source, w, kept, set.head(all), DEAD_BIN, s);
     }
-    sum_tiles(row, w, kept, set.least, s);
-    draw_by_tiles(a, r, row, w, set, kept, s);
+    sum_tiles(source, w, kept, set, true, s);
+    draw_by_tiles(a, r, source.row, w, set, kept, s);
 }
 
-// Rows of few logits: a workgroup each.
-template <class T> __global__ __launch_bounds__(THREADS) void k_sample_rows(she_sample_args a)
+// A workgroup for each row: of few logits, which it holds, or of calls for which the larger rows' scratch is too much.
+template <class T, bool FEW> __global__ __launch_bounds__(THREADS) void k_sample_rows(she_sample_args a)
 {
     __shared__ Shared s;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t r = blockIdx.x;
-    const Row<T> row = row_of<T>(a, r);
+    typename std::conditional<FEW, Held<T>, FromMemory<T>>::type source{row_of<T>(a, r)};
+    if constexpr (FEW) load_logits(source.row, threadIdx.x * 8, source.v);
     make_table(s.table);
 
     // the largest logit, and the first that is as large
     float top = -__builtin_inff();
     uint32_t where = 0;
-    for_all(row, [&](uint32_t at, const float v[8]) {
+    source.all(-__builtin_inff(), [&](uint32_t at, const float v[8], bool there) {
+        if (!there) return;
 #pragma unroll
         for (int i = 0; i < 8; i++)
             if (v[i] > top) {
@@ -456,7 +645,7 @@ template <class T> __global__ __launch_bounds__(THREADS) void k_sample_rows(she_
         if (threadIdx.x == 0) answer(a, r, none ? -1 : (int32_t)where, none ? 0.0f : 1.0f);
         return;
     }
-    pass_by_pass(a, r, row, Weights(top, set.temperature, s.table), set, false, s);
+    pass_by_pass<T>(a, r, source, Weights(top, set.temperature, s.table), set, false, 0, DEAD_BIN, s);
 }
 
 // Larger rows, in three launches.  First a row's parts have the largest logit of every eight neighbours, and their own.
@@ -466,7 +655,6 @@ struct Parts {
     uint64_t *bins;                      // [rows][BINS]: the histogram of weights for top_p, or the weights of tiles without a filter
     uint32_t parts, tiles;               // tiles of a part, a multiple of PART_THREADS * 8 / TILE
 };
-__device__ inline uint32_t eights_of(uint32_t vocab) { return (vocab + 7) / 8; }
 
 template <class T> __global__ __launch_bounds__(PART_THREADS) void k_sample_largest(she_sample_args a, Parts w)
 {
@@ -587,68 +775,68 @@ template <class T> __global__ __launch_bounds__(PART_THREADS) void k_sample_weig
         if (bins[i]) atomicAdd((unsigned long long *)&w.bins[(size_t)r * BINS + i], (unsigned long long)bins[i]);
 }
 
-// The tokens of bins up to `bin`, if they are no more than threads: a candidate a thread, in no order.  Returns how many there are.
-template <class T> __device__ __forceinline__ uint32_t pick_out(const Row<T> &row, const Weights &w, const float *eights, int bin, Shared &s)
+// The tokens of the bins up to `last`, if they are no more than threads, in no order: first the eights that have any, then these.  Returns how many there
+// are, or more than threads.
+template <class T> __device__ __forceinline__ uint32_t pick_few(const FromMemory<T> &source, const Weights &w, int last, Shared &s)
 {
-    constexpr int AHEAD = 8;
-    if (threadIdx.x == 0) s.count = 0;
+    constexpr int AHEAD = 16;
+    const uint32_t end = eights_of(source.row.vocab);
+    uint32_t *places = s.waiting[0];
     __syncthreads();
-    const uint32_t all = eights_of(row.vocab);
-    for (uint32_t e0 = threadIdx.x; e0 < all; e0 += THREADS * AHEAD) {
+    if (threadIdx.x == 0) s.count = s.eights = 0;
+    __syncthreads();
+    const float least = least_at(w, -8 * last - 8);
+#pragma unroll 1
+    for (uint32_t e0 = threadIdx.x; e0 < end; e0 += THREADS * AHEAD) {
         float m[AHEAD];
 #pragma unroll
-        for (int k = 0; k < AHEAD; k++) m[k] = e0 + k * THREADS < all ? eights[e0 + k * THREADS] : -__builtin_inff();
+        for (int k = 0; k < AHEAD; k++) m[k] = e0 + k * THREADS < end ? source.eights[e0 + k * THREADS] : -__builtin_inff();
 #pragma unroll
         for (int k = 0; k < AHEAD; k++) {
-            const double y = w.below(m[k]);
-            if (!(y > DEAD) || w.bin(y) > bin || s.count > THREADS) continue;
-            const uint32_t at = (e0 + k * THREADS) * 8;
-            float v[8];
-            load_logits(row, at, v);
-            for (int i = 0; i < 8; i++) {
-                const float l = w.plain(v[i]);
-                const double z = w.below_plain(l);
-                if (!(z > DEAD) || w.bin(z) > bin) continue;
-                const uint32_t n = atomicAdd(&s.count, 1u);
-                if (n < THREADS) s.list[n] = Candidate{(uint64_t)key_of(l) << 32 | (uint32_t)~(at + i), w.weight(z)};
-            }
+            if (!(m[k] >= least) || m[k] == -__builtin_inff()) continue;
+            const uint32_t n = atomicAdd(&s.eights, 1u);
+            if (n < THREADS) places[n] = (e0 + k * THREADS) * 8;
         }
     }
     __syncthreads();
-    return s.count;
+    const uint32_t eights = s.eights;
+    if (threadIdx.x < min(eights, (uint32_t)THREADS)) {
+        float v[8];
+        const uint32_t at = places[threadIdx.x];
+        load_logits(source.row, at, v);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float l = w.plain(v[i]);
+            const double y = w.below_plain(l);
+            if (!(y > DEAD) || w.bin(y) > last) continue;
+            const uint32_t n = atomicAdd(&s.count, 1u);
+            if (n < THREADS) s.list[n] = token_of(key_of(l), at + i);
+        }
+    }
+    __syncthreads();
+    // the eights that are left out, if any, may have no token: rounding is on the safe side there
+    return eights <= THREADS ? s.count : THREADS + 1;
 }
 
-// The draw from `count` candidates; `whole`: the row's weight, which top_p is of where there is no top_k.
-template <class T> __device__ __forceinline__ void draw_by_list(const she_sample_args &a, uint32_t r, const Weights &w, const Settings &set, uint64_t whole, uint32_t count, Shared &s)
+// The draw from `count` tokens in s.list; `whole`: the row's weight, which top_p is of where there is no top_k.
+__device__ __forceinline__ void draw_by_list(const she_sample_args &a, uint32_t r, const Weights &w, const Settings &set, uint64_t whole, uint32_t count, Shared &s)
 {
     const uint32_t i = threadIdx.x;
-    const Candidate mine = i < count ? s.list[i] : Candidate{0, 0};
-    uint32_t rank = 0;
-    uint64_t before = 0;
-    if ((i & ~63u) < count)
-        for (uint32_t j = 0; j < count; j++) {
-            const Candidate c = s.list[j];
-            const bool better = c.order > mine.order;
-            rank += better;
-            before += better ? c.weight : 0;
-        }
-    bool kept = i < count && rank < set.top_k;
+    const auto weight_of = [&](float logit) { return w.weight(w.below_plain(logit)); };
+    const uint64_t token = sorted(i < count ? s.list[i] : 0, count, s);
+    bool kept = i < count && i < set.top_k;
+    uint64_t weight = kept ? weight_of(logit_of(token)) : 0, all;
     if (set.top_p < 1.0f) {
-        if (set.top_k < a.vocab) whole = block_sum(kept ? mine.weight : 0, s);
-        kept &= before < set.head(whole);
+        const uint64_t before = running_sum(weight, all, s) - weight;
+        kept &= before < set.head(set.top_k < a.vocab ? all : whole);
     }
-    kept &= mine.weight >= set.least;
-    const uint64_t weight = kept ? mine.weight : 0, all = block_sum(weight, s), drawn = share_of(all, set.uniform, false);
-    if (i < count) s.list[i].weight = weight;
-    __syncthreads();
-    if ((i & ~63u) >= count) return;
-    uint64_t run = 0;
-    for (uint32_t j = 0; j < count; j++) {
-        const Candidate c = s.list[j];
-        run += (uint32_t)c.order > (uint32_t)mine.order ? c.weight : 0;       // an earlier index
-    }
-    if (weight && run <= drawn && run + weight > drawn)
-        answer(a, r, (int32_t)~(uint32_t)mine.order, (float)(exp2(w.below_plain(number_of((uint32_t)(mine.order >> 32))) / 256) * ((double)ONE / (double)all)));
+    // the first threads have what is kept: now by its index, the lowest first
+    const uint32_t left = (uint32_t)__syncthreads_count(kept);
+    const uint64_t turned = sorted(kept && weight >= set.least ? token << 32 | token >> 32 : 0, left, s);
+    const float logit = number_of((uint32_t)turned);
+    weight = turned ? weight_of(logit) : 0;
+    const uint64_t run = running_sum(weight, all, s), drawn = share_of(all, set.uniform, false);
+    if (run > drawn && run - weight <= drawn) answer(a, r, (int32_t)~(uint32_t)(turned >> 32), prob_of(w.below_plain(logit), all));
 }
 
 // And the rows' answers.
@@ -674,15 +862,24 @@ template <class T> __global__ __launch_bounds__(THREADS) void k_sample_answers(s
     }
     make_table(s.table);
     const Weights w(top, set.temperature, s.table);
-    const float *eights = parts.eights + (size_t)r * eights_of(a.vocab);
+    const FromMemory<T> source{row, parts.eights + (size_t)r * eights_of(a.vocab)};
     const bool counted = set.top_k < a.vocab, headed = set.top_p < 1.0f;
     uint64_t all = 0;
     if (counted) {
         // the k-th of the eights' largest is no larger than the k-th logit
         clear_bins(s);
-        for (uint32_t e = threadIdx.x; e < eights_of(a.vocab); e += THREADS) {
-            const double y = w.below(eights[e]);
-            if (y > DEAD) atomicAdd((unsigned long long *)&s.bins[w.bin(y)], 1ull);
+        constexpr int AHEAD = 8;
+        const uint32_t end = eights_of(a.vocab);
+#pragma unroll 1
+        for (uint32_t e0 = threadIdx.x; e0 < end; e0 += THREADS * AHEAD) {
+            float m[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; k++) m[k] = e0 + k * THREADS < end ? source.eights[e0 + k * THREADS] : -__builtin_inff();
+#pragma unroll
+            for (int k = 0; k < AHEAD; k++) {
+                const double y = w.below(m[k]);
+                if (y > DEAD) atomicAdd((unsigned long long *)&s.bins[w.bin(y)], 1ull);
+            }
         }
         __syncthreads();
     } else {
@@ -693,16 +890,26 @@ template <class T> __global__ __launch_bounds__(THREADS) void k_sample_answers(s
             return;
         }
     }
-    const Crossing c = find_crossing(s.bins, counted ? set.top_k : set.head(all), s.sums, &s.found);
-    const uint32_t count = pick_out(row, w, eights, c.bin < 0 ? DEAD_BIN : c.bin, s);
-    if (count <= THREADS) draw_by_list<T>(a, r, w, set, all, count, s);
-    else pass_by_pass(a, r, row, w, set, !counted, s);
+    const uint64_t target = counted ? set.top_k : set.head(all);
+    const Crossing c = find_crossing(s.bins, target, s.sums, &s.found);
+    const int bound = c.bin < 0 ? DEAD_BIN : c.bin;
+    uint32_t count = 0;
+    if (!counted) {
+        // at least as many tokens as their weight is of the largest that their bin has room for
+        float many = 0;
+        for (int b = threadIdx.x; b <= bound; b += THREADS) many += (float)s.bins[b] * (0.98f / (float)ONE) * __builtin_amdgcn_exp2f(b / 32.0f);
+        count = (uint32_t)block_sum((uint64_t)fminf(many, 2 * THREADS), s);
+    }
+    if (count <= THREADS) count = pick_few(source, w, bound, s);
+    if (count <= THREADS) draw_by_list(a, r, w, set, all, count, s);
+    else pass_by_pass<T>(a, r, source, w, set, !counted, target, bound, s);
 }
 
 template <class T> hipError_t sample(const she_sample_args &a, const SampleShape &s, void *scratch, hipStream_t st)
 {
     if (!s.parts) {
-        k_sample_rows<T><<<a.rows, THREADS, 0, st>>>(a);
+        if (a.vocab <= 8 * THREADS) k_sample_rows<T, true><<<a.rows, THREADS, 0, st>>>(a);
+        else k_sample_rows<T, false><<<a.rows, THREADS, 0, st>>>(a);
         return hipGetLastError();
     }
     Parts w{};
