@@ -27,7 +27,7 @@ constexpr double LOG2E = 1.4426950408889634074, LN2 = 0.69314718055994530942, DE
 
 __device__ inline uint32_t key_of(float v)                         // ordered as the numbers are
 {
-    const uint32_t u = __float_as_uint(v);
+    const uint32_t u = __float_as_uint(v + 0.0f);                  // no negative zero
     return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 __device__ inline float number_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
@@ -92,11 +92,13 @@ struct Weights {
     {
         if (infinite) top = 0;
     }
-    // a logit as it is compared: no NaN, no negative zero
-    __device__ __forceinline__ float plain(float v) const
+    // logits as they are compared, which NaN is not
+    __device__ __forceinline__ void plain(const float v[8], float l[8]) const
     {
-        if (infinite) return v == __builtin_inff() ? 0.0f : -__builtin_inff();
-        return v == v ? v + 0.0f : -__builtin_inff();
+#pragma unroll
+        for (int i = 0; i < 8; i++) l[i] = v[i];
+        if (infinite)
+            for (int i = 0; i < 8; i++) l[i] = v[i] == __builtin_inff() ? 0.0f : -__builtin_inff();
     }
     // in units of 1/256 octave, from 0 down to DEAD, which is where NaN goes too
     __device__ __forceinline__ double below(float v) const
@@ -183,11 +185,13 @@ __device__ __forceinline__ Crossing find_crossing(const uint64_t *hist, uint64_t
     return c;
 }
 
-// The tokens that are kept: of the logits of `key` those up to index `last`, and all with larger keys.
+// The tokens that are kept: those above a logit, and of those that have it the ones up to index `last`.
 struct Kept {
-    uint32_t key, last;
-    __device__ __forceinline__ bool has(uint32_t k, uint32_t index) const { return k > key || (k == key && index <= last); }
+    float logit;
+    uint32_t last;
+    __device__ __forceinline__ bool has(float l, uint32_t index) const { return l > logit || (l == logit && index <= last); }
 };
+__device__ __forceinline__ Kept all_kept() { return Kept{-__builtin_inff(), ~0u}; }
 
 struct Shared {
     uint64_t bins[BINS];                 // a histogram; sums or counts of tiles
@@ -200,7 +204,8 @@ struct Shared {
     uint32_t where[WAVES], answer, count, eights;
     uint32_t waiting[WAVES][TILE];       // logits that wait for their weight; places of eights
 };
-__device__ __forceinline__ uint64_t token_of(uint32_t key, uint32_t index) { return (uint64_t)key << 32 | (uint32_t)~index; }
+__device__ __forceinline__ uint64_t token_of(float l, uint32_t index) { return (uint64_t)key_of(l) << 32 | (uint32_t)~index; }
+__device__ __forceinline__ float logit_of(uint64_t token) { return number_of((uint32_t)(token >> 32)); }
 
 __device__ __host__ inline uint32_t eights_of(uint32_t vocab) { return (vocab + 7) / 8; }
 
@@ -210,23 +215,41 @@ template <class T> struct FromMemory {
     const float *eights;                 // the largest of each; may be null
     template <class F> __device__ __forceinline__ void all(float least, F f) const
     {
-        constexpr int AHEAD = 4;
+        // two at a time: while they are used the next two are on their way, and whether those after them have to be there
+        constexpr int AHEAD = 2;
         const uint32_t lane = threadIdx.x & 63, end = eights_of(row.vocab);
-#pragma unroll 1
-        for (uint32_t e0 = threadIdx.x; e0 - lane < end; e0 += THREADS * AHEAD) {
-            float v[AHEAD][8];
+        struct Two {
+            float largest[AHEAD], v[AHEAD][8];
             bool there[AHEAD];
+        } a, b;
+        const auto ask = [&](Two &t, uint32_t e0) {
+#pragma unroll
+            for (int k = 0; k < AHEAD; k++) t.largest[k] = eights && e0 + k * THREADS < end ? eights[e0 + k * THREADS] : __builtin_inff();
+        };
+        const auto fetch = [&](Two &t, uint32_t e0) {
 #pragma unroll
             for (int k = 0; k < AHEAD; k++) {
-                const uint32_t e = e0 + k * THREADS;
-                there[k] = e < end && (!eights || eights[e] >= least);
+                t.there[k] = e0 + k * THREADS < end && t.largest[k] >= least;
+                if (t.there[k]) load_logits(row, (e0 + k * THREADS) * 8, t.v[k]);
             }
+        };
+        const auto use = [&](const Two &t, uint32_t e0) {
 #pragma unroll
             for (int k = 0; k < AHEAD; k++)
-                if (there[k]) load_logits(row, (e0 + k * THREADS) * 8, v[k]);
-#pragma unroll
-            for (int k = 0; k < AHEAD; k++)
-                if (e0 + k * THREADS - lane < end) f((e0 + k * THREADS) * 8, v[k], there[k]);
+                if (e0 + k * THREADS - lane < end) f((e0 + k * THREADS) * 8, t.v[k], t.there[k]);
+        };
+        constexpr uint32_t BY = AHEAD * THREADS;
+        ask(a, threadIdx.x);
+        ask(b, threadIdx.x + BY);
+        fetch(a, threadIdx.x);
+#pragma unroll 1
+        for (uint32_t e0 = threadIdx.x; e0 - lane < end; e0 += 2 * BY) {
+            fetch(b, e0 + BY);
+            ask(a, e0 + 2 * BY);
+            use(a, e0);
+            fetch(a, e0 + 2 * BY);
+            ask(b, e0 + 3 * BY);
+            use(b, e0 + BY);
         }
     }
 };
@@ -297,33 +320,33 @@ __device__ __forceinline__ uint64_t sorted(uint64_t v, uint32_t count, Shared &s
     return v;
 }
 
-// A logit that is no larger than any of y or more, in units of 1/256 octave.
+// A logit that is no larger than any of y or more, in units of 1/256 octave; one that is no smaller than any of a bin.
 __device__ __forceinline__ float least_at(const Weights &w, double y) { return (float)((double)w.top + (y - 1) / w.unit); }
-__device__ __forceinline__ float least_of(const Kept &kept) { return kept.key ? number_of(kept.key) : -__builtin_inff(); }
+__device__ __forceinline__ float most_at(const Weights &w, int bin) { return bin ? (float)((double)w.top - (8 * bin - 1) / w.unit) : __builtin_inff(); }
 
-// Of what `kept` has, the tokens of the bins from `first` to `last`, if they are no more than threads, in no order.  Returns how many there are.
-template <class S> __device__ __forceinline__ uint32_t pick_out(const S &row, const Weights &w, Kept kept, int first, int last, Shared &s)
+// Of what `kept` has, the tokens of a bin, if they are no more than threads, in no order.  Returns how many there are.
+template <class S> __device__ __forceinline__ uint32_t pick_out(const S &row, const Weights &w, Kept kept, int bin, Shared &s)
 {
     __syncthreads();
     if (threadIdx.x == 0) s.count = 0;
     __syncthreads();
-    const float least = least_at(w, -8 * last - 8);
+    const float least = least_at(w, -8 * bin - 8), most = most_at(w, bin);
     row.all(least, [&](uint32_t at, const float v[8], bool there) {
         if (!there || s.count > THREADS) return;
+        float l[8];
+        w.plain(v, l);
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-            const float l = w.plain(v[i]);
-            if (!(l >= least)) continue;
-            const double y = w.below_plain(l);
-            if (!(y > DEAD) || w.bin(y) > last || w.bin(y) < first || !kept.has(key_of(l), at + i)) continue;
+            if (!(l[i] >= least) || l[i] > most) continue;
+            const double y = w.below_plain(l[i]);
+            if (!(y > DEAD) || w.bin(y) != bin || !kept.has(l[i], at + i)) continue;
             const uint32_t n = atomicAdd(&s.count, 1u);
-            if (n < THREADS) s.list[n] = token_of(key_of(l), at + i);
+            if (n < THREADS) s.list[n] = token_of(l[i], at + i);
         }
     });
     __syncthreads();
     return s.count;
 }
-__device__ __forceinline__ float logit_of(uint64_t token) { return number_of((uint32_t)(token >> 32)); }
 
 // Of what `kept` has, the first of the order whose measure (ones or weights) together reaches `target`; `kept` itself if all does not.
 // No token of a bin behind `bound` is among them.
@@ -331,15 +354,16 @@ template <bool COUNT, class S> __device__ __forceinline__ Kept select(const S &s
 {
     const auto &row = source.row;
     const auto measure = [&](double y) { return COUNT ? 1 : w.weight(y); };
-    const float least = fmaxf(least_of(kept), least_at(w, -8 * bound - 8));
+    const float least = fmaxf(kept.logit, least_at(w, -8 * bound - 8));
     clear_bins(s);
     source.all(least, [&](uint32_t at, const float v[8], bool there) {
         if (!there) return;
+        float l[8];
+        w.plain(v, l);
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-            const float l = w.plain(v[i]);
-            if (!(l >= least) || !kept.has(key_of(l), at + i)) continue;
-            const double y = w.below_plain(l);
+            if (!(l[i] >= least) || !kept.has(l[i], at + i)) continue;
+            const double y = w.below_plain(l[i]);
             if (y > DEAD) atomicAdd((unsigned long long *)&s.bins[w.bin(y)], (unsigned long long)measure(y));
         }
     });
@@ -348,12 +372,12 @@ template <bool COUNT, class S> __device__ __forceinline__ Kept select(const S &s
     if (c.bin < 0) return kept;
     const int bin = c.bin;
     target -= c.before;
-    const uint32_t count = pick_out(source, w, kept, bin, bin, s);
+    const uint32_t count = pick_out(source, w, kept, bin, s);
     if (count <= THREADS) {
         const uint64_t token = sorted(threadIdx.x < count ? s.list[threadIdx.x] : 0, count, s), mine = threadIdx.x < count ? measure(w.below_plain(logit_of(token))) : 0;
         uint64_t all;
         const uint64_t run = running_sum(mine, all, s);
-        if (run >= target && run - mine < target) s.cut = Kept{(uint32_t)(token >> 32), ~(uint32_t)token};
+        if (run >= target && run - mine < target) s.cut = Kept{logit_of(token), ~(uint32_t)token};
         __syncthreads();
         return s.cut;
     }
@@ -365,12 +389,13 @@ template <bool COUNT, class S> __device__ __forceinline__ Kept select(const S &s
         clear_bins(s);
         source.all(number_of(low), [&](uint32_t at, const float v[8], bool there) {
             if (!there) return;
+            float l[8];
+            w.plain(v, l);
 #pragma unroll
             for (int i = 0; i < 8; i++) {
-                const float l = w.plain(v[i]);
-                const uint32_t key = key_of(l);
-                if (key < low || key > high || !kept.has(key, at + i)) continue;
-                const double y = w.below_plain(l);
+                const uint32_t key = key_of(l[i]);
+                if (key < low || key > high || !kept.has(l[i], at + i)) continue;
+                const double y = w.below_plain(l[i]);
                 if (y > DEAD && w.bin(y) == bin) atomicAdd((unsigned long long *)&s.bins[(high - key) >> shift], (unsigned long long)measure(y));
             }
         });
@@ -387,15 +412,18 @@ template <bool COUNT, class S> __device__ __forceinline__ Kept select(const S &s
         low = first;
         break;
     }
-    // `low` is the last key that is kept; how many of the tokens that have it are
-    const uint64_t each = measure(w.below_plain(number_of(low))), all = s.bins[c.bin] / each, wanted = (target + each - 1) / each;
+    // `border` is the last logit that is kept; how many of the tokens that have it are
+    const float border = number_of(low);
+    const uint64_t each = measure(w.below_plain(border)), all = s.bins[c.bin] / each, wanted = (target + each - 1) / each;
     __syncthreads();
-    if (wanted >= all) return Kept{low, low == kept.key ? kept.last : ~0u};
+    if (wanted >= all) return Kept{border, border == kept.logit ? kept.last : ~0u};
     // the index of the last of them, by tile and then by place
-    source.all(number_of(low), [&](uint32_t at, const float v[8], bool there) {
+    source.all(border, [&](uint32_t at, const float v[8], bool there) {
+        float l[8];
+        w.plain(v, l);
         uint32_t here = 0;
 #pragma unroll
-        for (int i = 0; i < 8; i++) here += there && key_of(w.plain(v[i])) == low && kept.has(low, at + i);
+        for (int i = 0; i < 8; i++) here += there && l[i] == border && kept.has(border, at + i);
         const uint64_t sum = wave_sum(here);
         if ((threadIdx.x & 63) == 0) s.bins[at / TILE] = sum;
     });
@@ -406,9 +434,10 @@ template <bool COUNT, class S> __device__ __forceinline__ Kept select(const S &s
         float v[8];
         const uint32_t at = c.bin * TILE + threadIdx.x * 8;
         load_logits(row, at, v);
+        w.plain(v, v);
         uint32_t here = 0;
 #pragma unroll
-        for (int i = 0; i < 8; i++) here += key_of(w.plain(v[i])) == low && kept.has(low, at + i);
+        for (int i = 0; i < 8; i++) here += v[i] == border && kept.has(border, at + i);
         uint32_t run = here;
 #pragma unroll
         for (int m = 1; m < 64; m *= 2) {
@@ -418,12 +447,12 @@ template <bool COUNT, class S> __device__ __forceinline__ Kept select(const S &s
         uint32_t left = (uint32_t)(wanted - c.before), before = run - here;
 #pragma unroll
         for (int i = 0; i < 8; i++)
-            if (key_of(w.plain(v[i])) == low && kept.has(low, at + i) && ++before == left) s.answer = at + i;
+            if (v[i] == border && kept.has(border, at + i) && ++before == left) s.answer = at + i;
     }
     __syncthreads();
     const uint32_t last = s.answer;
     __syncthreads();
-    return Kept{low, last};
+    return Kept{border, last};
 }
 
 struct Settings {
@@ -465,11 +494,11 @@ template <class T> __device__ __forceinline__ void draw_by_tiles(const she_sampl
     float v[8];
     const uint32_t at = c.bin * TILE + lane * 8;
     load_logits(row, at, v);
+    w.plain(v, v);
     uint64_t weight[8], here = 0;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-        const float l = w.plain(v[i]);
-        weight[i] = kept.has(key_of(l), at + i) ? w.weight(w.below_plain(l)) : 0;
+        weight[i] = kept.has(v[i], at + i) ? w.weight(w.below_plain(v[i])) : 0;
         if (weight[i] < set.least) weight[i] = 0;
         here += weight[i];
     }
@@ -482,7 +511,7 @@ template <class T> __device__ __forceinline__ void draw_by_tiles(const she_sampl
     run = run - here + c.before;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-        if (run <= drawn && run + weight[i] > drawn) answer(a, r, (int32_t)(at + i), prob_of(w.below(v[i]), all));
+        if (run <= drawn && run + weight[i] > drawn) answer(a, r, (int32_t)(at + i), prob_of(w.below_plain(v[i]), all));
         run += weight[i];
     }
 }
@@ -515,16 +544,14 @@ __device__ __forceinline__ uint64_t tile_sum(const Weights &w, const float l[8],
 template <class S> __device__ __forceinline__ void sum_tiles(const S &source, const Weights &w, const Kept &kept, const Settings &set, bool filtered, Shared &s)
 {
     const uint64_t least = filtered ? set.least : 0;
-    const float floor = fmaxf(least_of(kept), filtered ? set.least_logit(w) : -__builtin_inff());
+    const float floor = fmaxf(kept.logit, filtered ? set.least_logit(w) : -__builtin_inff());
     __syncthreads();
     source.all(floor, [&](uint32_t at, const float v[8], bool there) {
         float l[8];
+        w.plain(v, l);
         uint32_t which = 0;
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            l[i] = w.plain(v[i]);
-            which |= (there && l[i] >= floor && kept.has(key_of(l[i]), at + i)) << i;
-        }
+        for (int i = 0; i < 8; i++) which |= (there && l[i] >= floor && kept.has(l[i], at + i)) << i;
         const uint64_t sum = tile_sum(w, l, which, least, s);
         if ((threadIdx.x & 63) == 0) s.bins[at / TILE] = sum;
     });
@@ -542,24 +569,29 @@ template <class S> __device__ __forceinline__ bool head_sums(const S &source, co
     if (threadIdx.x == 0) s.count = 0;
     clear_bins(s);
     // logits below `least` are behind the bin, and those above `most` before it
-    const float least = least_at(w, -8 * bin - 8), most = bin ? (float)((double)w.top - (8 * bin - 1) / w.unit) : __builtin_inff(), floor = set.least_logit(w);
+    const float least = least_at(w, -8 * bin - 8), most = most_at(w, bin), floor = set.least_logit(w);
     source.all(fmaxf(least, floor), [&](uint32_t at, const float v[8], bool there) {
         float l[8];
-        uint32_t which = 0;
+        w.plain(v, l);
+        uint32_t which = 0, close = 0;
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-            l[i] = w.plain(v[i]);
-            which |= (there && l[i] >= least) << i;
+            which |= (there && l[i] > most) << i;
+            close |= (there && l[i] >= least && !(l[i] > most)) << i;
         }
+        for (; close; close &= close - 1) {
+            const int at_i = __builtin_ctz(close);
+            float its = l[0];
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            if (!(which >> i & 1) || l[i] > most) continue;
-            const double y = w.below_plain(l[i]);
-            if (y > DEAD && w.bin(y) < bin) continue;
-            which &= ~(1u << i);
+            for (int i = 1; i < 8; i++) its = at_i == i ? l[i] : its;
+            const double y = w.below_plain(its);
             if (!(y > DEAD) || w.bin(y) > bin) continue;
+            if (w.bin(y) < bin) {
+                which |= 1u << at_i;
+                continue;
+            }
             const uint32_t n = atomicAdd(&s.count, 1u);
-            if (n < THREADS) s.list[n] = token_of(key_of(l[i]), at + i);
+            if (n < THREADS) s.list[n] = token_of(its, at + at_i);
         }
         const uint64_t sum = tile_sum(w, l, which, set.least, s);
         if ((threadIdx.x & 63) == 0) s.bins[at / TILE] = sum;
@@ -573,7 +605,7 @@ template <class S> __device__ __forceinline__ bool head_sums(const S &source, co
     const uint32_t index = ~(uint32_t)token;
     if (threadIdx.x < count && before < target) {
         if (mine >= set.least) atomicAdd((unsigned long long *)&s.bins[index / TILE], (unsigned long long)mine);
-        if (before + mine >= target) s.cut = Kept{(uint32_t)(token >> 32), index};
+        if (before + mine >= target) s.cut = Kept{logit_of(token), index};
     }
     __syncthreads();
     kept = s.cut;
@@ -584,7 +616,7 @@ template <class S> __device__ __forceinline__ bool head_sums(const S &source, co
 // them.  `bound`: as in select, of the first filter.
 template <class T, class S> __device__ __forceinline__ void pass_by_pass(const she_sample_args &a, uint32_t r, const S &source, const Weights &w, const Settings &set, bool known, uint64_t target, int bound, Shared &s)
 {
-    Kept kept{0, ~0u};
+    Kept kept = all_kept();
     if (set.top_k < a.vocab) kept = select<true>(source, w, kept, set.top_k, bound, s);
     if (known) {
         if (head_sums(source, w, set, target, kept, s)) {
@@ -804,13 +836,13 @@ template <class T> __device__ __forceinline__ uint32_t pick_few(const FromMemory
         float v[8];
         const uint32_t at = places[threadIdx.x];
         load_logits(source.row, at, v);
+        w.plain(v, v);
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-            const float l = w.plain(v[i]);
-            const double y = w.below_plain(l);
+            const double y = w.below_plain(v[i]);
             if (!(y > DEAD) || w.bin(y) > last) continue;
             const uint32_t n = atomicAdd(&s.count, 1u);
-            if (n < THREADS) s.list[n] = token_of(key_of(l), at + i);
+            if (n < THREADS) s.list[n] = token_of(v[i], at + i);
         }
     }
     __syncthreads();
@@ -886,7 +918,7 @@ template <class T> __global__ __launch_bounds__(THREADS) void k_sample_answers(s
         for (int i = threadIdx.x; i < BINS; i += THREADS) all += s.bins[i] = parts.bins[(size_t)r * BINS + i];
         all = block_sum(all, s);
         if (!headed) {
-            draw_by_tiles(a, r, row, w, set, Kept{0, ~0u}, s);
+            draw_by_tiles(a, r, row, w, set, all_kept(), s);
             return;
         }
     }
