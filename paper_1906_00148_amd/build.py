@@ -3,12 +3,15 @@ from __future__ import annotations
 
 import os
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libshe_hip.so")
-SOURCES = ["she_kernels.hip", "she_api.cpp", "she_host.cpp", "she_circuits.cpp", "she_leveled.cpp", "she_clear.cpp",
-           "she_clear_step.cpp", "clear_plan.hip", "clear_sample.hip", "clear_attend_shape.cpp", "clear_qk.hip", "clear_adapters.hip", "clear_attend.hip"]
+# those that take longest first
+SOURCES = ["clear_sample.hip", "clear_attend.hip", "she_kernels.hip", "clear_adapters.hip", "clear_qk.hip", "clear_plan.hip", "she_api.cpp", "she_host.cpp",
+           "she_circuits.cpp", "she_leveled.cpp", "she_clear.cpp", "she_clear_step.cpp", "clear_attend_shape.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
@@ -20,12 +23,21 @@ FLAGS = [
 
 
 def build(verbose: bool = False, extra: list[str] | None = None, out: str | None = None) -> str:
-    """Compiles every source each time it is called; returns the path of the shared library."""
+    """Compiles every source each time it is called, several at a time; returns the path of the shared library."""
     out = out or LIB_PATH
-    cmd = [HIPCC] + FLAGS + (extra or []) + [os.path.join(CSRC, s) for s in SOURCES] + ["-o", out + ".tmp"]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.check_call(cmd, stderr=None if verbose else subprocess.DEVNULL)
+    stderr = None if verbose else subprocess.DEVNULL
+    flags = [f for f in FLAGS if f != "-shared"] + (extra or [])
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        subprocess.check_call(cmd, stderr=stderr)
+
+    with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        for done in [pool.submit(run, [HIPCC] + flags + ["-c", os.path.join(CSRC, s), "-o", o]) for s, o in zip(SOURCES, objects)]:
+            done.result()
+        run([HIPCC] + FLAGS + objects + ["-o", out + ".tmp"])
     os.replace(out + ".tmp", out)
     return out
 

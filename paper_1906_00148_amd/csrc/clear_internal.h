@@ -75,7 +75,9 @@ hipError_t launch_plan_pages(const she_plan_pages_args &a, void *scratch, uint32
 
 // ---- the next token
 struct SampleShape {
-    uint32_t parts, tiles;               // workgroups that share a row, none if one has all of it at once; tiles of logits of each
+    uint32_t parts, tiles;               // workgroups that share a row, none if one has all of it; tiles of logits of each, or of its wavefronts if `plain`
+    bool plain;                          // no filters
+    uint32_t rows;                       // of a set of launches
 };
 SampleShape sample_shape(const she_sample_args &a, uint32_t cus);
 size_t sample_scratch(const she_sample_args &a, const SampleShape &s);

@@ -12,7 +12,6 @@
 // every eight neighbours, since k of these that reach a logit are k logits that do.  Where they are many, the logit is found by
 // histograms over the row, from the 32nds of an octave on to the bits of the bin's logits until a bin is one value.
 #include <algorithm>
-#include <type_traits>
 
 #include "clear_device.h"
 #include "clear_internal.h"
@@ -635,14 +634,14 @@ template <class T, class S> __device__ __forceinline__ void pass_by_pass(const s
     draw_by_tiles(a, r, source.row, w, set, kept, s);
 }
 
-// A workgroup for each row: of few logits, which it holds, or of calls for which the larger rows' scratch is too much.
-template <class T, bool FEW> __global__ __launch_bounds__(THREADS) void k_sample_rows(she_sample_args a)
+// Rows of few logits, which a workgroup holds.
+template <class T> __global__ __launch_bounds__(THREADS) void k_sample_rows(she_sample_args a)
 {
     __shared__ Shared s;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t r = blockIdx.x;
-    typename std::conditional<FEW, Held<T>, FromMemory<T>>::type source{row_of<T>(a, r)};
-    if constexpr (FEW) load_logits(source.row, threadIdx.x * 8, source.v);
+    Held<T> source{row_of<T>(a, r)};
+    load_logits(source.row, threadIdx.x * 8, source.v);
     make_table(s.table);
 
     // the largest logit, and the first that is as large
@@ -937,11 +936,146 @@ template <class T> __global__ __launch_bounds__(THREADS) void k_sample_answers(s
     else pass_by_pass<T>(a, r, source, w, set, !counted, target, bound, s);
 }
 
-template <class T> hipError_t sample(const she_sample_args &a, const SampleShape &s, void *scratch, hipStream_t st)
+// Larger rows of calls without filters, in two launches.  A wavefront has a tile of 512 logits, whose weights and sum are those against the tile's
+// own largest logit; what a tile counts in its row is its sum times 2^(how far its largest is below the row's), rounded.
+struct Tiles {
+    uint64_t *sums;                      // [rows][count]
+    float *tops;                         // [rows][count]
+    uint32_t count, each;                // tiles of a row, tiles of a wavefront
+};
+template <class T> __global__ __launch_bounds__(PART_THREADS) void k_sample_tiles(she_sample_args a, Tiles w)
+{
+    constexpr int AHEAD = 2;
+    __shared__ double table[256];
+    const uint32_t parts = (w.count + w.each * (PART_THREADS / 64) - 1) / (w.each * (PART_THREADS / 64)), lane = threadIdx.x & 63;
+    const uint32_t r = blockIdx.x / parts, part = blockIdx.x - r * parts, first = (part * (PART_THREADS / 64) + (threadIdx.x >> 6)) * w.each, last = min(first + w.each, w.count);
+    const Row<T> row = row_of<T>(a, r);
+    const float temperature = a.temperature ? a.temperature[r] : 1.0f;
+    float v[AHEAD][8];
+#pragma unroll
+    for (int k = 0; k < AHEAD; k++) load_logits(row, (first + k) * TILE + lane * 8, v[k]);
+    make_table(table);
+    __syncthreads();
+    for (uint32_t t0 = first; t0 < last; t0 += AHEAD) {
+#pragma unroll
+        for (int k = 0; k < AHEAD; k++) {
+            if (t0 + k >= last) break;
+            float top = -__builtin_inff();
+#pragma unroll
+            for (int i = 0; i < 8; i++) top = fmaxf(top, v[k][i]);
+#pragma unroll
+            for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
+            uint64_t sum = 0;
+            if (temperature > 0 && top > -__builtin_inff()) {
+                const Weights weights(top, temperature, table);
+#pragma unroll
+                for (int i = 0; i < 8; i++) sum += weights.raw_weight(weights.below(v[k][i])) - RAW;
+                sum = wave_sum(sum);
+            }
+            load_logits(row, (t0 + k + AHEAD < last ? t0 + k + AHEAD : w.count) * TILE + lane * 8, v[k]);
+            if (lane == 0) {
+                w.sums[(size_t)r * w.count + t0 + k] = sum;
+                w.tops[(size_t)r * w.count + t0 + k] = top;
+            }
+        }
+    }
+}
+template <class T> __global__ __launch_bounds__(THREADS) void k_sample_drawn(she_sample_args a, Tiles w)
+{
+    __shared__ Shared s;
+    constexpr int EACH = BINS / THREADS;
+    const uint32_t r = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const Settings set(a, r);
+    uint64_t sums[EACH];
+    float tops[EACH], top = -__builtin_inff();
+    uint32_t where = 0;
+#pragma unroll
+    for (int e = 0; e < EACH; e++) {
+        const uint32_t t = threadIdx.x * EACH + e;
+        sums[e] = t < w.count ? w.sums[(size_t)r * w.count + t] : 0;
+        tops[e] = t < w.count ? w.tops[(size_t)r * w.count + t] : -__builtin_inff();
+        if (tops[e] > top) {
+            top = tops[e];
+            where = t;
+        }
+    }
+    make_table(s.table);
+    const auto join = [&](float other, uint32_t place) {
+        if (other > top || (other == top && place < where)) {
+            top = other;
+            where = place;
+        }
+    };
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) join(__shfl_xor(top, m), __shfl_xor(where, m));
+    if (lane == 0) {
+        s.tops[wave] = top;
+        s.where[wave] = where;
+    }
+    __syncthreads();
+    for (int k = 0; k < WAVES; k++) join(s.tops[k], s.where[k]);
+    const Row<T> row = row_of<T>(a, r);
+    const bool none = top == -__builtin_inff();
+    if (none || !(set.temperature > 0)) {
+        if (threadIdx.x >= 64) return;
+        float v[8];
+        load_logits(row, where * TILE + lane * 8, v);
+        uint32_t here = 8;
+#pragma unroll
+        for (int i = 7; i >= 0; i--) here = v[i] == top ? i : here;
+        const uint64_t those = __ballot(here < 8);
+        if (none ? lane == 0 : (int)lane == __builtin_ctzll(those)) answer(a, r, none ? -1 : (int32_t)(where * TILE + lane * 8 + here), none ? 0.0f : 1.0f);
+        return;
+    }
+    const Weights weights(top, set.temperature, s.table);
+    // whole numbers below 2^53 times a factor, which every running sum is rounded with alike
+    const auto factor = [&](float its) { return exp2(weights.below(its) / 256); };
+    const auto counted = [](uint64_t sum, double f) { return (uint64_t)((double)sum * f + 0.5); };
+    uint64_t all = 0;
+#pragma unroll
+    for (int e = 0; e < EACH; e++) all += s.bins[threadIdx.x * EACH + e] = sums[e] ? counted(sums[e], factor(tops[e])) : 0;
+    all = block_sum(all, s);
+    const uint64_t drawn = share_of(all, set.uniform, false);
+    const Crossing c = find_crossing(s.bins, drawn + 1, s.sums, &s.found);
+    if (threadIdx.x >= 64) return;
+    float v[8];
+    const uint32_t at = c.bin * TILE + lane * 8;
+    load_logits(row, at, v);
+    const float its = w.tops[(size_t)r * w.count + c.bin];
+    const Weights mine(its, set.temperature, s.table);
+    const double f = factor(its);
+    uint64_t run = 0;
+    for (int i = 0; i < 8; i++) run += mine.weight(mine.below(v[i]));
+    const uint64_t own = run;
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) {
+        const uint64_t other = __shfl_up(run, m);
+        if ((int)lane >= m) run += other;
+    }
+    run -= own;
+    for (int i = 0; i < 8; i++) {
+        const uint64_t before = c.before + counted(run, f);
+        run += mine.weight(mine.below(v[i]));
+        if (before <= drawn && c.before + counted(run, f) > drawn) answer(a, r, (int32_t)(at + i), prob_of(weights.below(v[i]), all));
+    }
+}
+
+template <class T> hipError_t sample_rows(const she_sample_args &a, const SampleShape &s, void *scratch, hipStream_t st)
 {
     if (!s.parts) {
-        if (a.vocab <= 8 * THREADS) k_sample_rows<T, true><<<a.rows, THREADS, 0, st>>>(a);
-        else k_sample_rows<T, false><<<a.rows, THREADS, 0, st>>>(a);
+        k_sample_rows<T><<<a.rows, THREADS, 0, st>>>(a);
+        return hipGetLastError();
+    }
+    if (s.plain) {
+        Tiles w{};
+        w.count = (uint32_t)ceil_div(a.vocab, TILE);
+        w.each = s.tiles;
+        w.sums = static_cast<uint64_t *>(scratch);
+        w.tops = reinterpret_cast<float *>(w.sums + (size_t)a.rows * w.count);
+        k_sample_tiles<T><<<a.rows * s.parts, PART_THREADS, 0, st>>>(a, w);
+        const hipError_t rc = hipGetLastError();
+        if (rc != hipSuccess) return rc;
+        k_sample_drawn<T><<<a.rows, THREADS, 0, st>>>(a, w);
         return hipGetLastError();
     }
     Parts w{};
@@ -959,14 +1093,43 @@ template <class T> hipError_t sample(const she_sample_args &a, const SampleShape
     return hipGetLastError();
 }
 
+template <class T> hipError_t sample(const she_sample_args &a, const SampleShape &s, void *scratch, hipStream_t st)
+{
+    for (uint32_t r = 0; r < a.rows; r += s.rows) {
+        she_sample_args b = a;
+        b.rows = std::min(s.rows, a.rows - r);
+        b.logits = (const T *)a.logits + r * a.row_stride;
+        b.uniform += r;
+        b.tokens += r;
+        if (a.temperature) b.temperature += r;
+        if (a.top_k) b.top_k += r;
+        if (a.top_p) b.top_p += r;
+        if (a.min_p) b.min_p += r;
+        if (a.probs) b.probs += r;
+        const hipError_t rc = sample_rows<T>(b, s, scratch, st);
+        if (rc != hipSuccess) return rc;
+    }
+    return hipSuccess;
+}
+
 }  // namespace
 
 SampleShape sample_shape(const she_sample_args &a, uint32_t cus)
 {
-    SampleShape s{0, 0};
-    if (a.vocab <= 8192 || (uint64_t)a.rows * a.vocab > 1u << 30) return s;    // of larger calls the eights are much memory
+    SampleShape s{};
+    s.rows = a.rows;
+    if (a.vocab <= 8 * THREADS) return s;
+    s.plain = !a.top_k && !a.top_p && !a.min_p;
+    s.rows = std::min({a.rows, (1u << 28) / a.vocab, s.plain ? a.rows : 8192u});       // what rows with filters leave behind takes up to 270 MB
+    if (s.plain) {
+        // a tile a wavefront, or more of them where there are many
+        const uint64_t tiles = ceil_div(a.vocab, TILE), steps = ceil_div(tiles, PART_THREADS / 64), parts = std::max<uint64_t>(1, std::min<uint64_t>(steps, ceil_div(16 * cus, s.rows)));
+        s.tiles = (uint32_t)ceil_div(steps, parts);
+        s.parts = (uint32_t)ceil_div(tiles, s.tiles * (PART_THREADS / 64));
+        return s;
+    }
     constexpr uint32_t STEP = PART_THREADS * 8;                    // logits that a workgroup of a part has at once
-    const uint64_t steps = ceil_div(a.vocab, STEP), parts = std::max<uint64_t>(1, std::min<uint64_t>({16, steps, ceil_div(8 * cus, a.rows)}));
+    const uint64_t steps = ceil_div(a.vocab, STEP), parts = std::max<uint64_t>(1, std::min<uint64_t>({16, steps, ceil_div(8 * cus, s.rows)}));
     s.tiles = (uint32_t)(ceil_div(steps, parts) * (STEP / TILE));
     s.parts = (uint32_t)ceil_div(a.vocab, (uint64_t)s.tiles * TILE);
     return s;
@@ -975,7 +1138,8 @@ SampleShape sample_shape(const she_sample_args &a, uint32_t cus)
 size_t sample_scratch(const she_sample_args &a, const SampleShape &s)
 {
     if (!s.parts) return 0;
-    return (size_t)a.rows * (BINS * sizeof(uint64_t) + s.parts * sizeof(float2) + (a.top_k || a.top_p ? (a.vocab + 7) / 8 * sizeof(float) : 0));
+    if (s.plain) return (size_t)s.rows * ceil_div(a.vocab, TILE) * (sizeof(uint64_t) + sizeof(float));
+    return (size_t)s.rows * (BINS * sizeof(uint64_t) + s.parts * sizeof(float2) + (a.top_k || a.top_p ? eights_of(a.vocab) * sizeof(float) : 0));
 }
 
 hipError_t launch_sample(const she_sample_args &a, const SampleShape &s, void *scratch, hipStream_t st)

@@ -152,16 +152,16 @@ def test_a_captured_step_goes_on_by_itself(ctx):
 
 
 def test_many_rows_of_logits(ctx):
-    """More rows, of more than 8192 logits, than a grid has along its second axis."""
+    """More rows, of more than 8192 logits, than a grid has along its second axis, and than a set of launches takes."""
     rows, vocab = 70001, 8200
     x = torch.randn(1, vocab, generator=torch.Generator().manual_seed(3))
-    u = torch.rand(16, generator=torch.Generator().manual_seed(5))
-    many = u.repeat(-(-rows // 16))[:rows].cuda()
-    for settings in ({}, dict(top_p=torch.full((16,), 0.9))):
-        want, probs, bound = F.sample(x.expand(16, -1), u, **settings)
+    u = torch.rand(17, generator=torch.Generator().manual_seed(5))
+    many = u.repeat(-(-rows // 17))[:rows].cuda()
+    for settings in ({}, dict(top_p=torch.full((17,), 0.9))):
+        want, probs, bound = F.sample(x.expand(17, -1), u, **settings)
         got = ctx.sample(x.cuda().expand(rows, -1), many, **{k: v[:1].expand(rows).contiguous().cuda() for k, v in settings.items()})
-        assert torch.equal(got[0].cpu(), want.repeat(-(-rows // 16))[:rows])
-        assert bool(((got[1][-16:].cpu().double() - probs.roll(rows % 16 * -1)).abs() <= bound.roll(rows % 16 * -1)).all())
+        assert torch.equal(got[0].cpu(), want.repeat(-(-rows // 17))[:rows])
+        assert bool(((got[1][-17:].cpu().double() - probs.roll(-(rows % 17))).abs() <= bound.roll(-(rows % 17))).all())
 
 
 def test_tables_whose_rows_overlap_are_refused(ctx):
