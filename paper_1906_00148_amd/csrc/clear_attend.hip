@@ -28,7 +28,7 @@ constexpr int FEW_WAVES = 4, TILE_WAVES = TILE_ROWS / 32;
 constexpr float LOG2E = 1.4426950408889634f;
 
 // What a kernel walks: a call's requests; or in a call with shared prefixes these, each as a request of all tokens that have it, or what
-// the requests have behind them, or both as one, where a request has so many rows that sharing saves nothing.
+// the requests have behind them, or both as one, where sharing saves nothing: a request has many rows, or all places are few.
 enum Walk { REQUESTS, PREFIXES, BEHIND, WHOLE };
 // The first and the last of them write results, or pieces where a tile is cut; the others, which are joined, pieces only, all of them.
 constexpr bool joined_with_another(Walk walk) { return walk == PREFIXES || walk == BEHIND; }
@@ -348,6 +348,9 @@ __device__ __forceinline__ void attend_few(const she_attend_pages_args &a, uint3
             from = max(from, low_min & ~31);
             count = max(end - from, 0);
         }
+    } else if constexpr (WALK == WHOLE) {
+        high_min = reach_of<WALK>(a, owners, group, sp, sp.row).high;
+        low_max = reach_of<WALK>(a, owners, group, sp, sp.row + sp.rows - 1).low;
     } else {
         high_min = sp.first + sp.row / (int)group;
         low_max = a.window ? (int)max((int64_t)sp.first + (sp.row + sp.rows - 1) / (int)group - (int64_t)a.window + 1, (int64_t)0) : 0;
@@ -963,12 +966,8 @@ hipError_t walk(const she_attend_pages_args &a, const AttendShape &s, const Piec
     const uint32_t group = a.q_heads / a.kv_heads, slots = (uint32_t)s.slots;
     return by_head(a.head, [&](auto size) {
         constexpr int DP = decltype(size)::value;
-        if constexpr (WALK == REQUESTS)
-            if (s.few) {
-                k_attend_few<T, DP, WALK><<<dim3(slots, a.kv_heads, s.splits), 64 * FEW_WAVES, 0, st>>>(a, group, pieces, owners, d_bad);
-                return;
-            }
-        k_attend_tile<T, DP, WALK><<<dim3(slots * a.kv_heads, 1, s.splits), 64 * TILE_WAVES, 0, st>>>(a, group, pieces, owners, zeros_of(d_bad), d_bad);
+        if (s.few) k_attend_few<T, DP, WALK><<<dim3(slots, a.kv_heads, s.splits), 64 * FEW_WAVES, 0, st>>>(a, group, pieces, owners, d_bad);
+        else k_attend_tile<T, DP, WALK><<<dim3(slots * a.kv_heads, 1, s.splits), 64 * TILE_WAVES, 0, st>>>(a, group, pieces, owners, zeros_of(d_bad), d_bad);
     });
 }
 

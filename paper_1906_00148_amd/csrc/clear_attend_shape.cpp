@@ -114,6 +114,20 @@ SharedShape shared_shape(const she_attend_shared_args &a, uint32_t cus)
     const she_attend_pages_args call = shared_behind(a);
     s.behind = attend_shape(call, cus);
     if (!a.prefixes) return s;
+    // Few places, which workgroups that run at once walk in one launch: joining a prefix's pieces with the requests' own takes a second one.
+    // (Both, one launch; us on the device; single tokens with 40 places behind a prefix of 60, 330 and 450 places.)
+    //    2 requests, 8 / 2 heads of 64     9.9, 6.4   10.9, 9.5   11.3, 10.7       40 requests    10.5, 6.7   11.6, 9.6   11.7, 11.0
+    //    2 requests, 32 / 8 of 128        11.7, 7.6   13.7, 11.7  13.7, 13.4       40 requests    13.7, 9.0   16.5, 15.0  16.3, 17.2
+    //    2 requests, 8 / 8 of 256         14.3, 10.4  18.6, 18.3  18.5, 20.9       40 requests    23.7, 19.9  24.6, 34.7  24.6, 41.9
+    const uint64_t few_slots = a.requests == 1 ? ceil_div(rows, FEW_ROWS) : rows / FEW_ROWS + a.requests, few_groups = few_slots * a.kv_heads;
+    const uint64_t few_places = few_groups <= cus ? (a.head <= 128 ? 512 : 384) : few_groups <= 2 * cus && a.head <= 128 ? 384 : 0;
+    if (s.behind.few && places + own <= few_places) {
+        s.whole = true;
+        s.behind.slots = few_slots;
+        s.behind.splits = 1;
+        s.behind.chunk = 512;
+        return s;
+    }
     // rows of a prefix: the host knows their average
     const uint64_t each = ceil_div(rows, a.prefixes);
     s.prefix.few = s.behind.few && (each <= FEW_ROWS || each * places <= 1u << 18);

@@ -10,12 +10,12 @@ from test_gpu_clear_shared import compare, ctx, inputs  # noqa: F401
 pytestmark = pytest.mark.gpu
 BF16, F16 = torch.bfloat16, torch.float16
 
-# way: prefix walk, own walk, whether the pieces of the own walk (or of the one walk) are several
+# way: prefix walk (or both as one), own walk, whether the pieces of the own walk (or of the one walk) are several
 # name -> (way, heads, page, groups, requests before and after them)
 CALLS = {
-    "few_64": (("few", "few", False), (8, 2, 64), 16, [(300, [(1, n) for n in range(1, 20)]), (0, [(2, 2)])], [(1, 7)], [(3, 5)]),
-    "few_128": (("few", "few", False), (4, 4, 128), 1, [(333, [(1, n) for n in range(1, 20)])], [], [(1, 9)]),
-    "few_256": (("few", "few", False), (6, 2, 256), 24, [(300, [(1, n) for n in range(1, 20)])], [(4, 4)], []),
+    "few_64": (("few", "few", False), (8, 2, 64), 16, [(600, [(1, n) for n in range(1, 20)]), (0, [(2, 2)])], [(1, 7)], [(3, 5)]),
+    "few_128": (("few", "few", False), (4, 4, 128), 1, [(533, [(1, n) for n in range(1, 20)])], [], [(1, 9)]),
+    "few_256": (("few", "few", False), (6, 2, 256), 24, [(400, [(1, n) for n in range(1, 20)])], [(4, 4)], []),
     "few_cut_64": (("few", "few", True), (2, 2, 64), 16, [(600, [(1, 900), (2, 1500), (1, 3)])], [], []),
     "few_cut_128": (("few", "few", True), (4, 1, 96), 16, [(600, [(1, 900), (2, 1500), (1, 3)]), (50, [(1, 600)])], [(1, 800)], []),
     "few_cut_256": (("few", "few", True), (3, 1, 192), 16, [(600, [(1, 900), (2, 1500), (1, 3)])], [], [(1, 1)]),
@@ -30,6 +30,10 @@ CALLS = {
     "tile_tile_128": (("tile", "tile", False), (8, 1, 96), 64, [(2000, [(90, 400), (1, 300), (70, 70), (60, 390), (0, 8), (20, 300)]), (100, [(20, 40)])], [], []),
     "tile_tile_cut_64": (("tile", "tile", True), (8, 1, 64), 16, [(1200, [(40, 1500), (30, 900), (35, 40), (1, 1200), (50, 1300)])], [], [(5, 1200)]),
     "tile_tile_cut_128": (("tile", "tile", True), (8, 1, 128), 16, [(1200, [(40, 1500), (30, 900), (35, 40), (1, 1200)])], [(20, 700)], []),
+    "whole_few_64": (("whole", "few", False), (8, 2, 64), 16, [(300, [(1, n) for n in range(1, 20)]), (0, [(2, 2)]), (77, [(5, 9), (1, 100)])], [(1, 7)], [(3, 5)]),
+    "whole_few_128": (("whole", "few", False), (4, 4, 128), 1, [(333, [(1, n) for n in range(1, 20)]), (40, [(7, 7)])], [(6, 50)], [(1, 9)]),
+    "whole_few_80": (("whole", "few", False), (12, 2, 80), 24, [(200, [(1, 130), (9, 99)])], [], []),
+    "whole_few_256": (("whole", "few", False), (6, 2, 256), 24, [(250, [(1, n) for n in range(1, 20)]), (9, [(6, 12)])], [(4, 4)], []),
     "whole_64": (("whole", "tile", False), (16, 1, 64), 16, [(200, [(150, 160), (100, 101), (9, 150), (120, 130)]), (0, [(60, 90)])], [(50, 90)], [(3, 5)]),
     "whole_128": (("whole", "tile", False), (16, 1, 128), 24, [(200, [(150, 160), (100, 101), (9, 150), (120, 130)]), (77, [(60, 90)])], [], [(50, 60)]),
     "whole_cut_256": (("whole", "tile", True), (12, 2, 256), 16, [(900, [(60, 400), (1, 200), (35, 35), (50, 390)]), (333, [(20, 60)])], [(9, 200)], [(3, 50)]),

@@ -32,7 +32,7 @@ def test_the_calls_of_the_walks_tests_go_their_ways(shapes):
     ways = {(*got[name][:2], padded[name]) for name in calls}
     # heads of more than 128 have no tiles of many rows behind a prefix's: they go as one walk
     assert ways >= {(p, b, d) for p, b in (("few", "few"), ("tile", "few")) for d in (64, 128, 256)} | {("tile", "tile", 64), ("tile", "tile", 128)} | \
-        {("whole", "tile", d) for d in (64, 128, 256)}
+        {("whole", b, d) for b in ("few", "tile") for d in (64, 128, 256)}
 
 
 def test_scratch_follows_the_rows(shapes):
