@@ -370,8 +370,8 @@ class Calls:
         given = out is not None
         if not given:
             numbers = torch.empty(2 * R + tokens + 2, dtype=i32, device=table.device)
-            out = (*numbers.split((R + 1, R, tokens, 1)), torch.empty(tokens, dtype=torch.int64, device=table.device))
-            out = out[0], out[1], out[2], out[4], out[3]
+            starts, lengths, positions, now = numbers.split_with_sizes((R + 1, R, tokens, 1))
+            out = starts, lengths, positions, torch.empty(tokens, dtype=torch.int64, device=table.device), now
         starts, lengths, positions, slots, now = out
         self._call(self._L.she_plan_pages, _PLAN_PAGES.pack(
             R, tokens, pages, page_size, width, F, *inputs, table_at, ts[0], _line(starts, "starts", i32, R + 1, dev),

@@ -73,10 +73,24 @@ template <class T> __device__ __forceinline__ void load_logits(const Row<T> &row
     }
 }
 
-// 2^(j/256), to which a whole exponent is added in place.
-__device__ inline void make_table(double *table)
+// 2^(j/256), to which a whole exponent is added in place: the series of exp(j ln 2 / 256), which is worked out by the compiler, since exp2 takes
+// as long as a few tiles (k_sample_tiles for 64 rows of 100000 13.6 us, 14.5 with it).
+struct Powers {
+    double of[256];
+    constexpr Powers() : of()
+    {
+        for (int j = 0; j < 256; j++) {
+            const long double x = j * 0.693147180559945309417232121458L / 256;
+            long double sum = 1, term = 1;
+            for (int n = 1; n < 24; n++) sum += term *= x / n;
+            of[j] = (double)sum;
+        }
+    }
+};
+__device__ constexpr Powers POWERS{};
+__device__ __forceinline__ void make_table(double *table)
 {
-    for (int j = threadIdx.x; j < 256; j += blockDim.x) table[j] = exp2(j / 256.0);
+    for (int j = threadIdx.x; j < 256; j += blockDim.x) table[j] = POWERS.of[j];
 }
 
 // What the logits of a row weigh.
@@ -980,44 +994,38 @@ template <class T> __global__ __launch_bounds__(PART_THREADS) void k_sample_tile
         }
     }
 }
-template <class T> __global__ __launch_bounds__(THREADS) void k_sample_drawn(she_sample_args a, Tiles w)
+// A wavefront a row, which needs no barriers.  (Both launches with a workgroup of sixteen for each row, and so, in us on the device: 2000 rows of 20000
+// 99 and 58, one of 32001 12.5 and 9.3, 64 of 100000 21.7 and 21.5; two of 1000000, whose 1954 tiles are much for one, 14.9 and 23.5.)
+template <class T> __global__ __launch_bounds__(64) void k_sample_drawn(she_sample_args a, Tiles w)
 {
-    __shared__ Shared s;
-    constexpr int EACH = BINS / THREADS;
-    const uint32_t r = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ double table[256];
+    __shared__ uint64_t in_row[BINS];                              // what the tiles count
+    const uint32_t r = blockIdx.x, lane = threadIdx.x;
     const Settings set(a, r);
-    uint64_t sums[EACH];
-    float tops[EACH], top = -__builtin_inff();
+    const uint64_t *sums = w.sums + (size_t)r * w.count;
+    const float *tops = w.tops + (size_t)r * w.count;
+    make_table(table);
+    float top = -__builtin_inff();
     uint32_t where = 0;
-#pragma unroll
-    for (int e = 0; e < EACH; e++) {
-        const uint32_t t = threadIdx.x * EACH + e;
-        sums[e] = t < w.count ? w.sums[(size_t)r * w.count + t] : 0;
-        tops[e] = t < w.count ? w.tops[(size_t)r * w.count + t] : -__builtin_inff();
-        if (tops[e] > top) {
-            top = tops[e];
-            where = t;
-        }
+#pragma unroll 4
+    for (uint32_t t = lane; t < w.count; t += 64) {
+        const float its = tops[t];
+        where = its > top ? t : where;
+        top = fmaxf(top, its);
     }
-    make_table(s.table);
-    const auto join = [&](float other, uint32_t place) {
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) {
+        const float other = __shfl_xor(top, m);
+        const uint32_t place = __shfl_xor(where, m);
         if (other > top || (other == top && place < where)) {
             top = other;
             where = place;
         }
-    };
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) join(__shfl_xor(top, m), __shfl_xor(where, m));
-    if (lane == 0) {
-        s.tops[wave] = top;
-        s.where[wave] = where;
     }
     __syncthreads();
-    for (int k = 0; k < WAVES; k++) join(s.tops[k], s.where[k]);
     const Row<T> row = row_of<T>(a, r);
     const bool none = top == -__builtin_inff();
     if (none || !(set.temperature > 0)) {
-        if (threadIdx.x >= 64) return;
         float v[8];
         load_logits(row, where * TILE + lane * 8, v);
         uint32_t here = 8;
@@ -1027,25 +1035,47 @@ template <class T> __global__ __launch_bounds__(THREADS) void k_sample_drawn(she
         if (none ? lane == 0 : (int)lane == __builtin_ctzll(those)) answer(a, r, none ? -1 : (int32_t)(where * TILE + lane * 8 + here), none ? 0.0f : 1.0f);
         return;
     }
-    const Weights weights(top, set.temperature, s.table);
+    const Weights weights(top, set.temperature, table);
     // whole numbers below 2^53 times a factor, which every running sum is rounded with alike
     const auto factor = [&](float its) { return exp2(weights.below(its) / 256); };
     const auto counted = [](uint64_t sum, double f) { return (uint64_t)((double)sum * f + 0.5); };
     uint64_t all = 0;
-#pragma unroll
-    for (int e = 0; e < EACH; e++) all += s.bins[threadIdx.x * EACH + e] = sums[e] ? counted(sums[e], factor(tops[e])) : 0;
-    all = block_sum(all, s);
+#pragma unroll 4
+    for (uint32_t t = lane; t < w.count; t += 64) {
+        const uint64_t sum = sums[t];
+        const double f = factor(tops[t]);
+        all += in_row[t] = counted(sum, f);
+    }
+    all = wave_sum(all);
     const uint64_t drawn = share_of(all, set.uniform, false);
-    const Crossing c = find_crossing(s.bins, drawn + 1, s.sums, &s.found);
-    if (threadIdx.x >= 64) return;
+    // the tile that it falls into, and what is before that
+    Crossing c{0, 0};
+    for (uint32_t t0 = 0; t0 < w.count; t0 += 64) {
+        const uint64_t mine = t0 + lane < w.count ? in_row[t0 + lane] : 0;
+        uint64_t run = mine;
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) {
+            const uint64_t other = __shfl_up(run, m);
+            if ((int)lane >= m) run += other;
+        }
+        const uint64_t those = __ballot(c.before + run > drawn);
+        if (those) {
+            const int it = __builtin_ctzll(those);
+            c.bin = (int)t0 + it;
+            c.before += __shfl(run - mine, it);
+            break;
+        }
+        c.before += __shfl(run, 63);
+    }
     float v[8];
     const uint32_t at = c.bin * TILE + lane * 8;
     load_logits(row, at, v);
-    const float its = w.tops[(size_t)r * w.count + c.bin];
-    const Weights mine(its, set.temperature, s.table);
+    const float its = tops[c.bin];
+    const Weights mine(its, set.temperature, table);
     const double f = factor(its);
-    uint64_t run = 0;
-    for (int i = 0; i < 8; i++) run += mine.weight(mine.below(v[i]));
+    uint64_t weight[8], run = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++) run += weight[i] = mine.weight(mine.below(v[i]));
     const uint64_t own = run;
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) {
@@ -1053,9 +1083,10 @@ template <class T> __global__ __launch_bounds__(THREADS) void k_sample_drawn(she
         if ((int)lane >= m) run += other;
     }
     run -= own;
+#pragma unroll
     for (int i = 0; i < 8; i++) {
         const uint64_t before = c.before + counted(run, f);
-        run += mine.weight(mine.below(v[i]));
+        run += weight[i];
         if (before <= drawn && c.before + counted(run, f) > drawn) answer(a, r, (int32_t)(at + i), prob_of(weights.below(v[i]), all));
     }
 }
@@ -1075,7 +1106,7 @@ template <class T> hipError_t sample_rows(const she_sample_args &a, const Sample
         k_sample_tiles<T><<<a.rows * s.parts, PART_THREADS, 0, st>>>(a, w);
         const hipError_t rc = hipGetLastError();
         if (rc != hipSuccess) return rc;
-        k_sample_drawn<T><<<a.rows, THREADS, 0, st>>>(a, w);
+        k_sample_drawn<T><<<a.rows, 64, 0, st>>>(a, w);
         return hipGetLastError();
     }
     Parts w{};
