@@ -7,10 +7,15 @@
 // largest has no weight: it is taken as there, where the weight rounds to 0.
 //
 // The tokens that filters keep are the first of an order, larger logits first and of equals the lower index: all above a logit, and of
-// those equal to it the ones up to an index.  Mostly they are few.  Then those that may be among them are picked out, up to a thread of a
-// workgroup each, by a histogram of y in 32nds of an octave: of weights for top_p, which needs all of them anyway; for top_k of the largest of
-// every eight neighbours, since k of these that reach a logit are k logits that do.  Where they are many, the logit is found by
-// histograms over the row, from the 32nds of an octave on to the bits of the bin's logits until a bin is one value.
+// those equal to it the ones up to an index.  Which bin of 1/32 octave has that logit is seen from a histogram: of weights for top_p, which needs all
+// of them anyway; for top_k of the largest of every eight neighbours, since k of these that reach a logit are k logits that do.  Where the tokens up to
+// that bin are few, up to a thread of a workgroup each, they are picked out and sorted: by the order for the filters, by index for the draw.
+// Where they are many, only the bin's own are sorted, and the weights of all others are summed up by tile in the same pass over the row.  A bin that
+// is too full for that (equal or nearly equal logits) is divided by the bits of its logits until it is one value.
+//
+// Bound by latency where rows are few (one of 32001, bf16: 3.5, 5.0 and 10.5 us for the three launches), by memory and 64-bit arithmetic in turns where
+// they are many: 256 rows of 131072 numbers of 32 bits take 25 us for the largest (5.4 TB/s), 24 for the weights, and 61 for the answers of rows
+// with all kinds of filters; all three take 47 us with top_k = 50 for every row, 128 with top_p = 0.9 (19000 tokens kept), and the two without filters 47.
 #include <algorithm>
 
 #include "clear_device.h"
