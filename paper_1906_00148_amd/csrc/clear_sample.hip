@@ -584,7 +584,10 @@ template <class S> __device__ __forceinline__ bool head_sums(const S &source, co
     const Crossing c = find_crossing(s.bins, target, s.sums, &s.found);
     const int bin = c.bin;                                         // there is one: the target is at most all of it
     target -= c.before;
-    if (threadIdx.x == 0) s.count = 0;
+    if (threadIdx.x == 0) {
+        s.count = 0;
+        s.cut = all_kept();                                        // where min_p leaves none of the bin, or none behind the border
+    }
     clear_bins(s);
     // logits below `least` are behind the bin, and those above `most` before it
     const float least = least_at(w, -8 * bin - 8), most = most_at(w, bin), floor = set.least_logit(w);

@@ -67,6 +67,25 @@ def test_filters(ctx, dtype, vocab, filters):
     compare(ctx, x, torch.rand(rows, generator=g), **a)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32, SUMS])
+@pytest.mark.parametrize("vocab", [5000, 40000])
+@pytest.mark.parametrize("shift", [-60.0, 0.0, 60.0])
+def test_a_top_p_of_thousands_and_a_min_p_of_few(ctx, dtype, vocab, shift):
+    """Flat rows: the border of either filter lies far behind, before or beside the other's."""
+    rows = 20
+    g = torch.Generator().manual_seed(vocab)
+    x, step = torch.randn(rows, vocab, generator=g) * 1.5 + shift, {}
+    if dtype is SUMS:
+        x, step = (x * 500).round().to(SUMS), dict(step=torch.full((vocab,), 1 / 500))
+    else:
+        x = x.to(dtype)
+    p, m = each(rows, [0.9, 0.999, 0.5, 0.99]), each(rows, [0.5, 1e-3, 0.05, 0.9, 1e-5])
+    u = torch.rand(rows, generator=g)
+    u[::4] = 1.0
+    compare(ctx, x, u, top_p=p, min_p=m, **step)
+    compare(ctx, x, u, top_p=p, min_p=m, top_k=each(rows, [0, 5000, 300], torch.int32), **step)
+
+
 @pytest.mark.parametrize("rows", [1, 2, 3, 5, 17, 64, 255, 300])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_numbers_of_rows(ctx, rows, dtype):
