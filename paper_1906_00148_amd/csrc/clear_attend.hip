@@ -558,16 +558,16 @@ template <class T, int DP> struct alignas(16) TileShared {
     uint64_t missing[2][TILE_BLOCK / 64];                                            // places that their page id or the table's end keeps out
     int lows[TILE_WAVES];
 };
+// Its arrays one by one: what is on its way into one of them is not waited for where another is read.
 template <class T, int DP, Walk WALK>
 __device__ __forceinline__ void attend_tile(const she_attend_pages_args &a, uint32_t group, const Pieces &pieces, const Owners &owners, const void *zeros, uint32_t *d_bad,
-                                            TileShared<T, DP> &shared, uint32_t slot, int kv_head, int z)
+                                            T *__restrict__ even_keys, T *__restrict__ even_values, T *__restrict__ odd_keys, T *__restrict__ odd_values,
+                                            int64_t (*__restrict__ rows)[TILE_BLOCK], uint64_t (*__restrict__ missing)[TILE_BLOCK / 64], int *__restrict__ lows,
+                                            uint32_t slot, int kv_head, int z)
 {
     constexpr int UNITS = DP / 8, KS = DP / 16, DB = DP / 32, BLOCK = TILE_BLOCK;
     constexpr int EACH = STEP * UNITS / (64 * TILE_WAVES);                           // units of either tile that a thread brings
     constexpr float LEAD = std::is_same<T, __bf16>::value ? 8.0f : 0.0f;
-    T *even_keys = shared.even_keys, *even_values = shared.even_values, *odd_keys = shared.odd_keys, *odd_values = shared.odd_values;
-    auto &rows = shared.rows;
-    auto &missing = shared.missing;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
     const int D = (int)a.head;
     const Piece piece = tile_of<WALK>(a, owners, group, TILE_ROWS, slot);
@@ -595,7 +595,6 @@ __device__ __forceinline__ void attend_tile(const she_attend_pages_args &a, uint
         high = high_min = high_max = mine.high;
         low = low_min = low_max = mine.low;
         if (a.window) {                                           // requests in any order: the earliest and the latest place of the rows
-            auto &lows = shared.lows;
 #pragma unroll
             for (int m = 1; m < 32; m *= 2) {
                 low_min = min(low_min, __shfl_xor(low_min, m));
@@ -796,8 +795,10 @@ __device__ __forceinline__ void attend_tile(const she_attend_pages_args &a, uint
 template <class T, int DP, Walk WALK>
 __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_tile(she_attend_pages_args a, uint32_t group, Pieces pieces, Owners owners, const void *zeros, uint32_t *d_bad)
 {
-    __shared__ TileShared<T, DP> shared;
-    attend_tile<T, DP, WALK>(a, group, pieces, owners, zeros, d_bad, shared, gridDim.x / a.kv_heads - 1 - blockIdx.x / a.kv_heads, (int)(blockIdx.x % a.kv_heads), (int)blockIdx.z);
+    __shared__ alignas(16) T even_keys[STEP * DP], even_values[STEP * DP], odd_keys[STEP * DP], odd_values[STEP * DP];
+    __shared__ int64_t rows[2][TILE_BLOCK];
+    __shared__ uint64_t missing[2][TILE_BLOCK / 64];
+    attend_tile<T, DP, WALK>(a, group, pieces, owners, zeros, d_bad, even_keys, even_values, odd_keys, odd_values, rows, missing, nullptr, gridDim.x / a.kv_heads - 1 - blockIdx.x / a.kv_heads, (int)(blockIdx.x % a.kv_heads), (int)blockIdx.z);
 }
 
 // Rows that were cut, `each` of a tile a workgroup.  Up to JOIN_AHEAD pieces are a wavefront's work, and a workgroup of the tile kernel's
@@ -886,7 +887,9 @@ __device__ __forceinline__ void attend_block(const she_attend_pages_args &a, uin
     const uint32_t i = block / a.kv_heads, kv_head = block - i * a.kv_heads, z = i / slots, slot = i - z * slots;
     auto &its = *reinterpret_cast<SharedOf<T, DP, FEW> *>(shared);
     if constexpr (FEW) attend_few<T, DP, WALK>(a, group, pieces, owners, d_bad, its, slot, (int)kv_head, (int)z);
-    else attend_tile<T, DP, WALK>(a, group, pieces, owners, zeros, d_bad, its, slot, (int)kv_head, (int)z);
+    else
+        attend_tile<T, DP, WALK>(a, group, pieces, owners, zeros, d_bad, its.even_keys, its.even_values, its.odd_keys, its.odd_values, its.rows, its.missing, its.lows, slot,
+                                 (int)kv_head, (int)z);
 }
 template <class T, int DP, bool PREFIX_FEW, bool FEW>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_shared(she_attend_pages_args a, uint32_t group, Pieces prefix, Pieces pieces, Owners owners, const void *zeros,
