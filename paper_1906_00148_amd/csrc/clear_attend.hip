@@ -875,10 +875,10 @@ __global__ __launch_bounds__(256) void k_attend_join(she_attend_pages_args a, ui
 }
 
 // A call with shared prefixes, whose two walks are one launch: while the prefixes' workgroups, of many rows, wait for the matrix units, those
-// of the requests' own places wait for memory (64 tokens behind 32768 places with up to 500 of their own, 32 / 8 heads of 128, bf16: 67 us, 61 without
-// their own places; two launches 95 and not 87 for the whole call at that time).  Such a call is bound by what a wavefront does one after the
+// of the requests' own places wait for memory (64 tokens behind 32768 places with up to 500 of their own, 32 / 8 heads of 128, bf16: 67 to 76 us,
+// 6 less without their own places; two launches 95 and not 87 for the whole call at that time).  Such a call is bound by what a wavefront does one after the
 // other: a step of 64 places takes 1.7 us where a compute unit has one tile's workgroup, and two have theirs in 2.0.  97 requests of up to 4 tokens
-// behind five prefixes (16 heads of 64, f16) take 80 us, 3.4 TB/s.
+// behind five prefixes (16 heads of 64, f16) take 78 us, 3.5 TB/s.
 template <class T, int DP, bool FEW> using SharedOf = typename std::conditional<FEW, FewShared<DP>, TileShared<T, DP>>::type;
 template <class T, int DP, bool FEW, Walk WALK>
 __device__ __forceinline__ void attend_block(const she_attend_pages_args &a, uint32_t group, const Pieces &pieces, const Owners &owners, const void *zeros, uint32_t *d_bad, char *shared,
@@ -910,7 +910,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_shared(she_at
 }
 
 // Rows of such a call, in the order of the pieces: neighbours have different key heads, so that where there are eight a row's pieces come from
-// the XCD that wrote them.  Bound by memory where rows are many: 115000 rows of 128 in two pieces 48 us, 118 MB; 2048 rows in 17 pieces 8.6 us.  D/4 lanes have a piece's elements, and 4 * `lanes` / D pieces are read side by side by as many threads as
+// the XCD that wrote them.  Bound by memory where rows are many: 115000 rows of 128 in two pieces 48 us, 118 MB; 2048 rows in 17 pieces
+// 8.6 us.  D/4 lanes have a piece's elements, and 4 * `lanes` / D pieces are read side by side by as many threads as
 // have the row: a workgroup for many pieces, a wavefront for few, which then needs no barrier.
 template <class T, int ROW> __global__ __launch_bounds__(256) void k_shared_join(she_attend_pages_args a, uint32_t group, Pieces pieces)
 {

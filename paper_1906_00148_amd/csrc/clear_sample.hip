@@ -656,6 +656,27 @@ template <class T, class S> __device__ __forceinline__ void pass_by_pass(const s
     draw_by_tiles(a, r, source.row, w, set, kept, s);
 }
 
+// The draw from `count` tokens in s.list; `whole`: the row's weight, which top_p is of where there is no top_k.
+__device__ __forceinline__ void draw_by_list(const she_sample_args &a, uint32_t r, const Weights &w, const Settings &set, uint64_t whole, uint32_t count, Shared &s)
+{
+    const uint32_t i = threadIdx.x;
+    const auto weight_of = [&](float logit) { return w.weight(w.below_plain(logit)); };
+    const uint64_t token = sorted(i < count ? s.list[i] : 0, count, s);
+    bool kept = i < count && i < set.top_k;
+    uint64_t weight = kept ? weight_of(logit_of(token)) : 0, all;
+    if (set.top_p < 1.0f) {
+        const uint64_t before = running_sum(weight, all, s) - weight;
+        kept &= before < set.head(set.top_k < a.vocab ? all : whole);
+    }
+    // the first threads have what is kept: now by its index, the lowest first
+    const uint32_t left = (uint32_t)__syncthreads_count(kept);
+    const uint64_t turned = sorted(kept && weight >= set.least ? token << 32 | token >> 32 : 0, left, s);
+    const float logit = number_of((uint32_t)turned);
+    weight = turned ? weight_of(logit) : 0;
+    const uint64_t run = running_sum(weight, all, s), drawn = share_of(all, set.uniform, false);
+    if (run > drawn && run - weight <= drawn) answer(a, r, (int32_t)~(uint32_t)(turned >> 32), prob_of(w.below_plain(logit), all));
+}
+
 // Rows of few logits, which a workgroup holds.
 template <class T> __global__ __launch_bounds__(THREADS) void k_sample_rows(she_sample_args a)
 {
@@ -698,7 +719,23 @@ template <class T> __global__ __launch_bounds__(THREADS) void k_sample_rows(she_
         if (threadIdx.x == 0) answer(a, r, none ? -1 : (int32_t)where, none ? 0.0f : 1.0f);
         return;
     }
-    pass_by_pass<T>(a, r, source, Weights(top, set.temperature, s.table), set, false, 0, DEAD_BIN, s);
+    const Weights w(top, set.temperature, s.table);
+    if (a.vocab <= THREADS && (set.top_k < a.vocab || set.top_p < 1.0f)) {
+        // all of them are few (148 rows of 214 with all filters 24.9 us by passes, 18.1 so)
+        float l[8];
+        w.plain(source.v, l);
+        uint64_t sum = 0;
+        for (int i = 0; i < 8; i++) {
+            const uint32_t at = threadIdx.x * 8 + i;
+            if (at >= a.vocab) break;
+            s.list[at] = l[i] > -__builtin_inff() ? token_of(l[i], at) : 0;
+            sum += w.weight(w.below_plain(l[i]));
+        }
+        sum = block_sum(sum, s);
+        draw_by_list(a, r, w, set, sum, a.vocab, s);
+        return;
+    }
+    pass_by_pass<T>(a, r, source, w, set, false, 0, DEAD_BIN, s);
 }
 
 // Larger rows, in three launches.  First a row's parts have the largest logit of every eight neighbours, and their own.
@@ -869,27 +906,6 @@ template <class T> __device__ __forceinline__ uint32_t pick_few(const FromMemory
     __syncthreads();
     // the eights that are left out, if any, may have no token: rounding is on the safe side there
     return eights <= THREADS ? s.count : THREADS + 1;
-}
-
-// The draw from `count` tokens in s.list; `whole`: the row's weight, which top_p is of where there is no top_k.
-__device__ __forceinline__ void draw_by_list(const she_sample_args &a, uint32_t r, const Weights &w, const Settings &set, uint64_t whole, uint32_t count, Shared &s)
-{
-    const uint32_t i = threadIdx.x;
-    const auto weight_of = [&](float logit) { return w.weight(w.below_plain(logit)); };
-    const uint64_t token = sorted(i < count ? s.list[i] : 0, count, s);
-    bool kept = i < count && i < set.top_k;
-    uint64_t weight = kept ? weight_of(logit_of(token)) : 0, all;
-    if (set.top_p < 1.0f) {
-        const uint64_t before = running_sum(weight, all, s) - weight;
-        kept &= before < set.head(set.top_k < a.vocab ? all : whole);
-    }
-    // the first threads have what is kept: now by its index, the lowest first
-    const uint32_t left = (uint32_t)__syncthreads_count(kept);
-    const uint64_t turned = sorted(kept && weight >= set.least ? token << 32 | token >> 32 : 0, left, s);
-    const float logit = number_of((uint32_t)turned);
-    weight = turned ? weight_of(logit) : 0;
-    const uint64_t run = running_sum(weight, all, s), drawn = share_of(all, set.uniform, false);
-    if (run > drawn && run - weight <= drawn) answer(a, r, (int32_t)~(uint32_t)(turned >> 32), prob_of(w.below_plain(logit), all));
 }
 
 // And the rows' answers.
