@@ -1060,8 +1060,12 @@ template <class T> __global__ __launch_bounds__(64) void k_sample_drawn(she_samp
         return;
     }
     const Weights weights(top, set.temperature, table);
-    // whole numbers below 2^53 times a factor, which every running sum is rounded with alike
-    const auto factor = [&](float its) { return exp2(weights.below(its) / 256); };
+    // whole numbers below 2^53 times a factor, which every running sum is rounded with alike.  A tile whose largest has no weight counts nothing, however
+    // many logits it has that are equal to that.
+    const auto factor = [&](float its) {
+        const double y = weights.below(its);
+        return y > DEAD ? exp2(y / 256) : 0.0;
+    };
     const auto counted = [](uint64_t sum, double f) { return (uint64_t)((double)sum * f + 0.5); };
     uint64_t all = 0;
 #pragma unroll 4
