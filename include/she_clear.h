@@ -240,7 +240,10 @@ int she_attend_shared(she_ctx *ctx, const she_attend_shared_args *args);
  * top_k < 1, top_p >= 1 or NaN, and min_p <= 0 or NaN keep all, and the likeliest token is kept in any case.  A temperature of 0 (or
  * below, or NaN) takes the largest logit of lowest index with probability 1, and so does +infinity, shared equally by all that have
  * it where the temperature is above 0.  A row without a logit above -infinity gets token -1, probability 0.  uniform is taken as at
- * least 0 (NaN too) and at most 1 - 2^-24.  Weights are held to 2^-44 of the largest and their sums are exact. */
+ * least 0 (NaN too) and at most 1 - 2^-24.  Weights are held to 2^-44 of the largest, less than which is none, and their sums are exact;
+ * but where temperature is all that a call sets and vocab is more than 8192, every 512 tokens' running weight is held to 2^-44 of the
+ * row's largest, and each of theirs to 2^-44 of the largest among them: tokens of less than 2^-44.5 have some if others of the 512
+ * have more. */
 typedef struct {
     int32_t type;                        /* SHE_BF16, SHE_F16, SHE_F32 or SHE_I32 */
     uint32_t rows, vocab;                /* vocab at most 2^20 */

@@ -5,6 +5,9 @@
 // y = (logit - max) log2(e) / T in units of 1/256, the nearest whole k and the rest r, it is 2^(k/256) from a table and a power of two,
 // times 2^(r/256) by its series up to the fourth power (the fifth is below 2^-54).  What lies more than 44.5 octaves below the
 // largest has no weight: it is taken as there, where the weight rounds to 0.
+// Calls without filters on larger rows hold to this by tiles of 512 logits instead: weights are those against the tile's largest, and the running
+// sums in a tile, scaled to the row's largest, are rounded to whole numbers (k_sample_tiles, k_sample_drawn).  Both roundings are of half a unit at
+// most, for each token in the one and each tile in the other, and a border may fall as far from where the other forms have it.
 //
 // The tokens that filters keep are the first of an order, larger logits first and of equals the lower index: all above a logit, and of
 // those equal to it the ones up to an index.  Which bin of 1/32 octave has that logit is seen from a histogram: of weights for top_p, which needs all
@@ -118,12 +121,14 @@ struct Weights {
         if (infinite)
             for (int i = 0; i < 8; i++) l[i] = v[i] == __builtin_inff() ? 0.0f : -__builtin_inff();
     }
-    // in units of 1/256 octave, from 0 down to DEAD, which is where NaN goes too
-    __device__ __forceinline__ double below(float v) const
+    // in units of 1/256 octave, from 0 down
+    __device__ __forceinline__ double distance(float v) const
     {
         if (infinite) v = v == __builtin_inff() ? 0.0f : -__builtin_inff();
-        return fmax(((double)v - (double)top) * unit, DEAD);
+        return ((double)v - (double)top) * unit;
     }
+    // down to DEAD, which is where NaN goes too
+    __device__ __forceinline__ double below(float v) const { return fmax(distance(v), DEAD); }
     __device__ __forceinline__ double below_plain(float v) const { return fmax(((double)v - (double)top) * unit, DEAD); }
     __device__ __forceinline__ static int nearest(double s) { return __double2loint(s + 6755399441055744.0); }      // 1.5 * 2^52: the low bits have it
     __device__ __forceinline__ static int bin(double s) { return -nearest(s) >> 3; }
@@ -1115,7 +1120,8 @@ template <class T> __global__ __launch_bounds__(64) void k_sample_drawn(she_samp
     for (int i = 0; i < 8; i++) {
         const uint64_t before = c.before + counted(run, f);
         run += weight[i];
-        if (before <= drawn && c.before + counted(run, f) > drawn) answer(a, r, (int32_t)(at + i), prob_of(weights.below(v[i]), all));
+        // a tile that begins above DEAD has tokens beyond it
+        if (before <= drawn && c.before + counted(run, f) > drawn) answer(a, r, (int32_t)(at + i), prob_of(weights.distance(v[i]), all));
     }
 }
 

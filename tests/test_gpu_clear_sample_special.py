@@ -1,5 +1,7 @@
 """The choice of the next token from rows of more than 8192 logits, which several workgroups share: masks that leave little or nothing, the types' lowest
 and largest values, infinities and NaN, and numbers at the ends of their range, against the definition in 64 bits (include/she_clear.h)."""
+import math
+
 import pytest
 import torch
 
@@ -84,3 +86,17 @@ def test_settings_at_their_ends(ctx, vocab):  # noqa: F811
     compare(ctx, x, u, top_p=torch.tensor([NAN, INF, -INF, -1.0, 1.0, 0.0, 1 - 2.0 ** -24, 2.0 ** -149]))
     compare(ctx, x, u, min_p=torch.tensor([NAN, INF, -INF, -1.0, 1.0, 0.0, 1 - 2.0 ** -24, 2.0 ** -149]))
     compare(ctx, x, u, top_k=torch.tensor([0, -1, -2 ** 31, 2 ** 31 - 1, vocab, vocab - 1, 1, 2], dtype=torch.int32))
+
+
+@pytest.mark.parametrize("u", [0.0, 2.0 ** -46, 2.0 ** -42, 2.0 ** -39])
+def test_the_probability_of_a_token_of_hardly_any_weight(ctx, u):  # noqa: F811
+    """Among tiles of logits 44 octaves below the largest, where sums of tokens have weight that each has not: the token that is drawn gets its own share."""
+    octaves = torch.full((9216,), -60.0)
+    octaves[9000] = 0
+    octaves[0:2048:2], octaves[1:2048:2] = -44.6, -45.5
+    octaves[[511, 1023, 1535, 2047]] = -44.4
+    x = (octaves * math.log(2))[None]
+    share = torch.softmax(x[0].double(), 0)
+    token, prob = (t.item() for t in ctx.sample(x.cuda(), torch.tensor([u]).cuda()))
+    # 2^-24 for the result, and the whole weight's error
+    assert token < 2048 and abs(prob / share[token].item() - 1) <= 2.0 ** -24 + 9216 * 2.0 ** -44
