@@ -20,6 +20,7 @@
 
 #include "clear_device.h"
 #include "clear_internal.h"
+#include "clear_reach.h"
 
 namespace she { namespace clear {
 namespace {
@@ -129,11 +130,11 @@ __device__ inline Span span_of(const she_attend_pages_args &a, const Owners &own
         }
         room += s.own;
     }
-    const int p0 = WALK == WHOLE ? max(s.first + row / (int)group, 0) : s.first + row / (int)group, p1 = s.first + (row + s.rows - 1) / (int)group;
-    int64_t low = a.window ? (int64_t)p0 - (int64_t)a.window + 1 : WALK == WHOLE ? -(int64_t)0x7FFFFFFF : 0, to = (int64_t)p1 + 1;
+    const int p0 = s.first + row / (int)group, p1 = s.first + (row + s.rows - 1) / (int)group;
+    int64_t low = a.window ? (int64_t)p0 - (int64_t)a.window + 1 : 0, to = (int64_t)p1 + 1;
     if constexpr (WALK == WHOLE) {
-        low = p1 < 0 ? 0 : low >= 0 ? s.own + low : min(low + s.missing + s.own, (int64_t)s.own);
-        to = p1 < 0 ? 0 : s.own + to;
+        low = p1 < 0 ? 0 : first_behind(max(p0, 0), a.window, s.own, s.missing);
+        to = p1 < 0 ? 0 : to + s.own;
     }
     s.low = (int)max(low, (int64_t)0);
     s.from = s.low & ~31;
@@ -184,15 +185,12 @@ template <Walk WALK> __device__ inline Reach reach_of(const she_attend_pages_arg
         w.low = (int)min(max(s.to + s.missing + place - (int64_t)a.window + 1, (int64_t)0), (int64_t)s.to);
     } else {
         const int place = s.first + row / (int)group;
-        w.high = place;
-        const int64_t low = (int64_t)place - (int64_t)a.window + 1;
         if constexpr (WALK == WHOLE) {
             if (place < 0) return Reach{0, -1};
-            w.high += s.own;
-            if (a.window) w.low = (int)max(low >= 0 ? s.own + low : min(low + s.missing + s.own, (int64_t)s.own), (int64_t)0);
-        } else {
-            if (a.window) w.low = (int)max(low, (int64_t)0);
+            return Reach{first_behind(place, a.window, s.own, s.missing), last_behind(place, s.own)};
         }
+        w.high = place;
+        if (a.window) w.low = (int)max((int64_t)place - (int64_t)a.window + 1, (int64_t)0);
     }
     return w;
 }
