@@ -23,10 +23,12 @@ FLAGS = [
 
 
 def build(verbose: bool = False, extra: list[str] | None = None, out: str | None = None) -> str:
-    """Compiles every source each time it is called, several at a time; returns the path of the shared library."""
+    """Compiles every source each time it is called, several at a time, and links them, all with the flags `extra` too; returns the path of
+    the shared library."""
     out = out or LIB_PATH
     stderr = None if verbose else subprocess.DEVNULL
-    flags = [f for f in FLAGS if f != "-shared"] + (extra or [])
+    link = FLAGS + (extra or [])
+    flags = [f for f in link if f != "-shared"]
 
     def run(cmd):
         if verbose:
@@ -37,7 +39,7 @@ def build(verbose: bool = False, extra: list[str] | None = None, out: str | None
         objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
         for done in [pool.submit(run, [HIPCC] + flags + ["-c", os.path.join(CSRC, s), "-o", o]) for s, o in zip(SOURCES, objects)]:
             done.result()
-        run([HIPCC] + FLAGS + objects + ["-o", out + ".tmp"])
+        run([HIPCC] + link + objects + ["-o", out + ".tmp"])
     os.replace(out + ".tmp", out)
     return out
 
