@@ -1,10 +1,11 @@
 """The clear side of split inference on torch tensors (argument marshalling only; include/she_clear.h has the definitions).
 
 `Calls` is the part of a Context that runs between a decryption and the next encryption: adapters beside a shared projection,
-norms and rotation of queries and keys, attention over a paged cache.  Tensors are on the context's GPU (refused elsewhere), in
-bfloat16 or float16 where nothing else is said, with a contiguous last axis; their other strides are free.  Gradients have calls of
-their own: backward through a result raises, and what a call writes into (out, pages) counts as changed in place.  Work is enqueued
-on the context's stream: when torch's current stream is another one, that work waits for it and it waits for the work.
+norms and rotation of queries and keys, places of new tokens in a paged cache, attention over it and behind shared prefixes, the
+choice of the next token.  Tensors are on the context's GPU (refused elsewhere), in bfloat16 or float16 where nothing else is said,
+with a contiguous last axis; their other strides are free.  Gradients have calls of their own: backward through a result raises, a
+tensor with a tangent of forward mode is refused, and what a call writes into (out, pages, table) counts as changed in place.  Work
+is enqueued on the context's stream: when torch's current stream is another one, that work waits for it and it waits for the work.
 """
 from __future__ import annotations
 
@@ -150,6 +151,21 @@ def _barred(result, instead, *inputs):
     return _unrecorded.apply(result, instead, *inputs)
 
 
+_forward = None
+
+
+def _no_tangents(*tensors):
+    """Refuses those of forward-mode differentiation: a result has no tangent, and that of what is written over would stay."""
+    global _forward
+    if _forward is None:
+        _forward = torch.autograd.forward_ad
+    if _forward._current_level < 0 or not torch._C._is_fwd_grad_enabled():
+        return
+    for t in tensors:
+        if t is not None and _forward.unpack_dual(t).tangent is not None:
+            _refuse("this call has no forward-mode derivative: a tangent would get lost")
+
+
 class Calls:
     """Mixed into Context."""
 
@@ -180,6 +196,7 @@ class Calls:
         x [tokens, inputs]; down [adapters, rank, inputs], up [adapters, rank, outputs]; starts [segments + 1], which [segments],
         ranks [adapters] or None: int32; scale [adapters] float32; base [tokens, outputs] of x's type, float32, or int32 sums times
         step [outputs] float32, or None.  Returns out [tokens, outputs]; base itself may be given for it."""
+        _no_tangents(x, down, up, scale, base, step, out)
         dev = self._device
         ty, dtype, (T, K), x_at, xs = _first(x, "x", dev)
         A, r, N = up.shape
@@ -220,6 +237,7 @@ class Calls:
     def adapters_grad(self, dy, x, down, up, starts, which, scale, ranks=None, base=None):
         """Gradients of `adapters` for dy [tokens, outputs]: (dx, ddown, dup), dx with `base` (the gradient that reaches x through the
         projection itself, of x's type or float32) added to it."""
+        _no_tangents(dy, x, down, up, scale, base)
         dev = self._device
         ty, dtype, (T, K), x_at, xs = _first(x, "x", dev)
         A, r, N = up.shape
@@ -264,6 +282,7 @@ class Calls:
         """Norm of every head of q [tokens, q_heads, head] and k [tokens, kv_heads, head] with the weights wq, wk [head] float32 (or
         None), and the rotation by cos, sin [places, rot / 2] float32 at positions [tokens] int32.  Returns (q', k'); out: a pair
         for them, which may be (q, k)."""
+        _no_tangents(q, k, wq, wk, cos, sin, *(() if out is None else (out[0], out[1])))
         dev = self._device
         ty, dtype, (T, Hq, Hkv, D, rot, P), at, strides, tables = self._rotation(q, k, wq, wk, cos, sin, positions, dev)
         given = out is not None
@@ -283,6 +302,7 @@ class Calls:
     def qk_rotate_append(self, q, k, v, wq, wk, cos, sin, positions, k_pages, v_pages, slots, eps=1e-6, interleaved=False, out=None):
         """qk_rotate whose keys, with the values v [tokens, kv_heads, head], go to the places slots [tokens] int64 (-1: nowhere) of
         k_pages, v_pages [pages, page_size, kv_heads, head].  Returns q'."""
+        _no_tangents(q, k, v, wq, wk, cos, sin, k_pages, v_pages, out)
         dev = self._device
         ty, dtype, (T, Hq, Hkv, D, rot, P), at, strides, tables = self._rotation(q, k, wq, wk, cos, sin, positions, dev)
         v_at, vs = _see(v, "v", dtype, (T, Hkv, D), dev)
@@ -311,6 +331,7 @@ class Calls:
 
     def qk_rotate_grad(self, dq_out, dk_out, q, k, wq, wk, cos, sin, positions, eps=1e-6, interleaved=False):
         """Gradients of qk_rotate: (dq, dk, dwq, dwk), the weights' in float32."""
+        _no_tangents(dq_out, dk_out, q, k, wq, wk, cos, sin)
         dev = self._device
         ty, dtype, (T, Hq, Hkv, D, rot, P), at, strides, tables = self._rotation(q, k, wq, wk, cos, sin, positions, dev)
         dq_at, dqs = _see(dq_out, "dq_out", dtype, (T, Hq, D), dev)
@@ -329,6 +350,7 @@ class Calls:
         """Attention of the new tokens q [tokens, q_heads, head] of every request, starts [requests + 1] int32, over its lengths
         [requests] int32 places in k_pages, v_pages [pages, page_size, kv_heads, head], found through table [requests, width] int32;
         causal, and over the last `window` places alone if that is not 0.  scale: head ** -0.5 if None.  Returns out like q."""
+        _no_tangents(q, k_pages, v_pages, out)
         dev = self._device
         ty, dtype, (T, Hq, D), q_at, qs = _first(q, "q", dev)
         Hkv = k_pages.shape[2]
@@ -386,6 +408,7 @@ class Calls:
         ([prefixes + 1] int32) attend to the prefix_lengths[g] places ([prefixes] int32) found through prefix_table [prefixes, width]
         int32, which are read once for all of them, and then to their own, of which table, starts and lengths tell.  A window
         counts both.  Returns out like q."""
+        _no_tangents(q, k_pages, v_pages, out)
         dev = self._device
         ty, dtype, (T, Hq, D), q_at, qs = _first(q, "q", dev)
         Hkv = k_pages.shape[2]
@@ -417,6 +440,7 @@ class Calls:
         the first whose running weight among the kept ones exceeds uniform [rows] float32 of theirs.  temperature, top_p, min_p [rows]
         float32 and top_k [rows] int32: each row's own settings, or None.  Returns (tokens [rows] int32, -1 for a row without a
         logit above -infinity; probs [rows] float32, the token's share); out: a pair for them."""
+        _no_tangents(logits, step, temperature, *(() if out is None else (out[0], out[1])))
         dev = self._device
         kind = {torch.bfloat16: 0, torch.float16: 1, torch.float32: _F32, torch.int32: _I32}.get(logits.dtype)
         if kind is None:
