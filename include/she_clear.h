@@ -243,7 +243,8 @@ int she_attend_shared(she_ctx *ctx, const she_attend_shared_args *args);
  * least 0 (NaN too) and at most 1 - 2^-24.  Weights are held to 2^-44 of the largest, less than which is none, and their sums are exact;
  * but where temperature is all that a call sets and vocab is more than 8192, every 512 tokens' running weight is held to 2^-44 of the
  * row's largest, and each of theirs to 2^-44 of the largest among them: tokens of less than 2^-44.5 have some if others of the 512
- * have more. */
+ * have more.  tokens may be top_k, and probs may be uniform, temperature, top_p or min_p; neither shares memory with
+ * anything else. */
 typedef struct {
     int32_t type;                        /* SHE_BF16, SHE_F16, SHE_F32 or SHE_I32 */
     uint32_t rows, vocab;                /* vocab at most 2^20 */

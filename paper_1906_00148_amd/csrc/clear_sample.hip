@@ -688,6 +688,7 @@ template <class T> __global__ __launch_bounds__(THREADS) void k_sample_rows(she_
     __shared__ Shared s;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t r = blockIdx.x;
+    const Settings set(a, r);                                      // which the answer may overwrite: barriers follow
     Held<T> source{row_of<T>(a, r)};
     load_logits(source.row, threadIdx.x * 8, source.v);
     make_table(s.table);
@@ -718,7 +719,6 @@ template <class T> __global__ __launch_bounds__(THREADS) void k_sample_rows(she_
     }
     __syncthreads();
     for (int k = 0; k < WAVES; k++) join(s.tops[k], s.where[k]);
-    const Settings set(a, r);
     const bool none = top == -__builtin_inff();
     if (none || !(set.temperature > 0)) {
         if (threadIdx.x == 0) answer(a, r, none ? -1 : (int32_t)where, none ? 0.0f : 1.0f);
@@ -925,6 +925,7 @@ template <class T> __global__ __launch_bounds__(THREADS) void k_sample_answers(s
     largest_of(parts, r, top, where);
     const bool none = top == -__builtin_inff();
     if (none || !(set.temperature > 0)) {
+        __syncthreads();                                           // all have read the settings, which the answer may overwrite
         if (threadIdx.x >= 64) return;
         float v[8];
         load_logits(row, where * 8, v);

@@ -100,3 +100,21 @@ def test_the_probability_of_a_token_of_hardly_any_weight(ctx, u):  # noqa: F811
     token, prob = (t.item() for t in ctx.sample(x.cuda(), torch.tensor([u]).cuda()))
     # 2^-24 for the result, and the whole weight's error
     assert token < 2048 and abs(prob / share[token].item() - 1) <= 2.0 ** -24 + 9216 * 2.0 ** -44
+
+
+@pytest.mark.parametrize("vocab", [100, 5000, 9000, 20000])
+@pytest.mark.parametrize("setting", ["uniform", "temperature", "top_p", "min_p"])
+def test_answers_in_place_of_settings(ctx, vocab, setting):  # noqa: F811
+    """Rows that take the likeliest token answer early, and others' threads still look at their own settings."""
+    rows = 300
+    x, _, g = numbers(rows, vocab, BF16)
+    a = dict(uniform=torch.rand(rows, generator=g), temperature=torch.tensor([0.0, 1.0, 0.7] * 100), top_k=torch.tensor([0, 40, 3000, 0] * 75, dtype=torch.int32),
+             top_p=torch.tensor([1.0, 0.9] * 150), min_p=torch.tensor([0.0, 0.01, 0.2, 0.0] * 75))
+    for names in (("uniform", "temperature"), ("uniform", "temperature", "top_k", "top_p", "min_p"), ("uniform", "temperature", "min_p")):
+        if setting not in names:
+            continue
+        on = {k: a[k].cuda() for k in names}
+        want = ctx.sample(x.cuda(), **on)
+        tokens = on.get("top_k", torch.empty(rows, dtype=torch.int32, device="cuda"))
+        got = ctx.sample(x.cuda(), **on, out=(tokens, on[setting]))
+        assert all(torch.equal(g, w) for g, w in zip(got, want))
