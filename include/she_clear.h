@@ -19,7 +19,9 @@
  *    calls.
  *  - What the host can see is checked (SHE_EINVAL, SHE_ERANGE).  Ids in device arrays are checked by the kernels: one that is
  *    out of its range is left out, as each call says, never followed, and counted (she_clear_bad_ids).
- *  - Sums, softmax statistics and norms are held in 32 bits; results are rounded once, to nearest.
+ *  - Sums, softmax statistics and norms are held in 32 bits; results are rounded once, to nearest.  (Attention's weights are rounded to
+ *    the type before, their sum is not, where requests have many rows, new tokens times the query heads of a key head, over many
+ *    places.  Requests of up to 32 rows on average behind shared prefixes are not among them, nor single tokens of up to 8.)
  *  - No result depends on the order in which the GPU runs things: the same call gives the same bits.
  */
 #ifndef SHE_CLEAR_H

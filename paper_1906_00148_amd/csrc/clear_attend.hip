@@ -11,6 +11,8 @@
 // memory, takes the second product with the weights as two numbers of the type, the rounded value and the rest, so that nothing but the
 // result's own rounding shows.  k_attend_tile rounds the weights to the type (their sum is not): an error of the size of the result's
 // own rounding, 0.0024 and not 0.0017 of a result in bf16; with two numbers 2048 tokens over 32768 places take 1434 us and not 1065.
+// Behind shared prefixes tiles of many rows have one number or two by the requests' rows (beside shared_shape): 24 questions of up to 300 tokens behind
+// 8192 places 500 us, 636 with two; 64 single tokens behind 32768 78, and 88 with two, which they have.
 //
 // Masks: a place that no row of the tile attends to is not read at all.  A place that some rows attend to and others do not has weight
 // 0 for the others, which a matrix instruction multiplies with the value all the same.  So where some of such places' values are
@@ -556,8 +558,8 @@ template <class T, int DP> struct alignas(16) TileShared {
     uint64_t missing[2][TILE_BLOCK / 64];                                            // places that their page id or the table's end keeps out
     int lows[TILE_WAVES];
 };
-// Its arrays one by one: what is on its way into one of them is not waited for where another is read.
-template <class T, int DP, Walk WALK>
+// Its arrays one by one: what is on its way into one of them is not waited for where another is read.  TWO: weights are two numbers of the type.
+template <class T, int DP, Walk WALK, bool TWO>
 __device__ __forceinline__ void attend_tile(const she_attend_pages_args &a, uint32_t group, const Pieces &pieces, const Owners &owners, const void *zeros, uint32_t *d_bad,
                                             T *__restrict__ even_keys, T *__restrict__ even_values, T *__restrict__ odd_keys, T *__restrict__ odd_values,
                                             int64_t (*__restrict__ rows)[TILE_BLOCK], uint64_t (*__restrict__ missing)[TILE_BLOCK / 64], int *__restrict__ lows,
@@ -728,7 +730,7 @@ __device__ __forceinline__ void attend_tile(const she_attend_pages_args &a, uint
                     for (int i = 0; i < 16; i++) acc[b][i] *= alpha;
             }
             const float ref = m == -__builtin_inff() ? 0.0f : m;
-            x8<T> p[4];
+            x8<T> p[4], rest[4];
 #pragma unroll
             for (int t = 0; t < 2; t++)
 #pragma unroll
@@ -736,6 +738,7 @@ __device__ __forceinline__ void attend_tile(const she_attend_pages_args &a, uint
                     const float v = __builtin_amdgcn_exp2f(fmaf(s[t][i], scale, -ref));
                     l += v;
                     p[t * 2 + i / 8][i % 8] = (T)v;
+                    if constexpr (TWO) rest[t * 2 + i / 8][i % 8] = (T)(v - (float)p[t * 2 + i / 8][i % 8]);
                 }
             // V^T of the 32 elements from 32 b on and the sixteen places from 16 k on, in the scores' order
             auto columns = [&](int b, int k) {
@@ -751,7 +754,11 @@ __device__ __forceinline__ void attend_tile(const she_attend_pages_args &a, uint
 #pragma unroll
             for (int k = 0; k < 4; k++)
 #pragma unroll
-                for (int b = 0; b < DB; b++) acc[b] = mfma32(as_x8<T>(columns(b, k)), p[k], acc[b]);
+                for (int b = 0; b < DB; b++) {
+                    const x8<T> v = as_x8<T>(columns(b, k));
+                    if constexpr (TWO) acc[b] = mfma32(v, rest[k], acc[b]);
+                    acc[b] = mfma32(v, p[k], acc[b]);
+                }
         }
     };
     for (int step = 0; step < steps; step += 2) {
@@ -790,13 +797,13 @@ __device__ __forceinline__ void attend_tile(const she_attend_pages_args &a, uint
 }
 // A key head's tiles are one XCD's where there are eight of them: neighbouring workgroups have different heads.  Late tokens have
 // most to attend to: they come first.
-template <class T, int DP, Walk WALK>
+template <class T, int DP, Walk WALK, bool TWO>
 __global__ __launch_bounds__(64 * TILE_WAVES, DP == 256 ? 1 : 2) void k_attend_tile(she_attend_pages_args a, uint32_t group, Pieces pieces, Owners owners, const void *zeros, uint32_t *d_bad)
 {
     __shared__ alignas(16) T even_keys[STEP * DP], even_values[STEP * DP], odd_keys[STEP * DP], odd_values[STEP * DP];
     __shared__ int64_t rows[2][TILE_BLOCK];
     __shared__ uint64_t missing[2][TILE_BLOCK / 64];
-    attend_tile<T, DP, WALK>(a, group, pieces, owners, zeros, d_bad, even_keys, even_values, odd_keys, odd_values, rows, missing, nullptr, gridDim.x / a.kv_heads - 1 - blockIdx.x / a.kv_heads, (int)(blockIdx.x % a.kv_heads), (int)blockIdx.z);
+    attend_tile<T, DP, WALK, TWO>(a, group, pieces, owners, zeros, d_bad, even_keys, even_values, odd_keys, odd_values, rows, missing, nullptr, gridDim.x / a.kv_heads - 1 - blockIdx.x / a.kv_heads, (int)(blockIdx.x % a.kv_heads), (int)blockIdx.z);
 }
 
 // Rows that were cut, `each` of a tile a workgroup.  Up to JOIN_AHEAD pieces are a wavefront's work, and a workgroup of the tile kernel's
@@ -878,7 +885,7 @@ __global__ __launch_bounds__(256) void k_attend_join(she_attend_pages_args a, ui
 // other: a step of 64 places takes 1.7 us where a compute unit has one tile's workgroup, and two have theirs in 2.0.  97 requests of up to 4 tokens
 // behind five prefixes (16 heads of 64, f16) take 78 us, 3.5 TB/s.
 template <class T, int DP, bool FEW> using SharedOf = typename std::conditional<FEW, FewShared<DP>, TileShared<T, DP>>::type;
-template <class T, int DP, bool FEW, Walk WALK>
+template <class T, int DP, bool FEW, Walk WALK, bool TWO>
 __device__ __forceinline__ void attend_block(const she_attend_pages_args &a, uint32_t group, const Pieces &pieces, const Owners &owners, const void *zeros, uint32_t *d_bad, char *shared,
                                              uint32_t slots, uint32_t block)
 {
@@ -886,10 +893,10 @@ __device__ __forceinline__ void attend_block(const she_attend_pages_args &a, uin
     auto &its = *reinterpret_cast<SharedOf<T, DP, FEW> *>(shared);
     if constexpr (FEW) attend_few<T, DP, WALK>(a, group, pieces, owners, d_bad, its, slot, (int)kv_head, (int)z);
     else
-        attend_tile<T, DP, WALK>(a, group, pieces, owners, zeros, d_bad, its.even_keys, its.even_values, its.odd_keys, its.odd_values, its.rows, its.missing, its.lows, slot,
+        attend_tile<T, DP, WALK, TWO>(a, group, pieces, owners, zeros, d_bad, its.even_keys, its.even_values, its.odd_keys, its.odd_values, its.rows, its.missing, its.lows, slot,
                                  (int)kv_head, (int)z);
 }
-template <class T, int DP, bool PREFIX_FEW, bool FEW>
+template <class T, int DP, bool PREFIX_FEW, bool FEW, bool TWO>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_shared(she_attend_pages_args a, uint32_t group, Pieces prefix, Pieces pieces, Owners owners, const void *zeros,
                                                                           uint32_t prefix_slots, uint32_t prefix_blocks, uint32_t slots, uint32_t *d_bad)
 {
@@ -901,9 +908,9 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attend_shared(she_at
         p.table_stride = owners.prefix_stride;
         p.table_width = owners.prefix_width;
         p.lengths = owners.prefix_lengths;
-        attend_block<T, DP, PREFIX_FEW, PREFIXES>(p, group, prefix, owners, zeros, d_bad, shared, prefix_slots, blockIdx.x);
+        attend_block<T, DP, PREFIX_FEW, PREFIXES, TWO>(p, group, prefix, owners, zeros, d_bad, shared, prefix_slots, blockIdx.x);
     } else {
-        attend_block<T, DP, FEW, BEHIND>(a, group, pieces, owners, zeros, d_bad, shared, slots, blockIdx.x - prefix_blocks);
+        attend_block<T, DP, FEW, BEHIND, TWO>(a, group, pieces, owners, zeros, d_bad, shared, slots, blockIdx.x - prefix_blocks);
     }
 }
 
@@ -965,20 +972,20 @@ template <class F> hipError_t by_head(uint32_t head, F launch)
     return hipGetLastError();
 }
 
-template <class T, Walk WALK>
+template <class T, Walk WALK, bool TWO>
 hipError_t walk(const she_attend_pages_args &a, const AttendShape &s, const Pieces &pieces, const Owners &owners, uint32_t *d_bad, hipStream_t st)
 {
     const uint32_t group = a.q_heads / a.kv_heads, slots = (uint32_t)s.slots;
     return by_head(a.head, [&](auto size) {
         constexpr int DP = decltype(size)::value;
         if (s.few) k_attend_few<T, DP, WALK><<<dim3(slots, a.kv_heads, s.splits), 64 * FEW_WAVES, 0, st>>>(a, group, pieces, owners, d_bad);
-        else k_attend_tile<T, DP, WALK><<<dim3(slots * a.kv_heads, 1, s.splits), 64 * TILE_WAVES, 0, st>>>(a, group, pieces, owners, zeros_of(d_bad), d_bad);
+        else k_attend_tile<T, DP, WALK, TWO><<<dim3(slots * a.kv_heads, 1, s.splits), 64 * TILE_WAVES, 0, st>>>(a, group, pieces, owners, zeros_of(d_bad), d_bad);
     });
 }
 
-template <class T, Walk WALK> hipError_t attend(const she_attend_pages_args &a, const AttendShape &s, const Pieces &pieces, const Owners &owners, uint32_t *d_bad, hipStream_t st)
+template <class T, Walk WALK, bool TWO = false> hipError_t attend(const she_attend_pages_args &a, const AttendShape &s, const Pieces &pieces, const Owners &owners, uint32_t *d_bad, hipStream_t st)
 {
-    const hipError_t rc = walk<T, WALK>(a, s, pieces, owners, d_bad, st);
+    const hipError_t rc = walk<T, WALK, TWO>(a, s, pieces, owners, d_bad, st);
     if (rc != hipSuccess || s.splits == 1) return rc;
     const uint32_t group = a.q_heads / a.kv_heads, slots = (uint32_t)s.slots;
     const int each = s.few && s.splits > 4 * JOIN_AHEAD ? 1 : s.few || s.splits > JOIN_AHEAD ? 4 : 16;
@@ -996,9 +1003,9 @@ template <class T> hipError_t attend_shared(const she_attend_pages_args &a, cons
     const hipError_t rc = by_head(a.head, [&](auto size) {
         constexpr int DP = decltype(size)::value;
         const auto launch = [&](auto kernel) { kernel<<<blocks, 256, 0, st>>>(a, group, prefix, pieces, owners, zeros_of(d_bad), prefix_slots, prefix_blocks, slots, d_bad); };
-        if (s.prefix.few) launch(k_attend_shared<T, DP, true, true>);
-        else if (s.behind.few) launch(k_attend_shared<T, DP, false, true>);
-        else launch(k_attend_shared<T, DP, false, false>);
+        if (s.prefix.few) launch(k_attend_shared<T, DP, true, true, false>);
+        else if (s.behind.few) s.two ? launch(k_attend_shared<T, DP, false, true, true>) : launch(k_attend_shared<T, DP, false, true, false>);
+        else s.two ? launch(k_attend_shared<T, DP, false, false, true>) : launch(k_attend_shared<T, DP, false, false, false>);
     });
     if (rc != hipSuccess) return rc;
     const uint64_t rows = (uint64_t)a.tokens * a.q_heads;
@@ -1024,6 +1031,7 @@ hipError_t launch_attend_shared(const she_attend_shared_args &args, const Shared
     float2 *ml = reinterpret_cast<float2 *>(o + shared_pieces(args, s) * a.head);
     if (s.whole) {
         const Pieces pieces{o, ml, s.behind.splits, 0, s.behind.splits, s.behind.chunk};
+        if (s.two) return a.type == SHE_BF16 ? attend<__bf16, WHOLE, true>(a, s.behind, pieces, owners, d_bad, st) : attend<_Float16, WHOLE, true>(a, s.behind, pieces, owners, d_bad, st);
         return a.type == SHE_BF16 ? attend<__bf16, WHOLE>(a, s.behind, pieces, owners, d_bad, st) : attend<_Float16, WHOLE>(a, s.behind, pieces, owners, d_bad, st);
     }
     const uint32_t splits = s.prefix.splits + s.behind.splits;

@@ -113,6 +113,14 @@ SharedShape shared_shape(const she_attend_shared_args &a, uint32_t cus)
     const uint64_t group = a.q_heads / a.kv_heads, rows = a.tokens * group, places = (uint64_t)a.prefix_width * a.page_size, own = (uint64_t)a.table_width * a.page_size;
     const she_attend_pages_args call = shared_behind(a);
     s.behind = attend_shape(call, cus);
+    // Never fewer bits than she_attend_pages has for the same places, which takes few rows and single tokens with two numbers for a weight: by tiles of many
+    // rows with one, these would be off by 0.0023 of a bf16 result and not 0.0017.  The second product costs least where a wavefront waits otherwise, so
+    // other calls have it up to 32 rows of a request (one number, two; 8192 places, 8 key heads of 128, bf16; us; rows at a key head on average):
+    //    64 requests:  4 rows  32.3, 34.9   6    44.2, 49.0   18   71.7, 83.3   34  108.8, 139.0   66   213.7, 273.5
+    //    24 requests:  4 rows  25.3, 27.7   10   30.9, 33.4   18   43.9, 49.2   34   63.9, 74.6    258  294.4, 371.1
+    she_attend_pages_args both = call;
+    both.table_width += a.prefix_width;
+    s.two = rows <= 32 * (uint64_t)a.requests || attend_shape(both, cus).few;
     if (!a.prefixes) return s;
     // Few places, which workgroups that run at once walk in one launch: joining a prefix's pieces with the requests' own takes a second one.
     // (Both, one launch; us on the device; single tokens with 40 places behind a prefix of 60, 330 and 450 places.)
@@ -155,6 +163,7 @@ SharedShape shared_shape(const she_attend_shared_args &a, uint32_t cus)
     const uint64_t tiles = std::max<uint64_t>(rows / TILE_ROWS + a.requests / 2, std::min<uint64_t>(a.requests, a.tokens)) * a.kv_heads;
     SharedShape w{};
     w.whole = true;
+    w.two = s.two;
     w.behind.slots = a.requests == 1 ? ceil_div(rows, TILE_ROWS) : rows / TILE_ROWS + a.requests;
     uint64_t least = ~0ull;
     for (uint64_t splits = 1; splits <= std::max<uint64_t>(1, std::min<uint64_t>(64, ceil_div(places + own, 512))); splits++) {

@@ -58,6 +58,7 @@ hipError_t launch_attend_pages(const she_attend_pages_args &a, const AttendShape
 // A call with shared prefixes: the walk over these, and the one over what the requests have behind them; or each request's over both.
 struct SharedShape {
     bool whole;                          // `behind` is the walk over both
+    bool two;                            // tiles of many rows take weights as two numbers of the type, as those of few rows always do
     AttendShape prefix, behind;          // either joined with the other, whatever its pieces
 };
 she_attend_pages_args shared_behind(const she_attend_shared_args &a);            // the walk over the requests' own places as a call
