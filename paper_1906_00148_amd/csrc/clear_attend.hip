@@ -895,10 +895,10 @@ __global__ __launch_bounds__(256) void k_attend_join(she_attend_pages_args a, ui
 }
 
 // A call with shared prefixes, whose two walks are one launch: while the prefixes' workgroups, of many rows, wait for the matrix units, those
-// of the requests' own places wait for memory (64 tokens behind 32768 places with up to 500 of their own, 32 / 8 heads of 128, bf16: 67 to 76 us,
-// 6 less without their own places; two launches 95 and not 87 for the whole call at that time).  Such a call is bound by what a wavefront does one after the
-// other: a step of 64 places takes 1.7 us where a compute unit has one tile's workgroup, and two have theirs in 2.0.  97 requests of up to 4 tokens
-// behind five prefixes (16 heads of 64, f16) take 78 us, 3.5 TB/s.
+// of the requests' own places wait for memory (64 tokens behind 32768 places with up to 500 of their own, 32 / 8 heads of 128, bf16: 73 to 88 us,
+// 67 to 76 with weights of one number and then 6 less without their own places; two launches 95 and not 87 for the whole call at that time).  Such a call
+// is bound by what a wavefront does one after the other: with one number a step of 64 places takes 1.7 us where a compute unit has one tile's workgroup, and
+// two have theirs in 2.0.  97 requests of up to 4 tokens behind five prefixes (16 heads of 64, f16) take 83 us, 3.3 TB/s.
 template <class T, int DP, bool FEW> using SharedOf = typename std::conditional<FEW, FewShared<DP>, TileShared<T, DP>>::type;
 template <class T, int DP, bool FEW, Walk WALK, bool TWO>
 __device__ __forceinline__ void attend_block(const she_attend_pages_args &a, uint32_t group, const Pieces &pieces, const Owners &owners, const void *zeros, uint32_t *d_bad, char *shared,
