@@ -439,7 +439,7 @@ class Calls:
         """The next token of every row of logits [rows, vocab], in bfloat16, float16, float32, or int32 sums times step [vocab] float32:
         the first whose running weight among the kept ones exceeds uniform [rows] float32 of theirs.  temperature, top_p, min_p [rows]
         float32 and top_k [rows] int32: each row's own settings, or None.  Returns (tokens [rows] int32, -1 for a row without a
-        logit above -infinity; probs [rows] float32, the token's share); out: a pair for them."""
+        logit above -infinity; probs [rows] float32, the token's share); out: a pair for them, which may be top_k and one of the others."""
         _no_tangents(logits, step, temperature, *(() if out is None else (out[0], out[1])))
         dev = self._device
         kind = {torch.bfloat16: 0, torch.float16: 1, torch.float32: _F32, torch.int32: _I32}.get(logits.dtype)
